@@ -350,6 +350,94 @@ int sdp_coverage_grad_sqnorm(int K, int64_t R, int D, int gdtype, const void* co
  * as grad_scale_dev.  Errors: INVALID_ARG (null, misaligned, n < 1, max_norm not positive and finite). */
 int sdp_clip_scale(int n, const double* sqnorm, float max_norm, float* scale, void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * What stands around a stack of blocks: the norm in front of a block's half, the embedding of token ids and the
+ * loss of the logits, each with its gradient (the paper's models are LLaMA-style: Sec. 4, App. "Hyperparameters for
+ * LLM Architecture").  They differ from the calls above in three points:
+ *   - T = 0 is an empty batch: buffers with T in their size may be null, the others are written (zeros).
+ *   - Matrices may start at any element, not only at 16 bytes, and rows may have any length.
+ *   - `id_type` says what token ids and labels are: SDP_I32 or SDP_I64.  One outside [0, V) (-1, say) is no
+ *     token: it takes part in nothing, as below.  No id is trusted.
+ * Overlap: an output may lie where the call says so and nowhere else over an operand or another output
+ * (INVALID_ARG).
+ * ------------------------------------------------------------------------------------------- */
+typedef enum { SDP_NORM_LAYER = 0, SDP_NORM_RMS = 1 } sdp_norm_kind;
+typedef enum { SDP_I32 = 0, SDP_I64 = 1 } sdp_id_type;
+#define SDP_NORM_MAX_WIDTH 32768    /* largest d of the norm calls */
+#define SDP_MAX_TOKENS (1 << 30)    /* largest T of the calls below */
+
+/* ---------------------------------------------------------------------------------------------
+ * Norm of T tokens of width d, of their own or of a sum with a skip connection:
+ *   h = x + r, rounded to dtype (r = R's row; R null: h = x)
+ *   SDP_NORM_LAYER: mu = mean(h);  SDP_NORM_RMS: mu = 0
+ *   s = 1 / sqrt(mean((h - mu)^2) + eps);  y = (h - mu) s gamma + beta
+ * Statistics are taken of h as it is stored, in fp32 (the mean first, then the centred squares).
+ *   X [T][d], R [T][d] (may be NULL), gamma [d], beta [d] (may be NULL: no bias) in
+ *   H [T][d] out: the sum, written if and only if R is given (else NULL);  Y [T][d] out
+ *   mean, rstd [T] fp32 out: mu and s, for sdp_norm_bwd; mean is NULL with SDP_NORM_RMS
+ * H and Y may each take the place of X or R (the same pointer); H and Y are two buffers.
+ * Errors: INVALID_ARG (null, misaligned, overlapping, unknown kind or dtype, T < 0, d < 1, eps negative or not
+ * finite), SHAPE (d > SDP_NORM_MAX_WIDTH, T > SDP_MAX_TOKENS).
+ * ------------------------------------------------------------------------------------------- */
+int sdp_norm_fwd(int kind, int dtype, int T, int d, float eps, const void* X, const void* R, const void* gamma,
+                 const void* beta, void* H, void* Y, float* mean, float* rstd, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Its backward pass for upstream gradient dY = dL/dY, with xh = (h - mu) s and g = dY gamma:
+ *   dX = s (g - mean(g) [SDP_NORM_LAYER only] - xh mean(g xh)) + dH,   dgamma = sum_t dY xh,   dbeta = sum_t dY
+ *   H [T][d] in: what was normalised (the forward call's H, or X where there was no R);  dY [T][d] in
+ *   dH [T][d] in, may be NULL: the gradient that reaches h past the norm, over the skip connection.  dX is then the
+ *   gradient of both x and r.
+ *   gamma [d], mean, rstd [T] in: as in the forward call
+ *   dX [T][d] out; may take the place of H, dY or dH
+ *   dgamma, dbeta [d] out, of dtype, summed in fp32 in a fixed order; dbeta may be NULL (no bias), both may be (a
+ *   worker that does not train them)
+ *   ws: sdp_norm_bwd_workspace_bytes(dtype, T, d), 16-byte aligned; may be NULL where that is 0 or dgamma is NULL.
+ * Errors: as above, WORKSPACE.
+ * ------------------------------------------------------------------------------------------- */
+size_t sdp_norm_bwd_workspace_bytes(int dtype, int T, int d);
+int sdp_norm_bwd(int kind, int dtype, int T, int d, const void* H, const void* dY, const void* dH, const void* gamma,
+                 const float* mean, const float* rstd, void* dX, void* dgamma, void* dbeta, void* ws, size_t ws_bytes,
+                 void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Rows of an embedding matrix, scaled: Y[t] = scale E[ids[t]] (product in fp32, rounded once; scale = 1 keeps the
+ * bits), zeros where ids[t] lies outside [0, V).
+ *   E [V][d] in (row-major by token, as every matrix here is by neuron);  ids [T] in;  Y [T][d] out
+ * Errors: INVALID_ARG (null, misaligned, overlapping, unknown dtype or id_type, T < 0, V < 1, d < 1, scale not finite),
+ * SHAPE (T > SDP_MAX_TOKENS).
+ *
+ * sdp_embed_bwd: its gradient, dE[v] = scale sum_{t : ids[t] = v} dY[t], every row of [V][d]: rows of tokens that do not
+ * occur are zeros.  Tokens are sorted by id (stably, so each row's fp32 sum has one order, whatever the
+ * launch); a row is rounded once.  What goes into sdp_coverage_grad_avg and the fused update like any other gradient.
+ *   dY [T][d], ids [T] in;  dE [V][d] out;  ws: sdp_embed_bwd_workspace_bytes(dtype, T, V, d), 16-byte aligned.
+ * Errors: as above, WORKSPACE.
+ * ------------------------------------------------------------------------------------------- */
+int sdp_embed_fwd(int dtype, int id_type, int T, int V, int d, float scale, const void* E, const void* ids, void* Y,
+                  void* stream);
+size_t sdp_embed_bwd_workspace_bytes(int dtype, int T, int V, int d);
+int sdp_embed_bwd(int dtype, int id_type, int T, int V, int d, float scale, const void* dY, const void* ids, void* dE,
+                  void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Cross-entropy of T rows of V logits against labels, with its gradient from the same read of the logits:
+ *   lse[t] = log sum_j exp Z[t][j];   nll[t] = lse[t] - Z[t][labels[t]];
+ *   loss = c sum_t nll[t],  c = scale * scale_dev[0];   dZ[t][j] = dloss / dZ[t][j] = c (exp(Z[t][j] - lse[t]) - [j = labels[t]])
+ * A row whose label lies outside [0, V) has none: nll = lse = 0, dZ = 0, and its logits are not read.  Logits of -inf are
+ * masked ones (probability 0); a row of nothing else, or one with +inf or NaN, gives NaN, as the formulas do.
+ *   Z, dZ [T][ldz], ldz >= V: columns from V on are neither read nor written.  dZ may be NULL (loss alone) or Z.
+ *   labels [T] in;  scale_dev: device fp32, may be NULL (= 1): what sdp_label_scale wrote, or a loss scale; 4-byte aligned
+ *   nll [T] fp32 out;  lse [T] fp32 out, may be NULL;  loss [1] fp32 out (summed in fp64 in a fixed order), may be NULL
+ * Errors: INVALID_ARG (null, misaligned, overlapping, unknown dtype or id_type, T < 0, V < 1, scale not finite),
+ * SHAPE (ldz < V, T > SDP_MAX_TOKENS).
+ *
+ * sdp_label_scale: *scale = 1 / max(1, n), n = number of labels in [0, V): the scale of the mean over the rows that have
+ * a label.
+ * ------------------------------------------------------------------------------------------- */
+int sdp_token_loss(int dtype, int id_type, int T, int V, int64_t ldz, float scale, const void* Z, const void* labels,
+                   const float* scale_dev, float* nll, float* lse, void* dZ, float* loss, void* stream);
+int sdp_label_scale(int id_type, int T, int V, const void* labels, float* scale, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -100,6 +100,23 @@ def lib():
     L.sdp_clip_scale.argtypes = [i32, vp, ctypes.c_float, vp, vp]
     L.sdp_coverage_avg_adamw.restype = i32
     L.sdp_coverage_avg_adamw.argtypes = [i32, i64, i32, i32, ctypes.POINTER(vp), vp, vp, vp, vp, vp, vp, vp, vp]
+    f32 = ctypes.c_float
+    L.sdp_norm_fwd.restype = i32
+    L.sdp_norm_fwd.argtypes = [i32] * 4 + [f32] + [vp] * 9
+    L.sdp_norm_bwd_workspace_bytes.restype = sz
+    L.sdp_norm_bwd_workspace_bytes.argtypes = [i32] * 3
+    L.sdp_norm_bwd.restype = i32
+    L.sdp_norm_bwd.argtypes = [i32] * 4 + [vp] * 10 + [sz, vp]
+    L.sdp_embed_fwd.restype = i32
+    L.sdp_embed_fwd.argtypes = [i32] * 5 + [f32] + [vp] * 4
+    L.sdp_embed_bwd_workspace_bytes.restype = sz
+    L.sdp_embed_bwd_workspace_bytes.argtypes = [i32] * 4
+    L.sdp_embed_bwd.restype = i32
+    L.sdp_embed_bwd.argtypes = [i32] * 5 + [f32] + [vp] * 4 + [sz, vp]
+    L.sdp_token_loss.restype = i32
+    L.sdp_token_loss.argtypes = [i32] * 4 + [i64, f32] + [vp] * 8
+    L.sdp_label_scale.restype = i32
+    L.sdp_label_scale.argtypes = [i32] * 3 + [vp] * 3
     L.sdp_profile_enable.restype = i32
     L.sdp_profile_enable.argtypes = [i32]
     L.sdp_profile_filter.restype = i32
@@ -544,6 +561,208 @@ def coverage_avg_adamw(grads, mask, theta, m, v, lr, beta1, beta2, eps, weight_d
                                       _dev(v, torch.float32, "v"), lowp, _dev(cov, torch.uint8, "cov"), ctypes.byref(hp), _stream())
     _check(st, "sdp_coverage_avg_adamw")
     return cov
+
+
+# ---- around a stack of blocks: norms, token embedding, token loss.  Every tensor has to be on the current device. ----------
+
+_KINDS = {"layer": 0, "rms": 1, 0: 0, 1: 1}
+_ID_TYPES = {torch.int32: 0, torch.int64: 1}
+
+
+def _here():
+    """The current device and its current stream."""
+    device = torch._C._cuda_getDevice()
+    return device, torch._C._cuda_getCurrentRawStream(device)
+
+
+def _here_of(t):
+    """The same for a compiled call, which checks its tensors itself: t on the CPU is refused there."""
+    return _here() if t.is_cuda else (0, 0)
+
+
+def _dtype_of(t, name):
+    if t.dtype not in _DTYPES:
+        raise TypeError(f"{name}: expected torch.float32 or torch.bfloat16")
+    return _DTYPES[t.dtype]
+
+
+def _id_type_of(t, name):
+    if t.dtype not in _ID_TYPES:
+        raise TypeError(f"{name}: expected torch.int32 or torch.int64")
+    return _ID_TYPES[t.dtype]
+
+
+def _shape(t, shape, name):
+    if t.shape != shape:
+        raise ValueError(f"{name}: expected shape {tuple(shape)}")
+
+
+def norm_fwd(kind, X, gamma, beta=None, residual=None, eps=1e-5, out=None):
+    """Layer ("layer") or root-mean-square ("rms") norm of the tokens X [T][d], or of H = X + residual.
+
+    Returns (Y, H, mean, rstd): what norm_bwd takes; H is X itself without a residual, mean None for "rms".
+    `out` = (Y, H, mean, rstd) preallocated; H is not looked at without a residual, mean not for "rms"."""
+    k = _KINDS[kind]
+    T, d = X.shape
+    dt = _dtype_of(X, "X")
+    _shape(gamma, (d,), "gamma")
+    if beta is not None:
+        _shape(beta, (d,), "beta")
+    if residual is not None:
+        _shape(residual, X.shape, "residual")
+    if out is None:
+        Y, rstd = torch.empty_like(X), torch.empty((T,), dtype=torch.float32, device=X.device)
+        H = None if residual is None else torch.empty_like(X)
+        mean = None if k else torch.empty_like(rstd)
+    else:
+        Y, H, mean, rstd = out
+        _shape(Y, X.shape, "Y")
+        _shape(rstd, (T,), "rstd")
+        if residual is None:
+            H = None
+        else:
+            _shape(H, X.shape, "H")
+        if k:
+            mean = None
+        else:
+            _shape(mean, (T,), "mean")
+    device, stream = _here_of(X)
+    st = _native().norm_fwd(device, k, dt, T, d, eps, X, residual, gamma, beta, H, Y, mean, rstd, stream)
+    _check(st, "sdp_norm_fwd")
+    return Y, X if H is None else H, mean, rstd
+
+
+def norm_bwd_workspace_bytes(dtype, T, d):
+    return int(lib().sdp_norm_bwd_workspace_bytes(_DTYPES[dtype], T, d))
+
+
+def norm_bwd(kind, H, dY, gamma, mean, rstd, dH=None, want_dw=True, bias=None, out=None, ws=None):
+    """Backward of norm_fwd for dY [T][d]; dH [T][d] is the gradient that reaches H past the norm.
+
+    Returns (dX, dgamma, dbeta): dX is the gradient of X and of the residual.  dbeta is None without a bias (`bias`: by default
+    "layer" has one, "rms" has none, and what `out` says where it is given), both are None with want_dw=False."""
+    k = _KINDS[kind]
+    T, d = H.shape
+    dt = _dtype_of(H, "H")
+    _shape(dY, H.shape, "dY")
+    _shape(gamma, (d,), "gamma")
+    _shape(rstd, (T,), "rstd")
+    if dH is not None:
+        _shape(dH, H.shape, "dH")
+    if k:
+        mean = None
+    else:
+        _shape(mean, (T,), "mean")
+    if out is None:
+        if bias is None:
+            bias = not k
+        dX = torch.empty_like(H)
+        dgamma = torch.empty_like(gamma) if want_dw else None
+        dbeta = torch.empty_like(gamma) if want_dw and bias else None
+    else:
+        dX, dgamma, dbeta = out
+        _shape(dX, H.shape, "dX")
+        if not want_dw:
+            dgamma = dbeta = None
+        elif dgamma is None:
+            raise ValueError("dgamma: expected a tensor (or want_dw=False)")
+        else:
+            _shape(dgamma, (d,), "dgamma")
+        if bias is False:
+            dbeta = None
+        if dbeta is not None:
+            _shape(dbeta, (d,), "dbeta")
+    if ws is None and want_dw:
+        ws = _ws(norm_bwd_workspace_bytes(H.dtype, T, d), H.device)
+    device, stream = _here_of(H)
+    st = _native().norm_bwd(device, k, dt, T, d, H, dY, dH, gamma, mean, rstd, dX, dgamma, dbeta, ws,
+                            0 if ws is None else ws.numel(), stream)
+    _check(st, "sdp_norm_bwd")
+    return dX, dgamma, dbeta
+
+
+def embed_fwd(E, ids, scale=1.0, out=None):
+    """scale * E[ids] for E [V][d] and int32 or int64 ids [T]; zeros where an id lies outside [0, V) -> Y [T][d]."""
+    V, d = E.shape
+    (T,) = ids.shape
+    if out is None:
+        out = torch.empty((T, d), dtype=E.dtype, device=E.device)
+    else:
+        _shape(out, (T, d), "Y")
+    device, stream = _here_of(E)
+    st = _native().embed_fwd(device, _dtype_of(E, "E"), _id_type_of(ids, "ids"), T, V, d, scale, E, ids, out, stream)
+    _check(st, "sdp_embed_fwd")
+    return out
+
+
+def embed_bwd_workspace_bytes(dtype, T, V, d):
+    return int(lib().sdp_embed_bwd_workspace_bytes(_DTYPES[dtype], T, V, d))
+
+
+def embed_bwd(dY, ids, V, scale=1.0, out=None, ws=None):
+    """Gradient of embed_fwd's E: dE [V][d], every row (zeros where no id names it)."""
+    T, d = dY.shape
+    _shape(ids, (T,), "ids")
+    if out is None:
+        out = torch.empty((V, d), dtype=dY.dtype, device=dY.device)
+    else:
+        _shape(out, (V, d), "dE")
+    dt = _dtype_of(dY, "dY")
+    if ws is None:
+        ws = _ws(embed_bwd_workspace_bytes(dY.dtype, T, V, d), dY.device)
+    device, stream = _here_of(dY)
+    st = _native().embed_bwd(device, dt, _id_type_of(ids, "ids"), T, V, d, scale, dY, ids, out, ws, ws.numel(), stream)
+    _check(st, "sdp_embed_bwd")
+    return out
+
+
+def label_scale(labels, V, out=None):
+    """labels int32 or int64 [T] -> fp32 GPU tensor [1]: 1 / max(1, number of labels in [0, V)), token_loss's scale_dev for a mean."""
+    if out is None:
+        out = torch.empty((1,), dtype=torch.float32, device=labels.device)
+    else:
+        _shape(out, (1,), "scale")
+    device, stream = _here_of(labels)
+    st = _native().label_scale(device, _id_type_of(labels, "labels"), labels.numel(), V, labels, out, stream)
+    _check(st, "sdp_label_scale")
+    return out
+
+
+def token_loss(Z, labels, scale=1.0, scale_dev=None, want_grad=True, out=None):
+    """Cross-entropy of logits Z [T][V] (rows may lie apart) against int32 or int64 labels [T], with its gradient.
+
+    Rows whose label lies outside [0, V) have no part in it.  With c = scale * scale_dev[0] (scale_dev: fp32 tensor on the GPU,
+    None = 1), returns (nll [T], lse [T], dZ [T][V], loss [1]): loss = c * sum(nll) and its gradient by Z; dZ is None with
+    want_grad=False.  `out` = (nll, lse, dZ, loss) preallocated: dZ may be Z, lse and loss may be None (not wanted)."""
+    T, V = Z.shape
+    dt = _dtype_of(Z, "Z")
+    _shape(labels, (T,), "labels")
+    if scale_dev is not None:
+        _shape(scale_dev, (1,), "scale_dev")
+    if out is None:
+        nll, lse = (torch.empty((T,), dtype=torch.float32, device=Z.device) for _ in range(2))
+        dZ = torch.empty_strided(Z.shape, Z.stride(), dtype=Z.dtype, device=Z.device) if want_grad else None
+        loss = torch.empty((1,), dtype=torch.float32, device=Z.device)
+    else:
+        nll, lse, dZ, loss = out
+        _shape(nll, (T,), "nll")
+        if lse is not None:
+            _shape(lse, (T,), "lse")
+        if loss is not None:
+            _shape(loss, (1,), "loss")
+        if not want_grad:
+            dZ = None
+        elif dZ is None:
+            raise ValueError("dZ: expected a tensor (or want_grad=False)")
+        else:
+            _shape(dZ, Z.shape, "dZ")
+            if T > 1 and dZ.stride(0) != Z.stride(0):
+                raise ValueError("dZ: expected the strides of Z")
+    device, stream = _here_of(Z)
+    st = _native().token_loss(device, dt, _id_type_of(labels, "labels"), T, V, Z.stride(0) if T > 1 else V, scale, Z, labels,
+                              scale_dev, nll, lse, dZ, loss, stream)
+    _check(st, "sdp_token_loss")
+    return nll, lse, dZ, loss
 
 
 def profile_enable(on=True):

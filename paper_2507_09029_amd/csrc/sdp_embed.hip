@@ -1,0 +1,328 @@
+// Token embedding: rows of a matrix by token id, scaled, and the gradient of the matrix.
+//
+//   forward   Y[t] = scale E[id_t]            backward  dE[v] = scale sum_{t : id_t = v} dY[t]
+//
+// Both are bound by memory.  The backward pass turns the scatter into a gather: tokens are sorted by id, and the rows of dY that
+// belong to one row of dE are then neighbours in the sorted order, to be summed by one wave in registers.  No atomics on floats: each
+// row's sum has one order, given by the ids alone.
+//
+// The sort is one launch in which no workgroup waits for another.  Each owns a range of ids and goes through all T ids itself, twice:
+// the first time it counts, how many ids lie below its range (where its part of the order starts) and how often each id of its
+// range occurs; the second time it writes the tokens of its range to their places.  The ids are few bytes and come from
+// the cache for all workgroups but the first, so that T / 1024 steps a workgroup take less than the launches and the waiting of a sort
+// by digits.
+//
+// A token that occurs often (the most frequent of a text are several percent of it; in a padded batch one may be all) would be
+// one wave's long sum.  The sorted order is therefore cut into chunks of kChunk tokens, summed by a wave each (for 512 columns): a
+// row whose tokens lie within a chunk is finished there, the others leave partial sums in fp32, which a last launch adds up.
+#include <cmath>
+
+#include "sdp_internal.h"
+#include "sdp_rows.h"
+
+namespace {
+
+using sdp::Row;
+using sdp::u32x4;
+
+struct EmbedFwd {
+    const void *E, *ids;
+    void* Y;
+    int T, V, d, wide;
+    float scale;
+};
+
+// One wave copies a row.
+template <int BF16>
+__global__ __launch_bounds__(256) void embed_fwd_kernel(EmbedFwd a) {
+    typedef Row<BF16> Rw;
+    typedef typename Rw::Elem Elem;
+    constexpr int N = Rw::N;
+    const int64_t t = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    if (t >= a.T) return;
+    const int lane = threadIdx.x & 63, id = sdp::token_id(a.ids, a.wide, t, a.V);
+    const Elem* in = (const Elem*)a.E + (int64_t)id * a.d;
+    Elem* out = (Elem*)a.Y + t * a.d;
+    for (int e = lane * N; e < a.d; e += 64 * N) {
+        u32x4 w = {0, 0, 0, 0};
+        if (id >= 0) {
+            float v[N];
+            Rw::unpack(Rw::load(in, e, a.d), v);
+#pragma unroll
+            for (int k = 0; k < N; ++k) v[k] *= a.scale;
+            w = Rw::pack(v);
+        }
+        Rw::store(out, e, a.d, w);
+    }
+}
+
+constexpr int kSortWaves = 16, kSortGroups = 256, kMaxRange = 960, kChunk = 32;
+
+struct Sorted {
+    int32_t* order; // [T] tokens, by id, then by place
+    int32_t* ids;   // [T] their ids
+    int32_t* start; // [V + 1] where a row's tokens start; start[V] = number of tokens that have an id
+};
+
+// Ids per workgroup, and the workgroups
+int sort_range(int V) {
+    const int r = (V + kSortGroups - 1) / kSortGroups;
+    return r < kMaxRange ? r : kMaxRange;
+}
+
+__global__ __launch_bounds__(kSortWaves * 64) void embed_sort_kernel(const void* __restrict__ ids, int wide, int T, int V, int range,
+                                                                     int bits, Sorted out) {
+    extern __shared__ int hist[]; // [kSortWaves][range]: a wave's tokens of each id, then where its next one goes
+    __shared__ int sums[kSortWaves], below_all[kSortWaves];
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+    const int lo = blockIdx.x * range, n = min(range, V - lo);
+    for (int i = tid; i < kSortWaves * range; i += kSortWaves * 64) hist[i] = 0;
+    __syncthreads();
+    // each wave has an unbroken piece of the tokens
+    const int64_t piece = ((int64_t)T + kSortWaves * 64 - 1) / (kSortWaves * 64) * 64;
+    const int64_t begin = wave * piece, end = begin + piece < T ? begin + piece : T;
+    int below = 0;
+    int* mine = hist + wave * range;
+#pragma unroll 8
+    for (int64_t t = begin + lane; t < end; t += 64) {
+        const int id = sdp::token_id(ids, wide, t, V);
+        below += id >= 0 && id < lo;
+        const int k = id - lo;
+        if (id >= lo && k < n) atomicAdd(&mine[k], 1);
+    }
+#pragma unroll
+    for (int s = 32; s >= 1; s >>= 1) below += __shfl_xor(below, s, 64);
+    if (lane == 0) below_all[wave] = below;
+    __syncthreads();
+    // an id per thread (kMaxRange <= threads): its tokens, then exclusive sums over the ids before it
+    int total = 0;
+    if (tid < n)
+        for (int w = 0; w < kSortWaves; ++w) total += hist[w * range + tid];
+    int before = total;
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) {
+        const int v = __shfl_up(before, s, 64);
+        if (lane >= s) before += v;
+    }
+    if (lane == 63) sums[wave] = before;
+    __syncthreads();
+    int at = before - total;
+    for (int w = 0; w < kSortWaves; ++w) at += below_all[w] + (w < wave ? sums[w] : 0);
+    if (tid < n) {
+        out.start[lo + tid] = at;
+        if (lo + tid == V - 1) out.start[V] = at + total;
+        for (int w = 0; w < kSortWaves; ++w) {
+            const int c = hist[w * range + tid];
+            hist[w * range + tid] = at;
+            at += c;
+        }
+    }
+    __syncthreads();
+    // 64 tokens at a time: those with the same id as this lane's, by the bits of the id, and its rank among them
+    for (int64_t b = begin; b < end; b += 64) {
+        const int64_t t = b + lane;
+        const int id = t < end ? sdp::token_id(ids, wide, t, V) : -1;
+        const int k = id - lo;
+        const bool hit = id >= lo && k < n;
+        uint64_t peers = __ballot(hit);
+        if (peers == 0) continue;
+        for (int i = 0; i < bits; ++i) {
+            const uint64_t set = __ballot((k >> i) & 1);
+            peers &= (k >> i) & 1 ? set : ~set;
+        }
+        // the wave's own count, read here, was written by another of its lanes
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (hit) {
+            const int rank = __popcll(peers & ((1ull << lane) - 1));
+            const int place = mine[k] + rank;
+            out.order[place] = (int)t;
+            out.ids[place] = id;
+            if (rank == 0) mine[k] = place + __popcll(peers);
+        }
+    }
+}
+
+struct EmbedBwd {
+    const void* dY;
+    void* dE;
+    Sorted s;
+    float* part; // [chunks][2][d]: of a row that starts in an earlier chunk, of one that goes on in the next
+    int T, V, d, chunks, slabs;
+    float scale;
+};
+
+template <int BF16>
+__device__ inline void write_row(const EmbedBwd& a, int id, int e, const float (&acc)[Row<BF16>::N]) {
+    float v[Row<BF16>::N];
+#pragma unroll
+    for (int k = 0; k < Row<BF16>::N; ++k) v[k] = acc[k] * a.scale;
+    Row<BF16>::store((typename Row<BF16>::Elem*)a.dE + (int64_t)id * a.d, e, a.d, Row<BF16>::pack(v));
+}
+
+// A wave has a chunk of the sorted tokens, or 64 rows of dE of which it clears the empty ones, and a slab of 64 pieces of the columns.
+template <int BF16>
+__global__ __launch_bounds__(256) void embed_sum_kernel(EmbedBwd a) {
+    typedef Row<BF16> Rw;
+    typedef typename Rw::Elem Elem;
+    constexpr int N = Rw::N;
+    const int lane = threadIdx.x & 63;
+    const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int64_t job = item / a.slabs;
+    const int e = ((int)(item - job * a.slabs) * 64 + lane) * N;
+    if (job >= a.chunks) {
+        const int64_t v = (job - a.chunks) * 64;
+        if (v >= a.V) return;
+        const bool empty = v + lane < a.V && a.s.start[v + lane] == a.s.start[v + lane + 1];
+        uint64_t left = __ballot(empty);
+        while (left) {
+            const int i = __ffsll((unsigned long long)left) - 1;
+            left &= left - 1;
+            if (e < a.d) Rw::store((Elem*)a.dE + (v + i) * a.d, e, a.d, u32x4{0, 0, 0, 0});
+        }
+        return;
+    }
+    const int n = a.s.start[a.V], p0 = (int)job * kChunk;
+    if (p0 >= n) return;
+    const int cnt = min(kChunk, n - p0);
+    const int tok = lane < cnt ? a.s.order[p0 + lane] : 0, id = lane < cnt ? a.s.ids[p0 + lane] : -1;
+    const int prev = p0 > 0 ? a.s.ids[p0 - 1] : -1, next = p0 + cnt < n ? a.s.ids[p0 + cnt] : -1;
+    float acc[N] = {};
+    bool whole = __builtin_amdgcn_readlane(id, 0) != prev; // the row at hand starts in this chunk
+    for (int j0 = 0; j0 < cnt; j0 += 8) {
+        u32x4 w[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            w[j] = u32x4{0, 0, 0, 0};
+            if (j0 + j < cnt && e < a.d) w[j] = Rw::load((const Elem*)a.dY + (int64_t)__builtin_amdgcn_readlane(tok, j0 + j) * a.d, e, a.d);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (j0 + j >= cnt) break;
+            float v[N];
+            Rw::unpack(w[j], v);
+#pragma unroll
+            for (int k = 0; k < N; ++k) acc[k] += v[k];
+            const int row = __builtin_amdgcn_readlane(id, j0 + j);
+            const bool last = j0 + j == cnt - 1;
+            const int after = last ? next : __builtin_amdgcn_readlane(id, j0 + j + 1);
+            if (row == after && !last) continue;
+            if (e < a.d) {
+                if (whole && row != after) {
+                    write_row<BF16>(a, row, e, acc);
+                } else {
+                    float* p = a.part + (job * 2 + (whole ? 1 : 0)) * a.d;
+#pragma unroll
+                    for (int k = 0; k < N; ++k)
+                        if (e + k < a.d) p[e + k] = acc[k];
+                }
+            }
+            whole = true;
+#pragma unroll
+            for (int k = 0; k < N; ++k) acc[k] = 0.f;
+        }
+    }
+}
+
+// A wave looks at a chunk: if a row starts there and goes on, it adds up the row's partial sums, in the order of the chunks.
+template <int BF16>
+__global__ __launch_bounds__(256) void embed_join_kernel(EmbedBwd a) {
+    constexpr int N = Row<BF16>::N;
+    const int lane = threadIdx.x & 63;
+    const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int64_t job = item / a.slabs;
+    const int e = ((int)(item - job * a.slabs) * 64 + lane) * N;
+    const int n = a.s.start[a.V], p0 = (int)job * kChunk, p1 = p0 + kChunk;
+    if (job >= a.chunks || p1 >= n || e >= a.d) return;
+    const int row = a.s.ids[p1 - 1];
+    if (a.s.ids[p1] != row || a.s.start[row] < p0) return;
+    const int last = (a.s.start[row + 1] - 1) / kChunk;
+    float acc[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) acc[k] = e + k < a.d ? a.part[(job * 2 + 1) * a.d + e + k] : 0.f;
+#pragma unroll 4
+    for (int64_t c = job + 1; c <= last; ++c)
+#pragma unroll
+        for (int k = 0; k < N; ++k) acc[k] += e + k < a.d ? a.part[c * 2 * a.d + e + k] : 0.f;
+    write_row<BF16>(a, row, e, acc);
+}
+
+int check_embed(int dtype, int id_type, int T, int V, int d) {
+    if (dtype != SDP_F32 && dtype != SDP_BF16) return SDP_ERR_INVALID_ARG;
+    if (id_type != SDP_I32 && id_type != SDP_I64) return SDP_ERR_INVALID_ARG;
+    if (T < 0 || V < 1 || d < 1) return SDP_ERR_INVALID_ARG;
+    return T > SDP_MAX_TOKENS ? SDP_ERR_SHAPE : SDP_OK;
+}
+
+int chunks_of(int T) { return (int)(((int64_t)T + kChunk - 1) / kChunk); }
+int slabs_of(int dtype, int d) { return (d + (dtype == SDP_BF16 ? 511 : 255)) / (dtype == SDP_BF16 ? 512 : 256); }
+
+struct Layout {
+    size_t ids, start, part, all;
+};
+Layout layout(int T, int V, int d) {
+    Layout l;
+    l.ids = sdp::round_up((size_t)T * 4, 256);
+    l.start = 2 * l.ids;
+    l.part = l.start + sdp::round_up(((size_t)V + 1) * 4, 256);
+    l.all = l.part + sdp::round_up((size_t)chunks_of(T) * 2 * d * sizeof(float), 256);
+    return l;
+}
+
+} // namespace
+
+extern "C" int sdp_embed_fwd(int dtype, int id_type, int T, int V, int d, float scale, const void* E, const void* ids, void* Y,
+                             void* stream) {
+    const int rc = check_embed(dtype, id_type, T, V, d);
+    if (rc != SDP_OK) return rc;
+    if (!std::isfinite(scale)) return SDP_ERR_INVALID_ARG;
+    if (T == 0) return SDP_OK;
+    const size_t es = dtype == SDP_BF16 ? 2 : 4, is = id_type == SDP_I64 ? 8 : 4;
+    if (!E || !ids || !Y || !sdp::aligned_to(E, es) || !sdp::aligned_to(Y, es) || !sdp::aligned_to(ids, is)) return SDP_ERR_INVALID_ARG;
+    if (sdp::overlap({{Y, (size_t)T * d * es}}, {{E, (size_t)V * d * es}, {ids, (size_t)T * is}})) return SDP_ERR_INVALID_ARG;
+    hipStream_t s = (hipStream_t)stream;
+    const EmbedFwd a{E, ids, Y, T, V, d, id_type == SDP_I64, scale};
+    sdp::ProfileScope ps("embed_fwd", s);
+    const unsigned groups = (unsigned)(((int64_t)T + 3) / 4);
+    if (dtype == SDP_BF16) embed_fwd_kernel<1><<<groups, 256, 0, s>>>(a);
+    else embed_fwd_kernel<0><<<groups, 256, 0, s>>>(a);
+    return sdp::launch_status();
+}
+
+extern "C" size_t sdp_embed_bwd_workspace_bytes(int dtype, int T, int V, int d) {
+    if (check_embed(dtype, SDP_I32, T, V, d) != SDP_OK) return 0;
+    return layout(T, V, d).all;
+}
+
+extern "C" int sdp_embed_bwd(int dtype, int id_type, int T, int V, int d, float scale, const void* dY, const void* ids, void* dE,
+                             void* ws, size_t ws_bytes, void* stream) {
+    const int rc = check_embed(dtype, id_type, T, V, d);
+    if (rc != SDP_OK) return rc;
+    if (!std::isfinite(scale)) return SDP_ERR_INVALID_ARG;
+    const size_t es = dtype == SDP_BF16 ? 2 : 4, is = id_type == SDP_I64 ? 8 : 4;
+    if (!dE || (T > 0 && (!dY || !ids))) return SDP_ERR_INVALID_ARG;
+    if (!sdp::aligned_to(dE, es) || !sdp::aligned_to(dY, es) || !sdp::aligned_to(ids, is)) return SDP_ERR_INVALID_ARG;
+    if (T > 0 && sdp::overlap({{dE, (size_t)V * d * es}}, {{dY, (size_t)T * d * es}, {ids, (size_t)T * is}})) return SDP_ERR_INVALID_ARG;
+    const Layout l = layout(T, V, d);
+    if (!ws || !sdp::aligned16(ws) || ws_bytes < l.all) return SDP_ERR_WORKSPACE;
+    hipStream_t s = (hipStream_t)stream;
+    char* w = (char*)ws;
+    EmbedBwd a{dY, dE, {(int32_t*)w, (int32_t*)(w + l.ids), (int32_t*)(w + l.start)}, (float*)(w + l.part), T, V, d, chunks_of(T),
+               slabs_of(dtype, d), scale};
+    sdp::ProfileScope ps("embed_bwd", s);
+    const int range = sort_range(V);
+    int bits = 0;
+    while ((1 << bits) < range) ++bits;
+    embed_sort_kernel<<<(V + range - 1) / range, kSortWaves * 64, (size_t)kSortWaves * range * sizeof(int), s>>>(
+        ids, id_type == SDP_I64, T, V, range, bits, a.s);
+    int st = sdp::launch_status();
+    if (st != SDP_OK) return st;
+    const int64_t sum = ((int64_t)a.chunks + ((int64_t)V + 63) / 64) * a.slabs, join = (int64_t)a.chunks * a.slabs;
+    const unsigned gs = (unsigned)((sum + 3) / 4), gj = (unsigned)((join + 3) / 4);
+    if (dtype == SDP_BF16) embed_sum_kernel<1><<<gs, 256, 0, s>>>(a);
+    else embed_sum_kernel<0><<<gs, 256, 0, s>>>(a);
+    st = sdp::launch_status();
+    if (st != SDP_OK || a.chunks < 2) return st;
+    if (dtype == SDP_BF16) embed_join_kernel<1><<<gj, 256, 0, s>>>(a);
+    else embed_join_kernel<0><<<gj, 256, 0, s>>>(a);
+    return sdp::launch_status();
+}

@@ -37,6 +37,7 @@ inline int hip_status(hipError_t e) { return e == hipSuccess ? SDP_OK : SDP_ERR_
 inline int launch_status() { return hip_status(hipGetLastError()); }
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool aligned_to(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 inline size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 // Leading dimension of `rows` rows of `min` bf16 elements that a contraction reads from the workspace: whole 128-byte lines, so

@@ -1,0 +1,231 @@
+// Cross-entropy of rows of logits against labels, with the gradient from the same read of the logits.
+//
+//   lse = log sum_j exp z_j,  nll = lse - z_label,  dz_j = c (exp(z_j - lse) - [j = label])
+//
+// Bound by memory: the logits are the largest tensor of a training step (8192 x 32000 bf16: 524 MB), and the least that can be
+// moved is one read and one write of them.  A workgroup holds a row in registers, as it is stored, from the read to the write: 16 pieces of
+// 16 bytes a lane at most, so that a row of 32000 bf16 takes four waves and several rows are at work on a CU.  Rows of more
+// than 131072 bf16 or 65536 fp32 values are read twice.
+//
+// exp(z - max) is 2^((z - max) L), L = log2 e, on the hardware's 2^x.  The difference comes first: z L - max L in one step, with max L
+// rounded, overflows or is far off where a row's values are near the type's lowest, as masks write them.
+#include <cmath>
+#include <type_traits>
+
+#include "sdp_internal.h"
+#include "sdp_rows.h"
+
+namespace {
+
+using sdp::Row;
+using sdp::u32x4;
+
+constexpr float kLog2e = 1.44269504088896340736f;
+
+struct Loss {
+    const void *Z, *labels;
+    const float* scale_dev;
+    float *nll, *lse;
+    void* dZ;
+    int T, V, wide;
+    int64_t ldz;
+    float scale;
+};
+
+// maximum / sum over a workgroup, in a fixed order; every thread has the result
+template <int WAVES, bool MAX>
+__device__ inline float group_all(float x, float* lds) {
+    x = MAX ? sdp::wave_max(x) : sdp::wave_sum(x);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = lds[0];
+#pragma unroll
+    for (int i = 1; i < WAVES; ++i) x = MAX ? fmaxf(x, lds[i]) : x + lds[i];
+    return x;
+}
+
+// value of a piece's word behind the row's end: -inf
+template <int BF16>
+constexpr uint32_t minus_inf() {
+    return BF16 ? 0xFF80FF80u : 0xFF800000u;
+}
+
+// PIECES > 0: pieces a lane holds, the row has no more; 0: the row is read again for the gradient
+template <int BF16, int WAVES, int PIECES>
+__global__ __launch_bounds__(WAVES * 64) void token_loss_kernel(Loss a) {
+    typedef Row<BF16> Rw;
+    typedef typename Rw::Elem Elem;
+    constexpr int N = Rw::N, TH = WAVES * 64, P = PIECES ? PIECES : 1;
+    __shared__ float lds[2][WAVES], at_label;
+    const int64_t row = blockIdx.x;
+    const int tid = threadIdx.x, V = a.V, label = sdp::token_id(a.labels, a.wide, row, V);
+    const Elem* z = (const Elem*)a.Z + row * a.ldz;
+    Elem* dz = (Elem*)a.dZ + row * a.ldz;
+    if (label < 0) {
+        if (tid == 0) {
+            a.nll[row] = 0.f;
+            if (a.lse) a.lse[row] = 0.f;
+        }
+        if (a.dZ)
+            for (int64_t e = tid * N; e < V; e += TH * N) Rw::store(dz, (int)e, V, u32x4{0, 0, 0, 0});
+        return;
+    }
+    const float c = a.scale * (a.scale_dev ? *a.scale_dev : 1.f);
+    u32x4 w[P];
+    float m = -INFINITY, sum = 0.f;
+    if (tid == 0) at_label = Rw::one(z + label); // read before anything is written: dZ may be Z
+    if (PIECES) {
+#pragma unroll
+        for (int i = 0; i < P; ++i) w[i] = Rw::load(z, (tid + i * TH) * N, V, minus_inf<BF16>());
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            float v[N];
+            Rw::unpack(w[i], v);
+#pragma unroll
+            for (int k = 0; k < N; ++k) m = fmaxf(m, v[k]);
+        }
+    } else {
+        for (int64_t e = tid * N; e < V; e += TH * N) {
+            float v[N];
+            Rw::unpack(Rw::load(z, (int)e, V, minus_inf<BF16>()), v);
+#pragma unroll
+            for (int k = 0; k < N; ++k) m = fmaxf(m, v[k]);
+        }
+    }
+    m = group_all<WAVES, true>(m, lds[0]);
+    auto power = [&](float v) { return __builtin_amdgcn_exp2f((v - m) * kLog2e); };
+    if (PIECES) {
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            float v[N];
+            Rw::unpack(w[i], v);
+#pragma unroll
+            for (int k = 0; k < N; ++k) sum += power(v[k]);
+        }
+    } else {
+        for (int64_t e = tid * N; e < V; e += TH * N) {
+            float v[N];
+            Rw::unpack(Rw::load(z, (int)e, V, minus_inf<BF16>()), v);
+#pragma unroll
+            for (int k = 0; k < N; ++k) sum += power(v[k]);
+        }
+    }
+    sum = group_all<WAVES, false>(sum, lds[1]);
+    if (tid == 0) {
+        const float log_sum = logf(sum);
+        a.nll[row] = (m - at_label) + log_sum;
+        if (a.lse) a.lse[row] = m + log_sum;
+    }
+    if (!a.dZ) return;
+    const float inv = c / sum;
+    auto gradient = [&](int e, const u32x4& piece) {
+        float v[N];
+        Rw::unpack(piece, v);
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = power(v[k]) * inv - (e + k == label ? c : 0.f);
+        Rw::store(dz, e, V, Rw::pack(v));
+    };
+    if (PIECES) {
+#pragma unroll
+        for (int i = 0; i < P; ++i)
+            if ((tid + i * TH) * N < V) gradient((tid + i * TH) * N, w[i]);
+    } else {
+        for (int64_t e = tid * N; e < V; e += TH * N) gradient((int)e, Rw::load(z, (int)e, V));
+    }
+}
+
+// Sum of a double over a workgroup of 1024, in a fixed order; valid in thread 0
+template <class S>
+__device__ inline S group_sum(S x) {
+    __shared__ S lds[16];
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) x += __shfl_xor(x, d, 64);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = lds[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) x += lds[i];
+    return x;
+}
+
+__global__ __launch_bounds__(1024) void loss_sum_kernel(const float* __restrict__ nll, int T, float scale, const float* scale_dev,
+                                                        float* loss) {
+    double x = 0.0;
+#pragma unroll 8
+    for (int t = threadIdx.x; t < T; t += 1024) x += (double)nll[t];
+    x = group_sum(x);
+    if (threadIdx.x == 0) *loss = (float)(x * ((double)scale * (scale_dev ? (double)*scale_dev : 1.0)));
+}
+
+__global__ __launch_bounds__(1024) void label_scale_kernel(const void* __restrict__ labels, int wide, int T, int V, float* scale) {
+    int n = 0;
+#pragma unroll 8
+    for (int t = threadIdx.x; t < T; t += 1024) n += sdp::token_id(labels, wide, t, V) >= 0;
+    n = group_sum(n);
+    if (threadIdx.x == 0) *scale = 1.0f / (float)(n > 1 ? n : 1);
+}
+
+// The fewest waves that hold a row with 16 pieces a lane, fewer pieces where those do
+template <class F>
+void by_row(int bf16, int V, F&& launch) {
+    const int n = bf16 ? 8 : 4;
+    auto with = [&](auto b) {
+        const int64_t pieces = ((int64_t)V + n - 1) / n;
+        auto go = [&](auto waves, auto p) { launch(b, waves, p); };
+        using std::integral_constant;
+        if (pieces <= 256) go(integral_constant<int, 4>{}, integral_constant<int, 1>{});
+        else if (pieces <= 1024) go(integral_constant<int, 4>{}, integral_constant<int, 4>{});
+        else if (pieces <= 2048) go(integral_constant<int, 4>{}, integral_constant<int, 8>{});
+        else if (pieces <= 4096) go(integral_constant<int, 4>{}, integral_constant<int, 16>{});
+        else if (pieces <= 8192) go(integral_constant<int, 8>{}, integral_constant<int, 16>{});
+        else if (pieces <= 16384) go(integral_constant<int, 16>{}, integral_constant<int, 16>{});
+        else go(integral_constant<int, 16>{}, integral_constant<int, 0>{});
+    };
+    if (bf16) with(std::integral_constant<int, 1>{});
+    else with(std::integral_constant<int, 0>{});
+}
+
+} // namespace
+
+extern "C" int sdp_token_loss(int dtype, int id_type, int T, int V, int64_t ldz, float scale, const void* Z, const void* labels,
+                              const float* scale_dev, float* nll, float* lse, void* dZ, float* loss, void* stream) {
+    if (dtype != SDP_F32 && dtype != SDP_BF16) return SDP_ERR_INVALID_ARG;
+    if (id_type != SDP_I32 && id_type != SDP_I64) return SDP_ERR_INVALID_ARG;
+    if (T < 0 || V < 1 || !std::isfinite(scale)) return SDP_ERR_INVALID_ARG;
+    if (T > SDP_MAX_TOKENS || ldz < V || ldz > ((int64_t)1 << 40)) return SDP_ERR_SHAPE;
+    const size_t es = dtype == SDP_BF16 ? 2 : 4, is = id_type == SDP_I64 ? 8 : 4, st = (size_t)T * 4;
+    if (T > 0 && (!Z || !labels || !nll)) return SDP_ERR_INVALID_ARG;
+    if (!sdp::aligned_to(Z, es) || !sdp::aligned_to(dZ, es) || !sdp::aligned_to(labels, is)) return SDP_ERR_INVALID_ARG;
+    for (const float* p : {scale_dev, (const float*)nll, (const float*)lse, (const float*)loss})
+        if (!sdp::aligned_to(p, 4)) return SDP_ERR_INVALID_ARG;
+    const size_t rows = T > 0 ? ((size_t)(T - 1) * ldz + V) * es : 0;
+    const sdp::Extent eZ{Z, rows}, el{labels, (size_t)T * is}, ec{scale_dev, scale_dev ? 4u : 0u}, on{nll, st}, os{lse, lse ? st : 0},
+        oz{dZ, dZ ? rows : 0}, o1{loss, loss ? 4u : 0u};
+    if (T > 0 && ((dZ != Z && sdp::overlap({oz}, {eZ})) || sdp::overlap({oz, on, os, o1}, {el, ec}) || sdp::overlap({on, os, o1}, {eZ, oz}) ||
+                  sdp::overlap({on}, {os, o1}) || sdp::overlap({os}, {o1})))
+        return SDP_ERR_INVALID_ARG;
+    hipStream_t s = (hipStream_t)stream;
+    sdp::ProfileScope ps("token_loss", s);
+    int rc = SDP_OK;
+    if (T > 0) {
+        const Loss a{Z, labels, scale_dev, nll, lse, dZ, T, V, id_type == SDP_I64, ldz, scale};
+        by_row(dtype == SDP_BF16, V, [&](auto b, auto waves, auto p) {
+            token_loss_kernel<b.value, waves.value, p.value><<<(unsigned)T, waves.value * 64, 0, s>>>(a);
+        });
+        rc = sdp::launch_status();
+    }
+    if (rc != SDP_OK || !loss) return rc;
+    loss_sum_kernel<<<1, 1024, 0, s>>>(nll, T, scale, scale_dev, loss);
+    return sdp::launch_status();
+}
+
+extern "C" int sdp_label_scale(int id_type, int T, int V, const void* labels, float* scale, void* stream) {
+    if (id_type != SDP_I32 && id_type != SDP_I64) return SDP_ERR_INVALID_ARG;
+    if (T < 0 || V < 1 || !scale || (T > 0 && !labels)) return SDP_ERR_INVALID_ARG;
+    if (T > SDP_MAX_TOKENS) return SDP_ERR_SHAPE;
+    if (!sdp::aligned_to(labels, id_type == SDP_I64 ? 8 : 4) || !sdp::aligned_to(scale, 4)) return SDP_ERR_INVALID_ARG;
+    if (T > 0 && sdp::overlap({{scale, 4}}, {{labels, (size_t)T * (id_type == SDP_I64 ? 8 : 4)}})) return SDP_ERR_INVALID_ARG;
+    sdp::ProfileScope ps("label_scale", (hipStream_t)stream);
+    label_scale_kernel<<<1, 1024, 0, (hipStream_t)stream>>>(labels, id_type == SDP_I64, T, V, scale);
+    return sdp::launch_status();
+}

@@ -17,37 +17,49 @@
 namespace {
 
 // A pointer parameter: its name in messages and what it points to: 'a' the type given by the call's dtype argument,
-// 'i' int32, 'f' float32, in capitals where None stands for a null pointer; 0 for parameters passed as they are
-// (integers, workspace and stream addresses).
+// 'i' int32, 'f' float32, 't' int32 or int64, 'w' bytes, 'z' as 'a' but a
+// matrix whose rows may lie apart (the caller passes their distance), in capitals where None stands for a null pointer; 0 for parameters
+// passed as they are (numbers, workspace and stream addresses).
 struct Param {
     const char* name = nullptr;
     char kind = 0;
 };
 
 bool type_error(const Param& p, c10::ScalarType t) {
-    const char* n = t == c10::kFloat ? "torch.float32" : t == c10::kBFloat16 ? "torch.bfloat16" : "torch.int32";
+    const char* n = t == c10::kFloat ? "torch.float32" : t == c10::kBFloat16 ? "torch.bfloat16" : t == c10::kByte ? "torch.uint8" : "torch.int32";
     PyErr_Format(PyExc_TypeError, "%s: expected a contiguous %s tensor on the GPU", p.name, n);
     return false;
 }
 
+// `device`: where every tensor has to be, -1 = anywhere
 template <class A>
-bool take(PyObject* o, const Param& p, c10::ScalarType act, A& out) {
+bool take(PyObject* o, const Param& p, c10::ScalarType act, int device, A& out) {
     if constexpr (std::is_pointer_v<A>) {
         if (p.kind == 0) {
             out = (A)PyLong_AsVoidPtr(o);
             return !PyErr_Occurred();
         }
-        const bool optional = p.kind == 'A' || p.kind == 'I';
+        const bool optional = p.kind >= 'A' && p.kind <= 'Z';
+        const char kind = optional ? (char)(p.kind - 'A' + 'a') : p.kind;
         if (optional && o == Py_None) {
             out = nullptr;
             return true;
         }
-        const c10::ScalarType want = p.kind == 'f' ? c10::kFloat : p.kind == 'i' || p.kind == 'I' ? c10::kInt : act;
+        c10::ScalarType want = kind == 'f' ? c10::kFloat : kind == 'i' || kind == 't' ? c10::kInt : kind == 'w' ? c10::kByte : act;
         if (!THPVariable_Check(o)) return type_error(p, want);
         const at::Tensor& t = THPVariable_Unpack(o);
-        if (!t.is_cuda() || !t.is_contiguous() || t.scalar_type() != want) return type_error(p, want);
+        if (kind == 't' && t.scalar_type() == c10::kLong) want = c10::kLong;
+        const bool rows_apart = kind == 'z' && t.dim() == 2 && (t.size(1) <= 1 || t.stride(1) == 1);
+        if (!t.is_cuda() || !(rows_apart || t.is_contiguous()) || t.scalar_type() != want) return type_error(p, want);
+        if (device >= 0 && t.get_device() != device) {
+            PyErr_Format(PyExc_ValueError, "%s: on cuda:%d, but the current device is cuda:%d", p.name, (int)t.get_device(), device);
+            return false;
+        }
         out = (A)t.data_ptr();
         return true;
+    } else if constexpr (std::is_floating_point_v<A>) {
+        out = (A)PyFloat_AsDouble(o);
+        return !PyErr_Occurred();
     } else if constexpr (std::is_unsigned_v<A>) {
         out = (A)PyLong_AsUnsignedLongLong(o);
         return !PyErr_Occurred();
@@ -64,7 +76,8 @@ bool take(PyObject* o, const Param& p, c10::ScalarType act, A& out) {
 }
 
 template <class... A, size_t... I>
-PyObject* call(int (*fn)(A...), const Param* params, int dtype_at, PyObject* const* args, Py_ssize_t n, std::index_sequence<I...>) {
+PyObject* call(int (*fn)(A...), const Param* params, int dtype_at, PyObject* const* args, Py_ssize_t n, std::index_sequence<I...>,
+               int device = -1) {
     if (n != (Py_ssize_t)sizeof...(A)) {
         PyErr_Format(PyExc_TypeError, "expected %zd arguments, got %zd", (Py_ssize_t)sizeof...(A), n);
         return nullptr;
@@ -75,7 +88,7 @@ PyObject* call(int (*fn)(A...), const Param* params, int dtype_at, PyObject* con
     std::tuple<A...> v;
     int rc = 0;
     try {
-        if (!(take(args[I], params[I], act, std::get<I>(v)) && ...)) return nullptr;
+        if (!(take(args[I], params[I], act, device, std::get<I>(v)) && ...)) return nullptr;
     } catch (const std::exception& e) { // a tensor without storage
         PyErr_SetString(PyExc_RuntimeError, e.what());
         return nullptr;
@@ -92,6 +105,18 @@ PyObject* call(int (*fn)(A...), const Param* params, int dtype_at, PyObject* con
     PyObject* py##_call(int (*f)(A...), PyObject* const* args, Py_ssize_t n) {                               \
         static_assert(sizeof(py##_params) / sizeof(Param) == sizeof...(A), "one entry per parameter");       \
         return call(f, py##_params, dtype_at, args, n, std::index_sequence_for<A...>{});                     \
+    }                                                                                                        \
+    PyObject* py(PyObject*, PyObject* const* args, Py_ssize_t n) { return py##_call(&fn, args, n); }
+
+// the same for calls whose first argument is the current device, where every tensor has to be
+#define SDP_ENTRY_HERE(py, fn, dtype_at, ...)                                                                \
+    const Param py##_params[] = {__VA_ARGS__};                                                               \
+    template <class... A>                                                                                    \
+    PyObject* py##_call(int (*f)(A...), PyObject* const* args, Py_ssize_t n) {                               \
+        static_assert(sizeof(py##_params) / sizeof(Param) == sizeof...(A), "one entry per parameter");       \
+        const long device = n > 0 ? PyLong_AsLong(args[0]) : 0;                                              \
+        if (device == -1 && PyErr_Occurred()) return nullptr;                                                \
+        return call(f, py##_params, dtype_at, args + 1, n - 1, std::index_sequence_for<A...>{}, (int)device); \
     }                                                                                                        \
     PyObject* py(PyObject*, PyObject* const* args, Py_ssize_t n) { return py##_call(&fn, args, n); }
 
@@ -113,9 +138,21 @@ SDP_ENTRY(block_bwd, sdp_block_bwd, 3, {}, {}, {}, {}, {}, {}, {}, {}, {}, {}, {
           {"LSE_save", 'f'}, {"G_save", 'a'}, {"U_save", 'a'}, {"dX", 'a'}, {"dW", 'A'}, {"dW", 'A'}, {"dW", 'A'}, {"dW", 'A'},
           {"dW", 'A'}, {}, {}, {})
 
+SDP_ENTRY_HERE(norm_fwd, sdp_norm_fwd, 1, {}, {}, {}, {}, {}, {"X", 'a'}, {"residual", 'A'}, {"gamma", 'a'}, {"beta", 'A'}, {"H", 'A'},
+               {"Y", 'a'}, {"mean", 'F'}, {"rstd", 'f'}, {})
+SDP_ENTRY_HERE(norm_bwd, sdp_norm_bwd, 1, {}, {}, {}, {}, {"H", 'a'}, {"dY", 'a'}, {"dH", 'A'}, {"gamma", 'a'}, {"mean", 'F'},
+               {"rstd", 'f'}, {"dX", 'a'}, {"dgamma", 'A'}, {"dbeta", 'A'}, {"ws", 'W'}, {}, {})
+SDP_ENTRY_HERE(embed_fwd, sdp_embed_fwd, 0, {}, {}, {}, {}, {}, {}, {"E", 'a'}, {"ids", 't'}, {"Y", 'a'}, {})
+SDP_ENTRY_HERE(embed_bwd, sdp_embed_bwd, 0, {}, {}, {}, {}, {}, {}, {"dY", 'a'}, {"ids", 't'}, {"dE", 'a'}, {"ws", 'w'}, {}, {})
+SDP_ENTRY_HERE(token_loss, sdp_token_loss, 0, {}, {}, {}, {}, {}, {}, {"Z", 'z'}, {"labels", 't'}, {"scale_dev", 'F'}, {"nll", 'f'},
+               {"lse", 'F'}, {"dZ", 'Z'}, {"loss", 'F'}, {})
+SDP_ENTRY_HERE(label_scale, sdp_label_scale, 0, {}, {}, {}, {"labels", 't'}, {"scale", 'f'}, {})
+
 #define SDP_METHOD(py) {#py, (PyCFunction)(void (*)(void))py, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {SDP_METHOD(mlp_fwd),   SDP_METHOD(mlp_bwd),   SDP_METHOD(attn_fwd), SDP_METHOD(attn_bwd),
-                         SDP_METHOD(block_fwd), SDP_METHOD(block_bwd), {nullptr, nullptr, 0, nullptr}};
+                         SDP_METHOD(block_fwd), SDP_METHOD(block_bwd),
+                         SDP_METHOD(norm_fwd),  SDP_METHOD(norm_bwd),  SDP_METHOD(embed_fwd), SDP_METHOD(embed_bwd),
+                         SDP_METHOD(token_loss), SDP_METHOD(label_scale), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_sdp_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 } // namespace
