@@ -56,39 +56,50 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(EmbedFwd a) {
     }
 }
 
-constexpr int kSortWaves = 16, kSortGroups = 256, kMaxRange = 960, kChunk = 32;
+constexpr int kSortWaves = 16, kSortGroups = 256, kMaxRange = 960, kChunk = 32, kAhead = 16;
 
 struct Sorted {
     int32_t* order; // [T] tokens, by id, then by place
     int32_t* ids;   // [T] their ids
     int32_t* start; // [V + 1] where a row's tokens start; start[V] = number of tokens that have an id
+    int2* spans;    // [chunks] {row, last chunk} of the row that starts in the chunk and goes on in the next, or {-1, 0}
 };
 
-// Ids per workgroup, and the workgroups
+// Ids per workgroup
 int sort_range(int V) {
     const int r = (V + kSortGroups - 1) / kSortGroups;
     return r < kMaxRange ? r : kMaxRange;
 }
 
+// ONCE: a wave's tokens are kAhead to a lane at most and stay in registers between the two times
+template <int ONCE>
 __global__ __launch_bounds__(kSortWaves * 64) void embed_sort_kernel(const void* __restrict__ ids, int wide, int T, int V, int range,
                                                                      int bits, Sorted out) {
     extern __shared__ int hist[]; // [kSortWaves][range]: a wave's tokens of each id, then where its next one goes
     __shared__ int sums[kSortWaves], below_all[kSortWaves];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int lo = blockIdx.x * range, n = min(range, V - lo);
-    for (int i = tid; i < kSortWaves * range; i += kSortWaves * 64) hist[i] = 0;
-    __syncthreads();
-    // each wave has an unbroken piece of the tokens
+    // each wave has an unbroken piece of the tokens, of which a lane takes every 64th
     const int64_t piece = ((int64_t)T + kSortWaves * 64 - 1) / (kSortWaves * 64) * 64;
     const int64_t begin = wave * piece, end = begin + piece < T ? begin + piece : T;
+    int id[kAhead];
+    auto request = [&](int64_t b) { // kAhead loads in flight: one after the other, their latency would be most of the time
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) id[i] = b + i * 64 + lane < end ? sdp::token_id(ids, wide, b + i * 64 + lane, V) : -1;
+    };
+    if (ONCE) request(begin);
+    for (int i = tid; i < kSortWaves * range; i += kSortWaves * 64) hist[i] = 0;
+    __syncthreads();
     int below = 0;
     int* mine = hist + wave * range;
-#pragma unroll 8
-    for (int64_t t = begin + lane; t < end; t += 64) {
-        const int id = sdp::token_id(ids, wide, t, V);
-        below += id >= 0 && id < lo;
-        const int k = id - lo;
-        if (id >= lo && k < n) atomicAdd(&mine[k], 1);
+    for (int64_t b = begin; b < end; b += 64 * kAhead) {
+        if (!ONCE) request(b);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            below += id[i] >= 0 && id[i] < lo;
+            const int k = id[i] - lo;
+            if (id[i] >= lo && k < n) atomicAdd(&mine[k], 1);
+        }
     }
 #pragma unroll
     for (int s = 32; s >= 1; s >>= 1) below += __shfl_xor(below, s, 64);
@@ -97,6 +108,7 @@ __global__ __launch_bounds__(kSortWaves * 64) void embed_sort_kernel(const void*
     // an id per thread (kMaxRange <= threads): its tokens, then exclusive sums over the ids before it
     int total = 0;
     if (tid < n)
+#pragma unroll
         for (int w = 0; w < kSortWaves; ++w) total += hist[w * range + tid];
     int before = total;
 #pragma unroll
@@ -107,10 +119,15 @@ __global__ __launch_bounds__(kSortWaves * 64) void embed_sort_kernel(const void*
     if (lane == 63) sums[wave] = before;
     __syncthreads();
     int at = before - total;
+#pragma unroll
     for (int w = 0; w < kSortWaves; ++w) at += below_all[w] + (w < wave ? sums[w] : 0);
     if (tid < n) {
         out.start[lo + tid] = at;
         if (lo + tid == V - 1) out.start[V] = at + total;
+        // every chunk's first place lies in one row, which says what goes on from the chunk before
+        for (int c = (at + kChunk - 1) / kChunk; c * kChunk < at + total; ++c)
+            if (c > 0) out.spans[c - 1] = c == at / kChunk + 1 ? make_int2(lo + tid, (at + total - 1) / kChunk) : make_int2(-1, 0);
+#pragma unroll
         for (int w = 0; w < kSortWaves; ++w) {
             const int c = hist[w * range + tid];
             hist[w * range + tid] = at;
@@ -119,25 +136,27 @@ __global__ __launch_bounds__(kSortWaves * 64) void embed_sort_kernel(const void*
     }
     __syncthreads();
     // 64 tokens at a time: those with the same id as this lane's, by the bits of the id, and its rank among them
-    for (int64_t b = begin; b < end; b += 64) {
-        const int64_t t = b + lane;
-        const int id = t < end ? sdp::token_id(ids, wide, t, V) : -1;
-        const int k = id - lo;
-        const bool hit = id >= lo && k < n;
-        uint64_t peers = __ballot(hit);
-        if (peers == 0) continue;
-        for (int i = 0; i < bits; ++i) {
-            const uint64_t set = __ballot((k >> i) & 1);
-            peers &= (k >> i) & 1 ? set : ~set;
-        }
-        // the wave's own count, read here, was written by another of its lanes
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        if (hit) {
-            const int rank = __popcll(peers & ((1ull << lane) - 1));
-            const int place = mine[k] + rank;
-            out.order[place] = (int)t;
-            out.ids[place] = id;
-            if (rank == 0) mine[k] = place + __popcll(peers);
+    for (int64_t b = begin; b < end; b += 64 * kAhead) {
+        if (!ONCE) request(b);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int k = id[i] - lo;
+            const bool hit = id[i] >= lo && k < n;
+            uint64_t peers = __ballot(hit);
+            if (peers == 0) continue;
+            for (int j = 0; j < bits; ++j) {
+                const uint64_t set = __ballot((k >> j) & 1);
+                peers &= (k >> j) & 1 ? set : ~set;
+            }
+            // the wave's own count, read here, was written by another of its lanes
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            if (hit) {
+                const int rank = __popcll(peers & ((1ull << lane) - 1));
+                const int place = mine[k] + rank;
+                out.order[place] = (int)(b + i * 64 + lane);
+                out.ids[place] = id[i];
+                if (rank == 0) mine[k] = place + __popcll(peers);
+            }
         }
     }
 }
@@ -159,12 +178,29 @@ __device__ inline void write_row(const EmbedBwd& a, int id, int e, const float (
     Row<BF16>::store((typename Row<BF16>::Elem*)a.dE + (int64_t)id * a.d, e, a.d, Row<BF16>::pack(v));
 }
 
+// the values of a piece (of either type) of a row of partial sums
+template <int N>
+__device__ inline void store_part(float* row, int e, int d, const float (&v)[N]) {
+#pragma unroll
+    for (int k = 0; k < N; k += 4) Row<0>::store(row, e + k, d, Row<0>::pack({v[k], v[k + 1], v[k + 2], v[k + 3]}));
+}
+template <int N>
+__device__ inline void load_part(const float* row, int e, int d, u32x4 (&w)[N / 4]) {
+#pragma unroll
+    for (int k = 0; k < N; k += 4) w[k / 4] = Row<0>::load(row, e + k, d);
+}
+template <int N>
+__device__ inline void add_part(const u32x4 (&w)[N / 4], float (&acc)[N]) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) acc[k] += __uint_as_float(w[k / 4][k % 4]);
+}
+
 // A wave has a chunk of the sorted tokens, or 64 rows of dE of which it clears the empty ones, and a slab of 64 pieces of the columns.
 template <int BF16>
 __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedBwd a) {
     typedef Row<BF16> Rw;
     typedef typename Rw::Elem Elem;
-    constexpr int N = Rw::N;
+    constexpr int N = Rw::N, B = 8; // rows in flight
     const int lane = threadIdx.x & 63;
     const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int64_t job = item / a.slabs;
@@ -181,22 +217,24 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedBwd a) {
         }
         return;
     }
-    const int n = a.s.start[a.V], p0 = (int)job * kChunk;
+    // what lies behind the last token in order and ids is not used
+    const int p0 = (int)job * kChunk, at = min(p0 + lane, a.T - 1);
+    const int tok = a.s.order[at], id = a.s.ids[at], prev = a.s.ids[max(p0 - 1, 0)], behind = a.s.ids[min(p0 + kChunk, a.T - 1)];
+    const int n = a.s.start[a.V];
     if (p0 >= n) return;
     const int cnt = min(kChunk, n - p0);
-    const int tok = lane < cnt ? a.s.order[p0 + lane] : 0, id = lane < cnt ? a.s.ids[p0 + lane] : -1;
-    const int prev = p0 > 0 ? a.s.ids[p0 - 1] : -1, next = p0 + cnt < n ? a.s.ids[p0 + cnt] : -1;
+    const int next = p0 + cnt < n ? behind : -1;
     float acc[N] = {};
-    bool whole = __builtin_amdgcn_readlane(id, 0) != prev; // the row at hand starts in this chunk
-    for (int j0 = 0; j0 < cnt; j0 += 8) {
-        u32x4 w[8];
+    bool whole = p0 == 0 || __builtin_amdgcn_readlane(id, 0) != prev; // the row at hand starts in this chunk
+    for (int j0 = 0; j0 < cnt; j0 += B) {
+        u32x4 w[B];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int j = 0; j < B; ++j) {
             w[j] = u32x4{0, 0, 0, 0};
             if (j0 + j < cnt && e < a.d) w[j] = Rw::load((const Elem*)a.dY + (int64_t)__builtin_amdgcn_readlane(tok, j0 + j) * a.d, e, a.d);
         }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int j = 0; j < B; ++j) {
             if (j0 + j >= cnt) break;
             float v[N];
             Rw::unpack(w[j], v);
@@ -207,14 +245,8 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedBwd a) {
             const int after = last ? next : __builtin_amdgcn_readlane(id, j0 + j + 1);
             if (row == after && !last) continue;
             if (e < a.d) {
-                if (whole && row != after) {
-                    write_row<BF16>(a, row, e, acc);
-                } else {
-                    float* p = a.part + (job * 2 + (whole ? 1 : 0)) * a.d;
-#pragma unroll
-                    for (int k = 0; k < N; ++k)
-                        if (e + k < a.d) p[e + k] = acc[k];
-                }
+                if (whole && row != after) write_row<BF16>(a, row, e, acc);
+                else store_part<N>(a.part + (job * 2 + (whole ? 1 : 0)) * a.d, e, a.d, acc);
             }
             whole = true;
 #pragma unroll
@@ -223,27 +255,38 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedBwd a) {
     }
 }
 
-// A wave looks at a chunk: if a row starts there and goes on, it adds up the row's partial sums, in the order of the chunks.
+// A workgroup looks at a chunk and a slab: if a row starts there and goes on, it adds up the row's partial sums.  Each wave adds every
+// fourth chunk's, in their order, and the waves' sums follow in theirs.
 template <int BF16>
 __global__ __launch_bounds__(256) void embed_join_kernel(EmbedBwd a) {
-    constexpr int N = Row<BF16>::N;
-    const int lane = threadIdx.x & 63;
-    const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int64_t job = item / a.slabs;
-    const int e = ((int)(item - job * a.slabs) * 64 + lane) * N;
-    const int n = a.s.start[a.V], p0 = (int)job * kChunk, p1 = p0 + kChunk;
-    if (job >= a.chunks || p1 >= n || e >= a.d) return;
-    const int row = a.s.ids[p1 - 1];
-    if (a.s.ids[p1] != row || a.s.start[row] < p0) return;
-    const int last = (a.s.start[row + 1] - 1) / kChunk;
-    float acc[N];
+    constexpr int N = Row<BF16>::N, B = 4;
+    __shared__ float lds[4][N][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int64_t job = blockIdx.x / a.slabs;
+    const int e = ((int)(blockIdx.x - job * a.slabs) * 64 + lane) * N;
+    const int n = a.s.start[a.V];
+    const int2 span = a.s.spans[job]; // written where the next chunk has a token
+    if ((job + 1) * kChunk >= n || span.x < 0) return;
+    float acc[N] = {};
+    if (e < a.d) {
+        // the row's parts: of chunk `job`, then of those up to span.y
+        auto part = [&](int64_t c) { return a.part + (c * 2 + (c == job)) * a.d; };
+        for (int64_t c = job + wave; c <= span.y; c += 4 * B) {
+            u32x4 w[B][N / 4] = {};
 #pragma unroll
-    for (int k = 0; k < N; ++k) acc[k] = e + k < a.d ? a.part[(job * 2 + 1) * a.d + e + k] : 0.f;
-#pragma unroll 4
-    for (int64_t c = job + 1; c <= last; ++c)
+            for (int j = 0; j < B; ++j)
+                if (c + 4 * j <= span.y) load_part<N>(part(c + 4 * j), e, a.d, w[j]);
 #pragma unroll
-        for (int k = 0; k < N; ++k) acc[k] += e + k < a.d ? a.part[c * 2 * a.d + e + k] : 0.f;
-    write_row<BF16>(a, row, e, acc);
+            for (int j = 0; j < B; ++j) add_part<N>(w[j], acc); // zeros behind the last
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) lds[wave][k][lane] = acc[k];
+    __syncthreads();
+    if (wave > 0 || e >= a.d) return;
+#pragma unroll
+    for (int k = 0; k < N; ++k) acc[k] = ((lds[0][k][lane] + lds[1][k][lane]) + lds[2][k][lane]) + lds[3][k][lane];
+    write_row<BF16>(a, span.x, e, acc);
 }
 
 int check_embed(int dtype, int id_type, int T, int V, int d) {
@@ -257,13 +300,14 @@ int chunks_of(int T) { return (int)(((int64_t)T + kChunk - 1) / kChunk); }
 int slabs_of(int dtype, int d) { return (d + (dtype == SDP_BF16 ? 511 : 255)) / (dtype == SDP_BF16 ? 512 : 256); }
 
 struct Layout {
-    size_t ids, start, part, all;
+    size_t ids, start, spans, part, all;
 };
 Layout layout(int T, int V, int d) {
     Layout l;
     l.ids = sdp::round_up((size_t)T * 4, 256);
     l.start = 2 * l.ids;
-    l.part = l.start + sdp::round_up(((size_t)V + 1) * 4, 256);
+    l.spans = l.start + sdp::round_up(((size_t)V + 1) * 4, 256);
+    l.part = l.spans + sdp::round_up((size_t)chunks_of(T) * sizeof(int2), 256);
     l.all = l.part + sdp::round_up((size_t)chunks_of(T) * 2 * d * sizeof(float), 256);
     return l;
 }
@@ -306,18 +350,20 @@ extern "C" int sdp_embed_bwd(int dtype, int id_type, int T, int V, int d, float 
     if (!ws || !sdp::aligned16(ws) || ws_bytes < l.all) return SDP_ERR_WORKSPACE;
     hipStream_t s = (hipStream_t)stream;
     char* w = (char*)ws;
-    EmbedBwd a{dY, dE, {(int32_t*)w, (int32_t*)(w + l.ids), (int32_t*)(w + l.start)}, (float*)(w + l.part), T, V, d, chunks_of(T),
+    EmbedBwd a{dY, dE, {(int32_t*)w, (int32_t*)(w + l.ids), (int32_t*)(w + l.start), (int2*)(w + l.spans)}, (float*)(w + l.part), T, V, d, chunks_of(T),
                slabs_of(dtype, d), scale};
     sdp::ProfileScope ps("embed_bwd", s);
     const int range = sort_range(V);
     int bits = 0;
     while ((1 << bits) < range) ++bits;
-    embed_sort_kernel<<<(V + range - 1) / range, kSortWaves * 64, (size_t)kSortWaves * range * sizeof(int), s>>>(
-        ids, id_type == SDP_I64, T, V, range, bits, a.s);
+    const dim3 groups((V + range - 1) / range);
+    const size_t lds = (size_t)kSortWaves * range * sizeof(int);
+    if (T <= kSortWaves * 64 * kAhead) embed_sort_kernel<1><<<groups, kSortWaves * 64, lds, s>>>(ids, id_type == SDP_I64, T, V, range, bits, a.s);
+    else embed_sort_kernel<0><<<groups, kSortWaves * 64, lds, s>>>(ids, id_type == SDP_I64, T, V, range, bits, a.s);
     int st = sdp::launch_status();
     if (st != SDP_OK) return st;
-    const int64_t sum = ((int64_t)a.chunks + ((int64_t)V + 63) / 64) * a.slabs, join = (int64_t)a.chunks * a.slabs;
-    const unsigned gs = (unsigned)((sum + 3) / 4), gj = (unsigned)((join + 3) / 4);
+    const int64_t sum = ((int64_t)a.chunks + ((int64_t)V + 63) / 64) * a.slabs, join = (int64_t)(a.chunks - 1) * a.slabs;
+    const unsigned gs = (unsigned)((sum + 3) / 4), gj = (unsigned)join;
     if (dtype == SDP_BF16) embed_sum_kernel<1><<<gs, 256, 0, s>>>(a);
     else embed_sum_kernel<0><<<gs, 256, 0, s>>>(a);
     st = sdp::launch_status();
