@@ -13,7 +13,7 @@
 // by digits.
 //
 // A token that occurs often (the most frequent of a text are several percent of it; in a padded batch one may be all) would be
-// one wave's long sum.  The sorted order is therefore cut into chunks of kChunk tokens, summed by a wave each (for 512 columns): a
+// one wave's long sum.  The sorted order is therefore cut into chunks of kChunk tokens, of a workgroup each (for 512 columns of bf16): a
 // row whose tokens lie within a chunk is finished there, the others leave partial sums in fp32, which a last launch adds up.
 #include <cmath>
 
@@ -56,7 +56,9 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(EmbedFwd a) {
     }
 }
 
-constexpr int kSortWaves = 16, kSortGroups = 256, kMaxRange = 960, kChunk = 32, kAhead = 16;
+constexpr int kSortWaves = 16, kSortGroups = 256, kMaxRange = 960, kAhead = 16;
+// sorted tokens of a wave, all of whose rows are in flight at once, and of a workgroup
+constexpr int kPiece = 16, kSumWaves = 8, kChunk = kPiece * kSumWaves;
 
 struct Sorted {
     int32_t* order; // [T] tokens, by id, then by place
@@ -72,8 +74,8 @@ int sort_range(int V) {
 }
 
 // ONCE: a wave's tokens are kAhead to a lane at most and stay in registers between the two times
-template <int ONCE>
-__global__ __launch_bounds__(kSortWaves * 64) void embed_sort_kernel(const void* __restrict__ ids, int wide, int T, int V, int range,
+template <int WIDE, int ONCE>
+__global__ __launch_bounds__(kSortWaves * 64) void embed_sort_kernel(const void* __restrict__ ids, int T, int V, int range,
                                                                      int bits, Sorted out) {
     extern __shared__ int hist[]; // [kSortWaves][range]: a wave's tokens of each id, then where its next one goes
     __shared__ int sums[kSortWaves], below_all[kSortWaves];
@@ -85,7 +87,7 @@ __global__ __launch_bounds__(kSortWaves * 64) void embed_sort_kernel(const void*
     int id[kAhead];
     auto request = [&](int64_t b) { // kAhead loads in flight: one after the other, their latency would be most of the time
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) id[i] = b + i * 64 + lane < end ? sdp::token_id(ids, wide, b + i * 64 + lane, V) : -1;
+        for (int i = 0; i < kAhead; ++i) id[i] = b + i * 64 + lane < end ? sdp::token_id<WIDE>(ids, b + i * 64 + lane, V) : -1;
     };
     if (ONCE) request(begin);
     for (int i = tid; i < kSortWaves * range; i += kSortWaves * 64) hist[i] = 0;
@@ -135,28 +137,38 @@ __global__ __launch_bounds__(kSortWaves * 64) void embed_sort_kernel(const void*
         }
     }
     __syncthreads();
-    // 64 tokens at a time: those with the same id as this lane's, by the bits of the id, and its rank among them
+    // 64 tokens at a time: each one's place is the wave's count of its id plus its rank among the lanes with the same id.  Few ids, mostly
+    // one, are the rule (a group's tokens of 125 ids out of 32000, or a frequent one): up to three are taken one after the other, what is
+    // left by the bits of the id.
+    auto place = [&](bool hit, int k, int token, int whose, uint64_t peers) {
+        // the wave's own count, read here, was written by another of its lanes
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (!hit) return;
+        const int rank = __popcll(peers & ((1ull << lane) - 1)), at = mine[k] + rank;
+        out.order[at] = token;
+        out.ids[at] = whose;
+        if (rank == 0) mine[k] = at + __popcll(peers);
+    };
     for (int64_t b = begin; b < end; b += 64 * kAhead) {
         if (!ONCE) request(b);
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
             const int k = id[i] - lo;
             const bool hit = id[i] >= lo && k < n;
-            uint64_t peers = __ballot(hit);
-            if (peers == 0) continue;
+            uint64_t left = __ballot(hit);
+            for (int few = 0; left && few < 3; ++few) {
+                const int one = __builtin_amdgcn_readlane(k, __ffsll((unsigned long long)left) - 1);
+                const uint64_t peers = __ballot(hit && k == one);
+                place(hit && k == one, k, (int)(b + i * 64 + lane), id[i], peers);
+                left &= ~peers;
+            }
+            if (left == 0) continue;
+            uint64_t peers = left;
             for (int j = 0; j < bits; ++j) {
                 const uint64_t set = __ballot((k >> j) & 1);
                 peers &= (k >> j) & 1 ? set : ~set;
             }
-            // the wave's own count, read here, was written by another of its lanes
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            if (hit) {
-                const int rank = __popcll(peers & ((1ull << lane) - 1));
-                const int place = mine[k] + rank;
-                out.order[place] = (int)(b + i * 64 + lane);
-                out.ids[place] = id[i];
-                if (rank == 0) mine[k] = place + __popcll(peers);
-            }
+            place((left >> lane) & 1, k, (int)(b + i * 64 + lane), id[i], peers);
         }
     }
 }
@@ -195,18 +207,21 @@ __device__ inline void add_part(const u32x4 (&w)[N / 4], float (&acc)[N]) {
     for (int k = 0; k < N; ++k) acc[k] += __uint_as_float(w[k / 4][k % 4]);
 }
 
-// A wave has a chunk of the sorted tokens, or 64 rows of dE of which it clears the empty ones, and a slab of 64 pieces of the columns.
+// A workgroup has a chunk of the sorted tokens, a wave a piece of it, or 64 rows of dE for each wave to clear the empty ones of; and a slab of
+// 64 pieces of the columns.  What a wave has of a row that starts in an earlier one goes through LDS to the wave that has its start,
+// and to memory only where that lies in another chunk.
 template <int BF16>
-__global__ __launch_bounds__(256) void embed_sum_kernel(EmbedBwd a) {
+__global__ __launch_bounds__(kSumWaves * 64) void embed_sum_kernel(EmbedBwd a) {
     typedef Row<BF16> Rw;
     typedef typename Rw::Elem Elem;
-    constexpr int N = Rw::N, B = 8; // rows in flight
-    const int lane = threadIdx.x & 63;
-    const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int64_t job = item / a.slabs;
-    const int e = ((int)(item - job * a.slabs) * 64 + lane) * N;
+    constexpr int N = Rw::N;
+    __shared__ float heads[kSumWaves][N][64];
+    __shared__ int head_of[kSumWaves]; // 0: the wave starts with a row of its own; 1: its first row started earlier, 2: and goes on
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int64_t job = blockIdx.x / a.slabs;
+    const int e = ((int)(blockIdx.x - job * a.slabs) * 64 + lane) * N;
     if (job >= a.chunks) {
-        const int64_t v = (job - a.chunks) * 64;
+        const int64_t v = ((job - a.chunks) * kSumWaves + wave) * 64;
         if (v >= a.V) return;
         const bool empty = v + lane < a.V && a.s.start[v + lane] == a.s.start[v + lane + 1];
         uint64_t left = __ballot(empty);
@@ -217,41 +232,70 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedBwd a) {
         }
         return;
     }
-    // what lies behind the last token in order and ids is not used
-    const int p0 = (int)job * kChunk, at = min(p0 + lane, a.T - 1);
-    const int tok = a.s.order[at], id = a.s.ids[at], prev = a.s.ids[max(p0 - 1, 0)], behind = a.s.ids[min(p0 + kChunk, a.T - 1)];
+    // requested before it is known how many tokens there are: what lies behind the last one is not used
+    const int p0 = (int)job * kChunk + wave * kPiece, at = min(p0 + lane, a.T - 1);
+    const int tok = a.s.order[at], id = a.s.ids[at], prev = a.s.ids[max(min(p0, a.T) - 1, 0)], behind = a.s.ids[min(p0 + kPiece, a.T - 1)];
     const int n = a.s.start[a.V];
-    if (p0 >= n) return;
-    const int cnt = min(kChunk, n - p0);
-    const int next = p0 + cnt < n ? behind : -1;
+    if (job * kChunk >= n) return;
+    const int cnt = max(0, min(kPiece, n - p0)), next = p0 + cnt < n ? behind : -1;
     float acc[N] = {};
-    bool whole = p0 == 0 || __builtin_amdgcn_readlane(id, 0) != prev; // the row at hand starts in this chunk
-    for (int j0 = 0; j0 < cnt; j0 += B) {
-        u32x4 w[B];
+    bool own = p0 == 0 || __builtin_amdgcn_readlane(id, 0) != prev; // the row at hand starts in this piece
+    int head = 0, tail = -1; // tail: the row that starts here and goes on; acc is its sum then
+    u32x4 w[kPiece];
 #pragma unroll
-        for (int j = 0; j < B; ++j) {
-            w[j] = u32x4{0, 0, 0, 0};
-            if (j0 + j < cnt && e < a.d) w[j] = Rw::load((const Elem*)a.dY + (int64_t)__builtin_amdgcn_readlane(tok, j0 + j) * a.d, e, a.d);
-        }
+    for (int j = 0; j < kPiece; ++j) {
+        w[j] = u32x4{0, 0, 0, 0};
+        if (j < cnt && e < a.d) w[j] = Rw::load((const Elem*)a.dY + (int64_t)__builtin_amdgcn_readlane(tok, j) * a.d, e, a.d);
+    }
 #pragma unroll
-        for (int j = 0; j < B; ++j) {
-            if (j0 + j >= cnt) break;
+    for (int j = 0; j < kPiece; ++j) {
+        if (j < cnt) {
             float v[N];
             Rw::unpack(w[j], v);
 #pragma unroll
             for (int k = 0; k < N; ++k) acc[k] += v[k];
-            const int row = __builtin_amdgcn_readlane(id, j0 + j);
-            const bool last = j0 + j == cnt - 1;
-            const int after = last ? next : __builtin_amdgcn_readlane(id, j0 + j + 1);
-            if (row == after && !last) continue;
-            if (e < a.d) {
-                if (whole && row != after) write_row<BF16>(a, row, e, acc);
-                else store_part<N>(a.part + (job * 2 + (whole ? 1 : 0)) * a.d, e, a.d, acc);
-            }
-            whole = true;
+            const int row = __builtin_amdgcn_readlane(id, j);
+            const int after = j == cnt - 1 ? next : __builtin_amdgcn_readlane(id, (j + 1) % kPiece);
+            if (j == cnt - 1 && row == after && own) {
+                tail = row;
+            } else if (j == cnt - 1 || row != after) {
+                if (own) {
+                    if (e < a.d) write_row<BF16>(a, row, e, acc);
+                } else {
+                    head = row == after ? 2 : 1;
 #pragma unroll
-            for (int k = 0; k < N; ++k) acc[k] = 0.f;
+                    for (int k = 0; k < N; ++k) heads[wave][k][lane] = acc[k];
+                }
+                own = true;
+#pragma unroll
+                for (int k = 0; k < N; ++k) acc[k] = 0.f;
+            }
         }
+    }
+    if (lane == 0) head_of[wave] = head;
+    __syncthreads();
+    // adds what the waves from `from` on have of a row that goes on in them; whether it ends there
+    auto follow = [&](float (&sum)[N], int from) {
+        for (int u = from; u < kSumWaves; ++u) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) sum[k] += heads[u][k][lane];
+            if (__builtin_amdgcn_readfirstlane(head_of[u]) != 2) return true;
+        }
+        return false;
+    };
+    float* part = a.part + job * 2 * a.d;
+    if (tail >= 0) {
+        const bool ends = follow(acc, wave + 1);
+        if (e < a.d) {
+            if (ends) write_row<BF16>(a, tail, e, acc);
+            else store_part<N>(part + a.d, e, a.d, acc);
+        }
+    }
+    if (wave == 0 && head) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) acc[k] = heads[0][k][lane];
+        if (head == 2) follow(acc, 1);
+        if (e < a.d) store_part<N>(part, e, a.d, acc);
     }
 }
 
@@ -358,14 +402,21 @@ extern "C" int sdp_embed_bwd(int dtype, int id_type, int T, int V, int d, float 
     while ((1 << bits) < range) ++bits;
     const dim3 groups((V + range - 1) / range);
     const size_t lds = (size_t)kSortWaves * range * sizeof(int);
-    if (T <= kSortWaves * 64 * kAhead) embed_sort_kernel<1><<<groups, kSortWaves * 64, lds, s>>>(ids, id_type == SDP_I64, T, V, range, bits, a.s);
-    else embed_sort_kernel<0><<<groups, kSortWaves * 64, lds, s>>>(ids, id_type == SDP_I64, T, V, range, bits, a.s);
+    auto sort = [&](auto wide, auto once) {
+        embed_sort_kernel<wide.value, once.value><<<groups, kSortWaves * 64, lds, s>>>(ids, T, V, range, bits, a.s);
+    };
+    auto sort_of = [&](auto wide) {
+        if (T <= kSortWaves * 64 * kAhead) sort(wide, std::integral_constant<int, 1>{});
+        else sort(wide, std::integral_constant<int, 0>{});
+    };
+    if (id_type == SDP_I64) sort_of(std::integral_constant<int, 1>{});
+    else sort_of(std::integral_constant<int, 0>{});
     int st = sdp::launch_status();
     if (st != SDP_OK) return st;
-    const int64_t sum = ((int64_t)a.chunks + ((int64_t)V + 63) / 64) * a.slabs, join = (int64_t)(a.chunks - 1) * a.slabs;
-    const unsigned gs = (unsigned)((sum + 3) / 4), gj = (unsigned)join;
-    if (dtype == SDP_BF16) embed_sum_kernel<1><<<gs, 256, 0, s>>>(a);
-    else embed_sum_kernel<0><<<gs, 256, 0, s>>>(a);
+    const int64_t sum = ((int64_t)a.chunks + ((int64_t)V + kSumWaves * 64 - 1) / (kSumWaves * 64)) * a.slabs, join = (int64_t)(a.chunks - 1) * a.slabs;
+    const unsigned gs = (unsigned)sum, gj = (unsigned)join;
+    if (dtype == SDP_BF16) embed_sum_kernel<1><<<gs, kSumWaves * 64, 0, s>>>(a);
+    else embed_sum_kernel<0><<<gs, kSumWaves * 64, 0, s>>>(a);
     st = sdp::launch_status();
     if (st != SDP_OK || a.chunks < 2) return st;
     if (dtype == SDP_BF16) embed_join_kernel<1><<<gj, 256, 0, s>>>(a);

@@ -151,16 +151,27 @@ __device__ inline S group_sum(S x) {
 __global__ __launch_bounds__(1024) void loss_sum_kernel(const float* __restrict__ nll, int T, float scale, const float* scale_dev,
                                                         float* loss) {
     double x = 0.0;
-#pragma unroll 8
-    for (int t = threadIdx.x; t < T; t += 1024) x += (double)nll[t];
+    for (int t0 = threadIdx.x; t0 < T; t0 += 8 * 1024) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = t0 + i * 1024 < T ? nll[t0 + i * 1024] : 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x += (double)v[i];
+    }
     x = group_sum(x);
     if (threadIdx.x == 0) *loss = (float)(x * ((double)scale * (scale_dev ? (double)*scale_dev : 1.0)));
 }
 
-__global__ __launch_bounds__(1024) void label_scale_kernel(const void* __restrict__ labels, int wide, int T, int V, float* scale) {
+template <int WIDE>
+__global__ __launch_bounds__(1024) void label_scale_kernel(const void* __restrict__ labels, int T, int V, float* scale) {
     int n = 0;
-#pragma unroll 8
-    for (int t = threadIdx.x; t < T; t += 1024) n += sdp::token_id(labels, wide, t, V) >= 0;
+    for (int t0 = threadIdx.x; t0 < T; t0 += 8 * 1024) {
+        int id[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) id[i] = t0 + i * 1024 < T ? sdp::token_id<WIDE>(labels, t0 + i * 1024, V) : -1;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) n += id[i] >= 0;
+    }
     n = group_sum(n);
     if (threadIdx.x == 0) *scale = 1.0f / (float)(n > 1 ? n : 1);
 }
@@ -226,6 +237,7 @@ extern "C" int sdp_label_scale(int id_type, int T, int V, const void* labels, fl
     if (!sdp::aligned_to(labels, id_type == SDP_I64 ? 8 : 4) || !sdp::aligned_to(scale, 4)) return SDP_ERR_INVALID_ARG;
     if (T > 0 && sdp::overlap({{scale, 4}}, {{labels, (size_t)T * (id_type == SDP_I64 ? 8 : 4)}})) return SDP_ERR_INVALID_ARG;
     sdp::ProfileScope ps("label_scale", (hipStream_t)stream);
-    label_scale_kernel<<<1, 1024, 0, (hipStream_t)stream>>>(labels, id_type == SDP_I64, T, V, scale);
+    if (id_type == SDP_I64) label_scale_kernel<1><<<1, 1024, 0, (hipStream_t)stream>>>(labels, T, V, scale);
+    else label_scale_kernel<0><<<1, 1024, 0, (hipStream_t)stream>>>(labels, T, V, scale);
     return sdp::launch_status();
 }

@@ -8,6 +8,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 namespace sdp {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -110,10 +112,16 @@ __device__ inline float wave_max(float x) {
     return x;
 }
 
-// token id or label t; anything outside [0, V) is -1
+// Token id or label t; anything outside [0, V) is -1.  Where many are loaded at once the type has to be known at compile time: with a
+// branch around each load the next waits for the last.
+template <int WIDE>
+__device__ inline int token_id(const void* ids, int64_t t, int V) {
+    typedef std::conditional_t<WIDE, uint64_t, uint32_t> Id;
+    const Id v = ((const Id*)ids)[t];
+    return v < (Id)V ? (int)v : -1;
+}
 __device__ inline int token_id(const void* ids, int wide, int64_t t, int V) {
-    const int64_t v = wide ? ((const int64_t*)ids)[t] : ((const int32_t*)ids)[t];
-    return v >= 0 && v < V ? (int)v : -1;
+    return wide ? token_id<1>(ids, t, V) : token_id<0>(ids, t, V);
 }
 
 } // namespace sdp
