@@ -16,6 +16,7 @@
 // one wave's long sum.  The sorted order is therefore cut into chunks of kChunk tokens, of a workgroup each (for 512 columns of bf16): a
 // row whose tokens lie within a chunk is finished there, the others leave partial sums in fp32, which a last launch adds up.
 #include <cmath>
+#include <type_traits>
 
 #include "sdp_internal.h"
 #include "sdp_rows.h"
@@ -72,39 +73,88 @@ int sort_range(int V) {
     const int r = (V + kSortGroups - 1) / kSortGroups;
     return r < kMaxRange ? r : kMaxRange;
 }
+constexpr int kListed = 64 * kAhead; // tokens of a wave that are looked at, and of its workgroup's range at most, between two lists
 
-// ONCE: a wave's tokens are kAhead to a lane at most and stay in registers between the two times
+// ONCE: a wave's tokens make one list, which stays between the two times
 template <int WIDE, int ONCE>
-__global__ __launch_bounds__(kSortWaves * 64) void embed_sort_kernel(const void* __restrict__ ids, int T, int V, int range,
-                                                                     int bits, Sorted out) {
-    extern __shared__ int hist[]; // [kSortWaves][range]: a wave's tokens of each id, then where its next one goes
+__global__ __launch_bounds__(kSortWaves * 64) void embed_sort_kernel(const void* __restrict__ ids, int T, int V, int range, int bits,
+                                                                     Sorted out) {
+    extern __shared__ int lds[];
     __shared__ int sums[kSortWaves], below_all[kSortWaves];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
-    const int lo = blockIdx.x * range, n = min(range, V - lo);
+    const uint64_t lanes_below = (1ull << lane) - 1;
+    int* hist = lds + kSortWaves * kListed;      // [kSortWaves][range]: a wave's tokens of each id, then where its next one goes
+    int* mine = hist + wave * range;
+    int* list = lds + wave * kListed;            // the wave's tokens of the range, in order: token - first token of the list, id - lo
+    const uint32_t lo = blockIdx.x * range, n = min((uint32_t)range, (uint32_t)V - lo);
     // each wave has an unbroken piece of the tokens, of which a lane takes every 64th
     const int64_t piece = ((int64_t)T + kSortWaves * 64 - 1) / (kSortWaves * 64) * 64;
     const int64_t begin = wave * piece, end = begin + piece < T ? begin + piece : T;
-    int id[kAhead];
+    uint32_t id[kAhead]; // one outside [0, V) is never below a range nor in one: as an unsigned number it is V or more
     auto request = [&](int64_t b) { // kAhead loads in flight: one after the other, their latency would be most of the time
+        if (b >= end) { // a wave without tokens
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) id[i] = b + i * 64 + lane < end ? sdp::token_id<WIDE>(ids, b + i * 64 + lane, V) : -1;
+            for (int i = 0; i < kAhead; ++i) id[i] = 0xFFFFFFFFu;
+            return;
+        }
+        std::conditional_t<WIDE, uint64_t, uint32_t> v[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) v[i] = ((const std::conditional_t<WIDE, uint64_t, uint32_t>*)ids)[min(b + i * 64 + lane, end - 1)];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) id[i] = b + i * 64 + lane < end && v[i] <= 0xFFFFFFFFu ? (uint32_t)v[i] : 0xFFFFFFFFu;
     };
+    int below = 0;
+    auto make_list = [&]() { // of what was requested; its length
+        int m = 0;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            below += __popcll(__ballot(id[i] < lo));
+            const uint32_t k = id[i] - lo;
+            const uint64_t hits = __ballot(k < n);
+            if (hits == 0) continue;
+            if (k < n) list[m + __popcll(hits & lanes_below)] = (i * 64 + lane) << 16 | (int)k;
+            m += __popcll(hits);
+        }
+        __builtin_amdgcn_wave_barrier(); // read by other lanes of the wave
+        return m;
+    };
+    // 64 tokens of the list at a time: a token's place is the wave's count of its id and its rank among the lanes with the same id: all of
+    // them (a frequent token), or found by the bits of the id
+    auto take_list = [&](int m, int64_t b, bool write) {
+        for (int g = 0; g < m; g += 64) {
+            const bool live = g + lane < m;
+            const int entry = list[g + lane < m ? g + lane : g], k = entry & 0xFFFF;
+            uint64_t peers = __ballot(live);
+            if (__ballot(live && k == __builtin_amdgcn_readfirstlane(k)) != peers)
+                for (int j = 0; j < bits; ++j) {
+                    const uint64_t set = __ballot((k >> j) & 1);
+                    peers &= (k >> j) & 1 ? set : ~set;
+                }
+            const int rank = __popcll(peers & lanes_below), at = mine[k] + rank;
+            __builtin_amdgcn_wave_barrier(); // everyone's count is read before it is raised
+            if (live) {
+                if (write) {
+                    out.order[at] = (int)(b + (entry >> 16));
+                    out.ids[at] = (int)lo + k;
+                }
+                if (rank == 0) mine[k] = at + __popcll(peers);
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
+    };
+    int listed = 0;
     if (ONCE) request(begin);
     for (int i = tid; i < kSortWaves * range; i += kSortWaves * 64) hist[i] = 0;
     __syncthreads();
-    int below = 0;
-    int* mine = hist + wave * range;
-    for (int64_t b = begin; b < end; b += 64 * kAhead) {
-        if (!ONCE) request(b);
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            below += id[i] >= 0 && id[i] < lo;
-            const int k = id[i] - lo;
-            if (id[i] >= lo && k < n) atomicAdd(&mine[k], 1);
+    if (ONCE) {
+        listed = make_list();
+        take_list(listed, begin, false);
+    } else {
+        for (int64_t b = begin; b < end; b += kListed) {
+            request(b);
+            take_list(make_list(), b, false);
         }
     }
-#pragma unroll
-    for (int s = 32; s >= 1; s >>= 1) below += __shfl_xor(below, s, 64);
     if (lane == 0) below_all[wave] = below;
     __syncthreads();
     // an id per thread (kMaxRange <= threads): its tokens, then exclusive sums over the ids before it
@@ -137,38 +187,12 @@ __global__ __launch_bounds__(kSortWaves * 64) void embed_sort_kernel(const void*
         }
     }
     __syncthreads();
-    // 64 tokens at a time: each one's place is the wave's count of its id plus its rank among the lanes with the same id.  Few ids, mostly
-    // one, are the rule (a group's tokens of 125 ids out of 32000, or a frequent one): up to three are taken one after the other, what is
-    // left by the bits of the id.
-    auto place = [&](bool hit, int k, int token, int whose, uint64_t peers) {
-        // the wave's own count, read here, was written by another of its lanes
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        if (!hit) return;
-        const int rank = __popcll(peers & ((1ull << lane) - 1)), at = mine[k] + rank;
-        out.order[at] = token;
-        out.ids[at] = whose;
-        if (rank == 0) mine[k] = at + __popcll(peers);
-    };
-    for (int64_t b = begin; b < end; b += 64 * kAhead) {
-        if (!ONCE) request(b);
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const int k = id[i] - lo;
-            const bool hit = id[i] >= lo && k < n;
-            uint64_t left = __ballot(hit);
-            for (int few = 0; left && few < 3; ++few) {
-                const int one = __builtin_amdgcn_readlane(k, __ffsll((unsigned long long)left) - 1);
-                const uint64_t peers = __ballot(hit && k == one);
-                place(hit && k == one, k, (int)(b + i * 64 + lane), id[i], peers);
-                left &= ~peers;
-            }
-            if (left == 0) continue;
-            uint64_t peers = left;
-            for (int j = 0; j < bits; ++j) {
-                const uint64_t set = __ballot((k >> j) & 1);
-                peers &= (k >> j) & 1 ? set : ~set;
-            }
-            place((left >> lane) & 1, k, (int)(b + i * 64 + lane), id[i], peers);
+    if (ONCE) {
+        take_list(listed, begin, true);
+    } else {
+        for (int64_t b = begin; b < end; b += kListed) {
+            request(b);
+            take_list(make_list(), b, true);
         }
     }
 }
@@ -401,17 +425,19 @@ extern "C" int sdp_embed_bwd(int dtype, int id_type, int T, int V, int d, float 
     int bits = 0;
     while ((1 << bits) < range) ++bits;
     const dim3 groups((V + range - 1) / range);
-    const size_t lds = (size_t)kSortWaves * range * sizeof(int);
+    const size_t lds = (size_t)kSortWaves * (kListed + range) * sizeof(int);
     auto sort = [&](auto wide, auto once) {
-        embed_sort_kernel<wide.value, once.value><<<groups, kSortWaves * 64, lds, s>>>(ids, T, V, range, bits, a.s);
+        const auto kern = embed_sort_kernel<wide.value, once.value>;
+        static const hipError_t attr =
+            hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, kSortWaves * (kListed + kMaxRange) * sizeof(int));
+        if (attr != hipSuccess) return sdp::hip_status(attr);
+        kern<<<groups, kSortWaves * 64, lds, s>>>(ids, T, V, range, bits, a.s);
+        return sdp::launch_status();
     };
     auto sort_of = [&](auto wide) {
-        if (T <= kSortWaves * 64 * kAhead) sort(wide, std::integral_constant<int, 1>{});
-        else sort(wide, std::integral_constant<int, 0>{});
+        return T <= kSortWaves * kListed ? sort(wide, std::integral_constant<int, 1>{}) : sort(wide, std::integral_constant<int, 0>{});
     };
-    if (id_type == SDP_I64) sort_of(std::integral_constant<int, 1>{});
-    else sort_of(std::integral_constant<int, 0>{});
-    int st = sdp::launch_status();
+    int st = id_type == SDP_I64 ? sort_of(std::integral_constant<int, 1>{}) : sort_of(std::integral_constant<int, 0>{});
     if (st != SDP_OK) return st;
     const int64_t sum = ((int64_t)a.chunks + ((int64_t)V + kSumWaves * 64 - 1) / (kSumWaves * 64)) * a.slabs, join = (int64_t)(a.chunks - 1) * a.slabs;
     const unsigned gs = (unsigned)sum, gj = (unsigned)join;
