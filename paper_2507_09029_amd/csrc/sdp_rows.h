@@ -4,6 +4,9 @@
 // A piece is 8 bf16 or 4 fp32 values.  Rows of a matrix whose width is no whole number of pieces start at any element; the memory
 // instructions of 16 bytes take such addresses, and rows of 1501 bf16 stream at the rate of aligned ones, so there is one form for
 // both.  The last piece of a row may be short: its values are moved one by one.
+//
+// Stores are non-temporal: what is written here is far more than a cache holds, or read next by another kernel, and pushes what is being
+// read out of it (embedding of 16384 x 2048 bf16 22.0 -> 17.0 us, its gradient's sums 44 -> 34, norm 50.1 -> 48.8, loss of 8192 x 32000 186 -> 182).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -39,7 +42,7 @@ struct Row<1> {
     }
     static __device__ inline void store(Elem* row, int e, int n, const u32x4& w) {
         if (e + N <= n) {
-            *(u32x4_at2*)(row + e) = w;
+            __builtin_nontemporal_store(w, (u32x4_at2*)(row + e));
             return;
         }
 #pragma unroll
@@ -84,7 +87,7 @@ struct Row<0> {
     }
     static __device__ inline void store(Elem* row, int e, int n, const u32x4& w) {
         if (e + N <= n) {
-            *(u32x4_at4*)(row + e) = w;
+            __builtin_nontemporal_store(w, (u32x4_at4*)(row + e));
             return;
         }
 #pragma unroll
