@@ -53,7 +53,7 @@ __device__ inline float row_sum(float x, float* lds) {
     return s;
 }
 
-template <int BF16, int WPR, int VPL>
+template <int BF16, int WPR, int VPL, int ONCE>
 __global__ __launch_bounds__(waves_of(WPR) * 64) void norm_fwd_kernel(NormFwd a) {
     typedef Row<BF16> Rw;
     typedef typename Rw::Elem Elem;
@@ -67,11 +67,11 @@ __global__ __launch_bounds__(waves_of(WPR) * 64) void norm_fwd_kernel(NormFwd a)
     u32x4 x[VPL];
     float h[VPL][N];
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) x[i] = Rw::load((const Elem*)a.X + off, at + i * WPR * 64 * N, d);
+    for (int i = 0; i < VPL; ++i) x[i] = Rw::template load<ONCE>((const Elem*)a.X + off, at + i * WPR * 64 * N, d);
     if (a.R) {
         u32x4 r[VPL];
 #pragma unroll
-        for (int i = 0; i < VPL; ++i) r[i] = Rw::load((const Elem*)a.R + off, at + i * WPR * 64 * N, d);
+        for (int i = 0; i < VPL; ++i) r[i] = Rw::template load<ONCE>((const Elem*)a.R + off, at + i * WPR * 64 * N, d);
 #pragma unroll
         for (int i = 0; i < VPL; ++i) {
             float p[N], q[N];
@@ -295,10 +295,12 @@ extern "C" int sdp_norm_fwd(int kind, int dtype, int T, int d, float eps, const 
     hipStream_t s = (hipStream_t)stream;
     const Shape sh = shape(dtype, d);
     const NormFwd a{X, R, gamma, beta, H, Y, mean, rstd, T, d, layer, eps};
+    const bool once = sdp::read_once({eX, eR}, w);
     sdp::ProfileScope ps("norm_fwd", s);
     const unsigned groups = (unsigned)(((int64_t)T + rows_of(sh) - 1) / rows_of(sh));
     return by_shape(dtype, sh, [&](auto bf16, auto wpr, auto vpl) {
-        norm_fwd_kernel<bf16.value, wpr.value, vpl.value><<<groups, waves_of(wpr.value) * 64, 0, s>>>(a);
+        if (once) norm_fwd_kernel<bf16.value, wpr.value, vpl.value, 1><<<groups, waves_of(wpr.value) * 64, 0, s>>>(a);
+        else norm_fwd_kernel<bf16.value, wpr.value, vpl.value, 0><<<groups, waves_of(wpr.value) * 64, 0, s>>>(a);
         return sdp::launch_status();
     });
 }

@@ -13,12 +13,26 @@
 
 #include <type_traits>
 
+#include "sdp_internal.h"
+
 namespace sdp {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef u32x4 __attribute__((aligned(2))) u32x4_at2;
 typedef u32x4 __attribute__((aligned(4))) u32x4_at4;
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// Whether rows of `row_bytes` in these matrices are read around the caches: more than they hold (the eight L2s 32 MB), and rows of whole
+// lines, since a line that two rows share is else fetched twice.  Norm forward of 16384 x 2048 bf16 with / without 46.9 / 48.4 us, loss of
+// 8192 x 32000 185 / 190; but rows that are no whole lines: loss of 1000 x 50001 57.6 / 49.6.
+inline bool read_once(std::initializer_list<Extent> of, size_t row_bytes) {
+    size_t all = 0;
+    for (const Extent& m : of) {
+        if (m.bytes && !aligned_to(m.p, 128)) return false;
+        all += m.bytes;
+    }
+    return row_bytes % 128 == 0 && all >= (size_t)1 << 26;
+}
 
 template <int BF16>
 struct Row;
@@ -31,9 +45,11 @@ struct Row<1> {
     static __device__ inline float one(const Elem* p) { return __uint_as_float((uint32_t)*p << 16); }
     static __device__ inline void put(Elem* p, float v) { *p = __builtin_bit_cast(uint16_t, (__bf16)v); }
 
-    // the piece from value e on of a row of n; values past its end are `fill`'s (two bf16 in a word)
+    // the piece from value e on of a row of n; values past its end are `fill`'s (two bf16 in a word); ONCE: read_once's answer, at compile time (of two loads
+    // behind a condition the compiler makes one)
+    template <int ONCE = 0>
     static __device__ inline u32x4 load(const Elem* row, int e, int n, uint32_t fill = 0) {
-        if (e + N <= n) return *(const u32x4_at2*)(row + e);
+        if (e + N <= n) return ONCE ? __builtin_nontemporal_load((const u32x4_at2*)(row + e)) : *(const u32x4_at2*)(row + e);
         u32x4 w = {fill, fill, fill, fill};
 #pragma unroll
         for (int i = 0; i < N; ++i)
@@ -77,8 +93,9 @@ struct Row<0> {
     static __device__ inline float one(const Elem* p) { return *p; }
     static __device__ inline void put(Elem* p, float v) { *p = v; }
 
+    template <int ONCE = 0>
     static __device__ inline u32x4 load(const Elem* row, int e, int n, uint32_t fill = 0) {
-        if (e + N <= n) return *(const u32x4_at4*)(row + e);
+        if (e + N <= n) return ONCE ? __builtin_nontemporal_load((const u32x4_at4*)(row + e)) : *(const u32x4_at4*)(row + e);
         u32x4 w = {fill, fill, fill, fill};
 #pragma unroll
         for (int i = 0; i < N; ++i)
