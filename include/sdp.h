@@ -363,8 +363,8 @@ int sdp_clip_scale(int n, const double* sqnorm, float max_norm, float* scale, vo
  * ------------------------------------------------------------------------------------------- */
 typedef enum { SDP_NORM_LAYER = 0, SDP_NORM_RMS = 1 } sdp_norm_kind;
 typedef enum { SDP_I32 = 0, SDP_I64 = 1 } sdp_id_type;
-#define SDP_NORM_MAX_WIDTH 32768    /* largest d of the norm calls */
-#define SDP_MAX_TOKENS (1 << 30)    /* largest T of the calls below */
+#define SDP_NORM_MAX_WIDTH 16384    /* largest d of the norm calls */
+#define SDP_MAX_EXTENT (1 << 30)    /* largest T, V and d of the calls below */
 
 /* ---------------------------------------------------------------------------------------------
  * Norm of T tokens of width d, of their own or of a sum with a skip connection:
@@ -377,7 +377,7 @@ typedef enum { SDP_I32 = 0, SDP_I64 = 1 } sdp_id_type;
  *   mean, rstd [T] fp32 out: mu and s, for sdp_norm_bwd; mean is NULL with SDP_NORM_RMS
  * H and Y may each take the place of X or R (the same pointer); H and Y are two buffers.
  * Errors: INVALID_ARG (null, misaligned, overlapping, unknown kind or dtype, T < 0, d < 1, eps negative or not
- * finite), SHAPE (d > SDP_NORM_MAX_WIDTH, T > SDP_MAX_TOKENS).
+ * finite), SHAPE (d > SDP_NORM_MAX_WIDTH, T > SDP_MAX_EXTENT).
  * ------------------------------------------------------------------------------------------- */
 int sdp_norm_fwd(int kind, int dtype, int T, int d, float eps, const void* X, const void* R, const void* gamma,
                  const void* beta, void* H, void* Y, float* mean, float* rstd, void* stream);
@@ -405,7 +405,7 @@ int sdp_norm_bwd(int kind, int dtype, int T, int d, const void* H, const void* d
  * bits), zeros where ids[t] lies outside [0, V).
  *   E [V][d] in (row-major by token, as every matrix here is by neuron);  ids [T] in;  Y [T][d] out
  * Errors: INVALID_ARG (null, misaligned, overlapping, unknown dtype or id_type, T < 0, V < 1, d < 1, scale not finite),
- * SHAPE (T > SDP_MAX_TOKENS).
+ * SHAPE (T, V or d > SDP_MAX_EXTENT).
  *
  * sdp_embed_bwd: its gradient, dE[v] = scale sum_{t : ids[t] = v} dY[t], every row of [V][d]: rows of tokens that do not
  * occur are zeros.  Tokens are sorted by id (stably, so each row's fp32 sum has one order, whatever the
@@ -429,7 +429,7 @@ int sdp_embed_bwd(int dtype, int id_type, int T, int V, int d, float scale, cons
  *   labels [T] in;  scale_dev: device fp32, may be NULL (= 1): what sdp_label_scale wrote, or a loss scale; 4-byte aligned
  *   nll [T] fp32 out;  lse [T] fp32 out, may be NULL;  loss [1] fp32 out (summed in fp64 in a fixed order), may be NULL
  * Errors: INVALID_ARG (null, misaligned, overlapping, unknown dtype or id_type, T < 0, V < 1, scale not finite),
- * SHAPE (ldz < V, T > SDP_MAX_TOKENS).
+ * SHAPE (ldz < V, T or V > SDP_MAX_EXTENT).
  *
  * sdp_label_scale: *scale = 1 / max(1, n), n = number of labels in [0, V): the scale of the mean over the rows that have
  * a label.

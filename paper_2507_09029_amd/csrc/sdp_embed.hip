@@ -38,23 +38,29 @@ template <int BF16>
 __global__ __launch_bounds__(256) void embed_fwd_kernel(EmbedFwd a) {
     typedef Row<BF16> Rw;
     typedef typename Rw::Elem Elem;
-    constexpr int N = Rw::N;
+    constexpr int N = Rw::N, B = 4; // pieces in flight
     const int64_t t = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     if (t >= a.T) return;
-    const int lane = threadIdx.x & 63, id = sdp::token_id(a.ids, a.wide, t, a.V);
+    const int lane = threadIdx.x & 63, id = sdp::token_id(a.ids, a.wide, t, a.V), whole = Rw::whole(a.d);
     const Elem* in = (const Elem*)a.E + (int64_t)id * a.d;
     Elem* out = (Elem*)a.Y + t * a.d;
-    for (int e = lane * N; e < a.d; e += 64 * N) {
-        u32x4 w = {0, 0, 0, 0};
-        if (id >= 0) {
+    const bool tail = whole + lane < a.d; // this lane has a value behind the whole pieces
+    const float last = tail && id >= 0 ? Rw::one(in + whole + lane) : 0.f;
+    for (int e0 = lane * N; e0 - lane * N < whole; e0 += B * 64 * N) {
+        u32x4 w[B] = {};
+        if (id >= 0)
+#pragma unroll
+            for (int i = 0; i < B; ++i) w[i] = Rw::load(in, e0 + i * 64 * N, whole);
+#pragma unroll
+        for (int i = 0; i < B; ++i) {
             float v[N];
-            Rw::unpack(Rw::load(in, e, a.d), v);
+            Rw::unpack(w[i], v);
 #pragma unroll
             for (int k = 0; k < N; ++k) v[k] *= a.scale;
-            w = Rw::pack(v);
+            Rw::store(out, e0 + i * 64 * N, whole, Rw::pack(v));
         }
-        Rw::store(out, e, a.d, w);
     }
+    if (tail) Rw::put(out + whole + lane, last * a.scale);
 }
 
 constexpr int kSortWaves = 16, kSortGroups = 256, kMaxRange = 960, kAhead = 16;
@@ -206,53 +212,64 @@ struct EmbedBwd {
     float scale;
 };
 
-template <int BF16>
-__device__ inline void write_row(const EmbedBwd& a, int id, int e, const float (&acc)[Row<BF16>::N]) {
-    float v[Row<BF16>::N];
-#pragma unroll
-    for (int k = 0; k < Row<BF16>::N; ++k) v[k] = acc[k] * a.scale;
-    Row<BF16>::store((typename Row<BF16>::Elem*)a.dE + (int64_t)id * a.d, e, a.d, Row<BF16>::pack(v));
-}
+// What a lane has of a row in a slab of 64 pieces: a piece, and where rows have values behind their whole pieces, in the first slab, one
+// of those
+template <int BF16, int TAIL>
+struct Lane {
+    typedef Row<BF16> Rw;
+    typedef typename Rw::Elem Elem;
+    static constexpr int N = Rw::N, M = N + TAIL;
+    int e, whole, et;
+    bool tail;
+    __device__ Lane(int d, int slab, int lane)
+        : e((slab * 64 + lane) * N), whole(Rw::whole(d)), et(whole + lane), tail(TAIL && slab == 0 && et < d) {}
 
-// the values of a piece (of either type) of a row of partial sums
-template <int N>
-__device__ inline void store_part(float* row, int e, int d, const float (&v)[N]) {
+    __device__ void write(const EmbedBwd& a, int id, const float (&acc)[M]) const {
+        Elem* row = (Elem*)a.dE + (int64_t)id * a.d;
+        float v[N];
 #pragma unroll
-    for (int k = 0; k < N; k += 4) Row<0>::store(row, e + k, d, Row<0>::pack({v[k], v[k + 1], v[k + 2], v[k + 3]}));
-}
-template <int N>
-__device__ inline void load_part(const float* row, int e, int d, u32x4 (&w)[N / 4]) {
+        for (int k = 0; k < N; ++k) v[k] = acc[k] * a.scale;
+        Rw::store(row, e, whole, Rw::pack(v));
+        if constexpr (TAIL)
+            if (tail) Rw::put(row + et, acc[N] * a.scale);
+    }
+    // a row of partial sums
+    __device__ void write_part(float* row, const float (&acc)[M]) const {
+        if (e < whole)
 #pragma unroll
-    for (int k = 0; k < N; k += 4) w[k / 4] = Row<0>::load(row, e + k, d);
-}
-template <int N>
-__device__ inline void add_part(const u32x4 (&w)[N / 4], float (&acc)[N]) {
+            for (int k = 0; k < N; ++k) row[e + k] = acc[k];
+        if constexpr (TAIL)
+            if (tail) row[et] = acc[N];
+    }
+    __device__ void read_part(const float* row, float (&v)[M]) const {
 #pragma unroll
-    for (int k = 0; k < N; ++k) acc[k] += __uint_as_float(w[k / 4][k % 4]);
-}
+        for (int k = 0; k < N; ++k) v[k] = e < whole ? row[e + k] : 0.f;
+        if constexpr (TAIL) v[N] = tail ? row[et] : 0.f;
+    }
+};
 
 // A workgroup has a chunk of the sorted tokens, a wave a piece of it, or 64 rows of dE for each wave to clear the empty ones of; and a slab of
 // 64 pieces of the columns.  What a wave has of a row that starts in an earlier one goes through LDS to the wave that has its start,
 // and to memory only where that lies in another chunk.
-template <int BF16>
+template <int BF16, int TAIL>
 __global__ __launch_bounds__(kSumWaves * 64) void embed_sum_kernel(EmbedBwd a) {
     typedef Row<BF16> Rw;
     typedef typename Rw::Elem Elem;
-    constexpr int N = Rw::N;
-    __shared__ float heads[kSumWaves][N][64];
+    constexpr int N = Rw::N, M = N + TAIL;
+    __shared__ float heads[kSumWaves][M][64];
     __shared__ int head_of[kSumWaves]; // 0: the wave starts with a row of its own; 1: its first row started earlier, 2: and goes on
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int64_t job = blockIdx.x / a.slabs;
-    const int e = ((int)(blockIdx.x - job * a.slabs) * 64 + lane) * N;
+    const Lane<BF16, TAIL> mine(a.d, (int)(blockIdx.x - job * a.slabs), lane);
     if (job >= a.chunks) {
         const int64_t v = ((job - a.chunks) * kSumWaves + wave) * 64;
         if (v >= a.V) return;
         const bool empty = v + lane < a.V && a.s.start[v + lane] == a.s.start[v + lane + 1];
         uint64_t left = __ballot(empty);
+        const float zeros[M] = {};
         while (left) {
-            const int i = __ffsll((unsigned long long)left) - 1;
+            mine.write(a, (int)v + __ffsll((unsigned long long)left) - 1, zeros);
             left &= left - 1;
-            if (e < a.d) Rw::store((Elem*)a.dE + (v + i) * a.d, e, a.d, u32x4{0, 0, 0, 0});
         }
         return;
     }
@@ -262,14 +279,20 @@ __global__ __launch_bounds__(kSumWaves * 64) void embed_sum_kernel(EmbedBwd a) {
     const int n = a.s.start[a.V];
     if (job * kChunk >= n) return;
     const int cnt = max(0, min(kPiece, n - p0)), next = p0 + cnt < n ? behind : -1;
-    float acc[N] = {};
+    float acc[M] = {};
     bool own = p0 == 0 || __builtin_amdgcn_readlane(id, 0) != prev; // the row at hand starts in this piece
     int head = 0, tail = -1; // tail: the row that starts here and goes on; acc is its sum then
     u32x4 w[kPiece];
+    float wt[kPiece];
 #pragma unroll
     for (int j = 0; j < kPiece; ++j) {
-        w[j] = u32x4{0, 0, 0, 0};
-        if (j < cnt && e < a.d) w[j] = Rw::load((const Elem*)a.dY + (int64_t)__builtin_amdgcn_readlane(tok, j) * a.d, e, a.d);
+        w[j] = u32x4{0, 0, 0, 0}, wt[j] = 0.f;
+        if (j < cnt) {
+            const Elem* row = (const Elem*)a.dY + (int64_t)__builtin_amdgcn_readlane(tok, j) * a.d;
+            w[j] = Rw::load(row, mine.e, mine.whole);
+            if constexpr (TAIL)
+                if (mine.tail) wt[j] = Rw::one(row + mine.et);
+        }
     }
 #pragma unroll
     for (int j = 0; j < kPiece; ++j) {
@@ -278,94 +301,96 @@ __global__ __launch_bounds__(kSumWaves * 64) void embed_sum_kernel(EmbedBwd a) {
             Rw::unpack(w[j], v);
 #pragma unroll
             for (int k = 0; k < N; ++k) acc[k] += v[k];
+            if constexpr (TAIL) acc[N] += wt[j];
             const int row = __builtin_amdgcn_readlane(id, j);
             const int after = j == cnt - 1 ? next : __builtin_amdgcn_readlane(id, (j + 1) % kPiece);
             if (j == cnt - 1 && row == after && own) {
                 tail = row;
             } else if (j == cnt - 1 || row != after) {
                 if (own) {
-                    if (e < a.d) write_row<BF16>(a, row, e, acc);
+                    mine.write(a, row, acc);
                 } else {
                     head = row == after ? 2 : 1;
 #pragma unroll
-                    for (int k = 0; k < N; ++k) heads[wave][k][lane] = acc[k];
+                    for (int k = 0; k < M; ++k) heads[wave][k][lane] = acc[k];
                 }
                 own = true;
 #pragma unroll
-                for (int k = 0; k < N; ++k) acc[k] = 0.f;
+                for (int k = 0; k < M; ++k) acc[k] = 0.f;
             }
         }
     }
     if (lane == 0) head_of[wave] = head;
     __syncthreads();
     // adds what the waves from `from` on have of a row that goes on in them; whether it ends there
-    auto follow = [&](float (&sum)[N], int from) {
+    auto follow = [&](float (&sum)[M], int from) {
         for (int u = from; u < kSumWaves; ++u) {
 #pragma unroll
-            for (int k = 0; k < N; ++k) sum[k] += heads[u][k][lane];
+            for (int k = 0; k < M; ++k) sum[k] += heads[u][k][lane];
             if (__builtin_amdgcn_readfirstlane(head_of[u]) != 2) return true;
         }
         return false;
     };
     float* part = a.part + job * 2 * a.d;
     if (tail >= 0) {
-        const bool ends = follow(acc, wave + 1);
-        if (e < a.d) {
-            if (ends) write_row<BF16>(a, tail, e, acc);
-            else store_part<N>(part + a.d, e, a.d, acc);
-        }
+        if (follow(acc, wave + 1)) mine.write(a, tail, acc);
+        else mine.write_part(part + a.d, acc);
     }
     if (wave == 0 && head) {
 #pragma unroll
-        for (int k = 0; k < N; ++k) acc[k] = heads[0][k][lane];
+        for (int k = 0; k < M; ++k) acc[k] = heads[0][k][lane];
         if (head == 2) follow(acc, 1);
-        if (e < a.d) store_part<N>(part, e, a.d, acc);
+        mine.write_part(part, acc);
     }
 }
 
 // A workgroup looks at a chunk and a slab: if a row starts there and goes on, it adds up the row's partial sums.  Each wave adds every
 // fourth chunk's, in their order, and the waves' sums follow in theirs.
-template <int BF16>
+template <int BF16, int TAIL>
 __global__ __launch_bounds__(256) void embed_join_kernel(EmbedBwd a) {
-    constexpr int N = Row<BF16>::N, B = 4;
-    __shared__ float lds[4][N][64];
+    constexpr int M = Lane<BF16, TAIL>::M, B = 4;
+    __shared__ float lds[4][M][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int64_t job = blockIdx.x / a.slabs;
-    const int e = ((int)(blockIdx.x - job * a.slabs) * 64 + lane) * N;
+    const Lane<BF16, TAIL> mine(a.d, (int)(blockIdx.x - job * a.slabs), lane);
     const int n = a.s.start[a.V];
     const int2 span = a.s.spans[job]; // written where the next chunk has a token
     if ((job + 1) * kChunk >= n || span.x < 0) return;
-    float acc[N] = {};
-    if (e < a.d) {
-        // the row's parts: of chunk `job`, then of those up to span.y
-        auto part = [&](int64_t c) { return a.part + (c * 2 + (c == job)) * a.d; };
-        for (int64_t c = job + wave; c <= span.y; c += 4 * B) {
-            u32x4 w[B][N / 4] = {};
+    float acc[M] = {};
+    // the row's parts: of chunk `job`, then of those up to span.y
+    for (int64_t c = job + wave; c <= span.y; c += 4 * B) {
+        float v[B][M] = {};
 #pragma unroll
-            for (int j = 0; j < B; ++j)
-                if (c + 4 * j <= span.y) load_part<N>(part(c + 4 * j), e, a.d, w[j]);
-#pragma unroll
-            for (int j = 0; j < B; ++j) add_part<N>(w[j], acc); // zeros behind the last
+        for (int j = 0; j < B; ++j) {
+            const int64_t at = c + 4 * j;
+            if (at <= span.y) mine.read_part(a.part + (at * 2 + (at == job)) * a.d, v[j]);
         }
+#pragma unroll
+        for (int j = 0; j < B; ++j)
+#pragma unroll
+            for (int k = 0; k < M; ++k) acc[k] += v[j][k]; // zeros behind the last
     }
 #pragma unroll
-    for (int k = 0; k < N; ++k) lds[wave][k][lane] = acc[k];
+    for (int k = 0; k < M; ++k) lds[wave][k][lane] = acc[k];
     __syncthreads();
-    if (wave > 0 || e >= a.d) return;
+    if (wave > 0) return;
 #pragma unroll
-    for (int k = 0; k < N; ++k) acc[k] = ((lds[0][k][lane] + lds[1][k][lane]) + lds[2][k][lane]) + lds[3][k][lane];
-    write_row<BF16>(a, span.x, e, acc);
+    for (int k = 0; k < M; ++k) acc[k] = ((lds[0][k][lane] + lds[1][k][lane]) + lds[2][k][lane]) + lds[3][k][lane];
+    mine.write(a, span.x, acc);
 }
 
 int check_embed(int dtype, int id_type, int T, int V, int d) {
     if (dtype != SDP_F32 && dtype != SDP_BF16) return SDP_ERR_INVALID_ARG;
     if (id_type != SDP_I32 && id_type != SDP_I64) return SDP_ERR_INVALID_ARG;
     if (T < 0 || V < 1 || d < 1) return SDP_ERR_INVALID_ARG;
-    return T > SDP_MAX_TOKENS ? SDP_ERR_SHAPE : SDP_OK;
+    return T > SDP_MAX_EXTENT || V > SDP_MAX_EXTENT || d > SDP_MAX_EXTENT ? SDP_ERR_SHAPE : SDP_OK;
 }
 
 int chunks_of(int T) { return (int)(((int64_t)T + kChunk - 1) / kChunk); }
-int slabs_of(int dtype, int d) { return (d + (dtype == SDP_BF16 ? 511 : 255)) / (dtype == SDP_BF16 ? 512 : 256); }
+int slabs_of(int dtype, int d) { // one of a row of less than a piece, which is all tail
+    const int s = dtype == SDP_BF16 ? (Row<1>::whole(d) + 511) / 512 : (Row<0>::whole(d) + 255) / 256;
+    return s > 0 ? s : 1;
+}
 
 struct Layout {
     size_t ids, start, spans, part, all;
@@ -437,15 +462,19 @@ extern "C" int sdp_embed_bwd(int dtype, int id_type, int T, int V, int d, float 
     auto sort_of = [&](auto wide) {
         return T <= kSortWaves * kListed ? sort(wide, std::integral_constant<int, 1>{}) : sort(wide, std::integral_constant<int, 0>{});
     };
-    int st = id_type == SDP_I64 ? sort_of(std::integral_constant<int, 1>{}) : sort_of(std::integral_constant<int, 0>{});
-    if (st != SDP_OK) return st;
+    if (const int st = id_type == SDP_I64 ? sort_of(std::integral_constant<int, 1>{}) : sort_of(std::integral_constant<int, 0>{}); st != SDP_OK)
+        return st;
     const int64_t sum = ((int64_t)a.chunks + ((int64_t)V + kSumWaves * 64 - 1) / (kSumWaves * 64)) * a.slabs, join = (int64_t)(a.chunks - 1) * a.slabs;
     const unsigned gs = (unsigned)sum, gj = (unsigned)join;
-    if (dtype == SDP_BF16) embed_sum_kernel<1><<<gs, kSumWaves * 64, 0, s>>>(a);
-    else embed_sum_kernel<0><<<gs, kSumWaves * 64, 0, s>>>(a);
-    st = sdp::launch_status();
-    if (st != SDP_OK || a.chunks < 2) return st;
-    if (dtype == SDP_BF16) embed_join_kernel<1><<<gj, 256, 0, s>>>(a);
-    else embed_join_kernel<0><<<gj, 256, 0, s>>>(a);
-    return sdp::launch_status();
+    auto sums = [&](auto bf16, auto tail) {
+        embed_sum_kernel<bf16.value, tail.value><<<gs, kSumWaves * 64, 0, s>>>(a);
+        const int rc = sdp::launch_status();
+        if (rc != SDP_OK || a.chunks < 2) return rc;
+        embed_join_kernel<bf16.value, tail.value><<<gj, 256, 0, s>>>(a);
+        return sdp::launch_status();
+    };
+    auto sums_of = [&](auto bf16) {
+        return d % Row<bf16.value>::N ? sums(bf16, std::integral_constant<int, 1>{}) : sums(bf16, std::integral_constant<int, 0>{});
+    };
+    return dtype == SDP_BF16 ? sums_of(std::integral_constant<int, 1>{}) : sums_of(std::integral_constant<int, 0>{});
 }

@@ -50,14 +50,6 @@ constexpr uint32_t minus_inf() {
     return BF16 ? 0xFF80FF80u : 0xFF800000u;
 }
 
-// The row is unpacked anew from here on: the compiler would rather keep its fp32 values, twice the registers (177 instead of 96 for 16
-// pieces of bf16, two waves a SIMD instead of five).
-template <int P>
-__device__ inline void again(u32x4 (&w)[P]) {
-#pragma unroll
-    for (int i = 0; i < P; ++i) asm volatile("" : "+v"(w[i]));
-}
-
 // PIECES > 0: pieces a lane holds, the row has no more; 0: the row is read again for the gradient
 template <int BF16, int WAVES, int PIECES, int ONCE>
 __global__ __launch_bounds__(WAVES * 64) void token_loss_kernel(Loss a) {
@@ -66,43 +58,51 @@ __global__ __launch_bounds__(WAVES * 64) void token_loss_kernel(Loss a) {
     constexpr int N = Rw::N, TH = WAVES * 64, P = PIECES ? PIECES : 1;
     __shared__ float lds[2][WAVES], at_label;
     const int64_t row = blockIdx.x;
-    const int tid = threadIdx.x, V = a.V, label = sdp::token_id(a.labels, a.wide, row, V);
+    const int tid = threadIdx.x, V = a.V, whole = Rw::whole(V), label = sdp::token_id(a.labels, a.wide, row, V);
     const Elem* z = (const Elem*)a.Z + row * a.ldz;
     Elem* dz = (Elem*)a.dZ + row * a.ldz;
+    const bool tail = whole + tid < V; // this lane has a value behind the whole pieces
     if (label < 0) {
         if (tid == 0) {
             a.nll[row] = 0.f;
             if (a.lse) a.lse[row] = 0.f;
         }
-        if (a.dZ)
-            for (int64_t e = tid * N; e < V; e += TH * N) Rw::store(dz, (int)e, V, u32x4{0, 0, 0, 0});
+        if (a.dZ) {
+            for (int64_t e = tid * N; e < whole; e += TH * N) Rw::store(dz, (int)e, whole, u32x4{0, 0, 0, 0});
+            if (tail) Rw::put(dz + whole + tid, 0.f);
+        }
         return;
     }
     const float c = a.scale * (a.scale_dev ? *a.scale_dev : 1.f);
     u32x4 w[P];
-    float m = -INFINITY, sum = 0.f;
-    if (tid == 0) at_label = Rw::one(z + label); // read before anything is written: dZ may be Z
-    if (PIECES) {
+    auto piece = [&](int64_t e) { return Rw::mine(Rw::load(z, (int)e, whole), (int)e, whole, minus_inf<BF16>()); }; // of a row that is read twice
+    if (PIECES)
 #pragma unroll
-        for (int i = 0; i < P; ++i) w[i] = Rw::template load<ONCE>(z, (tid + i * TH) * N, V, minus_inf<BF16>());
+        for (int i = 0; i < P; ++i) w[i] = Rw::template load<ONCE>(z, (tid + i * TH) * N, whole);
+    const float zt = tail ? Rw::one(z + whole + tid) : -INFINITY;
+    if (tid == 0) at_label = Rw::one(z + label); // read before anything is written: dZ may be Z
+    float m = zt, sum = 0.f;
+    if (PIECES) {
 #pragma unroll
         for (int i = 0; i < P; ++i) {
             float v[N];
+            w[i] = Rw::mine(w[i], (tid + i * TH) * N, whole, minus_inf<BF16>());
             Rw::unpack(w[i], v);
 #pragma unroll
             for (int k = 0; k < N; ++k) m = fmaxf(m, v[k]);
         }
     } else {
-        for (int64_t e = tid * N; e < V; e += TH * N) {
+        for (int64_t e = tid * N; e < whole; e += TH * N) {
             float v[N];
-            Rw::unpack(Rw::load(z, (int)e, V, minus_inf<BF16>()), v);
+            Rw::unpack(piece(e), v);
 #pragma unroll
             for (int k = 0; k < N; ++k) m = fmaxf(m, v[k]);
         }
     }
     m = group_all<WAVES, true>(m, lds[0]);
-    if (PIECES) again(w);
+    if (PIECES) sdp::again(w);
     auto power = [&](float v) { return __builtin_amdgcn_exp2f((v - m) * kLog2e); };
+    if (tail) sum = power(zt);
     if (PIECES) {
 #pragma unroll
         for (int i = 0; i < P; ++i) {
@@ -112,15 +112,15 @@ __global__ __launch_bounds__(WAVES * 64) void token_loss_kernel(Loss a) {
             for (int k = 0; k < N; ++k) sum += power(v[k]);
         }
     } else {
-        for (int64_t e = tid * N; e < V; e += TH * N) {
+        for (int64_t e = tid * N; e < whole; e += TH * N) {
             float v[N];
-            Rw::unpack(Rw::load(z, (int)e, V, minus_inf<BF16>()), v);
+            Rw::unpack(piece(e), v);
 #pragma unroll
             for (int k = 0; k < N; ++k) sum += power(v[k]);
         }
     }
     sum = group_all<WAVES, false>(sum, lds[1]);
-    if (PIECES) again(w);
+    if (PIECES) sdp::again(w);
     if (tid == 0) {
         const float log_sum = logf(sum);
         a.nll[row] = (m - at_label) + log_sum;
@@ -128,20 +128,20 @@ __global__ __launch_bounds__(WAVES * 64) void token_loss_kernel(Loss a) {
     }
     if (!a.dZ) return;
     const float inv = c / sum;
-    auto gradient = [&](int e, const u32x4& piece) {
+    auto gradient = [&](int e, const u32x4& x) {
         float v[N];
-        Rw::unpack(piece, v);
+        Rw::unpack(x, v);
 #pragma unroll
         for (int k = 0; k < N; ++k) v[k] = power(v[k]) * inv - (e + k == label ? c : 0.f);
-        Rw::store(dz, e, V, Rw::pack(v));
+        Rw::store(dz, e, whole, Rw::pack(v));
     };
     if (PIECES) {
 #pragma unroll
-        for (int i = 0; i < P; ++i)
-            if ((tid + i * TH) * N < V) gradient((tid + i * TH) * N, w[i]);
+        for (int i = 0; i < P; ++i) gradient((tid + i * TH) * N, w[i]);
     } else {
-        for (int64_t e = tid * N; e < V; e += TH * N) gradient((int)e, Rw::load(z, (int)e, V));
+        for (int64_t e = tid * N; e < whole; e += TH * N) gradient((int)e, piece(e));
     }
+    if (tail) Rw::put(dz + whole + tid, power(zt) * inv - (whole + tid == label ? c : 0.f));
 }
 
 // Sum of a double over a workgroup of 1024, in a fixed order; valid in thread 0
@@ -161,13 +161,19 @@ __device__ inline S group_sum(S x) {
 __global__ __launch_bounds__(1024) void loss_sum_kernel(const float* __restrict__ nll, int T, float scale, const float* scale_dev,
                                                         float* loss) {
     double x = 0.0;
-    for (int t0 = threadIdx.x; t0 < T; t0 += 8 * 1024) {
-        float v[8];
+    const int whole = Row<0>::whole(T);
+    for (int t0 = threadIdx.x * 4; t0 < whole; t0 += 4 * 4096) {
+        u32x4 w[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = t0 + i * 1024 < T ? nll[t0 + i * 1024] : 0.f;
+        for (int i = 0; i < 4; ++i) w[i] = Row<0>::load_some(nll, t0 + i * 4096, whole);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x += (double)v[i];
+        for (int i = 0; i < 4; ++i) {
+            w[i] = Row<0>::mine(w[i], t0 + i * 4096, whole);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x += (double)__uint_as_float(w[i][k]);
+        }
     }
+    if (whole + (int)threadIdx.x < T) x += (double)nll[whole + threadIdx.x];
     x = group_sum(x);
     if (threadIdx.x == 0) *loss = (float)(x * ((double)scale * (scale_dev ? (double)*scale_dev : 1.0)));
 }
@@ -175,32 +181,53 @@ __global__ __launch_bounds__(1024) void loss_sum_kernel(const float* __restrict_
 template <int WIDE>
 __global__ __launch_bounds__(1024) void label_scale_kernel(const void* __restrict__ labels, int T, int V, float* scale) {
     int n = 0;
-    for (int t0 = threadIdx.x; t0 < T; t0 += 8 * 1024) {
-        int id[8];
+    // 16 bytes at a time, as words
+    constexpr int W = WIDE ? 2 : 1, N = 4 / W;
+    const int whole = T / N * N;
+    for (int t0 = threadIdx.x * N; t0 < whole; t0 += 4 * 1024 * N) {
+        u32x4 w[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) id[i] = t0 + i * 1024 < T ? sdp::token_id<WIDE>(labels, t0 + i * 1024, V) : -1;
+        for (int i = 0; i < 4; ++i) w[i] = *(const sdp::u32x4_at4*)((const char*)labels + (int64_t)min(t0 + i * 1024 * N, whole - N) * (4 * W));
 #pragma unroll
-        for (int i = 0; i < 8; ++i) n += id[i] >= 0;
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; k += W)
+                n += t0 + i * 1024 * N < whole && w[i][k] < (uint32_t)V && (!WIDE || w[i][(k + 1) % 4] == 0);
     }
+    if (whole + (int)threadIdx.x < T) n += sdp::token_id<WIDE>(labels, whole + threadIdx.x, V) >= 0;
     n = group_sum(n);
     if (threadIdx.x == 0) *scale = 1.0f / (float)(n > 1 ? n : 1);
 }
 
-// The fewest waves that hold a row with 16 pieces a lane, fewer pieces where those do
+// Waves of a row and pieces of a lane: the first pair in this order that holds the row.  Few waves leave no lane idle and wait for
+// each other less, many keep the registers few enough for two workgroups on a CU, so that one loads while the other computes or stores.  bf16,
+// us: 8192 x 1024 two waves of one piece 7, four 12.6; 8192 x 4000 4 x 2 23.3, 8 x 1 30.8; 8192 x 8000 4 x 4 45.7, 8 x 2 48.1, 16 x 1 65.8; 4096 x 16000
+// 8 x 4 47.4, 16 x 2 50.9; 8192 x 32000 16 x 4 172, 8 x 8 178, 4 x 16 181; 1000 x 50001 16 x 7 40.5, 8 x 16 43; 1000 x 65536 8 x 16 53.1, 16 x 8 (66
+// registers, one workgroup) 59.6.
 template <class F>
 void by_row(int bf16, int V, F&& launch) {
     const int n = bf16 ? 8 : 4;
     auto with = [&](auto b) {
         const int64_t pieces = ((int64_t)V + n - 1) / n;
-        auto go = [&](auto waves, auto p) { launch(b, waves, p); };
-        using std::integral_constant;
-        if (pieces <= 256) go(integral_constant<int, 4>{}, integral_constant<int, 1>{});
-        else if (pieces <= 1024) go(integral_constant<int, 4>{}, integral_constant<int, 4>{});
-        else if (pieces <= 2048) go(integral_constant<int, 4>{}, integral_constant<int, 8>{});
-        else if (pieces <= 4096) go(integral_constant<int, 4>{}, integral_constant<int, 16>{});
-        else if (pieces <= 8192) go(integral_constant<int, 8>{}, integral_constant<int, 16>{});
-        else if (pieces <= 16384) go(integral_constant<int, 16>{}, integral_constant<int, 16>{});
-        else go(integral_constant<int, 16>{}, integral_constant<int, 0>{});
+#define SDP_LOSS_ROW(WAVES, PIECES) \
+    if (pieces <= WAVES * 64 * PIECES) return launch(b, std::integral_constant<int, WAVES>{}, std::integral_constant<int, PIECES>{})
+        SDP_LOSS_ROW(1, 1);
+        SDP_LOSS_ROW(2, 1);
+        SDP_LOSS_ROW(4, 1);
+        SDP_LOSS_ROW(4, 2);
+        SDP_LOSS_ROW(4, 4);
+        SDP_LOSS_ROW(8, 3);
+        SDP_LOSS_ROW(8, 4);
+        SDP_LOSS_ROW(8, 6);
+        SDP_LOSS_ROW(16, 4);
+        SDP_LOSS_ROW(16, 5);
+        SDP_LOSS_ROW(16, 6);
+        SDP_LOSS_ROW(16, 7);
+        SDP_LOSS_ROW(8, 16);
+        SDP_LOSS_ROW(16, 12);
+        SDP_LOSS_ROW(16, 16);
+#undef SDP_LOSS_ROW
+        launch(b, std::integral_constant<int, 16>{}, std::integral_constant<int, 0>{});
     };
     if (bf16) with(std::integral_constant<int, 1>{});
     else with(std::integral_constant<int, 0>{});
@@ -213,7 +240,7 @@ extern "C" int sdp_token_loss(int dtype, int id_type, int T, int V, int64_t ldz,
     if (dtype != SDP_F32 && dtype != SDP_BF16) return SDP_ERR_INVALID_ARG;
     if (id_type != SDP_I32 && id_type != SDP_I64) return SDP_ERR_INVALID_ARG;
     if (T < 0 || V < 1 || !std::isfinite(scale)) return SDP_ERR_INVALID_ARG;
-    if (T > SDP_MAX_TOKENS || ldz < V || ldz > ((int64_t)1 << 40)) return SDP_ERR_SHAPE;
+    if (T > SDP_MAX_EXTENT || V > SDP_MAX_EXTENT || ldz < V || ldz > ((int64_t)1 << 40)) return SDP_ERR_SHAPE;
     const size_t es = dtype == SDP_BF16 ? 2 : 4, is = id_type == SDP_I64 ? 8 : 4, st = (size_t)T * 4;
     if (T > 0 && (!Z || !labels || !nll)) return SDP_ERR_INVALID_ARG;
     if (!sdp::aligned_to(Z, es) || !sdp::aligned_to(dZ, es) || !sdp::aligned_to(labels, is)) return SDP_ERR_INVALID_ARG;
@@ -245,7 +272,7 @@ extern "C" int sdp_token_loss(int dtype, int id_type, int T, int V, int64_t ldz,
 extern "C" int sdp_label_scale(int id_type, int T, int V, const void* labels, float* scale, void* stream) {
     if (id_type != SDP_I32 && id_type != SDP_I64) return SDP_ERR_INVALID_ARG;
     if (T < 0 || V < 1 || !scale || (T > 0 && !labels)) return SDP_ERR_INVALID_ARG;
-    if (T > SDP_MAX_TOKENS) return SDP_ERR_SHAPE;
+    if (T > SDP_MAX_EXTENT || V > SDP_MAX_EXTENT) return SDP_ERR_SHAPE;
     if (!sdp::aligned_to(labels, id_type == SDP_I64 ? 8 : 4) || !sdp::aligned_to(scale, 4)) return SDP_ERR_INVALID_ARG;
     if (T > 0 && sdp::overlap({{scale, 4}}, {{labels, (size_t)T * (id_type == SDP_I64 ? 8 : 4)}})) return SDP_ERR_INVALID_ARG;
     sdp::ProfileScope ps("label_scale", (hipStream_t)stream);

@@ -38,6 +38,9 @@ struct NormBwd {
 // waves of a workgroup: four rows of one wave each, or one row of four or sixteen
 constexpr int waves_of(int WPR) { return WPR > 4 ? WPR : 4; }
 
+constexpr int kBwdWaves = 8;
+constexpr int bwd_waves(int WPR) { return WPR > kBwdWaves ? WPR : kBwdWaves; }
+
 // Sum over the WPR waves of a row; every lane has the result.  `lds` holds one float a wave; two calls in a row need two of them.
 template <int WPR>
 __device__ inline float row_sum(float x, float* lds) {
@@ -53,25 +56,49 @@ __device__ inline float row_sum(float x, float* lds) {
     return s;
 }
 
-template <int BF16, int WPR, int VPL, int ONCE>
+// two sums at once
+template <int WPR>
+__device__ inline void row_sums(float& x, float& y, float2* lds) {
+    x = sdp::wave_sum(x), y = sdp::wave_sum(y);
+    if (WPR == 1) return;
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) lds[wave] = make_float2(x, y);
+    __syncthreads();
+    const int first = wave / WPR * WPR;
+    float2 s = lds[first];
+#pragma unroll
+    for (int i = 1; i < WPR; ++i) s.x += lds[first + i].x, s.y += lds[first + i].y;
+    x = s.x, y = s.y;
+}
+
+// FORM: rows of whole pieces, such rows read once (read_once), rows with values behind them, rows of less than a piece
+constexpr int FORM_WHOLE = 0, FORM_ONCE = 1, FORM_TAIL = 2, FORM_SHORT = 3;
+
+template <int BF16, int WPR, int VPL, int FORM>
 __global__ __launch_bounds__(waves_of(WPR) * 64) void norm_fwd_kernel(NormFwd a) {
     typedef Row<BF16> Rw;
     typedef typename Rw::Elem Elem;
-    constexpr int N = Rw::N, ROWS = waves_of(WPR) / WPR;
+    constexpr int N = Rw::N, ROWS = waves_of(WPR) / WPR, STEP = WPR * 64 * N, ONCE = FORM == FORM_ONCE;
     __shared__ float lds[2][waves_of(WPR)];
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int64_t row = (int64_t)blockIdx.x * ROWS + wave / WPR;
     if (ROWS > 1 && row >= a.T) return; // no barrier where a workgroup has several rows
-    const int d = a.d, at = (wave % WPR * 64 + lane) * N;
+    const int d = a.d, whole = Rw::whole(d), at = (wave % WPR * 64 + lane) * N, et = whole + lane;
+    const bool tail = FORM >= FORM_TAIL && wave % WPR == 0 && et < d; // this lane has a value behind the whole pieces
     const int64_t off = row * d;
     u32x4 x[VPL];
-    float h[VPL][N];
+    float h[VPL][N], ht = 0.f;
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) x[i] = Rw::template load<ONCE>((const Elem*)a.X + off, at + i * WPR * 64 * N, d);
+    for (int i = 0; i < VPL; ++i) x[i] = Rw::template load<ONCE>((const Elem*)a.X + off, at + i * STEP, whole);
+    if (tail) ht = Rw::one((const Elem*)a.X + off + et);
     if (a.R) {
         u32x4 r[VPL];
 #pragma unroll
-        for (int i = 0; i < VPL; ++i) r[i] = Rw::template load<ONCE>((const Elem*)a.R + off, at + i * WPR * 64 * N, d);
+        for (int i = 0; i < VPL; ++i) r[i] = Rw::template load<ONCE>((const Elem*)a.R + off, at + i * STEP, whole);
+        if (tail) {
+            ht = Rw::rounded(ht + Rw::one((const Elem*)a.R + off + et));
+            Rw::put((Elem*)a.H + off + et, ht);
+        }
 #pragma unroll
         for (int i = 0; i < VPL; ++i) {
             float p[N], q[N];
@@ -79,25 +106,26 @@ __global__ __launch_bounds__(waves_of(WPR) * 64) void norm_fwd_kernel(NormFwd a)
 #pragma unroll
             for (int k = 0; k < N; ++k) p[k] += q[k];
             x[i] = Rw::pack(p); // the statistics are those of what is stored
-            Rw::store((Elem*)a.H + off, at + i * WPR * 64 * N, d, x[i]);
+            Rw::store((Elem*)a.H + off, at + i * STEP, whole, x[i]);
         }
     }
-    float sum = 0.f;
+    float sum = ht;
 #pragma unroll
     for (int i = 0; i < VPL; ++i) {
-        Rw::unpack(x[i], h[i]);
+        Rw::unpack(Rw::mine(x[i], at + i * STEP, whole), h[i]);
 #pragma unroll
         for (int k = 0; k < N; ++k) sum += h[i][k];
     }
     const float mu = a.layer ? row_sum<WPR>(sum, lds[0]) / (float)d : 0.f;
-    float sq = 0.f;
+    ht -= mu;
+    float sq = tail ? ht * ht : 0.f;
 #pragma unroll
     for (int i = 0; i < VPL; ++i) {
-        const int left = d - (at + i * WPR * 64 * N); // what lies behind the row's end has no part in the squares
+        const bool live = at + i * STEP < whole;
 #pragma unroll
         for (int k = 0; k < N; ++k) {
             h[i][k] -= mu;
-            sq += k < left ? h[i][k] * h[i][k] : 0.f;
+            sq += live ? h[i][k] * h[i][k] : 0.f;
         }
     }
     const float rstd = 1.0f / __builtin_sqrtf(row_sum<WPR>(sq, lds[1]) / (float)d + a.eps);
@@ -107,51 +135,93 @@ __global__ __launch_bounds__(waves_of(WPR) * 64) void norm_fwd_kernel(NormFwd a)
     }
 #pragma unroll
     for (int i = 0; i < VPL; ++i) {
-        const int e = at + i * WPR * 64 * N;
-        if (e >= d) break;
-        float ga[N], be[N];
-        Rw::unpack(Rw::load((const Elem*)a.gamma, e, d), ga);
-        if (a.beta) Rw::unpack(Rw::load((const Elem*)a.beta, e, d), be);
+        const int e = at + i * STEP;
+        float ga[N], be[N] = {};
+        Rw::unpack(Rw::load((const Elem*)a.gamma, e, whole), ga);
+        if (a.beta) Rw::unpack(Rw::load((const Elem*)a.beta, e, whole), be);
 #pragma unroll
         for (int k = 0; k < N; ++k) {
             h[i][k] = h[i][k] * rstd * ga[k];
             if (a.beta) h[i][k] += be[k];
         }
-        Rw::store((Elem*)a.Y + off, e, d, Rw::pack(h[i]));
+        Rw::store((Elem*)a.Y + off, e, whole, Rw::pack(h[i]));
+    }
+    if (tail) {
+        ht = ht * rstd * Rw::one((const Elem*)a.gamma + et);
+        if (a.beta) ht += Rw::one((const Elem*)a.beta + et);
+        Rw::put((Elem*)a.Y + off + et, ht);
     }
 }
 
-// A workgroup takes rows in turn and keeps its columns' share of dgamma and dbeta in registers; at the end the shares of the
-// workgroup's rows are added up, in the order of its waves, and written as one row of `partial`.
-template <int BF16, int WPR, int VPL>
-__global__ __launch_bounds__(waves_of(WPR) * 64) void norm_bwd_kernel(NormBwd a) {
+// What a lane has of a row in the backward pass
+template <int BF16, int VPL>
+struct Held {
+    u32x4 h[VPL], dy[VPL], skip[VPL];
+    float ht, dyt, skipt; // behind the whole pieces
+    float rstd, mu;
+};
+
+// A workgroup of kBwdWaves waves (or those of a row) takes rows in turn and keeps its columns' share of dgamma and dbeta in registers; at
+// the end the shares of the workgroup's rows are added up, in the order of its waves, and written as one row of `partial`.  The next row is
+// requested before the one at hand is worked on, by the same number of loads whatever the row: with loads behind a condition the
+// wait for the row at hand would be one for the next as well.
+template <int BF16, int WPR, int VPL, int FORM, int SKIP>
+__global__ __launch_bounds__(bwd_waves(WPR) * 64) void norm_bwd_kernel(NormBwd a) {
     typedef Row<BF16> Rw;
     typedef typename Rw::Elem Elem;
-    constexpr int N = Rw::N, ROWS = waves_of(WPR) / WPR;
-    __shared__ float lds[2][2][waves_of(WPR)]; // two sums of a row, and the next row's
+    typedef Held<BF16, VPL> Row1;
+    constexpr int N = Rw::N, WAVES = bwd_waves(WPR), ROWS = WAVES / WPR, STEP = WPR * 64 * N;
+    __shared__ float2 lds[2][WAVES]; // the two sums of a row, and the next row's
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int d = a.d, at = (wave % WPR * 64 + lane) * N;
+    const int d = a.d, whole = Rw::whole(d), at = (wave % WPR * 64 + lane) * N, et = whole + lane;
+    const bool tail = FORM >= FORM_TAIL && wave % WPR == 0 && et < d;
     const float width = (float)d;
     u32x4 ga[VPL];
-    float dga[VPL][N] = {}, dbe[VPL][N] = {};
+    float dga[VPL][N] = {}, dbe[VPL][N] = {}, gat = 0.f, dgat = 0.f, dbet = 0.f;
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) ga[i] = Rw::load((const Elem*)a.gamma, at + i * WPR * 64 * N, d);
-    int turn = 0;
-    for (int64_t row = (int64_t)blockIdx.x * ROWS + wave / WPR; row < a.T; row += (int64_t)gridDim.x * ROWS, turn ^= 1) {
-        const int64_t off = row * d;
-        u32x4 hw[VPL], yw[VPL];
+    for (int i = 0; i < VPL; ++i) ga[i] = FORM == FORM_SHORT ? u32x4{0, 0, 0, 0} : Rw::load((const Elem*)a.gamma, at + i * STEP, whole);
+    if (tail) gat = Rw::one((const Elem*)a.gamma + et);
+    const int64_t step = (int64_t)gridDim.x * ROWS;
+    int64_t row = (int64_t)blockIdx.x * ROWS + wave / WPR;
+    const float* means = a.mean ? a.mean : a.rstd; // no mean: read, not used
+    const int ett = FORM >= FORM_TAIL ? min(et, d - 1) : 0;
+    auto request = [&](int64_t r, Row1& w) {
+        r = r < a.T ? r : a.T - 1; // behind the last row: read, not used
+        const int64_t off = r * d;
 #pragma unroll
         for (int i = 0; i < VPL; ++i) {
-            hw[i] = Rw::load((const Elem*)a.H + off, at + i * WPR * 64 * N, d);
-            yw[i] = Rw::load((const Elem*)a.dY + off, at + i * WPR * 64 * N, d);
+            if constexpr (FORM == FORM_SHORT) {
+                w.h[i] = w.dy[i] = w.skip[i] = u32x4{0, 0, 0, 0};
+            } else {
+                w.h[i] = Rw::load_some((const Elem*)a.H + off, at + i * STEP, whole);
+                w.dy[i] = Rw::load_some((const Elem*)a.dY + off, at + i * STEP, whole);
+                if constexpr (SKIP) w.skip[i] = Rw::load_some((const Elem*)a.dH + off, at + i * STEP, whole);
+            }
         }
-        const float rstd = a.rstd[row], mu = a.mean ? a.mean[row] : 0.f;
-        float s1 = 0.f, s2 = 0.f;
+        if constexpr (FORM >= FORM_TAIL) {
+            w.ht = Rw::one((const Elem*)a.H + off + ett), w.dyt = Rw::one((const Elem*)a.dY + off + ett);
+            if constexpr (SKIP) w.skipt = Rw::one((const Elem*)a.dH + off + ett);
+        }
+        w.rstd = a.rstd[r], w.mu = means[r];
+    };
+    // the row in `now`, while the one after it is on its way to `next`
+    auto take = [&](Row1& now, Row1& next, float2* sums) {
+        request(row + step, next);
+        const bool live = row < a.T;
+        const int held = live ? whole : 0;
+        const float mu = a.mean ? now.mu : 0.f, rstd = now.rstd;
+        float s1 = 0.f, s2 = 0.f, xht = 0.f, gt = 0.f;
+        if constexpr (FORM >= FORM_TAIL) {
+            const float dyt = tail && live ? now.dyt : 0.f;
+            xht = tail && live ? (now.ht - mu) * rstd : 0.f, gt = gat * dyt;
+            s1 = gt * xht, s2 = gt;
+            dgat += dyt * xht, dbet += dyt;
+        }
 #pragma unroll
         for (int i = 0; i < VPL; ++i) {
-            // behind the row's end dy and gamma are zeros
+            const int e = at + i * STEP;
             float h[N], dy[N], g[N];
-            Rw::unpack(hw[i], h), Rw::unpack(yw[i], dy), Rw::unpack(ga[i], g);
+            Rw::unpack(Rw::mine(now.h[i], e, held), h), Rw::unpack(Rw::mine(now.dy[i], e, held), dy), Rw::unpack(ga[i], g);
 #pragma unroll
             for (int k = 0; k < N; ++k) {
                 const float xh = (h[k] - mu) * rstd;
@@ -162,112 +232,144 @@ __global__ __launch_bounds__(waves_of(WPR) * 64) void norm_bwd_kernel(NormBwd a)
                 dbe[i][k] += dy[k];
             }
         }
-        s1 = row_sum<WPR>(s1, lds[turn][0]) / width;
-        s2 = a.mean ? row_sum<WPR>(s2, lds[turn][1]) / width : 0.f;
+        sdp::settle(dga), sdp::settle(dbe);
+        row_sums<WPR>(s1, s2, sums);
+        s1 /= width, s2 = a.mean ? s2 / width : 0.f;
+        sdp::again(now.h), sdp::again(now.dy), sdp::again(ga);
 #pragma unroll
         for (int i = 0; i < VPL; ++i) {
-            const int e = at + i * WPR * 64 * N;
-            if (e >= d) break;
-            float h[N], dy[N], g[N], skip[N];
-            Rw::unpack(hw[i], h), Rw::unpack(yw[i], dy), Rw::unpack(ga[i], g);
-            if (a.dH) Rw::unpack(Rw::load((const Elem*)a.dH + off, e, d), skip);
+            float h[N], dy[N], g[N], skip[N] = {};
+            Rw::unpack(now.h[i], h), Rw::unpack(now.dy[i], dy), Rw::unpack(ga[i], g);
+            if constexpr (SKIP) Rw::unpack(now.skip[i], skip);
 #pragma unroll
             for (int k = 0; k < N; ++k) {
                 h[k] = rstd * (g[k] * dy[k] - s2 - (h[k] - mu) * rstd * s1);
-                if (a.dH) h[k] += skip[k];
+                if constexpr (SKIP) h[k] += skip[k];
             }
-            Rw::store((Elem*)a.dX + off, e, d, Rw::pack(h));
+            Rw::store((Elem*)a.dX + row * d, at + i * STEP, held, Rw::pack(h));
         }
+        if (tail && live) Rw::put((Elem*)a.dX + row * d + et, rstd * (gt - s2 - xht * s1) + (SKIP ? now.skipt : 0.f));
+        row += step;
+    };
+    Row1 one, two;
+    request(row, one);
+    // all waves of a workgroup take the same number of turns: their sums of a row go through a barrier.  Two rows a round: handed over from
+    // `next` to `now`, a row would have to have arrived.
+    for (int64_t first = (int64_t)blockIdx.x * ROWS; first < a.T; first += 2 * step) {
+        take(one, two, lds[0]);
+        if (first + step < a.T) take(two, one, lds[1]);
     }
     if (!a.want_dw) return;
+    float* out = a.partial + (int64_t)blockIdx.x * 2 * d;
     extern __shared__ float share[]; // [2][d] where a workgroup has several rows
-    if (ROWS > 1) {
-        for (int r = 0; r < ROWS; ++r) {
-            if (r) __syncthreads();
-            if (wave / WPR != r) continue;
 #pragma unroll
-            for (int i = 0; i < VPL; ++i)
-#pragma unroll
-                for (int k = 0; k < N; ++k) {
-                    const int e = at + i * WPR * 64 * N + k;
-                    if (e >= d) continue;
-                    share[e] = r ? share[e] + dga[i][k] : dga[i][k];
-                    share[d + e] = r ? share[d + e] + dbe[i][k] : dbe[i][k];
-                }
-        }
-        __syncthreads();
-        for (int e = threadIdx.x; e < 2 * d; e += waves_of(WPR) * 64) a.partial[(int64_t)blockIdx.x * 2 * d + e] = share[e];
-    } else {
+    for (int r = 0; r < ROWS; ++r) {
+        if (r) __syncthreads();
+        if (wave / WPR != r) continue;
+        auto add = [&](int e, float g, float b) {
+            if (r) g += share[e], b += share[d + e];
+            if (r == ROWS - 1) out[e] = g, out[d + e] = b;
+            else share[e] = g, share[d + e] = b;
+        };
 #pragma unroll
         for (int i = 0; i < VPL; ++i)
+            if (at + i * STEP < whole)
 #pragma unroll
-            for (int k = 0; k < N; ++k) {
-                const int e = at + i * WPR * 64 * N + k;
-                if (e >= d) continue;
-                a.partial[(int64_t)blockIdx.x * 2 * d + e] = dga[i][k];
-                a.partial[(int64_t)blockIdx.x * 2 * d + d + e] = dbe[i][k];
-            }
+                for (int k = 0; k < N; ++k) add(at + i * STEP + k, dga[i][k], dbe[i][k]);
+        if (tail) add(et, dgat, dbet);
     }
 }
 
-// Sums of the workgroups' shares, in their order: 64 columns a workgroup, four waves with every fourth share.  n = 0: zeros.
+// Sums of the workgroups' shares, in their order: 64 columns a workgroup, sixteen waves with every sixteenth share.  n = 0: zeros.
 template <int BF16>
-__global__ __launch_bounds__(256) void norm_dw_kernel(const float* __restrict__ partial, int n, int d, void* dgamma, void* dbeta) {
+__global__ __launch_bounds__(1024) void norm_dw_kernel(const float* __restrict__ partial, int n, int d, void* dgamma, void* dbeta) {
     typedef typename Row<BF16>::Elem Elem;
-    __shared__ float lds[4][64];
+    constexpr int WAVES = 16, B = 8;
+    __shared__ float lds[WAVES][64];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int e = blockIdx.x * 64 + lane, part = blockIdx.y;
     float s = 0.f;
     if (e < d)
-#pragma unroll 8
-        for (int i = wave; i < n; i += 4) s += partial[((int64_t)i * 2 + part) * d + e];
+        for (int i0 = wave; i0 < n; i0 += WAVES * B) { // B shares in flight
+            float v[B];
+#pragma unroll
+            for (int j = 0; j < B; ++j) v[j] = i0 + j * WAVES < n ? partial[((int64_t)(i0 + j * WAVES) * 2 + part) * d + e] : 0.f;
+#pragma unroll
+            for (int j = 0; j < B; ++j) s += v[j];
+        }
     lds[wave][lane] = s;
     __syncthreads();
-    if (wave == 0 && e < d) Row<BF16>::put((Elem*)(part ? dbeta : dgamma) + e, ((lds[0][lane] + lds[1][lane]) + lds[2][lane]) + lds[3][lane]);
+    if (wave != 0 || e >= d) return;
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) s += lds[w][lane];
+    Row<BF16>::put((Elem*)(part ? dbeta : dgamma) + e, s);
 }
 
-// waves of a row and pieces of a lane: as few waves as hold it with four pieces a lane (eight where sixteen waves do not)
+// waves of a row and pieces of a lane
 struct Shape {
     int wpr, vpl;
 };
-Shape shape(int dtype, int d) {
+Shape fwd_shape(int dtype, int d) {
     const int n = dtype == SDP_BF16 ? 8 : 4, pieces = (d + n - 1) / n;
     if (pieces <= 256) return {1, (pieces + 63) / 64};
     if (pieces <= 1024) return {4, pieces <= 512 ? 2 : 4};
-    return {16, pieces <= 4096 ? 4 : 8};
+    return {16, pieces <= 2048 ? 2 : 4};
 }
-int rows_of(const Shape& s) { return s.wpr == 1 ? 4 : 1; }
+Shape bwd_shape(int dtype, int d) {
+    const int n = dtype == SDP_BF16 ? 8 : 4, pieces = (d + n - 1) / n, most = dtype == SDP_BF16 ? 1 : 2;
+    if (pieces <= 64 * most) return {1, (pieces + 63) / 64};
+    for (int w = 2; w < 16; w *= 2)
+        if (pieces <= 64 * most * w) return {w, most};
+    return {16, pieces <= 1024 * most ? most : 2 * most};
+}
+int fwd_rows(const Shape& s) { return s.wpr == 1 ? 4 : 1; }
+int bwd_rows(const Shape& s) { return bwd_waves(s.wpr) / s.wpr; }
 
-constexpr int kBwdGroups = 512;
+constexpr int kBwdGroups = 256;
 int bwd_groups(int T, const Shape& s) {
-    const int64_t all = ((int64_t)T + rows_of(s) - 1) / rows_of(s);
+    const int64_t all = ((int64_t)T + bwd_rows(s) - 1) / bwd_rows(s);
     return (int)(all < kBwdGroups ? all : kBwdGroups);
 }
 
-template <class F>
-int by_shape(int dtype, const Shape& s, F&& launch) {
-    auto with = [&](auto bf16) {
 #define SDP_NORM_SHAPE(W, V) \
     if (s.wpr == W && s.vpl == V) return launch(bf16, std::integral_constant<int, W>{}, std::integral_constant<int, V>{})
+template <class F>
+int by_fwd_shape(int dtype, const Shape& s, F&& launch) {
+    auto with = [&](auto bf16) {
         SDP_NORM_SHAPE(1, 1);
         SDP_NORM_SHAPE(1, 2);
         SDP_NORM_SHAPE(1, 3);
         SDP_NORM_SHAPE(1, 4);
         SDP_NORM_SHAPE(4, 2);
         SDP_NORM_SHAPE(4, 4);
-        SDP_NORM_SHAPE(16, 4);
-        if constexpr (!bf16.value) SDP_NORM_SHAPE(16, 8);
-#undef SDP_NORM_SHAPE
+        SDP_NORM_SHAPE(16, 2);
+        if constexpr (!bf16.value) SDP_NORM_SHAPE(16, 4);
         return (int)SDP_ERR_UNSUPPORTED;
     };
     return dtype == SDP_BF16 ? with(std::integral_constant<int, 1>{}) : with(std::integral_constant<int, 0>{});
 }
+template <class F>
+int by_bwd_shape(int dtype, const Shape& s, F&& launch) {
+    auto with = [&](auto bf16) {
+        constexpr int M = bf16.value ? 1 : 2;
+        SDP_NORM_SHAPE(1, 1);
+        if constexpr (!bf16.value) SDP_NORM_SHAPE(1, 2);
+        SDP_NORM_SHAPE(2, M);
+        SDP_NORM_SHAPE(4, M);
+        SDP_NORM_SHAPE(8, M);
+        SDP_NORM_SHAPE(16, M);
+        SDP_NORM_SHAPE(16, 2 * M);
+        return (int)SDP_ERR_UNSUPPORTED;
+    };
+    return dtype == SDP_BF16 ? with(std::integral_constant<int, 1>{}) : with(std::integral_constant<int, 0>{});
+}
+#undef SDP_NORM_SHAPE
 
 int check_norm(int kind, int dtype, int T, int d) {
     if (kind != SDP_NORM_LAYER && kind != SDP_NORM_RMS) return SDP_ERR_INVALID_ARG;
     if (dtype != SDP_F32 && dtype != SDP_BF16) return SDP_ERR_INVALID_ARG;
     if (T < 0 || d < 1) return SDP_ERR_INVALID_ARG;
-    return d > SDP_NORM_MAX_WIDTH || T > SDP_MAX_TOKENS ? SDP_ERR_SHAPE : SDP_OK;
+    return d > SDP_NORM_MAX_WIDTH || T > SDP_MAX_EXTENT ? SDP_ERR_SHAPE : SDP_OK;
 }
 
 } // namespace
@@ -293,21 +395,25 @@ extern "C" int sdp_norm_fwd(int kind, int dtype, int T, int d, float eps, const 
         sdp::overlap({em}, {es_}))
         return SDP_ERR_INVALID_ARG;
     hipStream_t s = (hipStream_t)stream;
-    const Shape sh = shape(dtype, d);
+    const Shape sh = fwd_shape(dtype, d);
     const NormFwd a{X, R, gamma, beta, H, Y, mean, rstd, T, d, layer, eps};
     const bool once = sdp::read_once({eX, eR}, w);
     sdp::ProfileScope ps("norm_fwd", s);
-    const unsigned groups = (unsigned)(((int64_t)T + rows_of(sh) - 1) / rows_of(sh));
-    return by_shape(dtype, sh, [&](auto bf16, auto wpr, auto vpl) {
-        if (once) norm_fwd_kernel<bf16.value, wpr.value, vpl.value, 1><<<groups, waves_of(wpr.value) * 64, 0, s>>>(a);
-        else norm_fwd_kernel<bf16.value, wpr.value, vpl.value, 0><<<groups, waves_of(wpr.value) * 64, 0, s>>>(a);
+    const unsigned groups = (unsigned)(((int64_t)T + fwd_rows(sh) - 1) / fwd_rows(sh));
+    return by_fwd_shape(dtype, sh, [&](auto bf16, auto wpr, auto vpl) {
+        auto go = [&](auto form) {
+            norm_fwd_kernel<bf16.value, wpr.value, vpl.value, form.value><<<groups, waves_of(wpr.value) * 64, 0, s>>>(a);
+        };
+        if (d % Row<bf16.value>::N) go(std::integral_constant<int, FORM_TAIL>{});
+        else if (once) go(std::integral_constant<int, FORM_ONCE>{});
+        else go(std::integral_constant<int, FORM_WHOLE>{});
         return sdp::launch_status();
     });
 }
 
 extern "C" size_t sdp_norm_bwd_workspace_bytes(int dtype, int T, int d) {
     if (check_norm(SDP_NORM_LAYER, dtype, T, d) != SDP_OK) return 0;
-    return sdp::round_up((size_t)bwd_groups(T, shape(dtype, d)) * 2 * d * sizeof(float), 256);
+    return sdp::round_up((size_t)bwd_groups(T, bwd_shape(dtype, d)) * 2 * d * sizeof(float), 256);
 }
 
 extern "C" int sdp_norm_bwd(int kind, int dtype, int T, int d, const void* H, const void* dY, const void* dH, const void* gamma,
@@ -330,21 +436,27 @@ extern "C" int sdp_norm_bwd(int kind, int dtype, int T, int d, const void* H, co
         return SDP_ERR_INVALID_ARG;
     if (need > 0 && (!ws || !sdp::aligned16(ws) || ws_bytes < need)) return SDP_ERR_WORKSPACE;
     hipStream_t s = (hipStream_t)stream;
-    const Shape sh = shape(dtype, d);
+    const Shape sh = bwd_shape(dtype, d);
     const int groups = bwd_groups(T, sh);
     sdp::ProfileScope ps("norm_bwd", s);
     int st2 = SDP_OK;
     if (groups > 0) {
         const NormBwd a{H, dY, dH, gamma, mean, rstd, dX, dgamma, dbeta, (float*)ws, T, d, dgamma != nullptr};
-        const size_t lds = sh.wpr == 1 && dgamma ? (size_t)2 * d * sizeof(float) : 0;
-        st2 = by_shape(dtype, sh, [&](auto bf16, auto wpr, auto vpl) {
-            norm_bwd_kernel<bf16.value, wpr.value, vpl.value><<<groups, waves_of(wpr.value) * 64, lds, s>>>(a);
+        const size_t lds = bwd_rows(sh) > 1 && dgamma ? (size_t)2 * d * sizeof(float) : 0;
+        st2 = by_bwd_shape(dtype, sh, [&](auto bf16, auto wpr, auto vpl) {
+            auto go = [&](auto form) {
+                if (dH) norm_bwd_kernel<bf16.value, wpr.value, vpl.value, form.value, 1><<<groups, bwd_waves(wpr.value) * 64, lds, s>>>(a);
+                else norm_bwd_kernel<bf16.value, wpr.value, vpl.value, form.value, 0><<<groups, bwd_waves(wpr.value) * 64, lds, s>>>(a);
+            };
+            if (d % Row<bf16.value>::N == 0) go(std::integral_constant<int, FORM_WHOLE>{});
+            else if (wpr.value > 1 || d > Row<bf16.value>::N) go(std::integral_constant<int, FORM_TAIL>{});
+            else go(std::integral_constant<int, wpr.value * vpl.value == 1 ? FORM_SHORT : FORM_TAIL>{});
             return sdp::launch_status();
         });
     }
     if (st2 != SDP_OK || !dgamma) return st2;
     const dim3 grid((d + 63) / 64, dbeta ? 2 : 1);
-    if (dtype == SDP_BF16) norm_dw_kernel<1><<<grid, 256, 0, s>>>((const float*)ws, groups, d, dgamma, dbeta);
-    else norm_dw_kernel<0><<<grid, 256, 0, s>>>((const float*)ws, groups, d, dgamma, dbeta);
+    if (dtype == SDP_BF16) norm_dw_kernel<1><<<grid, 1024, 0, s>>>((const float*)ws, groups, d, dgamma, dbeta);
+    else norm_dw_kernel<0><<<grid, 1024, 0, s>>>((const float*)ws, groups, d, dgamma, dbeta);
     return sdp::launch_status();
 }

@@ -3,7 +3,9 @@
 //
 // A piece is 8 bf16 or 4 fp32 values.  Rows of a matrix whose width is no whole number of pieces start at any element; the memory
 // instructions of 16 bytes take such addresses, and rows of 1501 bf16 stream at the rate of aligned ones, so there is one form for
-// both.  The last piece of a row may be short: its values are moved one by one.
+// both.  The values behind the last whole piece, 7 at most, are a lane's each.  A lane without a piece reads the last one again, which costs no
+// traffic, and looks away when it uses it: a load is then one instruction without a condition.  (Where the row's end was looked
+// for as it was loaded, every load of its wave waited for the one before: norm backward of 16384 x 768 bf16 49 us, now 26.)
 //
 // Stores are non-temporal: what is written here is far more than a cache holds, or read next by another kernel, and pushes what is being
 // read out of it (embedding of 16384 x 2048 bf16 22.0 -> 17.0 us, its gradient's sums 44 -> 34, norm 50.1 -> 48.8, loss of 8192 x 32000 186 -> 182).
@@ -35,101 +37,110 @@ inline bool read_once(std::initializer_list<Extent> of, size_t row_bytes) {
 }
 
 template <int BF16>
-struct Row;
+struct Row {
+    typedef std::conditional_t<BF16, uint16_t, float> Elem;
+    typedef std::conditional_t<BF16, u32x4_at2, u32x4_at4> Piece;
+    static constexpr int N = BF16 ? 8 : 4; // values of a piece
 
-template <>
-struct Row<1> {
-    typedef uint16_t Elem;
-    static constexpr int N = 8; // values of a piece
+    static __device__ inline float one(const Elem* p) {
+        if constexpr (BF16) return __uint_as_float((uint32_t)*p << 16);
+        else return *p;
+    }
+    static __device__ inline float rounded(float v) { return BF16 ? (float)(__bf16)v : v; }
+    static __device__ inline void put(Elem* p, float v) {
+        if constexpr (BF16) *p = __builtin_bit_cast(uint16_t, (__bf16)v);
+        else *p = v;
+    }
+    // values of a row of n that whole pieces hold
+    static __host__ __device__ inline int whole(int n) { return n / N * N; }
 
-    static __device__ inline float one(const Elem* p) { return __uint_as_float((uint32_t)*p << 16); }
-    static __device__ inline void put(Elem* p, float v) { *p = __builtin_bit_cast(uint16_t, (__bf16)v); }
-
-    // the piece from value e on of a row of n; values past its end are `fill`'s (two bf16 in a word); ONCE: read_once's answer, at compile time (of two loads
-    // behind a condition the compiler makes one)
+    // The piece from value e (a multiple of N) on of a row whose whole pieces hold `whole` values; the last one for lanes behind it.  ONCE:
+    // read_once's answer, at compile time (of two loads behind a condition the compiler makes one).
     template <int ONCE = 0>
-    static __device__ inline u32x4 load(const Elem* row, int e, int n, uint32_t fill = 0) {
-        if (e + N <= n) return ONCE ? __builtin_nontemporal_load((const u32x4_at2*)(row + e)) : *(const u32x4_at2*)(row + e);
-        u32x4 w = {fill, fill, fill, fill};
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (e + i < n) w[i / 2] = i % 2 ? (w[i / 2] & 0xFFFFu) | (uint32_t)row[e + i] << 16 : (w[i / 2] & 0xFFFF0000u) | row[e + i];
-        return w;
+    static __device__ inline u32x4 load(const Elem* row, int e, int whole) {
+        return whole ? load_some<ONCE>(row, e, whole) : u32x4{0, 0, 0, 0};
     }
-    static __device__ inline void store(Elem* row, int e, int n, const u32x4& w) {
-        if (e + N <= n) {
-            __builtin_nontemporal_store(w, (u32x4_at2*)(row + e));
-            return;
-        }
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (e + i < n) row[e + i] = (uint16_t)(i % 2 ? w[i / 2] >> 16 : w[i / 2]);
+    // the same of a row that has a whole piece
+    template <int ONCE = 0>
+    static __device__ inline u32x4 load_some(const Elem* row, int e, int whole) {
+        const Piece* p = (const Piece*)((const char*)row + (uint32_t)min(e, whole - N) * (uint32_t)sizeof(Elem));
+        return ONCE ? __builtin_nontemporal_load(p) : *p;
     }
-    // a bf16 is the high half of an fp32: even values sit in the low 16 bits of each word
+    // what load gave, or `fill` (every value of a word) in lanes behind the row's whole pieces
+    static __device__ inline u32x4 mine(const u32x4& w, int e, int whole, uint32_t fill = 0) {
+        return e < whole ? w : u32x4{fill, fill, fill, fill};
+    }
+    static __device__ inline void store(Elem* row, int e, int whole, const u32x4& w) {
+        if (e < whole) __builtin_nontemporal_store(w, (Piece*)((char*)row + (uint32_t)e * (uint32_t)sizeof(Elem)));
+    }
     static __device__ inline void unpack(const u32x4& w, float (&v)[N]) {
+        if constexpr (BF16) { // a bf16 is the high half of an fp32: even values sit in the low 16 bits of each word
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[2 * i] = __uint_as_float(w[i] << 16);
-            v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+            for (int i = 0; i < 4; ++i) {
+                v[2 * i] = __uint_as_float(w[i] << 16);
+                v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(w[i]);
         }
     }
     static __device__ inline u32x4 pack(const float (&v)[N]) {
-        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
         u32x4 w;
+        if constexpr (BF16) {
+            typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const bf16x2 p = {(__bf16)v[2 * i], (__bf16)v[2 * i + 1]}; // to nearest, ties to even
-            w[i] = __builtin_bit_cast(uint32_t, p);
+            for (int i = 0; i < 4; ++i) {
+                const bf16x2 p = {(__bf16)v[2 * i], (__bf16)v[2 * i + 1]}; // to nearest, ties to even
+                w[i] = __builtin_bit_cast(uint32_t, p);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(v[i]);
         }
         return w;
     }
 };
 
-template <>
-struct Row<0> {
-    typedef float Elem;
-    static constexpr int N = 4;
-
-    static __device__ inline float one(const Elem* p) { return *p; }
-    static __device__ inline void put(Elem* p, float v) { *p = v; }
-
-    template <int ONCE = 0>
-    static __device__ inline u32x4 load(const Elem* row, int e, int n, uint32_t fill = 0) {
-        if (e + N <= n) return ONCE ? __builtin_nontemporal_load((const u32x4_at4*)(row + e)) : *(const u32x4_at4*)(row + e);
-        u32x4 w = {fill, fill, fill, fill};
+// Pieces are unpacked anew from here on: the compiler would rather keep their fp32 values, twice the registers (16 pieces of logits 177
+// instead of 99, two waves a SIMD instead of four).
+template <int P>
+__device__ inline void again(u32x4 (&w)[P]) {
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (e + i < n) w[i] = __float_as_uint(row[e + i]);
-        return w;
-    }
-    static __device__ inline void store(Elem* row, int e, int n, const u32x4& w) {
-        if (e + N <= n) {
-            __builtin_nontemporal_store(w, (u32x4_at4*)(row + e));
-            return;
-        }
+    for (int i = 0; i < P; ++i) asm volatile("" : "+v"(w[i]));
+}
+// These sums are made here, not where they are next looked at: what they are made of would stay in registers till then.
+template <int P, int N>
+__device__ inline void settle(float (&x)[P][N]) {
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (e + i < n) row[e + i] = __uint_as_float(w[i]);
-    }
-    static __device__ inline void unpack(const u32x4& w, float (&v)[N]) {
+    for (int i = 0; i < P; ++i)
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = __uint_as_float(w[i]);
-    }
-    static __device__ inline u32x4 pack(const float (&v)[N]) {
-        return {__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
-    }
-};
+        for (int k = 0; k < N; ++k) asm volatile("" : "+v"(x[i][k]));
+}
 
-// Sums over a wave, in a fixed order; every lane has the result.
+// Sum and maximum over a wave, in a fixed order; every lane has the result.  Six steps on the vector unit's own lane moves (down the rows of
+// 16 lanes, then from row to row), not through LDS.
+template <int CTRL>
+__device__ inline float from_lane(float none, float x) { // x of the lane that CTRL names, `none` where there is none
+    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(none), __float_as_int(x), CTRL, 0xF, 0xF, false));
+}
 __device__ inline float wave_sum(float x) {
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) x += __shfl_xor(x, d, 64);
-    return x;
+    x += from_lane<0x111>(0.f, x); // row_shr 1, 2, 4, 8: a row's last lane has the row's sum
+    x += from_lane<0x112>(0.f, x);
+    x += from_lane<0x114>(0.f, x);
+    x += from_lane<0x118>(0.f, x);
+    x += from_lane<0x142>(0.f, x); // row_bcast 15, 31: the sums of the rows before
+    x += from_lane<0x143>(0.f, x);
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
 }
 __device__ inline float wave_max(float x) {
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) x = fmaxf(x, __shfl_xor(x, d, 64));
-    return x;
+    x = fmaxf(x, from_lane<0x111>(x, x));
+    x = fmaxf(x, from_lane<0x112>(x, x));
+    x = fmaxf(x, from_lane<0x114>(x, x));
+    x = fmaxf(x, from_lane<0x118>(x, x));
+    x = fmaxf(x, from_lane<0x142>(x, x));
+    x = fmaxf(x, from_lane<0x143>(x, x));
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
 }
 
 // Token id or label t; anything outside [0, V) is -1.  Where many are loaded at once the type has to be known at compile time: with a

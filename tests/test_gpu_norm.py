@@ -61,7 +61,7 @@ def _run(sdp, kind, dtype, T, d, skip, bias, at, seed=1):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("T,d", [(1, 6), (1, 8), (3, 5), (5, 64), (7, 255), (64, 256), (65, 257), (33, 511), (33, 512), (20, 513), (9, 768), (257, 1000),
                                  (100, 1024), (31, 1025), (300, 1200), (17, 1536), (9, 1537), (40, 1600), (130, 2048), (6, 2049), (5, 4096), (3, 4100),
-                                 (2, 8191), (3, 8192), (2, 8200), (2, 16384), (1, 16385), (2, 32768), (4099, 72), (2500, 264)])
+                                 (2, 8191), (3, 8192), (2, 8200), (2, 12289), (1, 16383), (2, 16384), (4099, 72), (2500, 264)])
 def test_norm_matches_64_bits(sdp, dtype, T, d):
     for kind, skip, bias, at in (("layer", True, True, 0), ("rms", False, False, 1), ("layer", False, False, 3)):
         print(f"norm {kind} {dtype} T={T} d={d} skip={skip} bias={bias} at={at}", flush=True)
@@ -110,7 +110,7 @@ def test_gradients_match_differences(sdp):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("T,d", [(37, 200), (300, 2048), (11, 5000), (3, 20000)])
+@pytest.mark.parametrize("T,d", [(37, 200), (300, 2048), (11, 5000), (3, 16000)])
 def test_in_place_is_the_same(sdp, dtype, T, d):
     dt = DT[dtype]
     X, R, dY, dH = (normal(T, d, dtype=dt, seed=s).cuda() for s in (1, 2, 3, 4))
