@@ -39,7 +39,7 @@ struct NormBwd {
 constexpr int waves_of(int WPR) { return WPR > 4 ? WPR : 4; }
 
 constexpr int kBwdWaves = 8;
-constexpr int bwd_waves(int WPR) { return WPR > kBwdWaves ? WPR : kBwdWaves; }
+constexpr int bwd_waves(int WPR) { return WPR > kBwdWaves ? WPR : WPR == 3 ? 9 : kBwdWaves; }
 
 // Sum over the WPR waves of a row; every lane has the result.  `lds` holds one float a wave; two calls in a row need two of them.
 template <int WPR>
@@ -217,36 +217,42 @@ __global__ __launch_bounds__(bwd_waves(WPR) * 64) void norm_bwd_kernel(NormBwd a
             s1 = gt * xht, s2 = gt;
             dgat += dyt * xht, dbet += dyt;
         }
+        float xh[VPL][N], g[VPL][N];
+        auto centre = [&](int i, float (&dy)[N]) {
+            const int e = at + i * STEP;
+            Rw::unpack(Rw::mine(now.h[i], e, held), xh[i]), Rw::unpack(Rw::mine(now.dy[i], e, held), dy), Rw::unpack(ga[i], g[i]);
+#pragma unroll
+            for (int k = 0; k < N; ++k) xh[i][k] = (xh[i][k] - mu) * rstd, g[i][k] *= dy[k];
+        };
 #pragma unroll
         for (int i = 0; i < VPL; ++i) {
-            const int e = at + i * STEP;
-            float h[N], dy[N], g[N];
-            Rw::unpack(Rw::mine(now.h[i], e, held), h), Rw::unpack(Rw::mine(now.dy[i], e, held), dy), Rw::unpack(ga[i], g);
+            float dy[N];
+            centre(i, dy);
 #pragma unroll
             for (int k = 0; k < N; ++k) {
-                const float xh = (h[k] - mu) * rstd;
-                g[k] *= dy[k];
-                s1 += g[k] * xh;
-                s2 += g[k];
-                dga[i][k] += dy[k] * xh;
+                s1 = __builtin_fmaf(g[i][k], xh[i][k], s1);
+                s2 += g[i][k];
+                dga[i][k] = __builtin_fmaf(dy[k], xh[i][k], dga[i][k]);
                 dbe[i][k] += dy[k];
             }
         }
         sdp::settle(dga), sdp::settle(dbe);
         row_sums<WPR>(s1, s2, sums);
         s1 /= width, s2 = a.mean ? s2 / width : 0.f;
-        sdp::again(now.h), sdp::again(now.dy), sdp::again(ga);
+        // xh and g: kept where registers are enough for it, else made again
+        constexpr bool KEPT = VPL * N <= 8;
+        if (!KEPT) sdp::again(now.h), sdp::again(now.dy), sdp::again(ga);
 #pragma unroll
         for (int i = 0; i < VPL; ++i) {
-            float h[N], dy[N], g[N], skip[N] = {};
-            Rw::unpack(now.h[i], h), Rw::unpack(now.dy[i], dy), Rw::unpack(ga[i], g);
+            float dx[N], skip[N] = {};
+            if (!KEPT) centre(i, dx);
             if constexpr (SKIP) Rw::unpack(now.skip[i], skip);
 #pragma unroll
             for (int k = 0; k < N; ++k) {
-                h[k] = rstd * (g[k] * dy[k] - s2 - (h[k] - mu) * rstd * s1);
-                if constexpr (SKIP) h[k] += skip[k];
+                dx[k] = __builtin_fmaf(-xh[i][k], s1, g[i][k] - s2);
+                dx[k] = SKIP ? __builtin_fmaf(dx[k], rstd, skip[k]) : dx[k] * rstd;
             }
-            Rw::store((Elem*)a.dX + row * d, at + i * STEP, held, Rw::pack(h));
+            Rw::store((Elem*)a.dX + row * d, at + i * STEP, held, Rw::pack(dx));
         }
         if (tail && live) Rw::put((Elem*)a.dX + row * d + et, rstd * (gt - s2 - xht * s1) + (SKIP ? now.skipt : 0.f));
         row += step;
@@ -318,7 +324,7 @@ Shape fwd_shape(int dtype, int d) {
 Shape bwd_shape(int dtype, int d) {
     const int n = dtype == SDP_BF16 ? 8 : 4, pieces = (d + n - 1) / n, most = dtype == SDP_BF16 ? 1 : 2;
     if (pieces <= 64 * most) return {1, (pieces + 63) / 64};
-    for (int w = 2; w < 16; w *= 2)
+    for (int w : {2, 3, 4, 8})
         if (pieces <= 64 * most * w) return {w, most};
     return {16, pieces <= 1024 * most ? most : 2 * most};
 }
@@ -355,6 +361,7 @@ int by_bwd_shape(int dtype, const Shape& s, F&& launch) {
         SDP_NORM_SHAPE(1, 1);
         if constexpr (!bf16.value) SDP_NORM_SHAPE(1, 2);
         SDP_NORM_SHAPE(2, M);
+        SDP_NORM_SHAPE(3, M);
         SDP_NORM_SHAPE(4, M);
         SDP_NORM_SHAPE(8, M);
         SDP_NORM_SHAPE(16, M);
