@@ -592,11 +592,6 @@ def _id_type_of(t, name):
     return _ID_TYPES[t.dtype]
 
 
-def _shape(t, shape, name):
-    if t.shape != shape:
-        raise ValueError(f"{name}: expected shape {tuple(shape)}")
-
-
 def norm_fwd(kind, X, gamma, beta=None, residual=None, eps=1e-5, out=None):
     """Layer ("layer") or root-mean-square ("rms") norm of the tokens X [T][d], or of H = X + residual.
 
@@ -605,30 +600,20 @@ def norm_fwd(kind, X, gamma, beta=None, residual=None, eps=1e-5, out=None):
     k = _KINDS[kind]
     T, d = X.shape
     dt = _dtype_of(X, "X")
-    _shape(gamma, (d,), "gamma")
-    if beta is not None:
-        _shape(beta, (d,), "beta")
-    if residual is not None:
-        _shape(residual, X.shape, "residual")
     if out is None:
         Y, rstd = torch.empty_like(X), torch.empty((T,), dtype=torch.float32, device=X.device)
         H = None if residual is None else torch.empty_like(X)
         mean = None if k else torch.empty_like(rstd)
     else:
         Y, H, mean, rstd = out
-        _shape(Y, X.shape, "Y")
-        _shape(rstd, (T,), "rstd")
         if residual is None:
             H = None
-        else:
-            _shape(H, X.shape, "H")
         if k:
             mean = None
-        else:
-            _shape(mean, (T,), "mean")
     device, stream = _here_of(X)
     st = _native().norm_fwd(device, k, dt, T, d, eps, X, residual, gamma, beta, H, Y, mean, rstd, stream)
-    _check(st, "sdp_norm_fwd")
+    if st:
+        _check(st, "sdp_norm_fwd")
     return Y, X if H is None else H, mean, rstd
 
 
@@ -644,15 +629,8 @@ def norm_bwd(kind, H, dY, gamma, mean, rstd, dH=None, want_dw=True, bias=None, o
     k = _KINDS[kind]
     T, d = H.shape
     dt = _dtype_of(H, "H")
-    _shape(dY, H.shape, "dY")
-    _shape(gamma, (d,), "gamma")
-    _shape(rstd, (T,), "rstd")
-    if dH is not None:
-        _shape(dH, H.shape, "dH")
     if k:
         mean = None
-    else:
-        _shape(mean, (T,), "mean")
     if out is None:
         if bias is None:
             bias = not k
@@ -661,37 +639,33 @@ def norm_bwd(kind, H, dY, gamma, mean, rstd, dH=None, want_dw=True, bias=None, o
         dbeta = torch.empty_like(gamma) if want_dw and bias else None
     else:
         dX, dgamma, dbeta = out
-        _shape(dX, H.shape, "dX")
         if not want_dw:
             dgamma = dbeta = None
         elif dgamma is None:
             raise ValueError("dgamma: expected a tensor (or want_dw=False)")
-        else:
-            _shape(dgamma, (d,), "dgamma")
-        if bias is False:
+        elif bias is False:
             dbeta = None
-        if dbeta is not None:
-            _shape(dbeta, (d,), "dbeta")
     if ws is None and want_dw:
         ws = _ws(norm_bwd_workspace_bytes(H.dtype, T, d), H.device)
     device, stream = _here_of(H)
     st = _native().norm_bwd(device, k, dt, T, d, H, dY, dH, gamma, mean, rstd, dX, dgamma, dbeta, ws,
                             0 if ws is None else ws.numel(), stream)
-    _check(st, "sdp_norm_bwd")
+    if st:
+        _check(st, "sdp_norm_bwd")
     return dX, dgamma, dbeta
 
 
 def embed_fwd(E, ids, scale=1.0, out=None):
     """scale * E[ids] for E [V][d] and int32 or int64 ids [T]; zeros where an id lies outside [0, V) -> Y [T][d]."""
     V, d = E.shape
-    (T,) = ids.shape
+    T = ids.numel()
+    dt, it = _dtype_of(E, "E"), _id_type_of(ids, "ids")
     if out is None:
         out = torch.empty((T, d), dtype=E.dtype, device=E.device)
-    else:
-        _shape(out, (T, d), "Y")
     device, stream = _here_of(E)
-    st = _native().embed_fwd(device, _dtype_of(E, "E"), _id_type_of(ids, "ids"), T, V, d, scale, E, ids, out, stream)
-    _check(st, "sdp_embed_fwd")
+    st = _native().embed_fwd(device, dt, it, T, V, d, scale, E, ids, out, stream)
+    if st:
+        _check(st, "sdp_embed_fwd")
     return out
 
 
@@ -702,29 +676,27 @@ def embed_bwd_workspace_bytes(dtype, T, V, d):
 def embed_bwd(dY, ids, V, scale=1.0, out=None, ws=None):
     """Gradient of embed_fwd's E: dE [V][d], every row (zeros where no id names it)."""
     T, d = dY.shape
-    _shape(ids, (T,), "ids")
+    dt, it = _dtype_of(dY, "dY"), _id_type_of(ids, "ids")
     if out is None:
         out = torch.empty((V, d), dtype=dY.dtype, device=dY.device)
-    else:
-        _shape(out, (V, d), "dE")
-    dt = _dtype_of(dY, "dY")
     if ws is None:
         ws = _ws(embed_bwd_workspace_bytes(dY.dtype, T, V, d), dY.device)
     device, stream = _here_of(dY)
-    st = _native().embed_bwd(device, dt, _id_type_of(ids, "ids"), T, V, d, scale, dY, ids, out, ws, ws.numel(), stream)
-    _check(st, "sdp_embed_bwd")
+    st = _native().embed_bwd(device, dt, it, T, V, d, scale, dY, ids, out, ws, ws.numel(), stream)
+    if st:
+        _check(st, "sdp_embed_bwd")
     return out
 
 
 def label_scale(labels, V, out=None):
-    """labels int32 or int64 [T] -> fp32 GPU tensor [1]: 1 / max(1, number of labels in [0, V)), token_loss's scale_dev for a mean."""
+    """labels int32 or int64 -> fp32 GPU tensor [1]: 1 / max(1, number of labels in [0, V)), token_loss's scale_dev for a mean."""
+    it = _id_type_of(labels, "labels")
     if out is None:
         out = torch.empty((1,), dtype=torch.float32, device=labels.device)
-    else:
-        _shape(out, (1,), "scale")
     device, stream = _here_of(labels)
-    st = _native().label_scale(device, _id_type_of(labels, "labels"), labels.numel(), V, labels, out, stream)
-    _check(st, "sdp_label_scale")
+    st = _native().label_scale(device, it, labels.numel(), V, labels, out, stream)
+    if st:
+        _check(st, "sdp_label_scale")
     return out
 
 
@@ -735,33 +707,21 @@ def token_loss(Z, labels, scale=1.0, scale_dev=None, want_grad=True, out=None):
     None = 1), returns (nll [T], lse [T], dZ [T][V], loss [1]): loss = c * sum(nll) and its gradient by Z; dZ is None with
     want_grad=False.  `out` = (nll, lse, dZ, loss) preallocated: dZ may be Z, lse and loss may be None (not wanted)."""
     T, V = Z.shape
-    dt = _dtype_of(Z, "Z")
-    _shape(labels, (T,), "labels")
-    if scale_dev is not None:
-        _shape(scale_dev, (1,), "scale_dev")
+    dt, it = _dtype_of(Z, "Z"), _id_type_of(labels, "labels")
     if out is None:
         nll, lse = (torch.empty((T,), dtype=torch.float32, device=Z.device) for _ in range(2))
         dZ = torch.empty_strided(Z.shape, Z.stride(), dtype=Z.dtype, device=Z.device) if want_grad else None
         loss = torch.empty((1,), dtype=torch.float32, device=Z.device)
     else:
         nll, lse, dZ, loss = out
-        _shape(nll, (T,), "nll")
-        if lse is not None:
-            _shape(lse, (T,), "lse")
-        if loss is not None:
-            _shape(loss, (1,), "loss")
         if not want_grad:
             dZ = None
         elif dZ is None:
             raise ValueError("dZ: expected a tensor (or want_grad=False)")
-        else:
-            _shape(dZ, Z.shape, "dZ")
-            if T > 1 and dZ.stride(0) != Z.stride(0):
-                raise ValueError("dZ: expected the strides of Z")
     device, stream = _here_of(Z)
-    st = _native().token_loss(device, dt, _id_type_of(labels, "labels"), T, V, Z.stride(0) if T > 1 else V, scale, Z, labels,
-                              scale_dev, nll, lse, dZ, loss, stream)
-    _check(st, "sdp_token_loss")
+    st = _native().token_loss(device, dt, it, T, V, Z.stride(0) if T > 1 else V, scale, Z, labels, scale_dev, nll, lse, dZ, loss, stream)
+    if st:
+        _check(st, "sdp_token_loss")
     return nll, lse, dZ, loss
 
 

@@ -6,7 +6,7 @@
 // belong to one row of dE are then neighbours in the sorted order, to be summed by one wave in registers.  No atomics on floats: each
 // row's sum has one order, given by the ids alone.
 //
-// The sort is one launch in which no workgroup waits for another.  Each owns a range of ids and goes through all T ids itself, twice:
+// Batches of few tokens have a launch of their own (embed_small_kernel).  Otherwise the sort is one launch in which no workgroup waits for another.  Each owns a range of ids and goes through all T ids itself, twice:
 // the first time it counts, how many ids lie below its range (where its part of the order starts) and how often each id of its
 // range occurs; the second time it writes the tokens of its range to their places.  The ids are few bytes and come from
 // the cache for all workgroups but the first, so that T / 1024 steps a workgroup take less than the launches and the waiting of a sort
@@ -251,13 +251,90 @@ struct Lane {
 // A workgroup has a chunk of the sorted tokens, a wave a piece of it, or 64 rows of dE for each wave to clear the empty ones of; and a slab of
 // 64 pieces of the columns.  What a wave has of a row that starts in an earlier one goes through LDS to the wave that has its start,
 // and to memory only where that lies in another chunk.
+//
+// Piece: the wave's sorted tokens: lane i < cnt has token `tok` of row `id`; `prev` and `next`: the rows of the tokens before and behind
+// them, -1 where there are none.
+struct Piece {
+    int tok, id, cnt, prev, next;
+};
+template <int BF16, int TAIL, int WAVES>
+struct Chunk {
+    static constexpr int N = Row<BF16>::N, M = N + TAIL;
+    float heads[WAVES][M][64];
+    int head_of[WAVES]; // 0: the wave starts with a row of its own; 1: its first row started earlier, 2: and goes on
+
+    // part: where sums go of rows that do not start ([0]) or end ([1]) in the chunk; not looked at where there are none
+    __device__ void sum(const EmbedBwd& a, const Lane<BF16, TAIL>& mine, const Piece& p, int wave, int lane, float* part) {
+        typedef Row<BF16> Rw;
+        typedef typename Rw::Elem Elem;
+        float acc[M] = {};
+        bool own = p.prev < 0 || __builtin_amdgcn_readlane(p.id, 0) != p.prev; // the row at hand starts in this piece
+        int head = 0, tail = -1; // tail: the row that starts here and goes on; acc is its sum then
+        u32x4 w[kPiece];
+        float wt[kPiece];
+#pragma unroll
+        for (int j = 0; j < kPiece; ++j) {
+            w[j] = u32x4{0, 0, 0, 0}, wt[j] = 0.f;
+            if (j < p.cnt) {
+                const Elem* row = (const Elem*)a.dY + (int64_t)__builtin_amdgcn_readlane(p.tok, j) * a.d;
+                w[j] = Rw::load(row, mine.e, mine.whole);
+                if constexpr (TAIL)
+                    if (mine.tail) wt[j] = Rw::one(row + mine.et);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < kPiece; ++j) {
+            if (j < p.cnt) {
+                float v[N];
+                Rw::unpack(w[j], v);
+#pragma unroll
+                for (int k = 0; k < N; ++k) acc[k] += v[k];
+                if constexpr (TAIL) acc[N] += wt[j];
+                const int row = __builtin_amdgcn_readlane(p.id, j);
+                const int after = j == p.cnt - 1 ? p.next : __builtin_amdgcn_readlane(p.id, (j + 1) % kPiece);
+                if (j == p.cnt - 1 && row == after && own) {
+                    tail = row;
+                } else if (j == p.cnt - 1 || row != after) {
+                    if (own) {
+                        mine.write(a, row, acc);
+                    } else {
+                        head = row == after ? 2 : 1;
+#pragma unroll
+                        for (int k = 0; k < M; ++k) heads[wave][k][lane] = acc[k];
+                    }
+                    own = true;
+#pragma unroll
+                    for (int k = 0; k < M; ++k) acc[k] = 0.f;
+                }
+            }
+        }
+        if (lane == 0) head_of[wave] = head;
+        __syncthreads();
+        // adds what the waves from `from` on have of a row that goes on in them; whether it ends there
+        auto follow = [&](float (&s)[M], int from) {
+            for (int u = from; u < WAVES; ++u) {
+#pragma unroll
+                for (int k = 0; k < M; ++k) s[k] += heads[u][k][lane];
+                if (__builtin_amdgcn_readfirstlane(head_of[u]) != 2) return true;
+            }
+            return false;
+        };
+        if (tail >= 0) {
+            if (follow(acc, wave + 1)) mine.write(a, tail, acc);
+            else mine.write_part(part + a.d, acc);
+        }
+        if (wave == 0 && head) {
+#pragma unroll
+            for (int k = 0; k < M; ++k) acc[k] = heads[0][k][lane];
+            if (head == 2) follow(acc, 1);
+            mine.write_part(part, acc);
+        }
+    }
+};
+
 template <int BF16, int TAIL>
 __global__ __launch_bounds__(kSumWaves * 64) void embed_sum_kernel(EmbedBwd a) {
-    typedef Row<BF16> Rw;
-    typedef typename Rw::Elem Elem;
-    constexpr int N = Rw::N, M = N + TAIL;
-    __shared__ float heads[kSumWaves][M][64];
-    __shared__ int head_of[kSumWaves]; // 0: the wave starts with a row of its own; 1: its first row started earlier, 2: and goes on
+    __shared__ Chunk<BF16, TAIL, kSumWaves> chunk;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int64_t job = blockIdx.x / a.slabs;
     const Lane<BF16, TAIL> mine(a.d, (int)(blockIdx.x - job * a.slabs), lane);
@@ -266,7 +343,7 @@ __global__ __launch_bounds__(kSumWaves * 64) void embed_sum_kernel(EmbedBwd a) {
         if (v >= a.V) return;
         const bool empty = v + lane < a.V && a.s.start[v + lane] == a.s.start[v + lane + 1];
         uint64_t left = __ballot(empty);
-        const float zeros[M] = {};
+        const float zeros[Lane<BF16, TAIL>::M] = {};
         while (left) {
             mine.write(a, (int)v + __ffsll((unsigned long long)left) - 1, zeros);
             left &= left - 1;
@@ -275,73 +352,63 @@ __global__ __launch_bounds__(kSumWaves * 64) void embed_sum_kernel(EmbedBwd a) {
     }
     // requested before it is known how many tokens there are: what lies behind the last one is not used
     const int p0 = (int)job * kChunk + wave * kPiece, at = min(p0 + lane, a.T - 1);
-    const int tok = a.s.order[at], id = a.s.ids[at], prev = a.s.ids[max(min(p0, a.T) - 1, 0)], behind = a.s.ids[min(p0 + kPiece, a.T - 1)];
+    Piece p{a.s.order[at], a.s.ids[at], 0, a.s.ids[max(min(p0, a.T) - 1, 0)], a.s.ids[min(p0 + kPiece, a.T - 1)]};
     const int n = a.s.start[a.V];
     if (job * kChunk >= n) return;
-    const int cnt = max(0, min(kPiece, n - p0)), next = p0 + cnt < n ? behind : -1;
-    float acc[M] = {};
-    bool own = p0 == 0 || __builtin_amdgcn_readlane(id, 0) != prev; // the row at hand starts in this piece
-    int head = 0, tail = -1; // tail: the row that starts here and goes on; acc is its sum then
-    u32x4 w[kPiece];
-    float wt[kPiece];
-#pragma unroll
-    for (int j = 0; j < kPiece; ++j) {
-        w[j] = u32x4{0, 0, 0, 0}, wt[j] = 0.f;
-        if (j < cnt) {
-            const Elem* row = (const Elem*)a.dY + (int64_t)__builtin_amdgcn_readlane(tok, j) * a.d;
-            w[j] = Rw::load(row, mine.e, mine.whole);
-            if constexpr (TAIL)
-                if (mine.tail) wt[j] = Rw::one(row + mine.et);
-        }
+    p.cnt = max(0, min(kPiece, n - p0));
+    if (p0 == 0) p.prev = -1;
+    if (p0 + p.cnt >= n) p.next = -1;
+    chunk.sum(a, mine, p, wave, lane, a.part + job * 2 * a.d);
+}
+
+// A batch of kSmall tokens at most, in one launch: a workgroup has a range of ids, as in the sort, and a slab of the columns.  Its tokens are
+// put in order by counting, for each, those before it (the ids are in LDS, the counting less than a wait for memory), and are one
+// chunk: no row goes on elsewhere.  256 tokens, 1024 rows of 256 fp32: one launch 5.5 us, three 12.3.
+constexpr int kSmallWaves = 16, kSmall = kSmallWaves * kPiece;
+
+template <int BF16, int TAIL>
+__global__ __launch_bounds__(kSmallWaves * 64) void embed_small_kernel(EmbedBwd a, const void* ids, int wide, int range) {
+    __shared__ Chunk<BF16, TAIL, kSmallWaves> chunk;
+    __shared__ uint32_t key[kSmall]; // id - lo, then token; the largest value for tokens that are not the range's
+    __shared__ int toks[kSmall], rows[kSmall], counts[kSmallWaves];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int job = blockIdx.x / a.slabs, lo = job * range, n = min(range, a.V - lo);
+    const Lane<BF16, TAIL> mine(a.d, (int)blockIdx.x - job * a.slabs, lane);
+    uint32_t k = 0xFFFFFFFFu;
+    if (tid < a.T) {
+        const int id = sdp::token_id(ids, wide, tid, a.V);
+        if (id >= lo && id - lo < n) k = (uint32_t)(id - lo) << 8 | tid;
     }
-#pragma unroll
-    for (int j = 0; j < kPiece; ++j) {
-        if (j < cnt) {
-            float v[N];
-            Rw::unpack(w[j], v);
-#pragma unroll
-            for (int k = 0; k < N; ++k) acc[k] += v[k];
-            if constexpr (TAIL) acc[N] += wt[j];
-            const int row = __builtin_amdgcn_readlane(id, j);
-            const int after = j == cnt - 1 ? next : __builtin_amdgcn_readlane(id, (j + 1) % kPiece);
-            if (j == cnt - 1 && row == after && own) {
-                tail = row;
-            } else if (j == cnt - 1 || row != after) {
-                if (own) {
-                    mine.write(a, row, acc);
-                } else {
-                    head = row == after ? 2 : 1;
-#pragma unroll
-                    for (int k = 0; k < M; ++k) heads[wave][k][lane] = acc[k];
-                }
-                own = true;
-#pragma unroll
-                for (int k = 0; k < M; ++k) acc[k] = 0.f;
-            }
-        }
-    }
-    if (lane == 0) head_of[wave] = head;
+    const uint64_t hits = __ballot(k != 0xFFFFFFFFu);
+    if (tid < kSmall) key[tid] = k;
+    if (lane == 0) counts[wave] = __popcll(hits);
     __syncthreads();
-    // adds what the waves from `from` on have of a row that goes on in them; whether it ends there
-    auto follow = [&](float (&sum)[M], int from) {
-        for (int u = from; u < kSumWaves; ++u) {
+    int m = 0;
 #pragma unroll
-            for (int k = 0; k < M; ++k) sum[k] += heads[u][k][lane];
-            if (__builtin_amdgcn_readfirstlane(head_of[u]) != 2) return true;
+    for (int w = 0; w < kSmall / 64; ++w) m += counts[w];
+    if (hits) {
+        int rank = 0;
+        for (int j = 0; j < a.T; j += 4) rank += (key[j] < k) + (key[j + 1] < k) + (key[j + 2] < k) + (key[j + 3] < k);
+        if (k != 0xFFFFFFFFu) toks[rank] = tid, rows[rank] = lo + (int)(k >> 8);
+    }
+    __syncthreads();
+    // rows that do not occur: a wave's own, against the rows that do
+    {
+        int held[kSmall / 64];
+#pragma unroll
+        for (int i = 0; i < kSmall / 64; ++i) held[i] = i * 64 + lane < m ? rows[i * 64 + lane] : -1;
+        const float zeros[Lane<BF16, TAIL>::M] = {};
+        for (int v = lo + wave; v < lo + n; v += kSmallWaves) {
+            bool occurs = false;
+#pragma unroll
+            for (int i = 0; i < kSmall / 64; ++i) occurs |= held[i] == v;
+            if (__ballot(occurs) == 0) mine.write(a, v, zeros);
         }
-        return false;
-    };
-    float* part = a.part + job * 2 * a.d;
-    if (tail >= 0) {
-        if (follow(acc, wave + 1)) mine.write(a, tail, acc);
-        else mine.write_part(part + a.d, acc);
     }
-    if (wave == 0 && head) {
-#pragma unroll
-        for (int k = 0; k < M; ++k) acc[k] = heads[0][k][lane];
-        if (head == 2) follow(acc, 1);
-        mine.write_part(part, acc);
-    }
+    if (m == 0) return;
+    const int p0 = wave * kPiece, cnt = max(0, min(kPiece, m - p0));
+    const Piece p{toks[min(p0 + lane, m - 1)], rows[min(p0 + lane, m - 1)], cnt, p0 > 0 && cnt ? rows[p0 - 1] : -1, p0 + cnt < m ? rows[p0 + cnt] : -1};
+    chunk.sum(a, mine, p, wave, lane, nullptr);
 }
 
 // A workgroup looks at a chunk and a slab: if a row starts there and goes on, it adds up the row's partial sums.  Each wave adds every
@@ -446,6 +513,20 @@ extern "C" int sdp_embed_bwd(int dtype, int id_type, int T, int V, int d, float 
     EmbedBwd a{dY, dE, {(int32_t*)w, (int32_t*)(w + l.ids), (int32_t*)(w + l.start), (int2*)(w + l.spans)}, (float*)(w + l.part), T, V, d, chunks_of(T),
                slabs_of(dtype, d), scale};
     sdp::ProfileScope ps("embed_bwd", s);
+    const auto by_form = [&](auto&& go) {
+        auto of = [&](auto bf16) {
+            return d % Row<bf16.value>::N ? go(bf16, std::integral_constant<int, 1>{}) : go(bf16, std::integral_constant<int, 0>{});
+        };
+        return dtype == SDP_BF16 ? of(std::integral_constant<int, 1>{}) : of(std::integral_constant<int, 0>{});
+    };
+    if (T <= kSmall) {
+        const int range = (V + kSortGroups - 1) / kSortGroups;
+        const unsigned groups = (unsigned)((V + range - 1) / range) * a.slabs;
+        return by_form([&](auto bf16, auto tail) {
+            embed_small_kernel<bf16.value, tail.value><<<groups, kSmallWaves * 64, 0, s>>>(a, ids, id_type == SDP_I64, range);
+            return sdp::launch_status();
+        });
+    }
     const int range = sort_range(V);
     int bits = 0;
     while ((1 << bits) < range) ++bits;
@@ -466,15 +547,11 @@ extern "C" int sdp_embed_bwd(int dtype, int id_type, int T, int V, int d, float 
         return st;
     const int64_t sum = ((int64_t)a.chunks + ((int64_t)V + kSumWaves * 64 - 1) / (kSumWaves * 64)) * a.slabs, join = (int64_t)(a.chunks - 1) * a.slabs;
     const unsigned gs = (unsigned)sum, gj = (unsigned)join;
-    auto sums = [&](auto bf16, auto tail) {
+    return by_form([&](auto bf16, auto tail) {
         embed_sum_kernel<bf16.value, tail.value><<<gs, kSumWaves * 64, 0, s>>>(a);
         const int rc = sdp::launch_status();
         if (rc != SDP_OK || a.chunks < 2) return rc;
         embed_join_kernel<bf16.value, tail.value><<<gj, 256, 0, s>>>(a);
         return sdp::launch_status();
-    };
-    auto sums_of = [&](auto bf16) {
-        return d % Row<bf16.value>::N ? sums(bf16, std::integral_constant<int, 1>{}) : sums(bf16, std::integral_constant<int, 0>{});
-    };
-    return dtype == SDP_BF16 ? sums_of(std::integral_constant<int, 1>{}) : sums_of(std::integral_constant<int, 0>{});
+    });
 }

@@ -20,10 +20,32 @@ namespace {
 // 'i' int32, 'f' float32, 't' int32 or int64, 'w' bytes, 'z' as 'a' but a
 // matrix whose rows may lie apart (the caller passes their distance), in capitals where None stands for a null pointer; 0 for parameters
 // passed as they are (numbers, workspace and stream addresses).
+// For calls that state their shapes: d0, d1 are the places of the integer arguments that are the tensor's sizes (kOne: size 1), ld that of
+// the distance of its rows.
+constexpr signed char kAny = -1, kOne = -2;
 struct Param {
     const char* name = nullptr;
     char kind = 0;
+    signed char d0 = kAny, d1 = kAny, ld = kAny;
 };
+
+// whether argument i has the shape that p states, in every call with such a statement before any tensor is looked at otherwise
+bool shape_fits(PyObject* const* args, size_t i, const Param& p) {
+    if (p.d0 == kAny || args[i] == Py_None || !THPVariable_Check(args[i])) return true;
+    const at::Tensor& t = THPVariable_Unpack(args[i]);
+    auto size = [&](signed char d) { return d == kOne ? 1LL : PyLong_AsLongLong(args[d]); };
+    const long long n0 = size(p.d0), n1 = p.d1 == kAny ? 0 : size(p.d1);
+    if (t.dim() != (p.d1 == kAny ? 1 : 2) || t.size(0) != n0 || (p.d1 != kAny && t.size(1) != n1)) {
+        if (p.d1 == kAny) PyErr_Format(PyExc_ValueError, "%s: expected shape (%lld,)", p.name, n0);
+        else PyErr_Format(PyExc_ValueError, "%s: expected shape (%lld, %lld)", p.name, n0, n1);
+        return false;
+    }
+    if (p.ld != kAny && n0 > 1 && t.stride(0) != size(p.ld)) {
+        PyErr_Format(PyExc_ValueError, "%s: expected rows %lld values apart (the strides of Z)", p.name, size(p.ld));
+        return false;
+    }
+    return true;
+}
 
 bool type_error(const Param& p, c10::ScalarType t) {
     const char* n = t == c10::kFloat ? "torch.float32" : t == c10::kBFloat16 ? "torch.bfloat16" : t == c10::kByte ? "torch.uint8" : "torch.int32";
@@ -88,6 +110,7 @@ PyObject* call(int (*fn)(A...), const Param* params, int dtype_at, PyObject* con
     std::tuple<A...> v;
     int rc = 0;
     try {
+        if (!(shape_fits(args, I, params[I]) && ...)) return nullptr;
         if (!(take(args[I], params[I], act, device, std::get<I>(v)) && ...)) return nullptr;
     } catch (const std::exception& e) { // a tensor without storage
         PyErr_SetString(PyExc_RuntimeError, e.what());
@@ -138,15 +161,15 @@ SDP_ENTRY(block_bwd, sdp_block_bwd, 3, {}, {}, {}, {}, {}, {}, {}, {}, {}, {}, {
           {"LSE_save", 'f'}, {"G_save", 'a'}, {"U_save", 'a'}, {"dX", 'a'}, {"dW", 'A'}, {"dW", 'A'}, {"dW", 'A'}, {"dW", 'A'},
           {"dW", 'A'}, {}, {}, {})
 
-SDP_ENTRY_HERE(norm_fwd, sdp_norm_fwd, 1, {}, {}, {}, {}, {}, {"X", 'a'}, {"residual", 'A'}, {"gamma", 'a'}, {"beta", 'A'}, {"H", 'A'},
-               {"Y", 'a'}, {"mean", 'F'}, {"rstd", 'f'}, {})
-SDP_ENTRY_HERE(norm_bwd, sdp_norm_bwd, 1, {}, {}, {}, {}, {"H", 'a'}, {"dY", 'a'}, {"dH", 'A'}, {"gamma", 'a'}, {"mean", 'F'},
-               {"rstd", 'f'}, {"dX", 'a'}, {"dgamma", 'A'}, {"dbeta", 'A'}, {"ws", 'W'}, {}, {})
-SDP_ENTRY_HERE(embed_fwd, sdp_embed_fwd, 0, {}, {}, {}, {}, {}, {}, {"E", 'a'}, {"ids", 't'}, {"Y", 'a'}, {})
-SDP_ENTRY_HERE(embed_bwd, sdp_embed_bwd, 0, {}, {}, {}, {}, {}, {}, {"dY", 'a'}, {"ids", 't'}, {"dE", 'a'}, {"ws", 'w'}, {}, {})
-SDP_ENTRY_HERE(token_loss, sdp_token_loss, 0, {}, {}, {}, {}, {}, {}, {"Z", 'z'}, {"labels", 't'}, {"scale_dev", 'F'}, {"nll", 'f'},
-               {"lse", 'F'}, {"dZ", 'Z'}, {"loss", 'F'}, {})
-SDP_ENTRY_HERE(label_scale, sdp_label_scale, 0, {}, {}, {}, {"labels", 't'}, {"scale", 'f'}, {})
+SDP_ENTRY_HERE(norm_fwd, sdp_norm_fwd, 1, {}, {}, {}, {}, {}, {"X", 'a', 2, 3}, {"residual", 'A', 2, 3}, {"gamma", 'a', 3}, {"beta", 'A', 3},
+               {"H", 'A', 2, 3}, {"Y", 'a', 2, 3}, {"mean", 'F', 2}, {"rstd", 'f', 2}, {})
+SDP_ENTRY_HERE(norm_bwd, sdp_norm_bwd, 1, {}, {}, {}, {}, {"H", 'a', 2, 3}, {"dY", 'a', 2, 3}, {"dH", 'A', 2, 3}, {"gamma", 'a', 3}, {"mean", 'F', 2},
+               {"rstd", 'f', 2}, {"dX", 'a', 2, 3}, {"dgamma", 'A', 3}, {"dbeta", 'A', 3}, {"ws", 'W'}, {}, {})
+SDP_ENTRY_HERE(embed_fwd, sdp_embed_fwd, 0, {}, {}, {}, {}, {}, {}, {"E", 'a', 3, 4}, {"ids", 't', 2}, {"Y", 'a', 2, 4}, {})
+SDP_ENTRY_HERE(embed_bwd, sdp_embed_bwd, 0, {}, {}, {}, {}, {}, {}, {"dY", 'a', 2, 4}, {"ids", 't', 2}, {"dE", 'a', 3, 4}, {"ws", 'w'}, {}, {})
+SDP_ENTRY_HERE(token_loss, sdp_token_loss, 0, {}, {}, {}, {}, {}, {}, {"Z", 'z', 2, 3, 4}, {"labels", 't', 2}, {"scale_dev", 'F', kOne}, {"nll", 'f', 2},
+               {"lse", 'F', 2}, {"dZ", 'Z', 2, 3, 4}, {"loss", 'F', kOne}, {})
+SDP_ENTRY_HERE(label_scale, sdp_label_scale, 0, {}, {}, {}, {"labels", 't'}, {"scale", 'f', kOne}, {})
 
 #define SDP_METHOD(py) {#py, (PyCFunction)(void (*)(void))py, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {SDP_METHOD(mlp_fwd),   SDP_METHOD(mlp_bwd),   SDP_METHOD(attn_fwd), SDP_METHOD(attn_bwd),

@@ -266,23 +266,33 @@ __global__ __launch_bounds__(bwd_waves(WPR) * 64) void norm_bwd_kernel(NormBwd a
         if (first + step < a.T) take(two, one, lds[1]);
     }
     if (!a.want_dw) return;
+    // one workgroup alone has the sums
+    const bool alone = gridDim.x == 1;
     float* out = a.partial + (int64_t)blockIdx.x * 2 * d;
-    extern __shared__ float share[]; // [2][d] where a workgroup has several rows
+    auto give = [&](int part, int e, float x) {
+        if (!alone) out[part * d + e] = x;
+        else if (part == 0) Rw::put((Elem*)a.dgamma + e, x);
+        else if (a.dbeta) Rw::put((Elem*)a.dbeta + e, x);
+    };
+    extern __shared__ float share[]; // [ROWS][2][d] where a workgroup has several rows
+    float* mine = share + wave / WPR * 2 * d;
+    auto add = [&](int e, float g, float b) {
+        if (ROWS == 1) give(0, e, g), give(1, e, b);
+        else mine[e] = g, mine[d + e] = b;
+    };
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-        if (r) __syncthreads();
-        if (wave / WPR != r) continue;
-        auto add = [&](int e, float g, float b) {
-            if (r) g += share[e], b += share[d + e];
-            if (r == ROWS - 1) out[e] = g, out[d + e] = b;
-            else share[e] = g, share[d + e] = b;
-        };
+    for (int i = 0; i < VPL; ++i)
+        if (at + i * STEP < whole)
 #pragma unroll
-        for (int i = 0; i < VPL; ++i)
-            if (at + i * STEP < whole)
+            for (int k = 0; k < N; ++k) add(at + i * STEP + k, dga[i][k], dbe[i][k]);
+    if (tail) add(et, dgat, dbet);
+    if (ROWS == 1) return;
+    __syncthreads();
+    for (int e = threadIdx.x; e < 2 * d; e += WAVES * 64) {
+        float x = share[e];
 #pragma unroll
-                for (int k = 0; k < N; ++k) add(at + i * STEP + k, dga[i][k], dbe[i][k]);
-        if (tail) add(et, dgat, dbet);
+        for (int r = 1; r < ROWS; ++r) x += share[r * 2 * d + e];
+        give(e >= d, e >= d ? e - d : e, x);
     }
 }
 
@@ -331,10 +341,12 @@ Shape bwd_shape(int dtype, int d) {
 int fwd_rows(const Shape& s) { return s.wpr == 1 ? 4 : 1; }
 int bwd_rows(const Shape& s) { return bwd_waves(s.wpr) / s.wpr; }
 
-constexpr int kBwdGroups = 256;
+// Workgroups of the backward pass: one on every CU; where that one would have so few turns that they take less than a second launch, one alone,
+// which also writes the sums.
+constexpr int kBwdGroups = 256, kBwdAlone = 4;
 int bwd_groups(int T, const Shape& s) {
     const int64_t all = ((int64_t)T + bwd_rows(s) - 1) / bwd_rows(s);
-    return (int)(all < kBwdGroups ? all : kBwdGroups);
+    return all <= kBwdAlone ? (all > 0) : (int)(all < kBwdGroups ? all : kBwdGroups);
 }
 
 #define SDP_NORM_SHAPE(W, V) \
@@ -449,7 +461,7 @@ extern "C" int sdp_norm_bwd(int kind, int dtype, int T, int d, const void* H, co
     int st2 = SDP_OK;
     if (groups > 0) {
         const NormBwd a{H, dY, dH, gamma, mean, rstd, dX, dgamma, dbeta, (float*)ws, T, d, dgamma != nullptr};
-        const size_t lds = bwd_rows(sh) > 1 && dgamma ? (size_t)2 * d * sizeof(float) : 0;
+        const size_t lds = bwd_rows(sh) > 1 && dgamma ? (size_t)bwd_rows(sh) * 2 * d * sizeof(float) : 0;
         st2 = by_bwd_shape(dtype, sh, [&](auto bf16, auto wpr, auto vpl) {
             auto go = [&](auto form) {
                 if (dH) norm_bwd_kernel<bf16.value, wpr.value, vpl.value, form.value, 1><<<groups, bwd_waves(wpr.value) * 64, lds, s>>>(a);
@@ -461,7 +473,7 @@ extern "C" int sdp_norm_bwd(int kind, int dtype, int T, int d, const void* H, co
             return sdp::launch_status();
         });
     }
-    if (st2 != SDP_OK || !dgamma) return st2;
+    if (st2 != SDP_OK || !dgamma || groups == 1) return st2;
     const dim3 grid((d + 63) / 64, dbeta ? 2 : 1);
     if (dtype == SDP_BF16) norm_dw_kernel<1><<<grid, 1024, 0, s>>>((const float*)ws, groups, d, dgamma, dbeta);
     else norm_dw_kernel<0><<<grid, 1024, 0, s>>>((const float*)ws, groups, d, dgamma, dbeta);
