@@ -362,14 +362,14 @@ __global__ __launch_bounds__(kSumWaves * 64) void embed_sum_kernel(EmbedBwd a) {
 }
 
 // A batch of kSmall tokens at most, in one launch: a workgroup has a range of ids, as in the sort, and a slab of the columns.  Its tokens are
-// put in order by counting, for each, those before it (the ids are in LDS, the counting less than a wait for memory), and are one
+// put in order by counting, for each, those before it, and are one
 // chunk: no row goes on elsewhere.  256 tokens, 1024 rows of 256 fp32: one launch 5.5 us, three 12.3.
 constexpr int kSmallWaves = 16, kSmall = kSmallWaves * kPiece;
 
 template <int BF16, int TAIL>
 __global__ __launch_bounds__(kSmallWaves * 64) void embed_small_kernel(EmbedBwd a, const void* ids, int wide, int range) {
     __shared__ Chunk<BF16, TAIL, kSmallWaves> chunk;
-    __shared__ uint32_t key[kSmall]; // id - lo, then token; the largest value for tokens that are not the range's
+    __shared__ uint32_t key[kSmall]; // of the range's tokens: id - lo, then token
     __shared__ int toks[kSmall], rows[kSmall], counts[kSmallWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int job = blockIdx.x / a.slabs, lo = job * range, n = min(range, a.V - lo);
@@ -380,16 +380,19 @@ __global__ __launch_bounds__(kSmallWaves * 64) void embed_small_kernel(EmbedBwd 
         if (id >= lo && id - lo < n) k = (uint32_t)(id - lo) << 8 | tid;
     }
     const uint64_t hits = __ballot(k != 0xFFFFFFFFu);
-    if (tid < kSmall) key[tid] = k;
     if (lane == 0) counts[wave] = __popcll(hits);
     __syncthreads();
-    int m = 0;
+    int m = 0, before = 0;
 #pragma unroll
-    for (int w = 0; w < kSmall / 64; ++w) m += counts[w];
-    if (hits) {
+    for (int w = 0; w < kSmall / 64; ++w) before += w < wave ? counts[w] : 0, m += counts[w];
+    if (k != 0xFFFFFFFFu) key[before + __popcll(hits & ((1ull << lane) - 1))] = k;
+    __syncthreads();
+    if (tid < m) {
+        const uint32_t own = key[tid];
         int rank = 0;
-        for (int j = 0; j < a.T; j += 4) rank += (key[j] < k) + (key[j + 1] < k) + (key[j + 2] < k) + (key[j + 3] < k);
-        if (k != 0xFFFFFFFFu) toks[rank] = tid, rows[rank] = lo + (int)(k >> 8);
+#pragma unroll 4
+        for (int j = 0; j < m; ++j) rank += key[j] < own;
+        toks[rank] = own & 255, rows[rank] = lo + (int)(own >> 8);
     }
     __syncthreads();
     // rows that do not occur: a wave's own, against the rows that do
