@@ -364,7 +364,8 @@ int sdp_clip_scale(int n, const double* sqnorm, float max_norm, float* scale, vo
 typedef enum { SDP_NORM_LAYER = 0, SDP_NORM_RMS = 1 } sdp_norm_kind;
 typedef enum { SDP_I32 = 0, SDP_I64 = 1 } sdp_id_type;
 #define SDP_NORM_MAX_WIDTH 16384    /* largest d of the norm calls */
-#define SDP_MAX_EXTENT (1 << 30)    /* largest T, V and d of the calls below */
+#define SDP_MAX_EXTENT (1 << 30)    /* largest T, V and d of the calls below, but: */
+#define SDP_EMBED_MAX_TOKENS (1 << 26) /* largest T of the embedding calls */
 
 /* ---------------------------------------------------------------------------------------------
  * Norm of T tokens of width d, of their own or of a sum with a skip connection:
@@ -405,7 +406,7 @@ int sdp_norm_bwd(int kind, int dtype, int T, int d, const void* H, const void* d
  * bits), zeros where ids[t] lies outside [0, V).
  *   E [V][d] in (row-major by token, as every matrix here is by neuron);  ids [T] in;  Y [T][d] out
  * Errors: INVALID_ARG (null, misaligned, overlapping, unknown dtype or id_type, T < 0, V < 1, d < 1, scale not finite),
- * SHAPE (T, V or d > SDP_MAX_EXTENT).
+ * SHAPE (T > SDP_EMBED_MAX_TOKENS, V or d > SDP_MAX_EXTENT).
  *
  * sdp_embed_bwd: its gradient, dE[v] = scale sum_{t : ids[t] = v} dY[t], every row of [V][d]: rows of tokens that do not
  * occur are zeros.  Tokens are sorted by id (stably, so each row's fp32 sum has one order, whatever the

@@ -66,6 +66,9 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(EmbedFwd a) {
 constexpr int kSortWaves = 16, kSortGroups = 256, kMaxRange = 960, kAhead = 16;
 // sorted tokens of a wave, all of whose rows are in flight at once, and of a workgroup
 constexpr int kPiece = 16, kSumWaves = 8, kChunk = kPiece * kSumWaves;
+// Rows that a wave clears if they do not occur: few, since waves that store once or twice and end write memory in its order, and faster
+// (sums of 16384 tokens, 32000 x 2048 bf16, and of 300, 64000 x 2048: 64 rows 42.1 and 57.9 us in all, 8 rows 44.8 and 53.4, two 40.9 and 49.4).
+constexpr int kClear = 2;
 
 struct Sorted {
     int32_t* order; // [T] tokens, by id, then by place
@@ -79,19 +82,21 @@ int sort_range(int V) {
     const int r = (V + kSortGroups - 1) / kSortGroups;
     return r < kMaxRange ? r : kMaxRange;
 }
-constexpr int kListed = 64 * kAhead; // tokens of a wave that are looked at, and of its workgroup's range at most, between two lists
+constexpr int kBlock = 64 * kAhead; // tokens of a wave that are requested at once
+constexpr size_t kSortLds = 159744; // LDS of the lists and counts: a CU's, less what is declared
 
-// ONCE: a wave's tokens make one list, which stays between the two times
+// ONCE: a wave has kBlock tokens at most, requested before anything else.  `room`: tokens that a wave's list holds, kBlock at least.  A wave whose
+// part of the range is longer counts each list that is full and starts another; it goes through its ids again to place them.
 template <int WIDE, int ONCE>
-__global__ __launch_bounds__(kSortWaves * 64) void embed_sort_kernel(const void* __restrict__ ids, int T, int V, int range, int bits,
+__global__ __launch_bounds__(kSortWaves * 64) void embed_sort_kernel(const void* __restrict__ ids, int T, int V, int range, int bits, int room,
                                                                      Sorted out) {
     extern __shared__ int lds[];
     __shared__ int sums[kSortWaves], below_all[kSortWaves];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const uint64_t lanes_below = (1ull << lane) - 1;
-    int* hist = lds + kSortWaves * kListed;      // [kSortWaves][range]: a wave's tokens of each id, then where its next one goes
+    int* hist = lds + kSortWaves * room; // [kSortWaves][range]: a wave's tokens of each id, then where its next one goes
     int* mine = hist + wave * range;
-    int* list = lds + wave * kListed;            // the wave's tokens of the range, in order: token - first token of the list, id - lo
+    int* list = lds + wave * room;       // the wave's tokens of the range, in order: place among the wave's tokens, id - lo (10 bits)
     const uint32_t lo = blockIdx.x * range, n = min((uint32_t)range, (uint32_t)V - lo);
     // each wave has an unbroken piece of the tokens, of which a lane takes every 64th
     const int64_t piece = ((int64_t)T + kSortWaves * 64 - 1) / (kSortWaves * 64) * 64;
@@ -110,26 +115,25 @@ __global__ __launch_bounds__(kSortWaves * 64) void embed_sort_kernel(const void*
         for (int i = 0; i < kAhead; ++i) id[i] = b + i * 64 + lane < end && v[i] <= 0xFFFFFFFFu ? (uint32_t)v[i] : 0xFFFFFFFFu;
     };
     int below = 0;
-    auto make_list = [&]() { // of what was requested; its length
-        int m = 0;
+    auto add_to_list = [&](int& m, uint32_t at) { // of what was requested, the wave's tokens from `at` on
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
             below += __popcll(__ballot(id[i] < lo));
             const uint32_t k = id[i] - lo;
             const uint64_t hits = __ballot(k < n);
             if (hits == 0) continue;
-            if (k < n) list[m + __popcll(hits & lanes_below)] = (i * 64 + lane) << 16 | (int)k;
+            if (k < n) list[m + __popcll(hits & lanes_below)] = (int)((at + i * 64 + lane) << 10 | k);
             m += __popcll(hits);
         }
         __builtin_amdgcn_wave_barrier(); // read by other lanes of the wave
-        return m;
     };
     // 64 tokens of the list at a time: a token's place is the wave's count of its id and its rank among the lanes with the same id: all of
     // them (a frequent token), or found by the bits of the id
-    auto take_list = [&](int m, int64_t b, bool write) {
+    auto take_list = [&](int m, bool write) {
         for (int g = 0; g < m; g += 64) {
             const bool live = g + lane < m;
-            const int entry = list[g + lane < m ? g + lane : g], k = entry & 0xFFFF;
+            const uint32_t entry = list[g + lane < m ? g + lane : g];
+            const int k = entry & 1023;
             uint64_t peers = __ballot(live);
             if (__ballot(live && k == __builtin_amdgcn_readfirstlane(k)) != peers)
                 for (int j = 0; j < bits; ++j) {
@@ -140,7 +144,7 @@ __global__ __launch_bounds__(kSortWaves * 64) void embed_sort_kernel(const void*
             __builtin_amdgcn_wave_barrier(); // everyone's count is read before it is raised
             if (live) {
                 if (write) {
-                    out.order[at] = (int)(b + (entry >> 16));
+                    out.order[at] = (int)(begin + (entry >> 10));
                     out.ids[at] = (int)lo + k;
                 }
                 if (rank == 0) mine[k] = at + __popcll(peers);
@@ -149,18 +153,21 @@ __global__ __launch_bounds__(kSortWaves * 64) void embed_sort_kernel(const void*
         }
     };
     int listed = 0;
+    bool again = false; // the list does not hold them all
     if (ONCE) request(begin);
     for (int i = tid; i < kSortWaves * range; i += kSortWaves * 64) hist[i] = 0;
     __syncthreads();
-    if (ONCE) {
-        listed = make_list();
-        take_list(listed, begin, false);
-    } else {
-        for (int64_t b = begin; b < end; b += kListed) {
+    for (int64_t b = begin; b < end; b += kBlock) {
+        if (!ONCE) {
             request(b);
-            take_list(make_list(), b, false);
+            if (listed > room - kBlock) {
+                take_list(listed, false);
+                listed = 0, again = true;
+            }
         }
+        add_to_list(listed, (uint32_t)(b - begin));
     }
+    take_list(listed, false);
     if (lane == 0) below_all[wave] = below;
     __syncthreads();
     // an id per thread (kMaxRange <= threads): its tokens, then exclusive sums over the ids before it
@@ -193,14 +200,20 @@ __global__ __launch_bounds__(kSortWaves * 64) void embed_sort_kernel(const void*
         }
     }
     __syncthreads();
-    if (ONCE) {
-        take_list(listed, begin, true);
-    } else {
-        for (int64_t b = begin; b < end; b += kListed) {
-            request(b);
-            take_list(make_list(), b, true);
-        }
+    if (ONCE || !again) {
+        take_list(listed, true);
+        return;
     }
+    listed = 0;
+    for (int64_t b = begin; b < end; b += kBlock) {
+        request(b);
+        if (listed > room - kBlock) {
+            take_list(listed, true);
+            listed = 0;
+        }
+        add_to_list(listed, (uint32_t)(b - begin));
+    }
+    take_list(listed, true);
 }
 
 struct EmbedBwd {
@@ -248,9 +261,9 @@ struct Lane {
     }
 };
 
-// A workgroup has a chunk of the sorted tokens, a wave a piece of it, or 64 rows of dE for each wave to clear the empty ones of; and a slab of
-// 64 pieces of the columns.  What a wave has of a row that starts in an earlier one goes through LDS to the wave that has its start,
-// and to memory only where that lies in another chunk.
+// A workgroup has a chunk of the sorted tokens, a wave a piece of it, or kClear rows of dE for each wave to clear; and a slab of 64 pieces of
+// the columns.  What a wave has of a row that starts in an earlier one goes through LDS to the wave that has its start, and to memory
+// only where that lies in another chunk.
 //
 // Piece: the wave's sorted tokens: lane i < cnt has token `tok` of row `id`; `prev` and `next`: the rows of the tokens before and behind
 // them, -1 where there are none.
@@ -339,15 +352,11 @@ __global__ __launch_bounds__(kSumWaves * 64) void embed_sum_kernel(EmbedBwd a) {
     const int64_t job = blockIdx.x / a.slabs;
     const Lane<BF16, TAIL> mine(a.d, (int)(blockIdx.x - job * a.slabs), lane);
     if (job >= a.chunks) {
-        const int64_t v = ((job - a.chunks) * kSumWaves + wave) * 64;
-        if (v >= a.V) return;
-        const bool empty = v + lane < a.V && a.s.start[v + lane] == a.s.start[v + lane + 1];
-        uint64_t left = __ballot(empty);
+        const int64_t first = ((job - a.chunks) * kSumWaves + wave) * kClear;
         const float zeros[Lane<BF16, TAIL>::M] = {};
-        while (left) {
-            mine.write(a, (int)v + __ffsll((unsigned long long)left) - 1, zeros);
-            left &= left - 1;
-        }
+#pragma unroll
+        for (int i = 0; i < kClear; ++i)
+            if (first + i < a.V && a.s.start[first + i] == a.s.start[first + i + 1]) mine.write(a, (int)(first + i), zeros);
         return;
     }
     // requested before it is known how many tokens there are: what lies behind the last one is not used
@@ -453,7 +462,7 @@ int check_embed(int dtype, int id_type, int T, int V, int d) {
     if (dtype != SDP_F32 && dtype != SDP_BF16) return SDP_ERR_INVALID_ARG;
     if (id_type != SDP_I32 && id_type != SDP_I64) return SDP_ERR_INVALID_ARG;
     if (T < 0 || V < 1 || d < 1) return SDP_ERR_INVALID_ARG;
-    return T > SDP_MAX_EXTENT || V > SDP_MAX_EXTENT || d > SDP_MAX_EXTENT ? SDP_ERR_SHAPE : SDP_OK;
+    return T > SDP_EMBED_MAX_TOKENS || V > SDP_MAX_EXTENT || d > SDP_MAX_EXTENT ? SDP_ERR_SHAPE : SDP_OK;
 }
 
 int chunks_of(int T) { return (int)(((int64_t)T + kChunk - 1) / kChunk); }
@@ -534,21 +543,23 @@ extern "C" int sdp_embed_bwd(int dtype, int id_type, int T, int V, int d, float 
     int bits = 0;
     while ((1 << bits) < range) ++bits;
     const dim3 groups((V + range - 1) / range);
-    const size_t lds = (size_t)kSortWaves * (kListed + range) * sizeof(int);
+    // one block's list for the shorter batches, so that two workgroups share a CU; else all that the counts leave
+    const int room = T <= kSortWaves * kBlock ? kBlock : (int)(kSortLds / (kSortWaves * sizeof(int))) - range;
+    const size_t lds = (size_t)kSortWaves * (room + range) * sizeof(int);
     auto sort = [&](auto wide, auto once) {
         const auto kern = embed_sort_kernel<wide.value, once.value>;
         static const hipError_t attr =
-            hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, kSortWaves * (kListed + kMaxRange) * sizeof(int));
+            hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kSortLds);
         if (attr != hipSuccess) return sdp::hip_status(attr);
-        kern<<<groups, kSortWaves * 64, lds, s>>>(ids, T, V, range, bits, a.s);
+        kern<<<groups, kSortWaves * 64, lds, s>>>(ids, T, V, range, bits, room, a.s);
         return sdp::launch_status();
     };
     auto sort_of = [&](auto wide) {
-        return T <= kSortWaves * kListed ? sort(wide, std::integral_constant<int, 1>{}) : sort(wide, std::integral_constant<int, 0>{});
+        return T <= kSortWaves * kBlock ? sort(wide, std::integral_constant<int, 1>{}) : sort(wide, std::integral_constant<int, 0>{});
     };
     if (const int st = id_type == SDP_I64 ? sort_of(std::integral_constant<int, 1>{}) : sort_of(std::integral_constant<int, 0>{}); st != SDP_OK)
         return st;
-    const int64_t sum = ((int64_t)a.chunks + ((int64_t)V + kSumWaves * 64 - 1) / (kSumWaves * 64)) * a.slabs, join = (int64_t)(a.chunks - 1) * a.slabs;
+    const int64_t sum = ((int64_t)a.chunks + ((int64_t)V + kSumWaves * kClear - 1) / (kSumWaves * kClear)) * a.slabs, join = (int64_t)(a.chunks - 1) * a.slabs;
     const unsigned gs = (unsigned)sum, gj = (unsigned)join;
     return by_form([&](auto bf16, auto tail) {
         embed_sum_kernel<bf16.value, tail.value><<<gs, kSumWaves * 64, 0, s>>>(a);
