@@ -189,9 +189,6 @@ __global__ __launch_bounds__(kSortWaves * 64) void embed_sort_kernel(const void*
     if (tid < n) {
         out.start[lo + tid] = at;
         if (lo + tid == V - 1) out.start[V] = at + total;
-        // every chunk's first place lies in one row, which says what goes on from the chunk before
-        for (int c = (at + kChunk - 1) / kChunk; c * kChunk < at + total; ++c)
-            if (c > 0) out.spans[c - 1] = c == at / kChunk + 1 ? make_int2(lo + tid, (at + total - 1) / kChunk) : make_int2(-1, 0);
 #pragma unroll
         for (int w = 0; w < kSortWaves; ++w) {
             const int c = hist[w * range + tid];
@@ -367,6 +364,11 @@ __global__ __launch_bounds__(kSumWaves * 64) void embed_sum_kernel(EmbedBwd a) {
     p.cnt = max(0, min(kPiece, n - p0));
     if (p0 == 0) p.prev = -1;
     if (p0 + p.cnt >= n) p.next = -1;
+    if (job > 0 && wave == 0 && blockIdx.x % a.slabs == 0 && lane == 0) {
+        // what goes on from the chunk before, if it starts there
+        const int before = (int)(job - 1) * kChunk;
+        a.s.spans[job - 1] = p.id == p.prev && a.s.start[p.id] >= before ? make_int2(p.id, (a.s.start[p.id + 1] - 1) / kChunk) : make_int2(-1, 0);
+    }
     chunk.sum(a, mine, p, wave, lane, a.part + job * 2 * a.d);
 }
 
@@ -433,7 +435,7 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedBwd a) {
     const int64_t job = blockIdx.x / a.slabs;
     const Lane<BF16, TAIL> mine(a.d, (int)(blockIdx.x - job * a.slabs), lane);
     const int n = a.s.start[a.V];
-    const int2 span = a.s.spans[job]; // written where the next chunk has a token
+    const int2 span = a.s.spans[job]; // written by the sums of the next chunk, where that has a token
     if ((job + 1) * kChunk >= n || span.x < 0) return;
     float acc[M] = {};
     // the row's parts: of chunk `job`, then of those up to span.y
