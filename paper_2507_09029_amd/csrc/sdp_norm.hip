@@ -124,8 +124,8 @@ __global__ __launch_bounds__(waves_of(WPR) * 64) void norm_fwd_kernel(NormFwd a)
         const bool live = at + i * STEP < whole;
 #pragma unroll
         for (int k = 0; k < N; ++k) {
-            h[i][k] -= mu;
-            sq += live ? h[i][k] * h[i][k] : 0.f;
+            h[i][k] = live ? h[i][k] - mu : 0.f;
+            sq = __builtin_fmaf(h[i][k], h[i][k], sq);
         }
     }
     const float rstd = 1.0f / __builtin_sqrtf(row_sum<WPR>(sq, lds[1]) / (float)d + a.eps);
@@ -140,10 +140,7 @@ __global__ __launch_bounds__(waves_of(WPR) * 64) void norm_fwd_kernel(NormFwd a)
         Rw::unpack(Rw::load((const Elem*)a.gamma, e, whole), ga);
         if (a.beta) Rw::unpack(Rw::load((const Elem*)a.beta, e, whole), be);
 #pragma unroll
-        for (int k = 0; k < N; ++k) {
-            h[i][k] = h[i][k] * rstd * ga[k];
-            if (a.beta) h[i][k] += be[k];
-        }
+        for (int k = 0; k < N; ++k) h[i][k] = __builtin_fmaf(h[i][k] * rstd, ga[k], be[k]);
         Rw::store((Elem*)a.Y + off, e, whole, Rw::pack(h[i]));
     }
     if (tail) {
