@@ -132,7 +132,10 @@ __global__ __launch_bounds__(WAVES * 64) void token_loss_kernel(Loss a) {
         float v[N];
         Rw::unpack(x, v);
 #pragma unroll
-        for (int k = 0; k < N; ++k) v[k] = power(v[k]) * inv - (e + k == label ? c : 0.f);
+        for (int k = 0; k < N; ++k) v[k] = power(v[k]) * inv;
+        if ((uint32_t)(label - e) < (uint32_t)N)
+#pragma unroll
+            for (int k = 0; k < N; ++k) v[k] -= e + k == label ? c : 0.f;
         Rw::store(dz, e, whole, Rw::pack(v));
     };
     if (PIECES) {
