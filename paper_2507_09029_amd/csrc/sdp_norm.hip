@@ -190,9 +190,9 @@ __global__ __launch_bounds__(bwd_waves(WPR) * 64) void norm_bwd_kernel(NormBwd a
             if constexpr (FORM == FORM_SHORT) {
                 w.h[i] = w.dy[i] = w.skip[i] = u32x4{0, 0, 0, 0};
             } else {
-                w.h[i] = Rw::load_some((const Elem*)a.H + off, at + i * STEP, whole);
-                w.dy[i] = Rw::load_some((const Elem*)a.dY + off, at + i * STEP, whole);
-                if constexpr (SKIP) w.skip[i] = Rw::load_some((const Elem*)a.dH + off, at + i * STEP, whole);
+                w.h[i] = Rw::template load_some<FORM == FORM_ONCE>((const Elem*)a.H + off, at + i * STEP, whole);
+                w.dy[i] = Rw::template load_some<FORM == FORM_ONCE>((const Elem*)a.dY + off, at + i * STEP, whole);
+                if constexpr (SKIP) w.skip[i] = Rw::template load_some<FORM == FORM_ONCE>((const Elem*)a.dH + off, at + i * STEP, whole);
             }
         }
         if constexpr (FORM >= FORM_TAIL) {
@@ -454,6 +454,7 @@ extern "C" int sdp_norm_bwd(int kind, int dtype, int T, int d, const void* H, co
     hipStream_t s = (hipStream_t)stream;
     const Shape sh = bwd_shape(dtype, d);
     const int groups = bwd_groups(T, sh);
+    const bool once = sdp::read_once({eH, eY, eS}, w);
     sdp::ProfileScope ps("norm_bwd", s);
     int st2 = SDP_OK;
     if (groups > 0) {
@@ -464,7 +465,8 @@ extern "C" int sdp_norm_bwd(int kind, int dtype, int T, int d, const void* H, co
                 if (dH) norm_bwd_kernel<bf16.value, wpr.value, vpl.value, form.value, 1><<<groups, bwd_waves(wpr.value) * 64, lds, s>>>(a);
                 else norm_bwd_kernel<bf16.value, wpr.value, vpl.value, form.value, 0><<<groups, bwd_waves(wpr.value) * 64, lds, s>>>(a);
             };
-            if (d % Row<bf16.value>::N == 0) go(std::integral_constant<int, FORM_WHOLE>{});
+            if (once) go(std::integral_constant<int, FORM_ONCE>{});
+            else if (d % Row<bf16.value>::N == 0) go(std::integral_constant<int, FORM_WHOLE>{});
             else if (wpr.value > 1 || d > Row<bf16.value>::N) go(std::integral_constant<int, FORM_TAIL>{});
             else go(std::integral_constant<int, wpr.value * vpl.value == 1 ? FORM_SHORT : FORM_TAIL>{});
             return sdp::launch_status();

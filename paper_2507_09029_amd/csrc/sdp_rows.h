@@ -24,16 +24,17 @@ typedef u32x4 __attribute__((aligned(2))) u32x4_at2;
 typedef u32x4 __attribute__((aligned(4))) u32x4_at4;
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-// Whether rows of `row_bytes` in these matrices are read around the caches: more than they hold (the eight L2s 32 MB), and rows of whole
-// lines, since a line that two rows share is else fetched twice.  Norm forward of 16384 x 2048 bf16 with / without 46.9 / 48.4 us, loss of
-// 8192 x 32000 185 / 190; but rows that are no whole lines: loss of 1000 x 50001 57.6 / 49.6.
+// Whether rows of `row_bytes` in these matrices are read around the caches: far more than the eight L2s' 32 MB, and rows of whole lines, since
+// a line that two rows share is else fetched twice.  With / without, us: norm forward of 16384 x 2048 bf16 and a sum (134 MB) 47.5 / 49.3,
+// backward with the skip connection (201 MB) 49.4 / 51.6, loss of 8192 x 32000 (524 MB) 177.7 / 182.1; but norm forward of 16384 x 768
+// (50 MB) 20.2 / 16.6, backward (75 MB) 24.1 / 22.4, and loss of 1000 x 50001, no whole lines, 57.6 / 49.6.
 inline bool read_once(std::initializer_list<Extent> of, size_t row_bytes) {
     size_t all = 0;
     for (const Extent& m : of) {
         if (m.bytes && !aligned_to(m.p, 128)) return false;
         all += m.bytes;
     }
-    return row_bytes % 128 == 0 && all >= (size_t)1 << 26;
+    return row_bytes % 128 == 0 && all >= (size_t)1 << 27;
 }
 
 template <int BF16>
