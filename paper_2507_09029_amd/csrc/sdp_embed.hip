@@ -6,11 +6,13 @@
 // belong to one row of dE are then neighbours in the sorted order, to be summed by one wave in registers.  No atomics on floats: each
 // row's sum has one order, given by the ids alone.
 //
-// Batches of few tokens have a launch of their own (embed_small_kernel).  Otherwise the sort is one launch in which no workgroup waits for another.  Each owns a range of ids and goes through all T ids itself, twice:
-// the first time it counts, how many ids lie below its range (where its part of the order starts) and how often each id of its
-// range occurs; the second time it writes the tokens of its range to their places.  The ids are few bytes and come from
-// the cache for all workgroups but the first, so that T / 1024 steps a workgroup take less than the launches and the waiting of a sort
-// by digits.
+// Batches of up to kSmall tokens have a launch of their own (embed_small_kernel).  Otherwise the sort is one launch in which no workgroup
+// waits for another.  Each owns a range of ids and goes through all T ids itself: it counts how many lie below its range (where its
+// part of the order starts) and lists the tokens of its range, counts how often each id of it occurs, and writes the listed tokens
+// to their places.  The ids are few bytes and come from the cache for all workgroups but the first, so that T / 1024 steps a workgroup
+// take less than the launches and the waiting of a sort by digits: 10 us for 16384 ids of 32000 whose frequencies fall as 1 / rank
+// (8 where all are as frequent, 6 with no id in range, 14 with one id alone), 37 for 131072.  Where one workgroup's range holds most of a
+// long batch it has most of the work: 123 us for 131072 ids in which the frequent ones are neighbours.
 //
 // A token that occurs often (the most frequent of a text are several percent of it; in a padded batch one may be all) would be
 // one wave's long sum.  The sorted order is therefore cut into chunks of kChunk tokens, of a workgroup each (for 512 columns of bf16): a
@@ -39,7 +41,7 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(EmbedFwd a) {
     typedef Row<BF16> Rw;
     typedef typename Rw::Elem Elem;
     constexpr int N = Rw::N, B = 4; // pieces in flight
-    const int64_t t = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int64_t t = (int64_t)sdp::group_id() * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     if (t >= a.T) return;
     const int lane = threadIdx.x & 63, id = sdp::token_id(a.ids, a.wide, t, a.V), whole = Rw::whole(a.d);
     const Elem* in = (const Elem*)a.E + (int64_t)id * a.d;
@@ -85,6 +87,13 @@ int sort_range(int V) {
 constexpr int kBlock = 64 * kAhead; // tokens of a wave that are requested at once
 constexpr size_t kSortLds = 159744; // LDS of the lists and counts: a CU's, less what is declared
 
+// orders a wave's own reads and writes of LDS, for the compiler: the instructions themselves take place in order
+__device__ inline void wave_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // ONCE: a wave has kBlock tokens at most, requested before anything else.  `room`: tokens that a wave's list holds, kBlock at least.  A wave whose
 // part of the range is longer counts each list that is full and starts another; it goes through its ids again to place them.
 template <int WIDE, int ONCE>
@@ -125,7 +134,7 @@ __global__ __launch_bounds__(kSortWaves * 64) void embed_sort_kernel(const void*
             if (k < n) list[m + __popcll(hits & lanes_below)] = (int)((at + i * 64 + lane) << 10 | k);
             m += __popcll(hits);
         }
-        __builtin_amdgcn_wave_barrier(); // read by other lanes of the wave
+        wave_fence(); // read by other lanes of the wave
     };
     // 64 tokens of the list at a time: a token's place is the wave's count of its id and its rank among the lanes with the same id: all of
     // them (a frequent token), or found by the bits of the id
@@ -141,7 +150,7 @@ __global__ __launch_bounds__(kSortWaves * 64) void embed_sort_kernel(const void*
                     peers &= (k >> j) & 1 ? set : ~set;
                 }
             const int rank = __popcll(peers & lanes_below), at = mine[k] + rank;
-            __builtin_amdgcn_wave_barrier(); // everyone's count is read before it is raised
+            wave_fence(); // everyone's count is read before it is raised
             if (live) {
                 if (write) {
                     out.order[at] = (int)(begin + (entry >> 10));
@@ -149,7 +158,7 @@ __global__ __launch_bounds__(kSortWaves * 64) void embed_sort_kernel(const void*
                 }
                 if (rank == 0) mine[k] = at + __popcll(peers);
             }
-            __builtin_amdgcn_wave_barrier();
+            wave_fence();
         }
     };
     int listed = 0;
@@ -346,8 +355,9 @@ template <int BF16, int TAIL>
 __global__ __launch_bounds__(kSumWaves * 64) void embed_sum_kernel(EmbedBwd a) {
     __shared__ Chunk<BF16, TAIL, kSumWaves> chunk;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int64_t job = blockIdx.x / a.slabs;
-    const Lane<BF16, TAIL> mine(a.d, (int)(blockIdx.x - job * a.slabs), lane);
+    const int64_t job = sdp::group_id() / (uint32_t)a.slabs;
+    const int slab = (int)(sdp::group_id() - (uint32_t)job * (uint32_t)a.slabs);
+    const Lane<BF16, TAIL> mine(a.d, slab, lane);
     if (job >= a.chunks) {
         const int64_t first = ((job - a.chunks) * kSumWaves + wave) * kClear;
         const float zeros[Lane<BF16, TAIL>::M] = {};
@@ -364,7 +374,7 @@ __global__ __launch_bounds__(kSumWaves * 64) void embed_sum_kernel(EmbedBwd a) {
     p.cnt = max(0, min(kPiece, n - p0));
     if (p0 == 0) p.prev = -1;
     if (p0 + p.cnt >= n) p.next = -1;
-    if (job > 0 && wave == 0 && blockIdx.x % a.slabs == 0 && lane == 0) {
+    if (job > 0 && wave == 0 && slab == 0 && lane == 0) {
         // what goes on from the chunk before, if it starts there
         const int before = (int)(job - 1) * kChunk;
         a.s.spans[job - 1] = p.id == p.prev && a.s.start[p.id] >= before ? make_int2(p.id, (a.s.start[p.id + 1] - 1) / kChunk) : make_int2(-1, 0);
@@ -373,8 +383,8 @@ __global__ __launch_bounds__(kSumWaves * 64) void embed_sum_kernel(EmbedBwd a) {
 }
 
 // A batch of kSmall tokens at most, in one launch: a workgroup has a range of ids, as in the sort, and a slab of the columns.  Its tokens are
-// put in order by counting, for each, those before it, and are one
-// chunk: no row goes on elsewhere.  256 tokens, 1024 rows of 256 fp32: one launch 5.5 us, three 12.3.
+// put in order by counting, for each, those before it, and are one chunk: no row goes on elsewhere.  256 tokens, 1024 rows of 256 fp32: one
+// launch 5.4 us, three 12.3; 256 tokens of one id 11.9, 12.4; 32000 rows of 2048 bf16 22.5, 31.9.
 constexpr int kSmallWaves = 16, kSmall = kSmallWaves * kPiece;
 
 template <int BF16, int TAIL>
@@ -383,8 +393,10 @@ __global__ __launch_bounds__(kSmallWaves * 64) void embed_small_kernel(EmbedBwd 
     __shared__ uint32_t key[kSmall]; // of the range's tokens: id - lo, then token
     __shared__ int toks[kSmall], rows[kSmall], counts[kSmallWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int job = blockIdx.x / a.slabs, lo = job * range, n = min(range, a.V - lo);
-    const Lane<BF16, TAIL> mine(a.d, (int)blockIdx.x - job * a.slabs, lane);
+    const int64_t job = sdp::group_id() / (uint32_t)a.slabs;
+    if (job * range >= a.V) return;
+    const int lo = (int)job * range, n = min(range, a.V - lo);
+    const Lane<BF16, TAIL> mine(a.d, (int)(sdp::group_id() - (uint32_t)job * (uint32_t)a.slabs), lane);
     uint32_t k = 0xFFFFFFFFu;
     if (tid < a.T) {
         const int id = sdp::token_id(ids, wide, tid, a.V);
@@ -432,8 +444,9 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedBwd a) {
     constexpr int M = Lane<BF16, TAIL>::M, B = 4;
     __shared__ float lds[4][M][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int64_t job = blockIdx.x / a.slabs;
-    const Lane<BF16, TAIL> mine(a.d, (int)(blockIdx.x - job * a.slabs), lane);
+    const int64_t job = sdp::group_id() / (uint32_t)a.slabs;
+    if (job >= a.chunks - 1) return;
+    const Lane<BF16, TAIL> mine(a.d, (int)(sdp::group_id() - (uint32_t)job * (uint32_t)a.slabs), lane);
     const int n = a.s.start[a.V];
     const int2 span = a.s.spans[job]; // written by the sums of the next chunk, where that has a token
     if ((job + 1) * kChunk >= n || span.x < 0) return;
@@ -500,7 +513,7 @@ extern "C" int sdp_embed_fwd(int dtype, int id_type, int T, int V, int d, float 
     hipStream_t s = (hipStream_t)stream;
     const EmbedFwd a{E, ids, Y, T, V, d, id_type == SDP_I64, scale};
     sdp::ProfileScope ps("embed_fwd", s);
-    const unsigned groups = (unsigned)(((int64_t)T + 3) / 4);
+    const dim3 groups = sdp::grid_of(((int64_t)T + 3) / 4);
     if (dtype == SDP_BF16) embed_fwd_kernel<1><<<groups, 256, 0, s>>>(a);
     else embed_fwd_kernel<0><<<groups, 256, 0, s>>>(a);
     return sdp::launch_status();
@@ -520,12 +533,16 @@ extern "C" int sdp_embed_bwd(int dtype, int id_type, int T, int V, int d, float 
     if (!dE || (T > 0 && (!dY || !ids))) return SDP_ERR_INVALID_ARG;
     if (!sdp::aligned_to(dE, es) || !sdp::aligned_to(dY, es) || !sdp::aligned_to(ids, is)) return SDP_ERR_INVALID_ARG;
     if (T > 0 && sdp::overlap({{dE, (size_t)V * d * es}}, {{dY, (size_t)T * d * es}, {ids, (size_t)T * is}})) return SDP_ERR_INVALID_ARG;
+    EmbedBwd a{dY, dE, {}, nullptr, T, V, d, chunks_of(T), slabs_of(dtype, d), scale};
+    const int64_t sum = ((int64_t)a.chunks + ((int64_t)V + kSumWaves * kClear - 1) / (kSumWaves * kClear)) * a.slabs;
+    const int64_t join = (int64_t)(a.chunks - 1) * a.slabs;
+    if (sum > UINT32_MAX || (int64_t)kSortGroups * a.slabs > UINT32_MAX) return SDP_ERR_SHAPE; // workgroups; no memory holds such a dE
     const Layout l = layout(T, V, d);
     if (!ws || !sdp::aligned16(ws) || ws_bytes < l.all) return SDP_ERR_WORKSPACE;
     hipStream_t s = (hipStream_t)stream;
     char* w = (char*)ws;
-    EmbedBwd a{dY, dE, {(int32_t*)w, (int32_t*)(w + l.ids), (int32_t*)(w + l.start), (int2*)(w + l.spans)}, (float*)(w + l.part), T, V, d, chunks_of(T),
-               slabs_of(dtype, d), scale};
+    a.s = {(int32_t*)w, (int32_t*)(w + l.ids), (int32_t*)(w + l.start), (int2*)(w + l.spans)};
+    a.part = (float*)(w + l.part);
     sdp::ProfileScope ps("embed_bwd", s);
     const auto by_form = [&](auto&& go) {
         auto of = [&](auto bf16) {
@@ -535,7 +552,7 @@ extern "C" int sdp_embed_bwd(int dtype, int id_type, int T, int V, int d, float 
     };
     if (T <= kSmall) {
         const int range = (V + kSortGroups - 1) / kSortGroups;
-        const unsigned groups = (unsigned)((V + range - 1) / range) * a.slabs;
+        const dim3 groups = sdp::grid_of((int64_t)((V + range - 1) / range) * a.slabs);
         return by_form([&](auto bf16, auto tail) {
             embed_small_kernel<bf16.value, tail.value><<<groups, kSmallWaves * 64, 0, s>>>(a, ids, id_type == SDP_I64, range);
             return sdp::launch_status();
@@ -561,13 +578,11 @@ extern "C" int sdp_embed_bwd(int dtype, int id_type, int T, int V, int d, float 
     };
     if (const int st = id_type == SDP_I64 ? sort_of(std::integral_constant<int, 1>{}) : sort_of(std::integral_constant<int, 0>{}); st != SDP_OK)
         return st;
-    const int64_t sum = ((int64_t)a.chunks + ((int64_t)V + kSumWaves * kClear - 1) / (kSumWaves * kClear)) * a.slabs, join = (int64_t)(a.chunks - 1) * a.slabs;
-    const unsigned gs = (unsigned)sum, gj = (unsigned)join;
     return by_form([&](auto bf16, auto tail) {
-        embed_sum_kernel<bf16.value, tail.value><<<gs, kSumWaves * 64, 0, s>>>(a);
+        embed_sum_kernel<bf16.value, tail.value><<<sdp::grid_of(sum), kSumWaves * 64, 0, s>>>(a);
         const int rc = sdp::launch_status();
         if (rc != SDP_OK || a.chunks < 2) return rc;
-        embed_join_kernel<bf16.value, tail.value><<<gj, 256, 0, s>>>(a);
+        embed_join_kernel<bf16.value, tail.value><<<sdp::grid_of(join), 256, 0, s>>>(a);
         return sdp::launch_status();
     });
 }

@@ -57,7 +57,8 @@ __global__ __launch_bounds__(WAVES * 64) void token_loss_kernel(Loss a) {
     typedef typename Rw::Elem Elem;
     constexpr int N = Rw::N, TH = WAVES * 64, P = PIECES ? PIECES : 1;
     __shared__ float lds[2][WAVES], at_label;
-    const int64_t row = blockIdx.x;
+    const int64_t row = sdp::group_id();
+    if (row >= a.T) return;
     const int tid = threadIdx.x, V = a.V, whole = Rw::whole(V), label = sdp::token_id(a.labels, a.wide, row, V);
     const Elem* z = (const Elem*)a.Z + row * a.ldz;
     Elem* dz = (Elem*)a.dZ + row * a.ldz;
@@ -262,8 +263,8 @@ extern "C" int sdp_token_loss(int dtype, int id_type, int T, int V, int64_t ldz,
         const Loss a{Z, labels, scale_dev, nll, lse, dZ, T, V, id_type == SDP_I64, ldz, scale};
         const bool once = sdp::read_once({eZ}, (size_t)ldz * es);
         by_row(dtype == SDP_BF16, V, [&](auto b, auto waves, auto p) {
-            if (p.value && once) token_loss_kernel<b.value, waves.value, p.value, p.value != 0><<<(unsigned)T, waves.value * 64, 0, s>>>(a);
-            else token_loss_kernel<b.value, waves.value, p.value, 0><<<(unsigned)T, waves.value * 64, 0, s>>>(a);
+            if (p.value && once) token_loss_kernel<b.value, waves.value, p.value, p.value != 0><<<sdp::grid_of(T), waves.value * 64, 0, s>>>(a);
+            else token_loss_kernel<b.value, waves.value, p.value, 0><<<sdp::grid_of(T), waves.value * 64, 0, s>>>(a);
         });
         rc = sdp::launch_status();
     }

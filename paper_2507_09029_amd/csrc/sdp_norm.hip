@@ -81,8 +81,8 @@ __global__ __launch_bounds__(waves_of(WPR) * 64) void norm_fwd_kernel(NormFwd a)
     constexpr int N = Rw::N, ROWS = waves_of(WPR) / WPR, STEP = WPR * 64 * N, ONCE = FORM == FORM_ONCE;
     __shared__ float lds[2][waves_of(WPR)];
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int64_t row = (int64_t)blockIdx.x * ROWS + wave / WPR;
-    if (ROWS > 1 && row >= a.T) return; // no barrier where a workgroup has several rows
+    const int64_t row = (int64_t)sdp::group_id() * ROWS + wave / WPR;
+    if (row >= a.T) return; // whole workgroups, or waves where a row has one: no barrier waits for them
     const int d = a.d, whole = Rw::whole(d), at = (wave % WPR * 64 + lane) * N, et = whole + lane;
     const bool tail = FORM >= FORM_TAIL && wave % WPR == 0 && et < d; // this lane has a value behind the whole pieces
     const int64_t off = row * d;
@@ -415,7 +415,7 @@ extern "C" int sdp_norm_fwd(int kind, int dtype, int T, int d, float eps, const 
     const NormFwd a{X, R, gamma, beta, H, Y, mean, rstd, T, d, layer, eps};
     const bool once = sdp::read_once({eX, eR}, w);
     sdp::ProfileScope ps("norm_fwd", s);
-    const unsigned groups = (unsigned)(((int64_t)T + fwd_rows(sh) - 1) / fwd_rows(sh));
+    const dim3 groups = sdp::grid_of(((int64_t)T + fwd_rows(sh) - 1) / fwd_rows(sh));
     return by_fwd_shape(dtype, sh, [&](auto bf16, auto wpr, auto vpl) {
         auto go = [&](auto form) {
             norm_fwd_kernel<bf16.value, wpr.value, vpl.value, form.value><<<groups, waves_of(wpr.value) * 64, 0, s>>>(a);

@@ -5,7 +5,7 @@
 // instructions of 16 bytes take such addresses, and rows of 1501 bf16 stream at the rate of aligned ones, so there is one form for
 // both.  The values behind the last whole piece, 7 at most, are a lane's each.  A lane without a piece reads the last one again, which costs no
 // traffic, and looks away when it uses it: a load is then one instruction without a condition.  (Where the row's end was looked
-// for as it was loaded, every load of its wave waited for the one before: norm backward of 16384 x 768 bf16 49 us, now 26.)
+// for as it was loaded, every load of its wave waited for the one before: norm backward of 16384 x 768 bf16 49 us, now 22.)
 //
 // Stores are non-temporal: what is written here is far more than a cache holds, or read next by another kernel, and pushes what is being
 // read out of it (embedding of 16384 x 2048 bf16 22.0 -> 17.0 us, its gradient's sums 44 -> 34, norm 50.1 -> 48.8, loss of 8192 x 32000 186 -> 182).
@@ -36,6 +36,14 @@ inline bool read_once(std::initializer_list<Extent> of, size_t row_bytes) {
     }
     return row_bytes % 128 == 0 && all >= (size_t)1 << 27;
 }
+
+// A launch of up to 2^32 - 1 workgroups: one dimension of a grid holds less than 2^32 threads.  Rows of a fixed length, so that no
+// kernel waits for the grid's size (reading it, and dividing in 64 bits, cost 0.1 to 0.4 us a launch).
+constexpr int kGridRow = 20; // 2^20 workgroups of at most 1024 threads
+inline dim3 grid_of(int64_t groups) {
+    return dim3((unsigned)(groups < (1 << kGridRow) ? groups : 1 << kGridRow), (unsigned)((groups - 1) >> kGridRow) + 1);
+}
+__device__ inline uint32_t group_id() { return blockIdx.y << kGridRow | blockIdx.x; } // the grid's last row may have more than are needed
 
 template <int BF16>
 struct Row {

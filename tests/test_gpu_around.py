@@ -257,3 +257,36 @@ def test_offsets_past_32_bits(sdp):
     # below 6 x 1.1e6^0.5 = 6300
     wb = sum(dY[i: i + 50000].double().sum(0) for i in range(0, T, 50000))
     assert ((db.double() - wb).abs() <= 2.0 ** -8 * wb.abs() + 2183 * 2.0 ** -24 * 6300).all()
+
+
+def test_more_workgroups_than_a_row_of_the_grid(sdp):
+    """Beyond 2^20 workgroups a launch has a second dimension: the last rows, and nothing behind them."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    T, d = 5000003, 8
+    X = torch.randn((T, d), generator=g, device="cuda")
+    gamma = torch.ones(d, device="cuda")
+    rows = torch.tensor([0, 4194303, 4194304, T - 1])
+    Y, H, mean, rstd = sdp.norm_fwd("rms", X, gamma, eps=EPS)
+    # relative: eight squares, their sum and mean, the root and two products, fewer than 20 roundings of 2^-24 = 1.2e-6
+    assert torch.allclose(Y[rows.cuda()].cpu().double(), norm_fwd64("rms", X[rows.cuda()].cpu(), None, gamma.cpu(), None, EPS)[0], rtol=1.2e-6, atol=1e-12)
+    V = 20000011
+    ids = torch.arange(T, device="cuda") * 4
+    E = torch.randn((V, d), generator=g, device="cuda")
+    assert torch.equal(sdp.embed_fwd(E, ids), E[ids])
+    dE = sdp.embed_bwd(X, ids, V, out=E)
+    assert torch.equal(dE[ids], X)
+    dE[ids] = 0
+    assert not dE.any()
+    few = ids[-200:]
+    dE = sdp.embed_bwd(X[-200:], few, V, out=E)
+    assert torch.equal(dE[few], X[-200:])
+    dE[few] = 0
+    assert not dE.any()
+    T = 1200007
+    nll, lse, dZ, loss = sdp.token_loss(X[:T], torch.arange(T, device="cuda") % d)
+    rows = torch.tensor([0, 1048575, 1048576, T - 1])
+    wn, _, wz, _ = loss64(X[rows.cuda()].cpu(), rows % d, 1.0)
+    # eight terms of one lane's: exponents 3 roundings of at most 16 (logits within 11), 3 x 16 x 2^-24 x ln 2 = 2e-6, a sum of 7 + 6 roundings 8e-7,
+    # 2^x 1.2e-7; log2 and the label's own value, at most 11, two roundings more: below 1.5e-5, and dZ, at most 1, below 2e-5
+    assert ((nll.cpu()[rows].double() - wn).abs() <= 1.5e-5 * wn.clamp(min=1)).all()
+    assert ((dZ.cpu()[rows].double() - wz).abs() <= 2e-5).all()
