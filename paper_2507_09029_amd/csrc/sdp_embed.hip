@@ -7,12 +7,11 @@
 // row's sum has one order, given by the ids alone.
 //
 // Batches of up to kSmall tokens have a launch of their own (embed_small_kernel).  Otherwise the sort is one launch in which no workgroup
-// waits for another.  Each owns a range of ids and goes through all T ids itself: it counts how many lie below its range (where its
-// part of the order starts) and lists the tokens of its range, counts how often each id of it occurs, and writes the listed tokens
-// to their places.  The ids are few bytes and come from the cache for all workgroups but the first, so that T / 1024 steps a workgroup
-// take less than the launches and the waiting of a sort by digits: 10 us for 16384 ids of 32000 whose frequencies fall as 1 / rank
-// (8 where all are as frequent, 6 with no id in range, 14 with one id alone), 37 for 131072.  Where one workgroup's range holds most of a
-// long batch it has most of the work: 123 us for 131072 ids in which the frequent ones are neighbours.
+// waits for another.  Each owns a share of the ids and goes through all T ids itself: it counts how many belong to workgroups before it
+// (where its part of the order starts) and lists its own, counts how often each id occurs, and writes the listed tokens to their
+// places.  The ids are few bytes and come from the cache for all workgroups but the first, so that T / 1024 steps a workgroup take
+// less than the launches and the waiting of a sort by digits: 10 us for 16384 ids of 32000 whose frequencies fall as 1 / rank (9 where
+// all are as frequent, 7 with none to sort, 16 with one id alone), 40 for 131072 (112 with one id alone: one workgroup places them).
 //
 // A token that occurs often (the most frequent of a text are several percent of it; in a padded batch one may be all) would be
 // one wave's long sum.  The sorted order is therefore cut into chunks of kChunk tokens, of a workgroup each (for 512 columns of bf16): a
@@ -65,7 +64,7 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(EmbedFwd a) {
     if (tail) Rw::put(out + whole + lane, last * a.scale);
 }
 
-constexpr int kSortWaves = 16, kSortGroups = 256, kMaxRange = 960, kAhead = 16;
+constexpr int kSortWaves = 16, kSortShift = 8, kSmallGroups = 256, kMaxRange = 960, kAhead = 16;
 // sorted tokens of a wave, all of whose rows are in flight at once, and of a workgroup
 constexpr int kPiece = 16, kSumWaves = 8, kChunk = kPiece * kSumWaves;
 // Rows that a wave clears if they do not occur: few, since waves that store once or twice and end write memory in its order, and faster
@@ -73,16 +72,31 @@ constexpr int kPiece = 16, kSumWaves = 8, kChunk = kPiece * kSumWaves;
 constexpr int kClear = 2;
 
 struct Sorted {
-    int32_t* order; // [T] tokens, by id, then by place
+    int32_t* order; // [T] tokens, by key of their id, then by place
     int32_t* ids;   // [T] their ids
-    int32_t* start; // [V + 1] where a row's tokens start; start[V] = number of tokens that have an id
+    int32_t* start; // [keys + 1] where the tokens of a key's row start; start[keys] = number of tokens that have an id
     int2* spans;    // [chunks] {row, last chunk} of the row that starts in the chunk and goes on in the next, or {-1, 0}
 };
 
-// Ids per workgroup
-int sort_range(int V) {
-    const int r = (V + kSortGroups - 1) / kSortGroups;
-    return r < kMaxRange ? r : kMaxRange;
+// What a workgroup sorts: `range` ids, one of each (1 << shift) neighbours, since the frequent ids of a vocabulary often are neighbours.  Which of
+// them changes from one to the next, so that rows written one after the other are not all a power of two apart.  The order is that of
+// the keys: ids of workgroup 0, of 1, ...; the last ones may lie beyond V.  Whole gradient, bf16, frequencies as 1 / rank, ids in order of
+// frequency and in any order: 16384 tokens, 32000 x 2048: 42.2 and 42.3 us, with neighbours in one workgroup 49.3 and 41.2; 131072
+// tokens: 184 and 185, 266 and 178.  Without the change 5000 tokens, 50001 x 1600 take 39.8 and 38.1, with it 38.0 and 36.8.
+struct Split {
+    int range, shift;
+    __host__ __device__ int groups() const { return 1 << shift; }
+    __host__ __device__ int keys() const { return range << shift; }
+    __device__ uint32_t place(uint32_t id) const { return id >> shift; }
+    __device__ uint32_t group(uint32_t id) const { return (id ^ place(id)) & (groups() - 1); }
+    __device__ uint32_t id(uint32_t group, uint32_t place) const { return place << shift | ((group ^ place) & (groups() - 1)); }
+    __device__ int key(uint32_t id) const { return (int)(group(id) * range + place(id)); }
+};
+Split split_of(int V) {
+    int shift = kSortShift;
+    const auto range = [&] { return (int)(((int64_t)V + (1 << shift) - 1) >> shift); };
+    while (range() > kMaxRange) ++shift;
+    return {range(), shift};
 }
 constexpr int kBlock = 64 * kAhead; // tokens of a wave that are requested at once
 constexpr size_t kSortLds = 159744; // LDS of the lists and counts: a CU's, less what is declared
@@ -97,41 +111,44 @@ __device__ inline void wave_fence() {
 // ONCE: a wave has kBlock tokens at most, requested before anything else.  `room`: tokens that a wave's list holds, kBlock at least.  A wave whose
 // part of the range is longer counts each list that is full and starts another; it goes through its ids again to place them.
 template <int WIDE, int ONCE>
-__global__ __launch_bounds__(kSortWaves * 64) void embed_sort_kernel(const void* __restrict__ ids, int T, int V, int range, int bits, int room,
+__global__ __launch_bounds__(kSortWaves * 64) void embed_sort_kernel(const void* __restrict__ ids, int T, int V, Split split, int bits, int room,
                                                                      Sorted out) {
     extern __shared__ int lds[];
+    const int range = split.range;
     __shared__ int sums[kSortWaves], below_all[kSortWaves];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const uint64_t lanes_below = (1ull << lane) - 1;
     int* hist = lds + kSortWaves * room; // [kSortWaves][range]: a wave's tokens of each id, then where its next one goes
     int* mine = hist + wave * range;
-    int* list = lds + wave * room;       // the wave's tokens of the range, in order: place among the wave's tokens, id - lo (10 bits)
-    const uint32_t lo = blockIdx.x * range, n = min((uint32_t)range, (uint32_t)V - lo);
+    int* list = lds + wave * room;       // the wave's tokens of the range, in order: place among the wave's tokens, id's place in the range (10 bits)
+    const uint32_t lo = blockIdx.x * range;
     // each wave has an unbroken piece of the tokens, of which a lane takes every 64th
     const int64_t piece = ((int64_t)T + kSortWaves * 64 - 1) / (kSortWaves * 64) * 64;
     const int64_t begin = wave * piece, end = begin + piece < T ? begin + piece : T;
-    uint32_t id[kAhead]; // one outside [0, V) is never below a range nor in one: as an unsigned number it is V or more
+    uint32_t id[kAhead], group[kAhead]; // an id outside [0, V) belongs to a workgroup behind all that there are
     auto request = [&](int64_t b) { // kAhead loads in flight: one after the other, their latency would be most of the time
         if (b >= end) { // a wave without tokens
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) id[i] = 0xFFFFFFFFu;
+            for (int i = 0; i < kAhead; ++i) group[i] = 0xFFFFFFFFu;
             return;
         }
         std::conditional_t<WIDE, uint64_t, uint32_t> v[kAhead];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) v[i] = ((const std::conditional_t<WIDE, uint64_t, uint32_t>*)ids)[min(b + i * 64 + lane, end - 1)];
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) id[i] = b + i * 64 + lane < end && v[i] <= 0xFFFFFFFFu ? (uint32_t)v[i] : 0xFFFFFFFFu;
+        for (int i = 0; i < kAhead; ++i) {
+            id[i] = (uint32_t)v[i];
+            group[i] = b + i * 64 + lane < end && v[i] < (uint32_t)V ? split.group(id[i]) : 0xFFFFFFFFu;
+        }
     };
     int below = 0;
     auto add_to_list = [&](int& m, uint32_t at) { // of what was requested, the wave's tokens from `at` on
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            below += __popcll(__ballot(id[i] < lo));
-            const uint32_t k = id[i] - lo;
-            const uint64_t hits = __ballot(k < n);
+            below += __popcll(__ballot(group[i] < blockIdx.x));
+            const uint64_t hits = __ballot(group[i] == blockIdx.x);
             if (hits == 0) continue;
-            if (k < n) list[m + __popcll(hits & lanes_below)] = (int)((at + i * 64 + lane) << 10 | k);
+            if (group[i] == blockIdx.x) list[m + __popcll(hits & lanes_below)] = (int)((at + i * 64 + lane) << 10 | split.place(id[i]));
             m += __popcll(hits);
         }
         wave_fence(); // read by other lanes of the wave
@@ -154,7 +171,7 @@ __global__ __launch_bounds__(kSortWaves * 64) void embed_sort_kernel(const void*
             if (live) {
                 if (write) {
                     out.order[at] = (int)(begin + (entry >> 10));
-                    out.ids[at] = (int)lo + k;
+                    out.ids[at] = (int)split.id(blockIdx.x, k);
                 }
                 if (rank == 0) mine[k] = at + __popcll(peers);
             }
@@ -181,7 +198,7 @@ __global__ __launch_bounds__(kSortWaves * 64) void embed_sort_kernel(const void*
     __syncthreads();
     // an id per thread (kMaxRange <= threads): its tokens, then exclusive sums over the ids before it
     int total = 0;
-    if (tid < n)
+    if (tid < range)
 #pragma unroll
         for (int w = 0; w < kSortWaves; ++w) total += hist[w * range + tid];
     int before = total;
@@ -195,9 +212,9 @@ __global__ __launch_bounds__(kSortWaves * 64) void embed_sort_kernel(const void*
     int at = before - total;
 #pragma unroll
     for (int w = 0; w < kSortWaves; ++w) at += below_all[w] + (w < wave ? sums[w] : 0);
-    if (tid < n) {
+    if (tid < range) {
         out.start[lo + tid] = at;
-        if (lo + tid == V - 1) out.start[V] = at + total;
+        if (lo + tid == split.keys() - 1) out.start[split.keys()] = at + total;
 #pragma unroll
         for (int w = 0; w < kSortWaves; ++w) {
             const int c = hist[w * range + tid];
@@ -226,6 +243,7 @@ struct EmbedBwd {
     const void* dY;
     void* dE;
     Sorted s;
+    Split split;
     float* part; // [chunks][2][d]: of a row that starts in an earlier chunk, of one that goes on in the next
     int T, V, d, chunks, slabs;
     float scale;
@@ -360,16 +378,20 @@ __global__ __launch_bounds__(kSumWaves * 64) void embed_sum_kernel(EmbedBwd a) {
     const Lane<BF16, TAIL> mine(a.d, slab, lane);
     if (job >= a.chunks) {
         const int64_t first = ((job - a.chunks) * kSumWaves + wave) * kClear;
+        if (first >= a.V) return;
+        int keys[kClear];
+#pragma unroll
+        for (int i = 0; i < kClear; ++i) keys[i] = a.split.key((uint32_t)first + i);
         const float zeros[Lane<BF16, TAIL>::M] = {};
 #pragma unroll
         for (int i = 0; i < kClear; ++i)
-            if (first + i < a.V && a.s.start[first + i] == a.s.start[first + i + 1]) mine.write(a, (int)(first + i), zeros);
+            if (first + i < a.V && a.s.start[keys[i]] == a.s.start[keys[i] + 1]) mine.write(a, (int)first + i, zeros);
         return;
     }
     // requested before it is known how many tokens there are: what lies behind the last one is not used
     const int p0 = (int)job * kChunk + wave * kPiece, at = min(p0 + lane, a.T - 1);
     Piece p{a.s.order[at], a.s.ids[at], 0, a.s.ids[max(min(p0, a.T) - 1, 0)], a.s.ids[min(p0 + kPiece, a.T - 1)]};
-    const int n = a.s.start[a.V];
+    const int n = a.s.start[a.split.keys()];
     if (job * kChunk >= n) return;
     p.cnt = max(0, min(kPiece, n - p0));
     if (p0 == 0) p.prev = -1;
@@ -377,14 +399,15 @@ __global__ __launch_bounds__(kSumWaves * 64) void embed_sum_kernel(EmbedBwd a) {
     if (job > 0 && wave == 0 && slab == 0 && lane == 0) {
         // what goes on from the chunk before, if it starts there
         const int before = (int)(job - 1) * kChunk;
-        a.s.spans[job - 1] = p.id == p.prev && a.s.start[p.id] >= before ? make_int2(p.id, (a.s.start[p.id + 1] - 1) / kChunk) : make_int2(-1, 0);
+        const int key = a.split.key(p.id);
+        a.s.spans[job - 1] = p.id == p.prev && a.s.start[key] >= before ? make_int2(p.id, (a.s.start[key + 1] - 1) / kChunk) : make_int2(-1, 0);
     }
     chunk.sum(a, mine, p, wave, lane, a.part + job * 2 * a.d);
 }
 
-// A batch of kSmall tokens at most, in one launch: a workgroup has a range of ids, as in the sort, and a slab of the columns.  Its tokens are
+// A batch of kSmall tokens at most, in one launch: a workgroup has a range of ids and a slab of the columns.  Its tokens are
 // put in order by counting, for each, those before it, and are one chunk: no row goes on elsewhere.  256 tokens, 1024 rows of 256 fp32: one
-// launch 5.4 us, three 12.3; 256 tokens of one id 11.9, 12.4; 32000 rows of 2048 bf16 22.5, 31.9.
+// launch 6.4 us, three 13.6; 256 tokens of one id 11.9, 12.4; 32000 rows of 2048 bf16 22.5, 31.9.
 constexpr int kSmallWaves = 16, kSmall = kSmallWaves * kPiece;
 
 template <int BF16, int TAIL>
@@ -447,7 +470,7 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedBwd a) {
     const int64_t job = sdp::group_id() / (uint32_t)a.slabs;
     if (job >= a.chunks - 1) return;
     const Lane<BF16, TAIL> mine(a.d, (int)(sdp::group_id() - (uint32_t)job * (uint32_t)a.slabs), lane);
-    const int n = a.s.start[a.V];
+    const int n = a.s.start[a.split.keys()];
     const int2 span = a.s.spans[job]; // written by the sums of the next chunk, where that has a token
     if ((job + 1) * kChunk >= n || span.x < 0) return;
     float acc[M] = {};
@@ -493,7 +516,7 @@ Layout layout(int T, int V, int d) {
     Layout l;
     l.ids = sdp::round_up((size_t)T * 4, 256);
     l.start = 2 * l.ids;
-    l.spans = l.start + sdp::round_up(((size_t)V + 1) * 4, 256);
+    l.spans = l.start + sdp::round_up(((size_t)split_of(V).keys() + 1) * 4, 256);
     l.part = l.spans + sdp::round_up((size_t)chunks_of(T) * sizeof(int2), 256);
     l.all = l.part + sdp::round_up((size_t)chunks_of(T) * 2 * d * sizeof(float), 256);
     return l;
@@ -533,10 +556,10 @@ extern "C" int sdp_embed_bwd(int dtype, int id_type, int T, int V, int d, float 
     if (!dE || (T > 0 && (!dY || !ids))) return SDP_ERR_INVALID_ARG;
     if (!sdp::aligned_to(dE, es) || !sdp::aligned_to(dY, es) || !sdp::aligned_to(ids, is)) return SDP_ERR_INVALID_ARG;
     if (T > 0 && sdp::overlap({{dE, (size_t)V * d * es}}, {{dY, (size_t)T * d * es}, {ids, (size_t)T * is}})) return SDP_ERR_INVALID_ARG;
-    EmbedBwd a{dY, dE, {}, nullptr, T, V, d, chunks_of(T), slabs_of(dtype, d), scale};
+    EmbedBwd a{dY, dE, {}, split_of(V), nullptr, T, V, d, chunks_of(T), slabs_of(dtype, d), scale};
     const int64_t sum = ((int64_t)a.chunks + ((int64_t)V + kSumWaves * kClear - 1) / (kSumWaves * kClear)) * a.slabs;
     const int64_t join = (int64_t)(a.chunks - 1) * a.slabs;
-    if (sum > UINT32_MAX || (int64_t)kSortGroups * a.slabs > UINT32_MAX) return SDP_ERR_SHAPE; // workgroups; no memory holds such a dE
+    if (sum > UINT32_MAX || (int64_t)kSmallGroups * a.slabs > UINT32_MAX) return SDP_ERR_SHAPE; // workgroups; no memory holds such a dE
     const Layout l = layout(T, V, d);
     if (!ws || !sdp::aligned16(ws) || ws_bytes < l.all) return SDP_ERR_WORKSPACE;
     hipStream_t s = (hipStream_t)stream;
@@ -551,17 +574,16 @@ extern "C" int sdp_embed_bwd(int dtype, int id_type, int T, int V, int d, float 
         return dtype == SDP_BF16 ? of(std::integral_constant<int, 1>{}) : of(std::integral_constant<int, 0>{});
     };
     if (T <= kSmall) {
-        const int range = (V + kSortGroups - 1) / kSortGroups;
+        const int range = (V + kSmallGroups - 1) / kSmallGroups;
         const dim3 groups = sdp::grid_of((int64_t)((V + range - 1) / range) * a.slabs);
         return by_form([&](auto bf16, auto tail) {
             embed_small_kernel<bf16.value, tail.value><<<groups, kSmallWaves * 64, 0, s>>>(a, ids, id_type == SDP_I64, range);
             return sdp::launch_status();
         });
     }
-    const int range = sort_range(V);
+    const int range = a.split.range;
     int bits = 0;
     while ((1 << bits) < range) ++bits;
-    const dim3 groups((V + range - 1) / range);
     // one block's list for the shorter batches, so that two workgroups share a CU; else all that the counts leave
     const int room = T <= kSortWaves * kBlock ? kBlock : (int)(kSortLds / (kSortWaves * sizeof(int))) - range;
     const size_t lds = (size_t)kSortWaves * (room + range) * sizeof(int);
@@ -570,7 +592,7 @@ extern "C" int sdp_embed_bwd(int dtype, int id_type, int T, int V, int d, float 
         static const hipError_t attr =
             hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kSortLds);
         if (attr != hipSuccess) return sdp::hip_status(attr);
-        kern<<<groups, kSortWaves * 64, lds, s>>>(ids, T, V, range, bits, room, a.s);
+        kern<<<a.split.groups(), kSortWaves * 64, lds, s>>>(ids, T, V, a.split, bits, room, a.s);
         return sdp::launch_status();
     };
     auto sort_of = [&](auto wide) {
