@@ -6,7 +6,9 @@
 //             dgamma = sum_t dy xh, dbeta = sum_t dy
 //
 // Both are bound by memory: a row is read once into registers, its sums are taken over the lanes that hold it, and it is written
-// once.  A row belongs to WPR waves, each lane holding up to VPL pieces of 16 bytes.
+// once.  A row belongs to WPR waves, each lane holding up to VPL pieces of 16 bytes (fwd_shape, bwd_shape).  16384 x 2048 bf16 with the
+// skip connection, four matrices of 67 MB: forward 47.5 us, 5.7 TB/s; backward 49.4, 5.4, of which the sums of the weight's gradients
+// are 4.8.  Small batches are bound by the launch: 256 x 256 fp32 forward 4.4 us, most of it the call's.
 #include <cmath>
 #include <type_traits>
 
@@ -35,9 +37,11 @@ struct NormBwd {
     int want_dw;
 };
 
-// waves of a workgroup: four rows of one wave each, or one row of four or sixteen
+// waves of a workgroup in the forward pass: four rows of one wave each, or one row of four or sixteen
 constexpr int waves_of(int WPR) { return WPR > 4 ? WPR : 4; }
 
+// and in the backward pass.  us, eight / four / sixteen: 16384 x 2048 bf16 50.9 / 61.7 / 50.4, 1024 x 2048 10.9 / 11.8 / 11.4, 8192 x 2000
+// 27.4 / 33.6 / 28.3, fp32 8192 x 2048 47.6 / 47.4 / 50.1; but bf16 4096 x 3200 25.7 / 25.6 / 22.6.
 constexpr int kBwdWaves = 8;
 constexpr int bwd_waves(int WPR) { return WPR > kBwdWaves ? WPR : WPR == 3 ? 9 : kBwdWaves; }
 
@@ -162,12 +166,17 @@ struct Held {
 // the end the shares of the workgroup's rows are added up, in the order of its waves, and written as one row of `partial`.  The next row is
 // requested before the one at hand is worked on, by the same number of loads whatever the row: with loads behind a condition the
 // wait for the row at hand would be one for the next as well.
+//
+// ROOM: registers are enough for that, and to keep what the sums are made of for the second use.  With more than 8 values of a matrix a lane
+// they are not, and spill: rows of more than 8192, us, each row requested as it is needed and values made again / otherwise: 2048 x 16384
+// fp32 118 / 248, bf16 74 / 133.  Where there is room, 16384 x 2048 bf16: values kept 51, made again 60.
 template <int BF16, int WPR, int VPL, int FORM, int SKIP>
 __global__ __launch_bounds__(bwd_waves(WPR) * 64) void norm_bwd_kernel(NormBwd a) {
     typedef Row<BF16> Rw;
     typedef typename Rw::Elem Elem;
     typedef Held<BF16, VPL> Row1;
     constexpr int N = Rw::N, WAVES = bwd_waves(WPR), ROWS = WAVES / WPR, STEP = WPR * 64 * N;
+    constexpr bool ROOM = VPL * N <= 8;
     __shared__ float2 lds[2][WAVES]; // the two sums of a row, and the next row's
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int d = a.d, whole = Rw::whole(d), at = (wave % WPR * 64 + lane) * N, et = whole + lane;
@@ -203,7 +212,7 @@ __global__ __launch_bounds__(bwd_waves(WPR) * 64) void norm_bwd_kernel(NormBwd a
     };
     // the row in `now`, while the one after it is on its way to `next`
     auto take = [&](Row1& now, Row1& next, float2* sums) {
-        request(row + step, next);
+        if (ROOM) request(row + step, next);
         const bool live = row < a.T;
         const int held = live ? whole : 0;
         const float mu = a.mean ? now.mu : 0.f, rstd = now.rstd;
@@ -236,13 +245,12 @@ __global__ __launch_bounds__(bwd_waves(WPR) * 64) void norm_bwd_kernel(NormBwd a
         sdp::settle(dga), sdp::settle(dbe);
         row_sums<WPR>(s1, s2, sums);
         s1 /= width, s2 = a.mean ? s2 / width : 0.f;
-        // xh and g: kept where registers are enough for it, else made again
-        constexpr bool KEPT = VPL * N <= 8;
-        if (!KEPT) sdp::again(now.h), sdp::again(now.dy), sdp::again(ga);
+        // xh and g: kept, or made again
+        if (!ROOM) sdp::again(now.h), sdp::again(now.dy), sdp::again(ga);
 #pragma unroll
         for (int i = 0; i < VPL; ++i) {
             float dx[N], skip[N] = {};
-            if (!KEPT) centre(i, dx);
+            if (!ROOM) centre(i, dx);
             if constexpr (SKIP) Rw::unpack(now.skip[i], skip);
 #pragma unroll
             for (int k = 0; k < N; ++k) {
@@ -255,12 +263,16 @@ __global__ __launch_bounds__(bwd_waves(WPR) * 64) void norm_bwd_kernel(NormBwd a
         row += step;
     };
     Row1 one, two;
-    request(row, one);
+    if (ROOM) request(row, one);
     // all waves of a workgroup take the same number of turns: their sums of a row go through a barrier.  Two rows a round: handed over from
     // `next` to `now`, a row would have to have arrived.
     for (int64_t first = (int64_t)blockIdx.x * ROWS; first < a.T; first += 2 * step) {
+        if (!ROOM) request(row, one);
         take(one, two, lds[0]);
-        if (first + step < a.T) take(two, one, lds[1]);
+        if (first + step < a.T) {
+            if (!ROOM) request(row, two);
+            take(two, one, lds[1]);
+        }
     }
     if (!a.want_dw) return;
     // one workgroup alone has the sums
@@ -318,16 +330,21 @@ __global__ __launch_bounds__(1024) void norm_dw_kernel(const float* __restrict__
     Row<BF16>::put((Elem*)(part ? dbeta : dgamma) + e, s);
 }
 
-// waves of a row and pieces of a lane
+// Waves of a row and pieces of a lane.
 struct Shape {
     int wpr, vpl;
 };
+// One wave where it can hold the row: its sums need no barrier.  us, one wave / four: 16384 x 768 bf16 16.5 / 22.6, 8192 x 1024 11.3 / 15.5,
+// 16384 x 2048 47.8 / 49.5, though 8192 x 2000 23.0 / 22.3.  Else four, if they can: four / sixteen: 8192 x 4096 46.6 / 60.6, 4096 x 3200 17.0 / 24.7.
 Shape fwd_shape(int dtype, int d) {
     const int n = dtype == SDP_BF16 ? 8 : 4, pieces = (d + n - 1) / n;
     if (pieces <= 256) return {1, (pieces + 63) / 64};
     if (pieces <= 1024) return {4, pieces <= 512 ? 2 : 4};
     return {16, pieces <= 2048 ? 2 : 4};
 }
+// A row of whole waves' pieces, one a lane in bf16 and two in fp32, eight values of each matrix either way: more waves leave lanes idle, fewer
+// take more registers.  us, bf16, one piece / two: 16384 x 2048 51.2 / 55.8, 16384 x 1200 34.7 / 38.0; but 16384 x 768
+// 21.7 / 20.8, 4096 x 3200 25.9 / 23.7.
 Shape bwd_shape(int dtype, int d) {
     const int n = dtype == SDP_BF16 ? 8 : 4, pieces = (d + n - 1) / n, most = dtype == SDP_BF16 ? 1 : 2;
     if (pieces <= 64 * most) return {1, (pieces + 63) / 64};
@@ -338,8 +355,9 @@ Shape bwd_shape(int dtype, int d) {
 int fwd_rows(const Shape& s) { return s.wpr == 1 ? 4 : 1; }
 int bwd_rows(const Shape& s) { return bwd_waves(s.wpr) / s.wpr; }
 
-// Workgroups of the backward pass: one on every CU; where that one would have so few turns that they take less than a second launch, one alone,
-// which also writes the sums.
+// Workgroups of the backward pass: one on every CU; with two, twice the shares are written and added up: 16384 x 2048 bf16 51.2 and 55.1 us,
+// 8192 x 8192 99.8 and 112.9.  Where one alone has kBwdAlone turns at most they take less than a second launch, and it writes the sums itself:
+// 16 x 768 one launch 5.8 us, two 7.7.
 constexpr int kBwdGroups = 256, kBwdAlone = 4;
 int bwd_groups(int T, const Shape& s) {
     const int64_t all = ((int64_t)T + bwd_rows(s) - 1) / bwd_rows(s);
