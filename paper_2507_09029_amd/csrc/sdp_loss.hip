@@ -3,9 +3,10 @@
 //   lse = log sum_j exp z_j,  nll = lse - z_label,  dz_j = c (exp(z_j - lse) - [j = label])
 //
 // Bound by memory: the logits are the largest tensor of a training step (8192 x 32000 bf16: 524 MB), and the least that can be
-// moved is one read and one write of them.  A workgroup holds a row in registers, as it is stored, from the read to the write: 16 pieces of
-// 16 bytes a lane at most, so that a row of 32000 bf16 takes four waves and several rows are at work on a CU.  Rows of more
-// than 131072 bf16 or 65536 fp32 values are read twice.
+// moved is one read and one write of them.  A workgroup holds a row in registers, as it is stored, from the read to the write: up to 16
+// waves with up to 16 pieces of 16 bytes a lane, as many as leave room for several rows on a CU (by_row).  Rows of more than 131072
+// bf16 or 65536 fp32 values are read twice.  8192 x 32000 bf16: 177 us with the scale and the sum of the loss, 5.9 TB/s, more than a
+// large copy reaches; 1000 x 50001, a quarter without a label: 42 us, 4.1 TB/s, with three rows to read a CU.
 //
 // exp(z - max) is 2^((z - max) L), L = log2 e, on the hardware's 2^x.  The difference comes first: z L - max L in one step, with max L
 // rounded, overflows or is far off where a row's values are near the type's lowest, as masks write them.

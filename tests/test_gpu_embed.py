@@ -131,3 +131,18 @@ def test_a_long_batch(sdp):
     dY = torch.ones((T, d), dtype=torch.float32)
     got = sdp.embed_bwd(dY.cuda(), ids.cuda(), V).cpu()
     assert (got[9] == 300).all() and (got[4] == T - 300).all() and got.abs().sum() == T * d
+
+
+@pytest.mark.parametrize("T,V", [(1000, 50001), (60000, 50001), (60000, 700000)])
+def test_ids_of_one_workgroup(sdp, T, V):
+    """All tokens belong to the share of ids that one workgroup of the sort has, whatever it is: ids that agree in what deals them out, and, for any
+    other deal, neighbours and ids a power of two apart.  dY is small integers: every sum is exact (below 60000 x 8 < 2^24)."""
+    g = torch.Generator().manual_seed(T)
+    v = torch.arange(V)
+    dY = torch.randint(-8, 9, (T, 24), generator=g).float()
+    for of in ((v ^ (v >> 8)) % 256 == 5, (v ^ (v >> 10)) % 1024 == 5, v % 1024 == 7, (v >= 1000) & (v < 1200)):
+        share = v[of]
+        ids = share[torch.randint(0, len(share), (T,), generator=g)]
+        want = torch.zeros((V, 24)).index_add_(0, ids, dY)
+        got = sdp.embed_bwd(dY.cuda(), ids.int().cuda(), V)
+        assert torch.equal(got.cpu(), want)

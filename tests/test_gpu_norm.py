@@ -70,6 +70,14 @@ def test_norm_matches_64_bits(sdp, dtype, T, d):
     _run(sdp, "rms", dtype, T, d, True, True, 0)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,d", [(700, 9001), (1100, 12296)])
+def test_many_wide_rows(sdp, dtype, T, d):
+    """Several turns of every workgroup at widths whose rows are not requested ahead."""
+    _run(sdp, "layer", dtype, T, d, True, True, 0)
+    _run(sdp, "rms", dtype, T, d, False, False, 1)
+
+
 def test_norm_of_one_value_and_of_constant_rows(sdp):
     """Width 1 and rows of one value: the layer form gives beta (variance 0, s = 1 / sqrt(eps)) and no gradient by x, exactly."""
     for dtype in ("f32", "bf16"):
