@@ -412,7 +412,7 @@ int sdp_norm_bwd(int kind, int dtype, int T, int d, const void* H, const void* d
  * occur are zeros.  Tokens are sorted by id (stably, so each row's fp32 sum has one order, whatever the
  * launch); a row is rounded once.  What goes into sdp_coverage_grad_avg and the fused update like any other gradient.
  *   dY [T][d], ids [T] in;  dE [V][d] out;  ws: sdp_embed_bwd_workspace_bytes(dtype, T, V, d), 16-byte aligned.
- * Errors: as above, WORKSPACE.
+ * Errors: as above, WORKSPACE; SHAPE also where V and d together are beyond any memory (2^32 pieces of work).
  * ------------------------------------------------------------------------------------------- */
 int sdp_embed_fwd(int dtype, int id_type, int T, int V, int d, float scale, const void* E, const void* ids, void* Y,
                   void* stream);

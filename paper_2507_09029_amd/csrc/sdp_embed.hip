@@ -554,12 +554,12 @@ extern "C" int sdp_embed_bwd(int dtype, int id_type, int T, int V, int d, float 
     if (!std::isfinite(scale)) return SDP_ERR_INVALID_ARG;
     const size_t es = dtype == SDP_BF16 ? 2 : 4, is = id_type == SDP_I64 ? 8 : 4;
     if (!dE || (T > 0 && (!dY || !ids))) return SDP_ERR_INVALID_ARG;
-    if (!sdp::aligned_to(dE, es) || !sdp::aligned_to(dY, es) || !sdp::aligned_to(ids, is)) return SDP_ERR_INVALID_ARG;
-    if (T > 0 && sdp::overlap({{dE, (size_t)V * d * es}}, {{dY, (size_t)T * d * es}, {ids, (size_t)T * is}})) return SDP_ERR_INVALID_ARG;
     EmbedBwd a{dY, dE, {}, split_of(V), nullptr, T, V, d, chunks_of(T), slabs_of(dtype, d), scale};
     const int64_t sum = ((int64_t)a.chunks + ((int64_t)V + kSumWaves * kClear - 1) / (kSumWaves * kClear)) * a.slabs;
     const int64_t join = (int64_t)(a.chunks - 1) * a.slabs;
-    if (sum > UINT32_MAX || (int64_t)kSmallGroups * a.slabs > UINT32_MAX) return SDP_ERR_SHAPE; // workgroups; no memory holds such a dE
+    if (sum > UINT32_MAX) return SDP_ERR_SHAPE; // workgroups; no memory holds such a dE
+    if (!sdp::aligned_to(dE, es) || !sdp::aligned_to(dY, es) || !sdp::aligned_to(ids, is)) return SDP_ERR_INVALID_ARG;
+    if (T > 0 && sdp::overlap({{dE, (size_t)V * d * es}}, {{dY, (size_t)T * d * es}, {ids, (size_t)T * is}})) return SDP_ERR_INVALID_ARG;
     const Layout l = layout(T, V, d);
     if (!ws || !sdp::aligned16(ws) || ws_bytes < l.all) return SDP_ERR_WORKSPACE;
     hipStream_t s = (hipStream_t)stream;

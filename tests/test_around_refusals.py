@@ -69,6 +69,7 @@ def test_embedding(L):
                 dict(dE=at(0)), dict(dE=at(1)), dict(dtype=0, dY=ctypes.c_void_p(0x1002))):
         assert f(**bad) == INVALID, bad
     assert f(T=(1 << 30) + 1) == SHAPE and f(ws=None) == WORKSPACE and f(ws_bytes=64) == WORKSPACE
+    assert f(V=1 << 30, d=1 << 30) == SHAPE and f(T=1000, V=1 << 30, d=1 << 20) == SHAPE
     w = L.sdp_embed_bwd_workspace_bytes
     assert w(1, 4, 0, 16) == 0 and w(2, 4, 10, 16) == 0 and w(1, -1, 10, 16) == 0
     assert w(1, 0, 10, 16) >= 11 * 4 and w(1, 1000, 10, 16) >= 2 * 4000
