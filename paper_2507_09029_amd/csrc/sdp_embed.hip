@@ -64,7 +64,7 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(EmbedFwd a) {
     if (tail) Rw::put(out + whole + lane, last * a.scale);
 }
 
-constexpr int kSortWaves = 16, kSortShift = 8, kSmallGroups = 256, kMaxRange = 960, kAhead = 16;
+constexpr int kSortWaves = 16, kSortShift = 8, kMaxRange = 960, kAhead = 16;
 // sorted tokens of a wave, all of whose rows are in flight at once, and of a workgroup
 constexpr int kPiece = 16, kSumWaves = 8, kChunk = kPiece * kSumWaves;
 // Rows that a wave clears if they do not occur: few, since waves that store once or twice and end write memory in its order, and faster
@@ -98,6 +98,7 @@ Split split_of(int V) {
     while (range() > kMaxRange) ++shift;
     return {range(), shift};
 }
+Split small_split_of(int V) { return {(int)(((int64_t)V + (1 << kSortShift) - 1) >> kSortShift), kSortShift}; } // of any range
 constexpr int kBlock = 64 * kAhead; // tokens of a wave that are requested at once
 constexpr size_t kSortLds = 159744; // LDS of the lists and counts: a CU's, less what is declared
 
@@ -300,8 +301,10 @@ struct Chunk {
     float heads[WAVES][M][64];
     int head_of[WAVES]; // 0: the wave starts with a row of its own; 1: its first row started earlier, 2: and goes on
 
-    // part: where sums go of rows that do not start ([0]) or end ([1]) in the chunk; not looked at where there are none
-    __device__ void sum(const EmbedBwd& a, const Lane<BF16, TAIL>& mine, const Piece& p, int wave, int lane, float* part) {
+    // goes_on(sum): of a row that starts here and does not end here; came(sum, ends): of the one that started in an earlier chunk.  One wave at
+    // most calls each.
+    template <class On, class Came>
+    __device__ void sum(const EmbedBwd& a, const Lane<BF16, TAIL>& mine, const Piece& p, int wave, int lane, On&& goes_on, Came&& came) {
         typedef Row<BF16> Rw;
         typedef typename Rw::Elem Elem;
         float acc[M] = {};
@@ -349,22 +352,23 @@ struct Chunk {
         __syncthreads();
         // adds what the waves from `from` on have of a row that goes on in them; whether it ends there
         auto follow = [&](float (&s)[M], int from) {
-            for (int u = from; u < WAVES; ++u) {
+            const uint64_t ends = __ballot(lane >= from && lane < WAVES && head_of[lane % WAVES] != 2);
+            const int last = ends ? __builtin_ctzll(ends) : WAVES - 1;
+#pragma unroll 2
+            for (int u = from; u <= last; ++u)
 #pragma unroll
                 for (int k = 0; k < M; ++k) s[k] += heads[u][k][lane];
-                if (__builtin_amdgcn_readfirstlane(head_of[u]) != 2) return true;
-            }
-            return false;
+            return ends != 0;
         };
         if (tail >= 0) {
             if (follow(acc, wave + 1)) mine.write(a, tail, acc);
-            else mine.write_part(part + a.d, acc);
+            else goes_on(acc);
         }
         if (wave == 0 && head) {
 #pragma unroll
             for (int k = 0; k < M; ++k) acc[k] = heads[0][k][lane];
-            if (head == 2) follow(acc, 1);
-            mine.write_part(part, acc);
+            const bool ends = head == 1 || follow(acc, 1);
+            came(acc, ends);
         }
     }
 };
@@ -402,62 +406,111 @@ __global__ __launch_bounds__(kSumWaves * 64) void embed_sum_kernel(EmbedBwd a) {
         const int key = a.split.key(p.id);
         a.s.spans[job - 1] = p.id == p.prev && a.s.start[key] >= before ? make_int2(p.id, (a.s.start[key + 1] - 1) / kChunk) : make_int2(-1, 0);
     }
-    chunk.sum(a, mine, p, wave, lane, a.part + job * 2 * a.d);
+    float* part = a.part + job * 2 * a.d;
+    chunk.sum(a, mine, p, wave, lane, [&](const auto& s) { mine.write_part(part + a.d, s); }, [&](const auto& s, bool) { mine.write_part(part, s); });
 }
 
-// A batch of kSmall tokens at most, in one launch: a workgroup has a range of ids and a slab of the columns.  Its tokens are
-// put in order by counting, for each, those before it, and are one chunk: no row goes on elsewhere.  256 tokens, 1024 rows of 256 fp32: one
-// launch 6.4 us, three 13.6; 256 tokens of one id 11.9, 12.4; 32000 rows of 2048 bf16 22.5, 31.9.
-constexpr int kSmallWaves = 16, kSmall = kSmallWaves * kPiece;
+// A batch of kSmall tokens at most, in one launch: a workgroup has a share of the ids, dealt out as in the sort, and a slab of the columns.  Its
+// tokens are put in order and summed a chunk at a time; a row that goes over a chunk's end is carried in LDS.  The order comes from counting,
+// for each token, those before it; where that is many, which a few ids' tokens are, from splitting by each bit in which places differ.
+// One launch / three, us, bf16, frequencies as 1 / rank: 512 tokens, 1024 rows of 256 7.2 / 15.1; 1000 tokens of these 8.4 / 16.4; 1024 tokens, 32000 x 768
+// 14.8 / 18.8, x 2048 24.7 / 30.6.  All tokens of one id are one workgroup's: 512 tokens 16.6 / 14.3, 1000 29.1 / 15.7.
+constexpr int kSmallWaves = 16, kSmall = kSmallWaves * 64, kSmallChunk = kSmallWaves * kPiece, kCounted = 256;
 
 template <int BF16, int TAIL>
-__global__ __launch_bounds__(kSmallWaves * 64) void embed_small_kernel(EmbedBwd a, const void* ids, int wide, int range) {
+__global__ __launch_bounds__(kSmallWaves * 64) void embed_small_kernel(EmbedBwd a, const void* ids, int wide, Split split) {
+    constexpr int M = Lane<BF16, TAIL>::M;
     __shared__ Chunk<BF16, TAIL, kSmallWaves> chunk;
-    __shared__ uint32_t key[kSmall]; // of the range's tokens: id - lo, then token
-    __shared__ int toks[kSmall], rows[kSmall], counts[kSmallWaves];
+    __shared__ __align__(16) uint32_t key[kSmall]; // of the share's tokens: place of the id, then token; behind the last one the largest
+    __shared__ uint32_t sorted[kSmall];
+    __shared__ int present[kSmall];
+    __shared__ int counts[2][kSmallWaves];
+    __shared__ float carry[2][M][64]; // from one chunk to the next: a chunk may read one and write one
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int64_t job = sdp::group_id() / (uint32_t)a.slabs;
-    if (job * range >= a.V) return;
-    const int lo = (int)job * range, n = min(range, a.V - lo);
-    const Lane<BF16, TAIL> mine(a.d, (int)(sdp::group_id() - (uint32_t)job * (uint32_t)a.slabs), lane);
-    uint32_t k = 0xFFFFFFFFu;
-    if (tid < a.T) {
-        const int id = sdp::token_id(ids, wide, tid, a.V);
-        if (id >= lo && id - lo < n) k = (uint32_t)(id - lo) << 8 | tid;
-    }
-    const uint64_t hits = __ballot(k != 0xFFFFFFFFu);
-    if (lane == 0) counts[wave] = __popcll(hits);
-    __syncthreads();
-    int m = 0, before = 0;
+    const uint32_t job = sdp::group_id() / (uint32_t)a.slabs;
+    if (job >= (uint32_t)split.groups()) return;
+    const Lane<BF16, TAIL> mine(a.d, (int)(sdp::group_id() - job * (uint32_t)a.slabs), lane);
+    // where a wave's lanes with `bit` go among those of all waves; `all`: how many there are
+    auto among = [&](bool bit, int turn, int& all) {
+        const uint64_t set = __ballot(bit);
+        if (lane == 0) counts[turn][wave] = __popcll(set);
+        __syncthreads();
+        int before = 0;
+        all = 0;
 #pragma unroll
-    for (int w = 0; w < kSmall / 64; ++w) before += w < wave ? counts[w] : 0, m += counts[w];
-    if (k != 0xFFFFFFFFu) key[before + __popcll(hits & ((1ull << lane) - 1))] = k;
+        for (int w = 0; w < kSmallWaves; ++w) before += w < wave ? counts[turn][w] : 0, all += counts[turn][w];
+        return before + __popcll(set & ((1ull << lane) - 1));
+    };
+    const int id = tid < a.T ? sdp::token_id(ids, wide, tid, a.V) : -1;
+    const bool held = id >= 0 && split.group(id) == job;
+    int m;
+    const int at = among(held, 0, m);
+    if (held) key[at] = split.place(id) << 10 | tid;
+    if (tid < (-m & 3)) key[m + tid] = 0xFFFFFFFFu;
     __syncthreads();
-    if (tid < m) {
-        const uint32_t own = key[tid];
-        int rank = 0;
+    if (m <= kCounted) {
+        if (tid < m) {
+            const uint32_t own = key[tid];
+            int rank = 0;
 #pragma unroll 4
-        for (int j = 0; j < m; ++j) rank += key[j] < own;
-        toks[rank] = own & 255, rows[rank] = lo + (int)(own >> 8);
+            for (int j = 0; j < m; j += 4) {
+                const u32x4 k = *(const u32x4*)(key + j);
+                rank += (k[0] < own) + (k[1] < own) + (k[2] < own) + (k[3] < own);
+            }
+            sorted[rank] = own;
+        }
+    } else {
+        uint32_t own = tid < m ? key[tid] : 0, differ = tid < m ? own ^ key[0] : 0;
+#pragma unroll
+        for (int s = 1; s < 64; s <<= 1) differ |= __shfl_xor(differ, s, 64);
+        if (lane == 0) counts[1][wave] = (int)differ;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kSmallWaves; ++w) differ |= (uint32_t)counts[1][w];
+        int turn = 0; // counts[0] was read before a barrier, counts[1] is free once a bit was split by
+        for (int b = 10; b < 32; ++b) {
+            if (!(__builtin_amdgcn_readfirstlane(differ) >> b & 1)) continue;
+            const bool low = tid < m && !(own >> b & 1);
+            int lows;
+            const int l = among(low, turn, lows);
+            if (tid < m) key[low ? l : lows + tid - l] = own;
+            __syncthreads();
+            own = tid < m ? key[tid] : 0;
+            turn ^= 1;
+        }
+        if (tid < m) sorted[tid] = own;
     }
     __syncthreads();
-    // rows that do not occur: a wave's own, against the rows that do
-    {
-        int held[kSmall / 64];
-#pragma unroll
-        for (int i = 0; i < kSmall / 64; ++i) held[i] = i * 64 + lane < m ? rows[i * 64 + lane] : -1;
-        const float zeros[Lane<BF16, TAIL>::M] = {};
-        for (int v = lo + wave; v < lo + n; v += kSmallWaves) {
-            bool occurs = false;
-#pragma unroll
-            for (int i = 0; i < kSmall / 64; ++i) occurs |= held[i] == v;
-            if (__ballot(occurs) == 0) mine.write(a, v, zeros);
-        }
+    auto row_of = [&](int i) { return (int)split.id(job, sorted[i] >> 10); };
+    // Rows that do not occur, of an unbroken range of split.range of them: memory is faster written in its order (256 tokens, 32000 x 2048 bf16
+    // 24.2 us, 25.6 where a workgroup clears rows of its share).  `present`: the tokens whose ids lie there.
+    const int lo = (int)job * split.range;
+    int n;
+    const bool in = id >= lo && id - lo < split.range;
+    const int place = among(in, 1, n);
+    if (in) present[place] = id - lo;
+    __syncthreads();
+    const float zeros[M] = {};
+    for (int v = wave; v < min(split.range, a.V - lo); v += kSmallWaves) {
+        bool occurs = false;
+        for (int i = lane; i < n; i += 64) occurs |= present[i] == v;
+        if (__ballot(occurs) == 0) mine.write(a, lo + v, zeros);
     }
-    if (m == 0) return;
-    const int p0 = wave * kPiece, cnt = max(0, min(kPiece, m - p0));
-    const Piece p{toks[min(p0 + lane, m - 1)], rows[min(p0 + lane, m - 1)], cnt, p0 > 0 && cnt ? rows[p0 - 1] : -1, p0 + cnt < m ? rows[p0 + cnt] : -1};
-    chunk.sum(a, mine, p, wave, lane, nullptr);
+    for (int c0 = 0; c0 < m; c0 += kSmallChunk) {
+        const int p0 = c0 + wave * kPiece, cnt = max(0, min(kPiece, m - p0)), i = min(p0 + lane, m - 1), turn = c0 / kSmallChunk & 1;
+        const Piece p{(int)(sorted[i] & 1023), row_of(i), cnt, p0 > 0 && cnt ? row_of(p0 - 1) : -1, p0 + cnt < m ? row_of(p0 + cnt) : -1};
+        auto put = [&](const float (&s)[M]) {
+#pragma unroll
+            for (int k = 0; k < M; ++k) carry[turn ^ 1][k][lane] = s[k];
+        };
+        chunk.sum(a, mine, p, wave, lane, put, [&](float (&s)[M], bool ends) {
+#pragma unroll
+            for (int k = 0; k < M; ++k) s[k] += carry[turn][k][lane];
+            if (ends) mine.write(a, row_of(c0), s);
+            else put(s);
+        });
+        if (c0 + kSmallChunk < m) __syncthreads(); // before the next chunk's sums take the place of this one's
+    }
 }
 
 // A workgroup looks at a chunk and a slab: if a row starts there and goes on, it adds up the row's partial sums.  Each wave adds every
@@ -574,10 +627,10 @@ extern "C" int sdp_embed_bwd(int dtype, int id_type, int T, int V, int d, float 
         return dtype == SDP_BF16 ? of(std::integral_constant<int, 1>{}) : of(std::integral_constant<int, 0>{});
     };
     if (T <= kSmall) {
-        const int range = (V + kSmallGroups - 1) / kSmallGroups;
-        const dim3 groups = sdp::grid_of((int64_t)((V + range - 1) / range) * a.slabs);
+        const Split share = small_split_of(V);
+        const dim3 groups = sdp::grid_of((int64_t)share.groups() * a.slabs);
         return by_form([&](auto bf16, auto tail) {
-            embed_small_kernel<bf16.value, tail.value><<<groups, kSmallWaves * 64, 0, s>>>(a, ids, id_type == SDP_I64, range);
+            embed_small_kernel<bf16.value, tail.value><<<groups, kSmallWaves * 64, 0, s>>>(a, ids, id_type == SDP_I64, share);
             return sdp::launch_status();
         });
     }

@@ -146,3 +146,21 @@ def test_ids_of_one_workgroup(sdp, T, V):
         want = torch.zeros((V, 24)).index_add_(0, ids, dY)
         got = sdp.embed_bwd(dY.cuda(), ids.int().cuda(), V)
         assert torch.equal(got.cpu(), want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [255, 256, 257, 271, 511, 512, 513, 767, 769, 1000, 1023, 1024, 1025, 1300])
+def test_rows_that_go_over_chunks(sdp, T, dtype):
+    """Few ids, so that a row's tokens reach over one, several and all chunks, begin and end at their borders and share them with others.  dY is 0
+    and 1 with few enough ones that every sum is exact in both types (at most 256)."""
+    g = torch.Generator().manual_seed(T)
+    for V, d in ((5, 72), (3000, 67)):
+        place = torch.arange(T)
+        for ids in (torch.full((T,), 3), place // 256 % V, (place >= 250).long() * 2, (place * 7 // T) % V, torch.randint(0, 3, (T,), generator=g),
+                    torch.where(place % 5 == 0, -1, place // 300)):
+            ids = ids[torch.randperm(T, generator=g)]  # sorted order differs from theirs
+            dY = (torch.rand((T, d), generator=g) < 0.1).to(DT[dtype])
+            want = torch.zeros((V, d)).index_add_(0, ids[ids >= 0], dY[ids >= 0].float())
+            assert want.max() <= 256
+            got = sdp.embed_bwd(dY.cuda(), ids.int().cuda(), V)
+            assert torch.equal(got.cpu().float(), want)
