@@ -68,7 +68,7 @@ constexpr int kSortWaves = 16, kSortShift = 8, kMaxRange = 960, kAhead = 16;
 // sorted tokens of a wave, all of whose rows are in flight at once, and of a workgroup
 constexpr int kPiece = 16, kSumWaves = 8, kChunk = kPiece * kSumWaves;
 // Rows that a wave clears if they do not occur: few, since waves that store once or twice and end write memory in its order, and faster
-// (sums of 16384 tokens, 32000 x 2048 bf16, and of 300, 64000 x 2048: 64 rows 42.1 and 57.9 us in all, 8 rows 44.8 and 53.4, two 40.9 and 49.4).
+// (whole gradient of 16384 tokens, 32000 x 2048 bf16, and of 1200, 64000 x 2048: two rows 42.3 and 50.1 us, eight 45.8 and 52.3, 64 47.7 and 63.9).
 constexpr int kClear = 2;
 
 struct Sorted {
