@@ -213,9 +213,9 @@ __global__ __launch_bounds__(bwd_waves(WPR) * 64) void norm_bwd_kernel(NormBwd a
     // the row in `now`, while the one after it is on its way to `next`
     auto take = [&](Row1& now, Row1& next, float2* sums) {
         if (ROOM) request(row + step, next);
-        const bool live = row < a.T;
+        const bool live = ROWS == 1 || row < a.T;
         const int held = live ? whole : 0;
-        const float mu = a.mean ? now.mu : 0.f, rstd = now.rstd;
+        const float mu = live && a.mean ? now.mu : 0.f, rstd = live ? now.rstd : 0.f;
         float s1 = 0.f, s2 = 0.f, xht = 0.f, gt = 0.f;
         if constexpr (FORM >= FORM_TAIL) {
             const float dyt = tail && live ? now.dyt : 0.f;
@@ -224,11 +224,13 @@ __global__ __launch_bounds__(bwd_waves(WPR) * 64) void norm_bwd_kernel(NormBwd a
             dgat += dyt * xht, dbet += dyt;
         }
         float xh[VPL][N], g[VPL][N];
+        // A lane without values of the row has dy = 0 and the last piece's xh: one of the row's own, where (0 - mu) rstd may be no fp32 value
+        // and its product with 0 NaN.  Behind the last row xh is 0: what was read there may have been written over (dX in the place of H).
         auto centre = [&](int i, float (&dy)[N]) {
-            const int e = at + i * STEP;
-            Rw::unpack(Rw::mine(now.h[i], e, held), xh[i]), Rw::unpack(Rw::mine(now.dy[i], e, held), dy), Rw::unpack(ga[i], g[i]);
+            Rw::unpack(FORM != FORM_SHORT && live ? now.h[i] : u32x4{0, 0, 0, 0}, xh[i]), Rw::unpack(Rw::mine(now.dy[i], at + i * STEP, held), dy);
+            Rw::unpack(ga[i], g[i]);
 #pragma unroll
-            for (int k = 0; k < N; ++k) xh[i][k] = (xh[i][k] - mu) * rstd, g[i][k] *= dy[k];
+            for (int k = 0; k < N; ++k) xh[i][k] = FORM == FORM_SHORT ? 0.f : (xh[i][k] - mu) * rstd, g[i][k] *= dy[k];
         };
 #pragma unroll
         for (int i = 0; i < VPL; ++i) {

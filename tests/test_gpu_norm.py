@@ -9,7 +9,7 @@ import pytest
 import torch
 
 from around import DT, Guarded, norm_bwd64, norm_fwd64, normal
-from helpers import assert_close
+from helpers import assert_close, assert_close_rows
 
 pytestmark = pytest.mark.gpu
 HALF = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}
@@ -172,3 +172,29 @@ def test_a_bad_row_stays_alone_and_scratch_does_not_matter(sdp):
     for fill in (0, 255, 0x7F):
         again = sdp.norm_bwd("layer", X, dY, gamma, ref[2], ref[3], ws=torch.full((n,), fill, dtype=torch.uint8, device="cuda"))
         assert all(torch.equal(a, b) for a, b in zip(again, want))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [5, 64, 100, 1200, 2050, 9001])
+def test_constant_rows_whose_mean_over_their_deviation_overflows(sdp, dtype, d):
+    """Rows of 2^110 throughout have variance 0, s = 1 / sqrt(1e-12) = 1e6 and xh = 0, though mu s = 1.3e39 is no fp32 value: dX, dgamma and
+    dbeta are finite.  The mean is exact: a row's partial sums are small integers times 2^110.  Among other rows, alone, and last, whatever share of a
+    workgroup's rows is then left without one."""
+    dt, eps, half = DT[dtype], 1e-12, HALF[dtype]
+    for T, at in ((1, [0]), (3, [2]), (9, [0, 4, 8]), (600, [1, 599])):
+        print(f"constant rows {dtype} T={T} d={d}", flush=True)
+        X, dY, dH = (normal(T, d, dtype=dt, seed=s) for s in (1, 2, 3))
+        X[at] = 2.0 ** 110
+        gamma = normal(d, dtype=dt, seed=4, std=0.3, mean=1.0)
+        Y, H, mean, rstd = sdp.norm_fwd("layer", X.cuda(), gamma.cuda(), eps=eps)
+        wY, _, wm, wr = norm_fwd64("layer", X, None, gamma, None, eps)
+        assert (mean.cpu()[at] == 2.0 ** 110).all() and (Y.cpu()[at] == 0).all()
+        for skip in (None, dH):
+            dX, dg, db = sdp.norm_bwd("layer", H, dY.cuda(), gamma.cuda(), mean, rstd, dH=None if skip is None else skip.cuda())
+            wX, wg, wb = norm_bwd64("layer", X, dY, skip, gamma, wm, wr)
+            assert_close_rows(dX.cpu().double(), wX, half + 1e-5, "dX")
+            if T > len(at):
+                assert_close(dg.cpu().double(), wg, half + 2e-5, "dgamma")
+            else:
+                assert (dg == 0).all()
+            assert_close(db.cpu().double(), wb, half + 2e-5, "dbeta")
