@@ -185,7 +185,10 @@ __global__ __launch_bounds__(bwd_waves(WPR) * 64) void norm_bwd_kernel(NormBwd a
     u32x4 ga[VPL];
     float dga[VPL][N] = {}, dbe[VPL][N] = {}, gat = 0.f, dgat = 0.f, dbet = 0.f;
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) ga[i] = FORM == FORM_SHORT ? u32x4{0, 0, 0, 0} : Rw::load((const Elem*)a.gamma, at + i * STEP, whole);
+    for (int i = 0; i < VPL; ++i) { // 0 behind the row's whole pieces: g = gamma dy has to be 0 there, whatever the last piece's gamma is
+        const int e = at + i * STEP;
+        ga[i] = FORM == FORM_SHORT ? u32x4{0, 0, 0, 0} : Rw::mine(Rw::load((const Elem*)a.gamma, e, whole), e, whole);
+    }
     if (tail) gat = Rw::one((const Elem*)a.gamma + et);
     const int64_t step = (int64_t)gridDim.x * ROWS;
     int64_t row = (int64_t)blockIdx.x * ROWS + wave / WPR;

@@ -198,3 +198,30 @@ def test_constant_rows_whose_mean_over_their_deviation_overflows(sdp, dtype, d):
             else:
                 assert (dg == 0).all()
             assert_close(db.cpu().double(), wb, half + 2e-5, "dbeta")
+
+
+def _same(got, want, tol, what):
+    """Equal where the formula's value is not finite, within tol of it (or of 1) elsewhere."""
+    got, fin = got.cpu().double(), want.isfinite()
+    assert torch.equal(got[~fin].nan_to_num(nan=7.0), want[~fin].nan_to_num(nan=7.0)), f"{what}: values that are not finite"
+    off = (got - want)[fin].abs() / want[fin].abs().clamp(min=1.0)
+    assert off.numel() == 0 or off.max() <= tol, f"{what}: {float(off.max()):.2e}"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 1000, 2064, 9008])
+def test_weights_that_are_not_finite_count_once(sdp, dtype, d):
+    """gamma's last value infinite: the root-mean-square form's dX is what the formula gives, infinities of its signs and one NaN a row, whatever
+    lanes have no value of the row; dgamma and dbeta do not depend on gamma.  Widths of whole pieces, not of whole waves of them."""
+    T, dt = 5, DT[dtype]
+    X, dY = (normal(T, d, dtype=dt, seed=s) for s in (1, 2))
+    gamma = torch.ones(d, dtype=dt)
+    gamma[-1] = float("inf")
+    _, H, _, rstd = sdp.norm_fwd("rms", X.cuda(), gamma.cuda(), eps=EPS)
+    dX, dg, db = sdp.norm_bwd("rms", H, dY.cuda(), gamma.cuda(), None, rstd, bias=True)
+    _, _, wm, wr = norm_fwd64("rms", X, None, gamma, None, EPS)
+    wX, wg, wb = norm_bwd64("rms", X, dY, None, gamma, wm, wr)
+    assert wX.isinf().sum() == T * (d - 1) and wX[:, -1].isnan().all()
+    _same(dX, wX, 0.0, "dX")
+    _same(dg, wg, HALF[dtype] + 2e-5, "dgamma")
+    _same(db, wb, HALF[dtype] + 2e-5, "dbeta")
