@@ -376,7 +376,8 @@ typedef enum { SDP_I32 = 0, SDP_I64 = 1 } sdp_id_type;
  *   X [T][d], R [T][d] (may be NULL), gamma [d], beta [d] (may be NULL: no bias) in
  *   H [T][d] out: the sum, written if and only if R is given (else NULL);  Y [T][d] out
  *   mean, rstd [T] fp32 out: mu and s, for sdp_norm_bwd; mean is NULL with SDP_NORM_RMS
- * H and Y may each take the place of X or R (the same pointer); H and Y are two buffers.
+ * H and Y may each take the place of X or R (the same pointer); H and Y are two buffers.  Without R, a Y in X's place leaves
+ * nothing for sdp_norm_bwd, which reads X.
  * Errors: INVALID_ARG (null, misaligned, overlapping, unknown kind or dtype, T < 0, d < 1, eps negative or not
  * finite), SHAPE (d > SDP_NORM_MAX_WIDTH, T > SDP_MAX_EXTENT).
  * ------------------------------------------------------------------------------------------- */

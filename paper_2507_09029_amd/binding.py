@@ -596,7 +596,8 @@ def norm_fwd(kind, X, gamma, beta=None, residual=None, eps=1e-5, out=None):
     """Layer ("layer") or root-mean-square ("rms") norm of the tokens X [T][d], or of H = X + residual.
 
     Returns (Y, H, mean, rstd): what norm_bwd takes; H is X itself without a residual, mean None for "rms".
-    `out` = (Y, H, mean, rstd) preallocated; H is not looked at without a residual, mean not for "rms"."""
+    `out` = (Y, H, mean, rstd) preallocated; H is not looked at without a residual, mean not for "rms".  Y may take the place of X or
+    of the residual: of X without a residual, H is None, since what norm_bwd would need is written over."""
     k = _KINDS[kind]
     T, d = X.shape
     dt = _dtype_of(X, "X")
@@ -614,7 +615,9 @@ def norm_fwd(kind, X, gamma, beta=None, residual=None, eps=1e-5, out=None):
     st = _native().norm_fwd(device, k, dt, T, d, eps, X, residual, gamma, beta, H, Y, mean, rstd, stream)
     if st:
         _check(st, "sdp_norm_fwd")
-    return Y, X if H is None else H, mean, rstd
+    if residual is None and not (out and T and Y.data_ptr() == X.data_ptr()):
+        H = X
+    return Y, H, mean, rstd
 
 
 def norm_bwd_workspace_bytes(dtype, T, d):
@@ -627,6 +630,8 @@ def norm_bwd(kind, H, dY, gamma, mean, rstd, dH=None, want_dw=True, bias=None, o
     Returns (dX, dgamma, dbeta): dX is the gradient of X and of the residual.  dbeta is None without a bias (`bias`: by default
     "layer" has one, "rms" has none, and what `out` says where it is given), both are None with want_dw=False."""
     k = _KINDS[kind]
+    if H is None:
+        raise TypeError("H: expected a tensor (norm_fwd has none to give where Y takes X's place)")
     T, d = H.shape
     dt = _dtype_of(H, "H")
     if k:

@@ -225,3 +225,28 @@ def test_weights_that_are_not_finite_count_once(sdp, dtype, d):
     _same(dX, wX, 0.0, "dX")
     _same(dg, wg, HALF[dtype] + 2e-5, "dgamma")
     _same(db, wb, HALF[dtype] + 2e-5, "dbeta")
+
+
+def test_a_norm_in_its_tokens_place_leaves_nothing_to_normalise_again(sdp):
+    """Without a residual H is X itself.  Where Y takes X's place there is none, and the backward call says so; everywhere else the
+    returned tuple is what the backward call takes."""
+    T, d = 6, 40
+    X, dY = (normal(T, d, seed=s).cuda() for s in (1, 2))
+    gamma, st = normal(d, seed=3, mean=1.0).cuda(), lambda: torch.empty((T,), device="cuda")
+    Y, H, mean, rstd = sdp.norm_fwd("layer", X, gamma)
+    assert H is X
+    want = sdp.norm_bwd("layer", H, dY, gamma, mean, rstd)
+    Y2, H2, m2, r2 = sdp.norm_fwd("layer", X, gamma, out=(torch.empty_like(X), None, st(), st()))
+    assert H2 is X and all(torch.equal(a, b) for a, b in zip(sdp.norm_bwd("layer", H2, dY, gamma, m2, r2), want))
+    for view in (lambda x: x, lambda x: x.view(-1).view(T, d)):  # the same memory, the same tensor or not
+        x = X.clone()
+        y, h, m2, r2 = sdp.norm_fwd("layer", x, gamma, out=(view(x), None, st(), st()))
+        assert torch.equal(y, Y) and h is None
+        with pytest.raises(TypeError, match="H: expected a tensor"):
+            sdp.norm_bwd("layer", h, dY, gamma, m2, r2)
+        # with a residual H is a buffer of its own, whatever Y takes the place of
+        x, r = X.clone(), dY.clone()
+        y, h, m2, r2 = sdp.norm_fwd("layer", x, gamma, residual=r, out=(view(x), r, st(), st()))
+        assert h is r and torch.equal(h, X + dY)
+    empty = torch.empty((0, d), device="cuda")
+    assert sdp.norm_fwd("rms", empty, gamma)[1] is empty
