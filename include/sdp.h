@@ -422,7 +422,8 @@ int sdp_embed_bwd(int dtype, int id_type, int T, int V, int d, float scale, cons
                   void* ws, size_t ws_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------------------------
- * Cross-entropy of T rows of V logits against labels, with its gradient from the same read of the logits:
+ * Cross-entropy of T rows of V logits against labels, with its gradient, from one read of the logits (three where a row has
+ * more than 131072 bf16 or 65536 fp32 values, two of them for the loss alone):
  *   lse[t] = log sum_j exp Z[t][j];   nll[t] = lse[t] - Z[t][labels[t]];
  *   loss = c sum_t nll[t],  c = scale * scale_dev[0];   dZ[t][j] = dloss / dZ[t][j] = c (exp(Z[t][j] - lse[t]) - [j = labels[t]])
  * A row whose label lies outside [0, V) has none: nll = lse = 0, dZ = 0, and its logits are not read.  Logits of -inf are

@@ -5,8 +5,9 @@
 // Bound by memory: the logits are the largest tensor of a training step (8192 x 32000 bf16: 524 MB), and the least that can be
 // moved is one read and one write of them.  A workgroup holds a row in registers, as it is stored, from the read to the write: up to 16
 // waves with up to 16 pieces of 16 bytes a lane, as many as leave room for several rows on a CU (by_row).  Rows of more than 131072
-// bf16 or 65536 fp32 values are read twice.  8192 x 32000 bf16: 177 us with the scale and the sum of the loss, 5.9 TB/s, more than a
-// large copy reaches; 1000 x 50001, a quarter without a label: 42 us, 4.1 TB/s, with three rows to read a CU.
+// bf16 or 65536 fp32 values are read for the maximum, for the sum and for the gradient: 1024 x 152000 bf16 176 us, 89 without a gradient,
+// 512 x 128256 fp32 148 and 73.  8192 x 32000 bf16: 177 us with the scale and the sum of the loss, 5.9 TB/s, more than a large copy
+// reaches; 1000 x 50001, a quarter without a label: 42 us, 4.1 TB/s, with three rows to read a CU.
 //
 // exp(z - max) is 2^((z - max) L), L = log2 e, on the hardware's 2^x.  The difference comes first: z L - max L in one step, with max L
 // rounded, overflows or is far off where a row's values are near the type's lowest, as masks write them.
@@ -51,7 +52,7 @@ constexpr uint32_t minus_inf() {
     return BF16 ? 0xFF80FF80u : 0xFF800000u;
 }
 
-// PIECES > 0: pieces a lane holds, the row has no more; 0: the row is read again for the gradient
+// PIECES > 0: pieces a lane holds, the row has no more; 0: the row is read again for the sum, and again for the gradient
 template <int BF16, int WAVES, int PIECES, int ONCE>
 __global__ __launch_bounds__(WAVES * 64) void token_loss_kernel(Loss a) {
     typedef Row<BF16> Rw;
@@ -77,7 +78,7 @@ __global__ __launch_bounds__(WAVES * 64) void token_loss_kernel(Loss a) {
     }
     const float c = a.scale * (a.scale_dev ? *a.scale_dev : 1.f);
     u32x4 w[P];
-    auto piece = [&](int64_t e) { return Rw::mine(Rw::load(z, (int)e, whole), (int)e, whole, minus_inf<BF16>()); }; // of a row that is read twice
+    auto piece = [&](int64_t e) { return Rw::mine(Rw::load(z, (int)e, whole), (int)e, whole, minus_inf<BF16>()); }; // of a row that is read again
     if (PIECES)
 #pragma unroll
         for (int i = 0; i < P; ++i) w[i] = Rw::template load<ONCE>(z, (tid + i * TH) * N, whole);
@@ -113,13 +114,17 @@ __global__ __launch_bounds__(WAVES * 64) void token_loss_kernel(Loss a) {
 #pragma unroll
             for (int k = 0; k < N; ++k) sum += power(v[k]);
         }
-    } else {
+    } else { // up to 2^18 pieces: a running fp32 sum of terms of one size drifts to one side (65536 terms: 1e-3)
+        double all = 0.0;
         for (int64_t e = tid * N; e < whole; e += TH * N) {
             float v[N];
             Rw::unpack(piece(e), v);
+            float part = 0.f;
 #pragma unroll
-            for (int k = 0; k < N; ++k) sum += power(v[k]);
+            for (int k = 0; k < N; ++k) part += power(v[k]);
+            all += (double)part;
         }
+        sum += (float)all;
     }
     sum = group_all<WAVES, false>(sum, lds[1]);
     if (PIECES) sdp::again(w);

@@ -5,6 +5,8 @@ Tolerances: fp32 arithmetic on top of one rounding of dZ.  The exponents (z - ma
 each (logits within 44 of the maximum; smaller terms are below 2^-64 of the sum), that is 3 x 64 x 2^-24 x ln 2 = 8e-6 relative to such a
 term and 2e-6 to those that make up the sum (within 2^-16 of the largest); a sum of positive terms adds at most 128 + 6 + 16 roundings, 9e-6;
 the hardware's 2^x 1.2e-7.  So lse and nll are within 1.2e-5, dZ's terms within 2e-5 of c p beside their rounding (2^-8 bf16)."""
+import math
+
 import pytest
 import torch
 
@@ -160,3 +162,25 @@ def test_many_rows(sdp):
     assert float(scale) == torch.tensor(1.0 / int(((labels >= 0) & (labels < V)).sum()), dtype=torch.float32)
     got = sdp.token_loss(Z.cuda(), labels.cuda(), scale_dev=scale)
     _check(got, Z, labels, float(scale), "f32")
+
+
+@pytest.mark.parametrize("dtype,V,tops", [("bf16", 2 ** 26 - 3, (4.71875, 1.5)), ("f32", 2 ** 25 - 3, (3.453125, 6.28125))])
+def test_sums_of_long_rows_do_not_drift(sdp, dtype, V, tops):
+    """Rows of zeros and one larger logit m: V - 1 equal terms exp(-m), whose roundings in a running fp32 sum all fall to the same side (1e-3 off at these
+    m and V).  In closed form lse = m + log(1 + (V - 1) exp(-m)).  The sum: 3 roundings of an exponent below 9.1, 3 x 9.1 x 2^-24 x ln 2 = 1.2e-6; the
+    hardware's 2^x 1.2e-7; the values of a piece, 7 roundings, 4.2e-7; 64 bits over pieces, exact here; 1 + 6 + 15 over lanes and waves, 1.3e-6: 3.1e-6
+    together.  Then lse's own rounding and its logarithm's, 2^-23 of it."""
+    dt, c = DT[dtype], 3.0
+    Z = torch.zeros((2, V), dtype=dt, device="cuda")
+    Z[0, 12345], Z[1, V - 1] = tops
+    labels = torch.tensor([12345, 7], device="cuda")
+    nll, lse, dZ, loss = sdp.token_loss(Z, labels, scale=c)
+    for t, m in enumerate(tops):
+        want = m + math.log1p((V - 1) * math.exp(-m))
+        room = 3.1e-6 + 2.0 ** -23 * want
+        assert abs(float(lse[t]) - want) <= room
+        assert abs(float(nll[t]) - (want - float(Z[t, labels[t]]))) <= room
+        p = c * math.exp(-want)
+        # beside the sum's error: the quotient's, the product's and the result's own roundings
+        assert abs(float(dZ[t, 99]) - p) <= (HALF[dtype] + 3.1e-6 + 2.0 ** -22) * p
+    assert torch.equal(sdp.token_loss(Z, labels, want_grad=False)[1], lse)
