@@ -569,27 +569,26 @@ _KINDS = {"layer": 0, "rms": 1, 0: 0, 1: 1}
 _ID_TYPES = {torch.int32: 0, torch.int64: 1}
 
 
-def _here():
-    """The current device and its current stream."""
+def _here_of(t):
+    """The current device and its current stream, for a compiled call, which checks its tensors itself: t on the CPU is refused there."""
+    if not t.is_cuda:
+        return 0, 0
     device = torch._C._cuda_getDevice()
     return device, torch._C._cuda_getCurrentRawStream(device)
 
 
-def _here_of(t):
-    """The same for a compiled call, which checks its tensors itself: t on the CPU is refused there."""
-    return _here() if t.is_cuda else (0, 0)
-
-
 def _dtype_of(t, name):
-    if t.dtype not in _DTYPES:
+    dt = _DTYPES.get(t.dtype)
+    if dt is None:
         raise TypeError(f"{name}: expected torch.float32 or torch.bfloat16")
-    return _DTYPES[t.dtype]
+    return dt
 
 
 def _id_type_of(t, name):
-    if t.dtype not in _ID_TYPES:
+    it = _ID_TYPES.get(t.dtype)
+    if it is None:
         raise TypeError(f"{name}: expected torch.int32 or torch.int64")
-    return _ID_TYPES[t.dtype]
+    return it
 
 
 def norm_fwd(kind, X, gamma, beta=None, residual=None, eps=1e-5, out=None):
