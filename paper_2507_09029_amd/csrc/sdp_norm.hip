@@ -7,7 +7,7 @@
 //
 // Both are bound by memory: a row is read once into registers, its sums are taken over the lanes that hold it, and it is written
 // once.  A row belongs to WPR waves, each lane holding up to VPL pieces of 16 bytes (fwd_shape, bwd_shape).  16384 x 2048 bf16 with the
-// skip connection, four matrices of 67 MB: forward 47.5 us, 5.7 TB/s; backward 49.4, 5.4, of which the sums of the weight's gradients
+// skip connection, four matrices of 67 MB: forward 47.3 us, 5.7 TB/s; backward 49.1, 5.5, of which the sums of the weight's gradients
 // are 4.8.  Small batches are bound by the launch: 256 x 256 fp32 forward 4.4 us, most of it the call's.
 #include <cmath>
 #include <type_traits>
@@ -169,7 +169,7 @@ struct Held {
 //
 // ROOM: registers are enough for that, and to keep what the sums are made of for the second use.  With more than 8 values of a matrix a lane
 // they are not, and spill: rows of more than 8192, us, each row requested as it is needed and values made again / otherwise: 2048 x 16384
-// fp32 118 / 248, bf16 74 / 133.  Where there is room, 16384 x 2048 bf16: values kept 51, made again 60.
+// fp32 114 / 248, bf16 74 / 133.  Where there is room, 16384 x 2048 bf16: values kept 51, made again 60.
 template <int BF16, int WPR, int VPL, int FORM, int SKIP>
 __global__ __launch_bounds__(bwd_waves(WPR) * 64) void norm_bwd_kernel(NormBwd a) {
     typedef Row<BF16> Rw;

@@ -2,7 +2,8 @@
 name no row, rows that occur in every chunk, both id types.
 
 Tolerances, per row (relative to max(rms of the row, value)): an output is rounded once (2^-8 bf16, 2^-24 fp32); a sum of n rows in
-fp32 adds at most n roundings of 2^-24 of partial sums, chunks of 32 and then their sums: for n <= 4096, 32 + 128 of them: 1e-5 where
+fp32 adds at most n roundings of 2^-24 of partial sums: 16 tokens of a wave's piece, the 8 or 16 pieces of a chunk of 128 or 256 tokens, then the chunks',
+one after the other up to 1024 tokens, every fourth a wave beyond: for n <= 4096, 16 + 16 + 4 or 16 + 8 + 8 + 3 of them: 2.1e-6, below 1e-5 where
 partial sums are no larger than the result.  Values have one sign in the columns that are compared element by element (mean 1), so they are not."""
 import pytest
 import torch

@@ -4,7 +4,8 @@ widths and row counts around every change of tile, matrices that start at any el
 Tolerances (relative to max(rms, value)): an output is rounded once, by at most half a step (2^-8 bf16), on top of fp32 arithmetic.
 fp32: a sum of n values adds n roundings of 2^-24 of a partial sum.  A row's sums have at most 32 values a lane, 6 steps of a wave and 16
 waves: 54 x 2^-24 = 3.2e-6 each, two of them (mean, squares) and a handful of products: 1e-5.  dgamma, dbeta: partial sums of values of
-random sign stay near the result's rms, along at most 16 rows a wave, 16 waves and 128 + 4 shares: 164 x 2^-24 = 9.8e-6; with xh's own error 2e-5."""
+random sign stay near the result's rms, along at most 5 rows a wave here, 8 waves' rows of a workgroup, 16 of at most 256 workgroups' shares a wave and
+16 waves: 45 x 2^-24 = 2.7e-6; with xh's own error, 1e-5, below 2e-5."""
 import pytest
 import torch
 

@@ -3,8 +3,8 @@ that start at any element or lie apart, labels that name no logit, masked logits
 
 Tolerances: fp32 arithmetic on top of one rounding of dZ.  The exponents (z - max) log2 e are rounded twice, and log2 e once, 2^-24 of at most 64
 each (logits within 44 of the maximum; smaller terms are below 2^-64 of the sum), that is 3 x 64 x 2^-24 x ln 2 = 8e-6 relative to such a
-term and 2e-6 to those that make up the sum (within 2^-16 of the largest); a sum of positive terms adds at most 128 + 6 + 16 roundings, 9e-6;
-the hardware's 2^x 1.2e-7.  So lse and nll are within 1.2e-5, dZ's terms within 2e-5 of c p beside their rounding (2^-8 bf16)."""
+term and 2e-6 to those that make up the sum (within 2^-16 of the largest); a sum of positive terms adds at most 128 + 6 + 16 roundings, 9e-6
+(rows beyond the registers: 8 values of a piece in fp32, pieces in 64 bits, 1 + 6 + 16 roundings, 2e-6); the hardware's 2^x 1.2e-7.  So lse and nll are within 1.2e-5, dZ's terms within 2e-5 of c p beside their rounding (2^-8 bf16)."""
 import math
 
 import pytest
