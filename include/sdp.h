@@ -441,6 +441,59 @@ int sdp_token_loss(int dtype, int id_type, int T, int V, int64_t ldz, float scal
                    const float* scale_dev, float* nll, float* lse, void* dZ, float* loss, void* stream);
 int sdp_label_scale(int id_type, int T, int V, const void* labels, float* scale, void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Learning from a teacher of whom k entries a token are known, ids with their logits (the k highest, as a rule), with the gradient,
+ * from one read of the student's logits.  With the temperature tau > 0 on both sides:
+ *   L[t] = top_lse[t], or without it log sum_i exp(top[t][i] / tau): the entries alone, renormalised
+ *   q_i = exp(top[t][i] / tau - L[t]);   lse[t] = log sum_j exp(Z[t][j] / tau)
+ *   kl[t] = sum_i q_i (log q_i - Z[t][ids[t][i]] / tau + lse[t])
+ *   loss = c sum_t kl[t],  c = scale * scale_dev[0] (the usual factor tau^2 belongs into scale);
+ *   dZ[t][j] = dloss / dZ[t][j] = c / tau (exp(Z[t][j] / tau - lse[t]) sum_i q_i - sum_{i : ids[t][i] = j} q_i)
+ * top_lse is the teacher's log-sum-exp of all its logits over tau, for a teacher whose mass outside the entries counts as known to be
+ * elsewhere: q then sums to less than 1.  An entry whose id lies outside [0, V), or whose logit is -inf, is none, so that shorter lists
+ * are padded with either.  A token without entries has no teacher: kl = lse = 0, dZ = 0, its logits are not read.  Entries of
+ * one id add up.  Logits Z of -inf are masked ones (probability 0; kl = +inf where an entry names one); a row of nothing else, or one with
+ * +inf or NaN, gives NaN, and so do a NaN among the entries or in top_lse; an entry of +inf gives what the formulas do.
+ *   Z, dZ [T][ldz], ldz >= V: columns from V on are neither read nor written.  dZ may be NULL (loss alone) or Z.
+ *   ids, top [T][k] in, top of top_dtype (SDP_F32 or SDP_BF16);  top_lse [T] fp32 in, may be NULL
+ *   scale_dev: device fp32, may be NULL (= 1)
+ *   kl [T] fp32 out;  lse [T] fp32 out, may be NULL;  loss [1] fp32 out (summed in fp64 in a fixed order), may be NULL
+ * Errors: INVALID_ARG (null, misaligned, overlapping, unknown dtype, top_dtype or id_type, T < 0, V < 1, k < 1, temperature not positive
+ * and finite or below 2^-20, scale not finite), SHAPE (ldz < V, T or V > SDP_MAX_EXTENT, k > SDP_MAX_ENTRIES).
+ * ------------------------------------------------------------------------------------------- */
+#define SDP_MAX_ENTRIES 1024 /* largest k */
+int sdp_distill_loss(int dtype, int id_type, int top_dtype, int T, int V, int k, int64_t ldz, float temperature, float scale,
+                     const void* Z, const void* ids, const void* top, const float* top_lse, const float* scale_dev, float* kl,
+                     float* lse, void* dZ, float* loss, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * The output head and its loss in one: sdp_token_loss on the logits Z = X W^T, with the gradients of the tokens and of the head,
+ * without the logits in memory.
+ *   nll, lse, loss as there (Z in fp32);   dX = dZ W  [T][d];   dW = dZ^T X  [V][d]
+ * It works on as many tokens at a time as keep what it holds of their logits within SDP_HEAD_PIECE_BYTES (2 bytes a logit with SDP_BF16, 4
+ * with SDP_F32).  Tokens without a label cost nothing but the zeros of their dX: with SDP_BF16 their products are not computed.  Their X is not
+ * looked at.
+ *   X [T][d], W [V][d] (row-major by token of the vocabulary, like an embedding, which it may be), labels [T] in
+ *   nll [T] fp32 out;  lse [T] fp32, may be NULL;  loss [1] fp32, may be NULL
+ *   dX [T][d], dW [V][d] out, either may be NULL (not wanted); dX may take the place of X.  dW has every row; sums over tokens are
+ *   fp32 and rounded once.
+ *   ws: sdp_head_loss_workspace_bytes(dtype, T, V, d, want_dx, want_dw), 256-byte aligned
+ * With SDP_BF16 dZ is rounded once to bf16 where it enters the two products, as the logits' gradient that sdp_token_loss stores.
+ * Limits: for SDP_BF16 d a multiple of 8, X, W, dX, dW 16-byte aligned, V < 2^22, V d < 2^31; T <= SDP_EMBED_MAX_TOKENS.
+ * Errors: as for sdp_token_loss, SHAPE where a limit is exceeded, WORKSPACE.
+ *
+ * sdp_head_distill: the same for sdp_distill_loss on Z = X W^T.
+ * ------------------------------------------------------------------------------------------- */
+#define SDP_HEAD_PIECE_BYTES (1 << 30)
+size_t sdp_head_loss_workspace_bytes(int dtype, int T, int V, int d, int want_dx, int want_dw);
+int sdp_head_loss(int dtype, int id_type, int T, int V, int d, float scale, const void* X, const void* W, const void* labels,
+                  const float* scale_dev, float* nll, float* lse, void* dX, void* dW, float* loss, void* ws, size_t ws_bytes,
+                  void* stream);
+size_t sdp_head_distill_workspace_bytes(int dtype, int T, int V, int d, int k, int want_dx, int want_dw);
+int sdp_head_distill(int dtype, int id_type, int top_dtype, int T, int V, int d, int k, float temperature, float scale, const void* X,
+                     const void* W, const void* ids, const void* top, const float* top_lse, const float* scale_dev, float* kl,
+                     float* lse, void* dX, void* dW, float* loss, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

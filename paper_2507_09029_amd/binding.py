@@ -101,6 +101,16 @@ def lib():
     L.sdp_coverage_avg_adamw.restype = i32
     L.sdp_coverage_avg_adamw.argtypes = [i32, i64, i32, i32, ctypes.POINTER(vp), vp, vp, vp, vp, vp, vp, vp, vp]
     f32 = ctypes.c_float
+    L.sdp_distill_loss.restype = i32
+    L.sdp_distill_loss.argtypes = [i32] * 6 + [i64, f32, f32] + [vp] * 10
+    L.sdp_head_loss_workspace_bytes.restype = sz
+    L.sdp_head_loss_workspace_bytes.argtypes = [i32] * 6
+    L.sdp_head_loss.restype = i32
+    L.sdp_head_loss.argtypes = [i32] * 5 + [f32] + [vp] * 10 + [sz, vp]
+    L.sdp_head_distill_workspace_bytes.restype = sz
+    L.sdp_head_distill_workspace_bytes.argtypes = [i32] * 7
+    L.sdp_head_distill.restype = i32
+    L.sdp_head_distill.argtypes = [i32] * 7 + [f32, f32] + [vp] * 12 + [sz, vp]
     L.sdp_norm_fwd.restype = i32
     L.sdp_norm_fwd.argtypes = [i32] * 4 + [f32] + [vp] * 9
     L.sdp_norm_bwd_workspace_bytes.restype = sz
@@ -563,7 +573,7 @@ def coverage_avg_adamw(grads, mask, theta, m, v, lr, beta1, beta2, eps, weight_d
     return cov
 
 
-# ---- around a stack of blocks: norms, token embedding, token loss.  Every tensor has to be on the current device. ----------
+# ---- around a stack of blocks: norms, token embedding, losses and the head.  Every tensor has to be on the current device. ----------
 
 _KINDS = {"layer": 0, "rms": 1, 0: 0, 1: 1}
 _ID_TYPES = {torch.int32: 0, torch.int64: 1}
@@ -727,6 +737,99 @@ def token_loss(Z, labels, scale=1.0, scale_dev=None, want_grad=True, out=None):
     if st:
         _check(st, "sdp_token_loss")
     return nll, lse, dZ, loss
+
+
+def distill_loss(Z, ids, top, temperature=1.0, top_lse=None, scale=1.0, scale_dev=None, want_grad=True, out=None):
+    """Divergence of logits Z [T][V] (rows may lie apart) from a teacher of whom k logits a token are known, with its gradient.
+
+    ids [T][k] (int32 or int64) names them, top [T][k] (fp32 or bf16) holds them; an id outside [0, V) or a logit of -inf is no entry, a
+    token without entries has no part in it.  The teacher's probabilities are those of its entries over `temperature`, renormalised, or with
+    top_lse [T] (fp32, the log-sum-exp of all its logits over temperature) as they are.  With c = scale * scale_dev[0] (scale_dev: fp32 tensor
+    on the GPU, None = 1), returns (kl [T], lse [T], dZ [T][V], loss [1]): loss = c * sum(kl) and its gradient by Z; dZ is None with
+    want_grad=False.  `out` = (kl, lse, dZ, loss) preallocated: dZ may be Z, lse and loss may be None (not wanted)."""
+    T, V = Z.shape
+    dt, it, tt = _dtype_of(Z, "Z"), _id_type_of(ids, "ids"), _dtype_of(top, "top")
+    if out is None:
+        kl, lse = (torch.empty((T,), dtype=torch.float32, device=Z.device) for _ in range(2))
+        dZ = torch.empty_strided(Z.shape, Z.stride(), dtype=Z.dtype, device=Z.device) if want_grad else None
+        loss = torch.empty((1,), dtype=torch.float32, device=Z.device)
+    else:
+        kl, lse, dZ, loss = out
+        if not want_grad:
+            dZ = None
+        elif dZ is None:
+            raise ValueError("dZ: expected a tensor (or want_grad=False)")
+    device, stream = _here_of(Z)
+    st = _native().distill_loss(device, dt, it, tt, T, V, _entries_of(ids), Z.stride(0) if T > 1 else V, temperature, scale, Z, ids, top, top_lse,
+                                scale_dev, kl, lse, dZ, loss, stream)
+    if st:
+        _check(st, "sdp_distill_loss")
+    return kl, lse, dZ, loss
+
+
+def _entries_of(ids):
+    if ids.dim() != 2:
+        raise ValueError("ids: expected shape (T, k)")
+    return ids.shape[1]
+
+
+def _head_out(X, W, want_dx, want_dw, out):
+    """The five outputs of a head's call, checked or made."""
+    if out is None:
+        per_token, lse = (torch.empty((X.shape[0],), dtype=torch.float32, device=X.device) for _ in range(2))
+        return (per_token, lse, torch.empty_like(X) if want_dx else None, torch.empty_like(W) if want_dw else None,
+                torch.empty((1,), dtype=torch.float32, device=X.device))
+    per_token, lse, dX, dW, loss = out
+    if want_dx and dX is None:
+        raise ValueError("dX: expected a tensor (or want_dx=False)")
+    if want_dw and dW is None:
+        raise ValueError("dW: expected a tensor (or want_dw=False)")
+    return per_token, lse, dX if want_dx else None, dW if want_dw else None, loss
+
+
+def head_loss_workspace_bytes(dtype, T, V, d, want_dx=True, want_dw=True):
+    return int(lib().sdp_head_loss_workspace_bytes(_DTYPES[dtype], T, V, d, bool(want_dx), bool(want_dw)))
+
+
+def head_loss(X, W, labels, scale=1.0, scale_dev=None, want_dx=True, want_dw=True, out=None, ws=None):
+    """Cross-entropy of the logits X W^T of tokens X [T][d] and head W [V][d] against int32 or int64 labels [T], with the gradients of
+    both, without the logits in memory.
+
+    As token_loss on X W^T: returns (nll [T], lse [T], dX [T][d], dW [V][d], loss [1]); dX and dW are None where they are not wanted.
+    `out` = (nll, lse, dX, dW, loss) preallocated: dX may be X, lse and loss may be None."""
+    T, d = X.shape
+    V = W.shape[0]
+    dt, it = _dtype_of(X, "X"), _id_type_of(labels, "labels")
+    nll, lse, dX, dW, loss = _head_out(X, W, want_dx, want_dw, out)
+    if ws is None:
+        ws = _ws(head_loss_workspace_bytes(X.dtype, T, V, d, want_dx, want_dw), X.device)
+    device, stream = _here_of(X)
+    st = _native().head_loss(device, dt, it, T, V, d, scale, X, W, labels, scale_dev, nll, lse, dX, dW, loss, ws, ws.numel(), stream)
+    if st:
+        _check(st, "sdp_head_loss")
+    return nll, lse, dX, dW, loss
+
+
+def head_distill_workspace_bytes(dtype, T, V, d, k, want_dx=True, want_dw=True):
+    return int(lib().sdp_head_distill_workspace_bytes(_DTYPES[dtype], T, V, d, k, bool(want_dx), bool(want_dw)))
+
+
+def head_distill(X, W, ids, top, temperature=1.0, top_lse=None, scale=1.0, scale_dev=None, want_dx=True, want_dw=True, out=None, ws=None):
+    """distill_loss on the logits X W^T of tokens X [T][d] and head W [V][d], with the gradients of both, without the logits in memory.
+
+    Returns (kl [T], lse [T], dX [T][d], dW [V][d], loss [1]), as head_loss does; the teacher's arguments are distill_loss's."""
+    T, d = X.shape
+    V = W.shape[0]
+    dt, it, tt, k = _dtype_of(X, "X"), _id_type_of(ids, "ids"), _dtype_of(top, "top"), _entries_of(ids)
+    kl, lse, dX, dW, loss = _head_out(X, W, want_dx, want_dw, out)
+    if ws is None:
+        ws = _ws(head_distill_workspace_bytes(X.dtype, T, V, d, k, want_dx, want_dw), X.device)
+    device, stream = _here_of(X)
+    st = _native().head_distill(device, dt, it, tt, T, V, d, k, temperature, scale, X, W, ids, top, top_lse, scale_dev, kl, lse, dX, dW, loss, ws,
+                                ws.numel(), stream)
+    if st:
+        _check(st, "sdp_head_distill")
+    return kl, lse, dX, dW, loss
 
 
 def profile_enable(on=True):

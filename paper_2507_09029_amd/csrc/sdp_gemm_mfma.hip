@@ -107,6 +107,26 @@ struct Dev {
     int n_head, tail;
 };
 
+// The output head's contractions (kHead* below), beside Dev.  Rows of X and of the logits are those of tokens that have a target, first
+// to last; how many they are is known on the device alone.
+struct HeadArgs {
+    const int32_t* live; // rows of all pieces together; this launch has min(its rows, *live - base) of them
+    int base;
+    // EPI_CODES
+    float rate, to_code; // log2(e) / tau; rate / kCodeRange
+    int codes;           // whether they are wanted, or the statistics alone
+    float2* stats;       // [row][nblk]
+    int nblk;
+    const int32_t* labels; // [row], optional
+    float* at_label;       // [row]
+    // OP_HEAD_DX_SPLIT, OP_HEAD_DW: rows of the outputs (of one range's partial sums; that are stored)
+    int out_rows;
+    // OP_HEAD_DW: sums of the pieces of tokens before this one, fp32 as the accumulators lie; 0: there are no others, 1: the first of
+    // several, 2: neither first nor last, 3: the last
+    float* sums;
+    int piece;
+};
+
 // two fp32 -> packed bf16, round to nearest even (the hardware's v_cvt_pk_bf16_f32)
 __device__ inline uint32_t pack_bf16(float lo, float hi) {
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -116,6 +136,18 @@ __device__ inline uint32_t pack_bf16(float lo, float hi) {
 __device__ inline u32x2 pack4(float a, float b, float c, float d) { return u32x2{pack_bf16(a, b), pack_bf16(c, d)}; }
 __device__ inline float lo_bf16(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ inline float hi_bf16(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+
+// x of the lanes l16, l16 + 16, l16 + 32 and l16 + 48 together: the larger, or the sum in one order
+template <bool MAX>
+__device__ inline float across_rows(float x) {
+    typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+    u32x2_t p = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+    x = MAX ? fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1])) : __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    p = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+    return MAX ? fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1])) : __uint_as_float(p[0]) + __uint_as_float(p[1]);
+}
+// two values of [0, 1] as 16 bits each, 65535 = 1 and beyond
+__device__ inline uint32_t code_pair(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pknorm_u16(a, b)); }
 
 // source of the chunks that lie beyond the depth of the matrices in a partial last step
 __device__ __attribute__((aligned(256))) const uint32_t kZeroChunk[64] = {0};
@@ -281,6 +313,9 @@ struct Geometry {
 // tiles at a time.
 struct NoSide {};
 constexpr bool carries_side(int op) { return op == OP_GATE_UP || op == OP_DACT || op == OP_DW; }
+constexpr bool is_batched(int op) { return op == OP_DW || op == OP_DW_SPLIT || op == OP_DW_TAIL; }
+constexpr bool is_split(int op) { return op == OP_DW_SPLIT || op == OP_HEAD_DX_SPLIT; }
+constexpr bool is_head(int op) { return op >= OP_HEAD_LOGITS; }
 // the launches of the attention block, whose lists may be of heads
 constexpr bool takes_heads(int op) { return op == OP_DOWN || op == OP_DW || op == OP_DW_SPLIT; }
 template <int OP>
@@ -293,7 +328,7 @@ constexpr int side_tiles(int threads, int lds) {
 // One workgroup's tile (id `block` of the launch).  KM: bit 0 = A is depth-major ([K][lda]), bit 1 = B is, bit 2 = B's depth rows
 // are listed (b_gather)
 template <int BM, int BN, int WAVES_M, int WAVES_N, int EPI, int OP, int KM>
-__device__ __attribute__((always_inline)) inline void gemm_tile(const Dev& g, const int block, unsigned char* const smem) {
+__device__ __attribute__((always_inline)) inline void gemm_tile(const Dev& g, const int block, unsigned char* const smem, const HeadArgs& head = HeadArgs{}) {
     using Geo = Geometry<BM, BN, WAVES_M, WAVES_N, EPI, KM>;
     constexpr int NW = Geo::NW, WM = Geo::WM, WN = Geo::WN, FM = Geo::FM, FN = Geo::FN;
     constexpr int A_BYTES = Geo::A_BYTES, B_BYTES = Geo::B_BYTES;
@@ -328,9 +363,10 @@ __device__ __attribute__((always_inline)) inline void gemm_tile(const Dev& g, co
     } else {
         bid = head_position(bid, g.ntot);
     }
-    constexpr bool kBatched = OP == OP_DW || OP == OP_DW_SPLIT || kTail;
-    constexpr bool kSplit = OP == OP_DW_SPLIT;
-    const int nb = kBatched ? g.nbatch * (kSplit ? g.ksplit : 1) : 1;
+    constexpr bool kBatched = is_batched(OP);
+    constexpr bool kSplit = is_split(OP);
+    constexpr bool kHeadDw = OP == OP_HEAD_DW;
+    const int nb = (kBatched ? g.nbatch : 1) * (kSplit ? g.ksplit : 1);
     int tile_m, tile_n, batch;
     if (kBatched && g.np0 > 0) {
         tile_of_shared(bid, g.tiles_m, g.tiles_n, g.np0, g.nbatch, g.ksplit, g.group_m, batch, tile_m, tile_n);
@@ -350,7 +386,7 @@ __device__ __attribute__((always_inline)) inline void gemm_tile(const Dev& g, co
     uint16_t* gC = g.C;
     int64_t lda = g.lda;
     int kpart = 0; // depth range of this workgroup (OP_DW_SPLIT, and the cut tiles of OP_DW_TAIL)
-    if (kSplit) kpart = batch / g.nbatch, batch -= kpart * g.nbatch;
+    if (kSplit) kpart = kBatched ? batch / g.nbatch : batch, batch -= kpart * (kBatched ? g.nbatch : 1);
     if (kTail) kpart = tail_part;
     if (kBatched) {
         // selected by comparisons: a runtime index into a by-value kernel argument would go through scratch
@@ -361,6 +397,7 @@ __device__ __attribute__((always_inline)) inline void gemm_tile(const Dev& g, co
         gC = batch == 0 ? g.Cb[0] : (batch == 1 ? g.Cb[1] : (batch == 2 ? g.Cb[2] : g.Cb[3]));
     }
     const int m0 = tile_m * BM;
+    if (is_head(OP) && m0 >= g.M) return; // no token there
     const int n0 = kFwd ? tile_n * (BN / 2) : tile_n * BN; // SWIGLU_FWD: BN columns = BN/2 neurons x {gate, up}
     // SWIGLU_BWD with neuron-major copies: the encoded rank of each of this wave's output columns (at most two
     // per lane), fetched now so that the epilogue does not wait for it; a column outside the matrix counts as
@@ -376,7 +413,7 @@ __device__ __attribute__((always_inline)) inline void gemm_tile(const Dev& g, co
 
     // ---- depth steps; a partial last step (K % 64 != 0, K % 8 == 0) reads its missing chunks from a
     // zero buffer, so that every step issues the same loads and runs all four MFMA sub-steps ----
-    const int nk_all = (g.K + BK - 1) / BK;
+    const int nk_all = kHeadDw && g.K == 0 ? 1 : (g.K + BK - 1) / BK; // no token: one step of zeros
     const bool ranged = kSplit || (kTail && cut);
     const int kt0 = ranged ? kpart * g.ksteps : 0; // first depth step of this workgroup
     const int nk1 = ranged ? (nk_all - kt0 < g.ksteps ? nk_all - kt0 : g.ksteps) : nk_all;
@@ -562,7 +599,7 @@ __device__ __attribute__((always_inline)) inline void gemm_tile(const Dev& g, co
                 }
             }
         };
-        if (g.K % BK == 0) run(std::true_type{}); else run(std::false_type{});
+        if (g.K % BK == 0 && (!kHeadDw || g.K > 0)) run(std::true_type{}); else run(std::false_type{});
         __syncthreads(); // every wave is done with its stages
         f32x4* const parts = (f32x4*)smem; // [wave][fragment][lane]
 #pragma unroll
@@ -861,7 +898,7 @@ __device__ __attribute__((always_inline)) inline void gemm_tile(const Dev& g, co
     //                             n = n0 + (column base of block j) + 16 (q & 1) + 4 lq + r.
     if constexpr (kSplit) {
         // fp32 partial sums of this depth range, 16 bytes (4 columns) per store; N % 8 == 0
-        float* P = g.partial + ((int64_t)kpart * g.nbatch + batch) * g.M * g.N;
+        float* P = g.partial + (is_head(OP) ? (int64_t)kpart * head.out_rows : ((int64_t)kpart * g.nbatch + batch) * g.M) * g.N;
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
 #pragma unroll
@@ -914,7 +951,8 @@ __device__ __attribute__((always_inline)) inline void gemm_tile(const Dev& g, co
     // the wait would be for everything).  Offsets inside a wave's part stay below 2^30 (see gemm_mfma_supported).
     constexpr uint32_t kOutside = 0x80000000u;
     const int wrow0 = m0 + WM * wm; // first output row of this wave
-    const int wrows = g.M - wrow0 < 0 ? 0 : (g.M - wrow0 > WM ? WM : g.M - wrow0); // its rows inside the matrix
+    const int out_rows = kHeadDw ? head.out_rows : g.M;
+    const int wrows = out_rows - wrow0 < 0 ? 0 : (out_rows - wrow0 > WM ? WM : out_rows - wrow0); // its rows inside the matrix
     // the base is the same in all lanes; saying so keeps the resource in scalar registers
     auto uniform_rsrc = [](const uint16_t* base, uint32_t bytes) {
         const uint64_t a = (uint64_t)base;
@@ -1016,8 +1054,87 @@ __device__ __attribute__((always_inline)) inline void gemm_tile(const Dev& g, co
         }
     };
 
+    if constexpr (EPI == EPI_CODES) {
+        // A row's WN columns lie with the four lanes l16, l16 + 16, ..: their largest logit and the sum of the others' powers beside it, in
+        // fp32, and every logit's distance from it as 16 bits (kCodeRange).
+        int label[FM][2];
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int r = 32 * i + 16 * h + l16;
+                label[i][h] = head.labels && r < wrows ? head.labels[wrow0 + r] - wcol0 : -1;
+            }
+        const bool edge = wcol0 + WN > g.N;
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float v[FN][2][4], m = -INFINITY, sum = 0.f;
+#pragma unroll
+                for (int j = 0; j < FN; ++j)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const float x = acc[i][j][2 * h + c][r];
+                            v[j][c][r] = edge && wcol0 + 32 * j + 16 * c + 4 * lq + r >= g.N ? -INFINITY : x;
+                            m = fmaxf(m, v[j][c][r]);
+                        }
+                m = across_rows<true>(m);
+                const float from = m == -INFINITY ? 0.f : m; // nothing but -inf: a sum of 0
+#pragma unroll
+                for (int j = 0; j < FN; ++j)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        float t[4];
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            t[r] = from - v[j][c][r];
+                            sum += __builtin_amdgcn_exp2f(t[r] * -head.rate);
+                        }
+                        if (head.codes)
+                            strip_put(strip0, 32 * j, 2 * h + c,
+                                      u32x2{code_pair(t[0] * head.to_code, t[1] * head.to_code), code_pair(t[2] * head.to_code, t[3] * head.to_code)});
+                    }
+                sum = across_rows<false>(sum);
+                const int row = 32 * i + 16 * h + l16;
+                if (lq == 0 && row < wrows && wcol0 < g.N) head.stats[(int64_t)(wrow0 + row) * head.nblk + wcol0 / WN] = float2{m, sum};
+                const int at = label[i][h];
+                if ((uint32_t)at < (uint32_t)WN && ((at >> 2) & 3) == lq) {
+#pragma unroll
+                    for (int j = 0; j < FN; ++j)
+#pragma unroll
+                        for (int c = 0; c < 2; ++c)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r)
+                                if (at == 32 * j + 16 * c + 4 * lq + r) head.at_label[wrow0 + row] = v[j][c][r];
+                }
+            }
+            if (head.codes) strip_store(strip0, g.C, g.ldc, i, std::integral_constant<int, kKeep>{});
+        }
+        return;
+    }
+    if constexpr (kHeadDw) {
+        if (head.piece > 0) { // this lane's accumulators of the tile, 16 bytes a lane side by side
+            f32x4* const sums = (f32x4*)head.sums + ((int64_t)(tile_m * g.tiles_n + tile_n) * NW + wave) * (FM * FN * 4 * 64) + lane;
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int j = 0; j < FN; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        f32x4* const at = sums + ((i * FN + j) * 4 + q) * 64;
+                        if (head.piece > 1) acc[i][j][q] += *at;
+                        if (head.piece < 3) *at = acc[i][j][q];
+                    }
+            if (head.piece < 3) return;
+        }
+    }
+
     // residual of a single-problem store (the skip connection of a block): fetched one fragment row ahead like G, U
-    constexpr bool kResidual = (EPI == EPI_STORE || EPI == EPI_DUAL_ACC) && !kBatched;
+    constexpr bool kResidual = (EPI == EPI_STORE || EPI == EPI_DUAL_ACC) && !kBatched && !is_head(OP);
     u32x4 rpre[kResidual ? NLD : 1];
     const bool has_r = kResidual && g.R != nullptr;
     if constexpr (kResidual) {
@@ -1353,8 +1470,8 @@ int describe(const GemmDesc& d, Dev& g) {
     const int ncols = EPI == EPI_SWIGLU_FWD ? BN / 2 : BN;
     g.tiles_n = (d.N + ncols - 1) / ncols;
     const int64_t ntiles = (int64_t)g.tiles_m * g.tiles_n;
-    constexpr bool kBatched = OP == OP_DW || OP == OP_DW_SPLIT || OP == OP_DW_TAIL;
-    const int ksplit = OP == OP_DW_SPLIT ? d.ksplit : 1;
+    constexpr bool kBatched = is_batched(OP);
+    const int ksplit = is_split(OP) ? d.ksplit : 1;
     const int nbatch = (kBatched ? d.nbatch : 1) * ksplit; // problems of the launch
     if (ntiles * nbatch > 0x7FFFFFFF) return SDP_ERR_SHAPE;
     g.ntot = (int)(ntiles * nbatch);
@@ -1470,10 +1587,11 @@ struct EpilogueCost {
     double e0, e1;
 };
 constexpr EpilogueCost epilogue_cost(int epi) {
-    return epi == EPI_SWIGLU_FWD ? EpilogueCost{5.0, 0.055} : epi == EPI_SWIGLU_BWD ? EpilogueCost{2.4, 0.36} : EpilogueCost{2.8, 0.03};
+    return epi == EPI_CODES ? EpilogueCost{4.0, 0.09} : epi == EPI_SWIGLU_FWD ? EpilogueCost{5.0, 0.055} : epi == EPI_SWIGLU_BWD ? EpilogueCost{2.4, 0.36} : EpilogueCost{2.8, 0.03};
 }
 // the SwiGLU-forward epilogue pairs gate and up columns inside a wave's columns and has no 192- or 64-wide variant
 constexpr bool shape_exists(int epi, int shape) {
+    if (epi == EPI_CODES) return shape != T256x192 && shape != T128x192; // blocks of 64 columns, of 32 with 64 x 64
     return epi != EPI_SWIGLU_FWD || (shape != T256x192 && shape != T128x192 && shape != T64x64);
 }
 
@@ -1855,6 +1973,132 @@ int gemm_mfma_bf16(const GemmDesc& d, hipStream_t s) {
     if (d.epilogue == EPI_SWIGLU_FWD) return launch<EPI_SWIGLU_FWD, OP_GATE_UP>(d, s);
     if (d.epilogue == EPI_SWIGLU_BWD) return launch<EPI_SWIGLU_BWD, OP_DACT>(d, s);
     return SDP_ERR_UNSUPPORTED;
+}
+
+// ---- the output head's contractions -----------------------------------------------------------------------------------
+namespace {
+
+template <int BM, int BN, int WAVES_M, int WAVES_N, int EPI, int OP, int KM>
+__global__ __launch_bounds__(WAVES_M* WAVES_N * 64, BM == 64 && BN == 64 ? 2 : 1) void sdp_head_gemm_kernel(Dev g, HeadArgs head) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    const int n = *head.live - head.base;
+    if constexpr (OP == OP_HEAD_DW) {
+        g.K = n < 0 ? 0 : n < g.K ? n : g.K;
+        if (g.K == 0 && head.piece == 2) return; // the sums stay
+    } else {
+        if (n <= 0) return;
+        g.M = n < g.M ? n : g.M;
+    }
+    gemm_tile<BM, BN, WAVES_M, WAVES_N, EPI, OP, KM>(g, (int)blockIdx.x, smem, head);
+}
+
+template <int BM, int BN, int WAVES_M, int WAVES_N, int EPI, int OP, int KM>
+int launch_head_cfg(const GemmDesc& d, const HeadArgs& head, hipStream_t s) {
+    constexpr int LDS = Geometry<BM, BN, WAVES_M, WAVES_N, EPI, KM>::LDS;
+    Dev g;
+    const int drc = describe<BM, BN, EPI, OP>(d, g);
+    if (drc != SDP_OK) return drc;
+    auto kern = sdp_head_gemm_kernel<BM, BN, WAVES_M, WAVES_N, EPI, OP, KM>;
+    static const hipError_t attr = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+    if (attr != hipSuccess) return SDP_ERR_HIP;
+    ProfileScope ps(d.name, s);
+    kern<<<dim3((unsigned)g.ntot), WAVES_M * WAVES_N * 64, LDS, s>>>(g, head);
+    return launch_status();
+}
+template <int EPI, int OP, int KM>
+int launch_head(const GemmDesc& d, const HeadArgs& head, Shape shape, hipStream_t s) {
+    if (shape == T256x256) return launch_head_cfg<256, 256, 2, 4, EPI, OP, KM>(d, head, s);
+    if (shape == T128x256) return launch_head_cfg<128, 256, 2, 4, EPI, OP, KM>(d, head, s);
+    if (shape == T128x128) return launch_head_cfg<128, 128, 4, 2, EPI, OP, KM>(d, head, s);
+    if (shape == T64x64) return launch_head_cfg<64, 64, 2, 2, EPI, OP, KM>(d, head, s);
+    if constexpr (EPI != EPI_CODES) {
+        if (shape == T256x192) return launch_head_cfg<256, 192, 4, 2, EPI, OP, KM>(d, head, s);
+        if (shape == T128x192) return launch_head_cfg<128, 192, 4, 2, EPI, OP, KM>(d, head, s);
+    }
+    return SDP_ERR_INVALID_ARG; // not reached: the shapes that choose_shape has for EPI
+}
+
+GemmDesc extents(int M, int N, int K) {
+    GemmDesc d;
+    d.M = M, d.N = N, d.K = K;
+    return d;
+}
+
+// Depth ranges of dX: its outputs are few and its depth is the vocabulary.  As many as the tiles' model, the traffic of the partial sums at 4 TB/s
+// and a launch more make worth it, each of 4 steps at least.
+int head_dx_ranges(int rows, int V, int d) {
+    const GemmDesc g = extents(rows, d, V);
+    const int nk = (V + BK - 1) / BK;
+    int best = 1;
+    double least = -1;
+    for (int r = 1; r <= 64; r += r < 4 ? 1 : r / 4) {
+        const int steps = (nk + r - 1) / r;
+        if (r > 1 && (steps < 4 || (nk + steps - 1) / steps != r)) continue; // no empty range
+        double cost = 0;
+        choose_shape<EPI_STORE>(g, 1, r, nullptr, &cost);
+        if (r > 1) cost += 3.0 + (double)r * rows * d * 8.0 / 4e6;
+        if (least < 0 || cost < least) least = cost, best = r;
+    }
+    return best;
+}
+
+// sums of the ranges of dX, in their order -> bf16 rows of the tokens; one thread per 8 columns
+__global__ __launch_bounds__(256) void head_dx_reduce_kernel(const float* partial, int ranges, int rows, int d, const int32_t* list, const int32_t* live, int base,
+                                                             uint16_t* dX) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int m = (int)(i / (d / 8)), n = (int)(i % (d / 8)) * 8;
+    if (m >= rows || m >= *live - base) return;
+    f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
+    for (int k = 0; k < ranges; ++k) {
+        const float* p = partial + ((int64_t)k * rows + m) * d + n;
+        a += *(const f32x4*)p;
+        b += *(const f32x4*)(p + 4);
+    }
+    *(u32x4*)(dX + (int64_t)list[m] * d + n) = u32x4{pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3]), pack_bf16(b[0], b[1]), pack_bf16(b[2], b[3])};
+}
+
+} // namespace
+
+int head_block(int rows, int V, int d) { return choose_shape<EPI_CODES>(extents(rows, V, d), 1, 1) == T64x64 ? 32 : 64; }
+
+int gemm_head_logits(const HeadGemm& h, float inv_tau, bool codes, float2* stats, int nblk, const int32_t* labels, float* at_label, hipStream_t s) {
+    GemmDesc d = extents(h.rows, h.V, h.d);
+    d.A = h.X, d.lda = h.d, d.B = h.W, d.ldb = h.d, d.epilogue = EPI_CODES, d.C = h.P, d.ldc = h.ldp, d.name = "head_logits";
+    HeadArgs a{};
+    a.live = h.live, a.base = h.base, a.rate = inv_tau * 1.44269504088896340736f, a.to_code = a.rate / kCodeRange;
+    a.codes = codes, a.stats = stats, a.nblk = nblk, a.labels = labels, a.at_label = at_label;
+    return launch_head<EPI_CODES, OP_HEAD_LOGITS, 0>(d, a, choose_shape<EPI_CODES>(d, 1, 1), s);
+}
+
+size_t head_dx_ws_bytes(int rows, int V, int d) {
+    const int r = head_dx_ranges(rows, V, d);
+    return r > 1 ? (size_t)r * rows * d * 4 : 0;
+}
+
+int gemm_head_dx(const HeadGemm& h, const int32_t* list, void* dX, float* split_ws, hipStream_t s) {
+    GemmDesc d = extents(h.rows, h.d, h.V);
+    d.A = h.P, d.lda = h.ldp, d.B = h.W, d.ldb = h.d, d.b_km = 1, d.C = dX, d.ldc = h.d, d.c_scatter = list, d.name = "head_dx";
+    HeadArgs a{};
+    a.live = h.live, a.base = h.base, a.out_rows = h.rows;
+    const int r = head_dx_ranges(h.rows, h.V, h.d);
+    if (r < 2) return launch_head<EPI_STORE, OP_HEAD_DX, 2>(d, a, choose_shape<EPI_STORE>(d, 1, 1), s);
+    d.ksplit = r, d.split_ws = split_ws;
+    const int rc = launch_head<EPI_STORE, OP_HEAD_DX_SPLIT, 2>(d, a, choose_shape<EPI_STORE>(d, 1, r), s);
+    if (rc != SDP_OK) return rc;
+    const int64_t threads = (int64_t)h.rows * (h.d / 8);
+    ProfileScope ps("head_dx_reduce", s);
+    head_dx_reduce_kernel<<<(unsigned)((threads + 255) / 256), 256, 0, s>>>(split_ws, r, h.rows, h.d, list, h.live, h.base, (uint16_t*)dX);
+    return launch_status();
+}
+
+size_t head_sums_bytes(int V, int d) { return (size_t)((V + 255) / 256 * 256) * ((d + 767) / 768 * 768) * 4; } // whole tiles of any shape
+
+int gemm_head_dw(const HeadGemm& h, void* dW, float* sums, int piece, hipStream_t s) {
+    GemmDesc d = extents((h.V + 7) / 8 * 8, h.d, h.rows); // columns of the logits' rows in whole chunks: the last ones are zeros
+    d.A = h.P, d.lda = h.ldp, d.a_km = 1, d.B = h.X, d.ldb = h.d, d.b_km = 1, d.C = dW, d.ldc = h.d, d.name = "head_dw";
+    HeadArgs a{};
+    a.live = h.live, a.base = h.base, a.out_rows = h.V, a.sums = sums, a.piece = piece;
+    return launch_head<EPI_STORE, OP_HEAD_DW, 3>(d, a, choose_shape<EPI_STORE>(d, 1, 1), s);
 }
 
 } // namespace sdp

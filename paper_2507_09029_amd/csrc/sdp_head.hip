@@ -1,0 +1,447 @@
+// The output head and its loss in one: logits Z = X W^T of the tokens that have a target, their loss, dX = dZ W and dW = dZ^T X, without Z.
+//
+// 6 T V d operations, three contractions of the same size, with [T][V] between them.  Bound by the matrix cores as soon as tokens are some
+// hundreds; by reading W and writing dW for a few.  The logits exist for a piece of tokens at a time, as large as SDP_HEAD_PIECE_BYTES: all V
+// columns of it are there before anything goes on, so that no contraction is done twice (pieces of the vocabulary would need the first one
+// again behind the softmax: 8 T V d).  A piece:
+//   gather   rows of X of its tokens, side by side; tokens without a target are left out, at the cost of a copy of X (one part in
+//            thousands of the contractions' time)
+//   logits   bf16: the contraction's epilogue takes each block's maximum and sum in fp32 and keeps a logit as 16 bits (kCodeRange)
+//   rows     a row's blocks -> its lse and loss; its codes -> its gradient, bf16, in their place.  4 bytes a logit moved beside 6 d operations
+//   dX, dW   contractions on what is stored; dW goes on from piece to piece in fp32 (head.sums), and is rounded once
+// fp32: the same with the logits themselves in fp32 (target_rows) and the fp32 contractions.
+#include <cmath>
+
+#include "sdp_internal.h"
+#include "sdp_loss_rows.h"
+#include "sdp_rows.h"
+#include "sdp_targets.h"
+
+namespace {
+
+using sdp::Row;
+using sdp::Targets;
+using sdp::u32x4;
+
+// tokens of 1024 threads' turn in the list's kernel: 16 a thread
+constexpr int kListTurn = 1024 * 16;
+
+// whether a token has an entry; a wave a token
+__global__ __launch_bounds__(256) void entries_kernel(Targets t, int T, int V, uint8_t* __restrict__ has) {
+    const int64_t token = (int64_t)sdp::group_id() * 4 + (threadIdx.x >> 6);
+    if (token >= T) return;
+    bool any = false;
+    for (int i = threadIdx.x & 63; i < t.k; i += 64) {
+        const int64_t at = token * t.k + i;
+        const float v = t.top_bf16 ? Row<1>::one((const uint16_t*)t.top + at) : ((const float*)t.top)[at];
+        any |= sdp::token_id(t.ids, t.wide, at, V) >= 0 && !(v == -INFINITY);
+    }
+    any = __any(any);
+    if ((threadIdx.x & 63) == 0) has[token] = any;
+}
+
+// list: the tokens with a target in order, from its front; the others as -1 - token, from its end.  *live: how many the first are.  One
+// workgroup: 16384 tokens are one turn.
+__global__ __launch_bounds__(1024) void list_kernel(const void* __restrict__ labels, int wide, const uint8_t* __restrict__ has, int T, int V,
+                                                    int32_t* __restrict__ list, int32_t* live) {
+    __shared__ int wave_sums[16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int before = 0; // tokens with a target in earlier turns
+    for (int64_t t0 = 0; t0 < T; t0 += kListTurn) {
+        const int64_t first = t0 + tid * 16;
+        uint32_t mask = 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (first + i < T && (has ? has[first + i] != 0 : sdp::token_id(labels, wide, first + i, V) >= 0)) mask |= 1u << i;
+        const int n = __popc(mask);
+        int upto = n; // over the wave, then the waves
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int x = __shfl_up(upto, d, 64);
+            if (lane >= d) upto += x;
+        }
+        if (lane == 63) wave_sums[wave] = upto;
+        __syncthreads();
+        int at = before + upto - n, all = 0;
+#pragma unroll
+        for (int w = 0; w < 16; ++w) {
+            if (w < wave) at += wave_sums[w];
+            all += wave_sums[w];
+        }
+        for (int i = 0; i < 16 && first + i < T; ++i) {
+            if (mask >> i & 1) list[at++] = (int32_t)(first + i);
+            else list[T - 1 - (first + i - at)] = -1 - (int32_t)(first + i); // first + i - at: those without before it
+        }
+        before += all;
+        __syncthreads();
+    }
+    if (tid == 0) *live = before;
+}
+
+struct Gather {
+    const void *X, *W;
+    void *Xc, *dX; // dX: zeros for tokens without a target, may be null
+    const int32_t* list;
+    Targets t;
+    int32_t* labels; // [row], -1 for none; or
+    float* z;        // [row][k]: the entries' logits
+    int rows, V, d;
+};
+
+// A workgroup a row.  bf16: of d a multiple of 8 and 16-byte aligned.
+template <int BF16, int TH>
+__global__ __launch_bounds__(TH) void gather_kernel(Gather a) {
+    typedef Row<BF16> Rw;
+    typedef typename Rw::Elem Elem;
+    constexpr int N = Rw::N;
+    const int64_t row = sdp::group_id();
+    if (row >= a.rows) return;
+    const int listed = a.list[row], tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, d = a.d, whole = Rw::whole(d);
+    const bool live = listed >= 0;
+    const int64_t token = live ? listed : -1 - listed;
+    const Elem* x = (const Elem*)a.X + token * d;
+    Elem* xc = (Elem*)a.Xc + row * d;
+    Elem* dx = (Elem*)a.dX + token * d;
+    if (!live) {
+        for (int e = tid * N; e < whole; e += TH * N) {
+            if (!BF16) Rw::store(xc, e, whole, u32x4{0, 0, 0, 0}); // the fp32 contractions go over all rows
+            if (a.dX) Rw::store(dx, e, whole, u32x4{0, 0, 0, 0});
+        }
+        if (whole + tid < d) {
+            if (!BF16) Rw::put(xc + whole + tid, 0.f);
+            if (a.dX) Rw::put(dx + whole + tid, 0.f);
+        }
+        if (a.labels && tid == 0) a.labels[row] = -1;
+        return;
+    }
+    if (a.labels && tid == 0) a.labels[row] = sdp::token_id(a.t.ids, a.t.wide, token, a.V);
+    for (int e = tid * N; e < whole; e += TH * N) *(typename Rw::Piece*)(xc + e) = Rw::load_some(x, e, whole); // read next
+    if (whole + tid < d) xc[whole + tid] = x[whole + tid];
+    if constexpr (BF16) {
+        if (!a.z) return;
+        // the entries' logits in fp32, a wave four entries at a time
+        constexpr int WAVES = TH / 64, M = 4;
+        for (int i0 = wave * M; i0 < a.t.k; i0 += WAVES * M) {
+            const Elem* w[M];
+            float sum[M];
+            int id[M];
+#pragma unroll
+            for (int j = 0; j < M; ++j) {
+                id[j] = i0 + j < a.t.k ? sdp::token_id(a.t.ids, a.t.wide, token * a.t.k + i0 + j, a.V) : -1;
+                w[j] = (const Elem*)a.W + (int64_t)(id[j] < 0 ? 0 : id[j]) * d;
+                sum[j] = 0.f;
+            }
+            for (int e = lane * N; e < d; e += 64 * N) {
+                float xv[N];
+                Rw::unpack(Rw::load_some(x, e, whole), xv);
+#pragma unroll
+                for (int j = 0; j < M; ++j) {
+                    float wv[N];
+                    Rw::unpack(Rw::load_some(w[j], e, whole), wv);
+#pragma unroll
+                    for (int n = 0; n < N; ++n) sum[j] = fmaf(xv[n], wv[n], sum[j]);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < M; ++j) {
+                const float z = sdp::wave_sum(sum[j]);
+                if (lane == 0 && i0 + j < a.t.k) a.z[row * a.t.k + i0 + j] = z;
+            }
+        }
+    }
+}
+
+struct CodeRows {
+    uint16_t* P; // may be null: the loss alone
+    int64_t ldp;
+    const float2* stats;
+    int nblk, shift; // columns of a block: 1 << shift
+    const float* z;  // [row][k]
+    Targets t;
+    const int32_t* list;
+    float *kl, *lse;
+    int rows, V;
+};
+
+// A row of codes and its blocks' statistics -> its loss, lse and gradient.  One workgroup a row.
+constexpr int kCodeThreads = 256;
+__global__ __launch_bounds__(kCodeThreads) void code_rows_kernel(CodeRows a) {
+    typedef Row<1> Rw;
+    constexpr int TH = kCodeThreads, WAVES = TH / 64;
+    __shared__ float lds[3][2][WAVES];
+    extern __shared__ unsigned char entry_lds[];
+    const int64_t row = sdp::group_id();
+    if (row >= a.rows) return;
+    const int tid = threadIdx.x, k = a.t.k, listed = a.list[row];
+    if (listed < 0) {
+        if (tid == 0) {
+            a.kl[-1 - listed] = 0.f;
+            if (a.lse) a.lse[-1 - listed] = 0.f;
+        }
+        return;
+    }
+    const sdp::Entries en(entry_lds, k);
+    const float2* stats = a.stats + row * a.nblk;
+    float vmax = en.load<TH>(a.t, listed, a.V);
+    for (int i = tid; i < k; i += TH) en.z[i] = en.id[i] >= 0 ? a.z[row * k + i] : 0.f;
+    const float rate = sdp::kLog2e * a.t.inv_tau;
+    float m = -INFINITY, sum = 0.f;
+    for (int b = tid; b < a.nblk; b += TH) {
+        const float2 s = stats[b];
+        const float top = fmaxf(m, s.x), from = top == -INFINITY ? 0.f : top;
+        sum = sum * __builtin_amdgcn_exp2f((m - from) * rate) + s.y * __builtin_amdgcn_exp2f((s.x - from) * rate);
+        m = top;
+    }
+    const float mine = m;
+    sdp::group_both<WAVES, true>(m, vmax, lds[0]);
+    // a thread without blocks, or with nothing but -inf: 0; nothing but -inf in the whole row: NaN
+    sum *= __builtin_amdgcn_exp2f((mine - m) * rate);
+    float of_entries = en.sum<TH>(a.t, vmax);
+    sdp::group_both<WAVES, false>(sum, of_entries, lds[1]);
+    const float log_sum = logf(sum);
+    float mass = 0.f, kl = 0.f;
+    en.masses<TH>(a.t, listed, vmax, of_entries, [&](int i, float q, float log_q) {
+        mass += q;
+        if (q != 0.f) kl += q * ((log_q - (en.z[i] - m) * a.t.inv_tau) + log_sum);
+    });
+    sdp::group_both<WAVES, false>(mass, kl, lds[2]);
+    if (!a.t.top_lse && mass == mass) mass = 1.f;
+    if (tid == 0) {
+        a.kl[listed] = !a.t.top && kl < 0.f ? 0.f : kl; // a label's logit that is all of its row's sum, but for roundings
+        if (a.lse) a.lse[listed] = m * a.t.inv_tau + log_sum;
+    }
+    if (!a.P) return;
+    const float c = a.t.scale * (a.t.scale_dev ? *a.t.scale_dev : 1.f) * a.t.inv_tau, inv = c * mass / sum;
+    uint16_t* p = a.P + row * a.ldp;
+    constexpr float kStep = sdp::kCodeRange / 65535.f;
+    const int end = (a.V + 7) / 8 * 8; // codes of columns behind V say 0
+    auto value = [&](uint32_t code, float from) { return code == 65535u ? 0.f : __builtin_amdgcn_exp2f(fmaf((float)code, -kStep, from)) * inv; };
+    auto turn = [&](int e, const u32x4& w, float block) {
+        const float from = (block - m) * rate;
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[2 * i] = value(w[i] & 0xFFFFu, from), v[2 * i + 1] = value(w[i] >> 16, from);
+        *(u32x4*)(p + e) = Rw::pack(v); // read next
+    };
+    constexpr int U = 4;
+    for (int e0 = tid * 8; e0 < end; e0 += U * TH * 8) {
+        u32x4 w[U];
+        float block[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int e = min(e0 + u * TH * 8, end - 8);
+            w[u] = *(const u32x4*)(p + e);
+            block[u] = stats[e >> a.shift].x;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (e0 + u * TH * 8 < end) turn(e0 + u * TH * 8, w[u], block[u]);
+    }
+    // The entries' elements are written twice: the first time has to have reached memory, whichever wave it came from.
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    for (int i = tid; i < k; i += TH)
+        if (en.id[i] >= 0) Rw::put(p + en.id[i], __builtin_amdgcn_exp2f((en.z[i] - m) * rate) * inv - c * en.all_of(i, k));
+}
+
+__global__ __launch_bounds__(256) void zero_kernel(uint16_t* p, int64_t n) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += 4096 * 256) p[i] = 0;
+}
+
+// What a call needs, and where it lies in the workspace
+struct Plan {
+    int rows = 0, pieces = 0, block = 0, nblk = 0; // tokens of a piece; columns of a statistic's block
+    int64_t ldz = 0;                               // of the codes, or of the fp32 logits
+    size_t list = 0, live = 0, has = 0, X = 0, Z = 0, stats = 0, labels = 0, z = 0, sums = 0, split = 0, bytes = 0;
+};
+Plan plan(int dtype, int T, int V, int d, int k, bool teacher, bool dx, bool dw) {
+    Plan p;
+    const bool bf16 = dtype == SDP_BF16, grads = dx || dw;
+    // per token: codes and statistics, or logits
+    const size_t row = bf16 ? (grads ? ((size_t)V + 191) * 2 : 0) + ((size_t)V + 31) / 32 * 8 : ((size_t)V + 3) * 4;
+    const int64_t most = (int64_t)(SDP_HEAD_PIECE_BYTES / row) / 64 * 64;
+    const int64_t rows_max = most < 64 ? 64 : most;
+    p.pieces = (int)((T + rows_max - 1) / rows_max);
+    p.rows = T;
+    if (p.pieces > 1) {
+        p.rows = (int)(((T + p.pieces - 1) / p.pieces + 63) / 64 * 64); // equal pieces
+        p.pieces = (T + p.rows - 1) / p.rows;
+    }
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += sdp::round_up(bytes, 256);
+        return here;
+    };
+    const size_t rows = (size_t)p.rows;
+    p.list = take((size_t)T * 4), p.live = take(4);
+    if (teacher) p.has = take((size_t)T);
+    p.X = take(rows * d * (bf16 ? 2 : 4));
+    if (bf16) {
+        p.ldz = sdp::line_ld(V, p.rows);
+        p.block = sdp::head_block(p.rows, V, d), p.nblk = (V + p.block - 1) / p.block;
+        if (grads) p.Z = take(rows * p.ldz * 2);
+        p.stats = take(rows * p.nblk * 8);
+        if (!teacher) p.labels = take(rows * 4);
+        p.z = take(rows * k * 4);
+        if (dw && p.pieces > 1) p.sums = take(sdp::head_sums_bytes(V, d));
+        if (dx) p.split = take(sdp::head_dx_ws_bytes(p.rows, V, d));
+    } else {
+        p.ldz = (V + 3) / 4 * 4;
+        p.Z = take(rows * p.ldz * 4);
+    }
+    p.bytes = at;
+    return p;
+}
+
+struct Call {
+    int dtype, T, V, d;
+    const void *X, *W;
+    Targets t;
+    float *kl, *lse;
+    void *dX, *dW;
+    float* loss;
+};
+
+int run(const Call& c, unsigned char* ws, hipStream_t s) {
+    const bool bf16 = c.dtype == SDP_BF16, teacher = c.t.top != nullptr, grads = c.dX || c.dW;
+    const Plan p = plan(c.dtype, c.T, c.V, c.d, c.t.k, teacher, c.dX, c.dW);
+    int32_t *list = (int32_t*)(ws + p.list), *live = (int32_t*)(ws + p.live);
+    uint8_t* has = teacher ? ws + p.has : nullptr;
+    if (teacher) {
+        sdp::ProfileScope ps("head_entries", s);
+        entries_kernel<<<sdp::grid_of((c.T + 3) / 4), 256, 0, s>>>(c.t, c.T, c.V, has);
+    }
+    {
+        sdp::ProfileScope ps("head_list", s);
+        list_kernel<<<1, 1024, 0, s>>>(c.t.ids, c.t.wide, has, c.T, c.V, list, live);
+    }
+    int rc = sdp::launch_status();
+    for (int i = 0; i < p.pieces && rc == SDP_OK; ++i) {
+        const int base = i * p.rows, rows = c.T - base < p.rows ? c.T - base : p.rows;
+        Gather g{c.X, c.W, ws + p.X, c.dX, list + base, c.t, nullptr, nullptr, rows, c.V, c.d};
+        if (bf16 && !teacher) g.labels = (int32_t*)(ws + p.labels);
+        if (bf16 && teacher) g.z = (float*)(ws + p.z);
+        {
+            sdp::ProfileScope ps("head_gather", s);
+            if (!bf16) gather_kernel<0, 64><<<sdp::grid_of(rows), 64, 0, s>>>(g);
+            else if (teacher) gather_kernel<1, 256><<<sdp::grid_of(rows), 256, 0, s>>>(g);
+            else gather_kernel<1, 64><<<sdp::grid_of(rows), 64, 0, s>>>(g);
+        }
+        rc = sdp::launch_status();
+        if (rc != SDP_OK) return rc;
+        if (bf16) {
+            sdp::HeadGemm h;
+            h.X = ws + p.X, h.W = c.W, h.P = ws + p.Z, h.ldp = p.ldz, h.rows = p.rows, h.V = c.V, h.d = c.d, h.live = live, h.base = base;
+            float2* stats = (float2*)(ws + p.stats);
+            float* z = (float*)(ws + p.z);
+            rc = sdp::gemm_head_logits(h, c.t.inv_tau, grads, stats, p.nblk, g.labels, z, s);
+            if (rc != SDP_OK) return rc;
+            const CodeRows r{grads ? (uint16_t*)h.P : nullptr, p.ldz, stats, p.nblk, p.block == 64 ? 6 : 5, z, c.t, list + base, c.kl, c.lse, rows, c.V};
+            {
+                sdp::ProfileScope ps("head_rows", s);
+                code_rows_kernel<<<sdp::grid_of(rows), kCodeThreads, sdp::Entries::bytes(c.t.k), s>>>(r);
+            }
+            rc = sdp::launch_status();
+            if (rc == SDP_OK && c.dX) rc = sdp::gemm_head_dx(h, list + base, c.dX, (float*)(ws + p.split), s);
+            if (rc == SDP_OK && c.dW)
+                rc = sdp::gemm_head_dw(h, c.dW, (float*)(ws + p.sums), p.pieces == 1 ? 0 : i == 0 ? 1 : i == p.pieces - 1 ? 3 : 2, s);
+            continue;
+        }
+        sdp::GemmDesc d;
+        d.M = rows, d.N = c.V, d.K = c.d, d.A = ws + p.X, d.lda = c.d, d.B = c.W, d.ldb = c.d, d.C = ws + p.Z, d.ldc = p.ldz, d.name = "head_logits";
+        rc = sdp::gemm_f32(d, s);
+        if (rc != SDP_OK) return rc;
+        sdp::TargetRows r;
+        r.Z = ws + p.Z, r.dZ = grads ? ws + p.Z : nullptr, r.ldz = p.ldz, r.t = c.t, r.kl = c.kl, r.lse = c.lse, r.rows = rows, r.V = c.V, r.list = list + base;
+        rc = sdp::target_rows(SDP_F32, r, "head_rows", s);
+        if (rc == SDP_OK && c.dX) {
+            sdp::GemmDesc x;
+            x.M = rows, x.N = c.d, x.K = c.V, x.A = ws + p.Z, x.lda = p.ldz, x.B = c.W, x.ldb = c.d, x.b_km = 1, x.C = c.dX, x.ldc = c.d;
+            x.c_scatter = list + base, x.name = "head_dx";
+            rc = sdp::gemm_f32(x, s);
+        }
+        if (rc == SDP_OK && c.dW) {
+            sdp::GemmDesc w;
+            w.M = c.V, w.N = c.d, w.K = rows, w.A = ws + p.Z, w.lda = p.ldz, w.a_km = 1, w.B = ws + p.X, w.ldb = c.d, w.b_km = 1, w.C = c.dW, w.ldc = c.d;
+            if (i > 0) w.R = c.dW, w.ldr = c.d; // the pieces before
+            w.name = "head_dw";
+            rc = sdp::gemm_f32(w, s);
+        }
+    }
+    if (rc != SDP_OK || !c.loss) return rc;
+    return sdp::loss_sum(c.kl, c.T, c.t.scale, c.t.scale_dev, c.loss, s);
+}
+
+bool sizes_ok(int dtype, int T, int V, int d, int k) {
+    if (T > SDP_EMBED_MAX_TOKENS || V >= 1 << 22 || d > SDP_MAX_EXTENT || k > SDP_MAX_ENTRIES) return false;
+    if ((int64_t)V * d >= (int64_t)1 << 31) return false;
+    return dtype != SDP_BF16 || (d % 8 == 0 && d < 1 << 22);
+}
+size_t workspace(int dtype, int T, int V, int d, int k, bool teacher, bool dx, bool dw) {
+    if ((dtype != SDP_F32 && dtype != SDP_BF16) || T < 1 || V < 1 || d < 1 || k < 1 || !sizes_ok(dtype, T, V, d, k)) return 0;
+    return plan(dtype, T, V, d, k, teacher, dx, dw).bytes;
+}
+
+int head(const Call& c, int id_type, int top_dtype, float temperature, void* ws, size_t ws_bytes, void* stream) {
+    const bool teacher = top_dtype >= 0;
+    if ((c.dtype != SDP_F32 && c.dtype != SDP_BF16) || (id_type != SDP_I32 && id_type != SDP_I64)) return SDP_ERR_INVALID_ARG;
+    if (teacher && top_dtype != SDP_F32 && top_dtype != SDP_BF16) return SDP_ERR_INVALID_ARG;
+    if (c.T < 0 || c.V < 1 || c.d < 1 || c.t.k < 1 || !sdp::temperature_ok(temperature) || !std::isfinite(c.t.scale)) return SDP_ERR_INVALID_ARG;
+    if (!sizes_ok(c.dtype, c.T, c.V, c.d, c.t.k)) return SDP_ERR_SHAPE;
+    const bool bf16 = c.dtype == SDP_BF16;
+    const size_t es = bf16 ? 2 : 4, is = id_type == SDP_I64 ? 8 : 4, ts = top_dtype == SDP_BF16 ? 2 : 4, st = (size_t)c.T * 4;
+    if (!c.W || (c.T > 0 && (!c.X || !c.t.ids || (teacher && !c.t.top) || !c.kl))) return SDP_ERR_INVALID_ARG;
+    for (const void* p : {c.X, c.W, (const void*)c.dX, (const void*)c.dW})
+        if (!sdp::aligned_to(p, bf16 ? 16 : 4)) return SDP_ERR_INVALID_ARG;
+    if (!sdp::aligned_to(c.t.ids, is) || (teacher && !sdp::aligned_to(c.t.top, ts))) return SDP_ERR_INVALID_ARG;
+    for (const float* p : {c.t.top_lse, c.t.scale_dev, (const float*)c.kl, (const float*)c.lse, (const float*)c.loss})
+        if (!sdp::aligned_to(p, 4)) return SDP_ERR_INVALID_ARG;
+    const size_t tokens = (size_t)c.T * c.d * es, vocabulary = (size_t)c.V * c.d * es, entries = (size_t)c.T * c.t.k;
+    const size_t need = workspace(c.dtype, c.T, c.V, c.d, c.t.k, teacher, c.dX, c.dW);
+    const sdp::Extent eX{c.X, tokens}, eW{c.W, vocabulary}, ei{c.t.ids, entries * is}, ev{c.t.top, teacher ? entries * ts : 0},
+        eL{c.t.top_lse, c.t.top_lse ? st : 0}, ec{c.t.scale_dev, c.t.scale_dev ? 4u : 0u}, on{c.kl, st}, os{c.lse, c.lse ? st : 0},
+        ox{c.dX, c.dX ? tokens : 0}, ow{c.dW, c.dW ? vocabulary : 0}, o1{c.loss, c.loss ? 4u : 0u};
+    if ((c.dX != c.X && sdp::overlap({ox}, {eX})) || sdp::overlap({on, os, ow, o1}, {eX}) || sdp::overlap({on, os, ox, ow, o1}, {eW, ei, ev, eL, ec}) ||
+        sdp::overlap({on}, {os, ox, ow, o1}) || sdp::overlap({os}, {ox, ow, o1}) || sdp::overlap({ox}, {ow, o1}) || sdp::overlap({ow}, {o1}))
+        return SDP_ERR_INVALID_ARG;
+    hipStream_t s = (hipStream_t)stream;
+    if (c.T == 0) {
+        if (c.dW) { // no token: zeros
+            zero_kernel<<<4096, 256, 0, s>>>((uint16_t*)c.dW, (int64_t)(vocabulary / 2));
+            const int rc = sdp::launch_status();
+            if (rc != SDP_OK) return rc;
+        }
+        return c.loss ? sdp::loss_sum(c.kl, 0, c.t.scale, c.t.scale_dev, c.loss, s) : SDP_OK;
+    }
+    if (!ws || ws_bytes < need || !sdp::aligned_to(ws, 256)) return SDP_ERR_WORKSPACE;
+    const sdp::Extent scratch{ws, need};
+    if (sdp::overlap({scratch}, {eX, eW, ei, ev, eL, ec, on, os, ox, ow, o1})) return SDP_ERR_INVALID_ARG;
+    return run(c, (unsigned char*)ws, s);
+}
+
+} // namespace
+
+extern "C" size_t sdp_head_loss_workspace_bytes(int dtype, int T, int V, int d, int want_dx, int want_dw) {
+    return workspace(dtype, T, V, d, 1, false, want_dx, want_dw);
+}
+
+extern "C" int sdp_head_loss(int dtype, int id_type, int T, int V, int d, float scale, const void* X, const void* W, const void* labels,
+                             const float* scale_dev, float* nll, float* lse, void* dX, void* dW, float* loss, void* ws, size_t ws_bytes,
+                             void* stream) {
+    const Call c{dtype, T, V, d, X, W, {labels, nullptr, nullptr, 1, id_type == SDP_I64, 0, 1.f, scale, scale_dev}, nll, lse, dX, dW, loss};
+    return head(c, id_type, -1, 1.f, ws, ws_bytes, stream);
+}
+
+extern "C" size_t sdp_head_distill_workspace_bytes(int dtype, int T, int V, int d, int k, int want_dx, int want_dw) {
+    return workspace(dtype, T, V, d, k, true, want_dx, want_dw);
+}
+
+extern "C" int sdp_head_distill(int dtype, int id_type, int top_dtype, int T, int V, int d, int k, float temperature, float scale, const void* X,
+                                const void* W, const void* ids, const void* top, const float* top_lse, const float* scale_dev, float* kl,
+                                float* lse, void* dX, void* dW, float* loss, void* ws, size_t ws_bytes, void* stream) {
+    if (top_dtype < 0) return SDP_ERR_INVALID_ARG;
+    const Call c{dtype, T, V, d, X, W, {ids, top, top_lse, k, id_type == SDP_I64, top_dtype == SDP_BF16, 1.f / temperature, scale, scale_dev},
+                 kl, lse, dX, dW, loss};
+    return head(c, id_type, top_dtype, temperature, ws, ws_bytes, stream);
+}

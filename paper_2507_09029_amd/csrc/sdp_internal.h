@@ -108,6 +108,7 @@ enum Epilogue {
     EPI_STORE = 0,       // C[rc(m) * ldc + n] = acc      (rc: optional row scatter; rc(m) < 0 drops row m)
     EPI_DUAL_ACC = 1,    // as STORE with acc = A.B + A2.B2
     EPI_SWIGLU_FWD = 2,  // g = A.B, u = A.B2: G = g, U = u, Act = silu(g) * u, all [M][N] (ld = ldc; Act: ldc3)
+    EPI_CODES = 4,       // the output head's logits: statistics of blocks of columns and 16-bit codes (gemm_head_logits)
     EPI_SWIGLU_BWD = 3   // da = A.B; with g = Gin[m][n], u = Uin[m][n]  (ld = ldg):
                          //   dU = da silu(g), dG = da u silu'(g), act = silu(g) u, all [M][N] (ld = ldc);
                          //   plain bf16 kernel: with cidx != null also the column-compacted copies [M][pc]
@@ -191,7 +192,7 @@ struct GemmDesc {
 };
 
 // tags that give each call site of the MFMA contraction its own kernel symbol
-enum GemmOp { OP_GATE_UP = 0, OP_DOWN = 1, OP_DACT = 2, OP_DX = 3, OP_DW = 4, OP_DW_SPLIT = 5, OP_DW_TAIL = 6 };
+enum GemmOp { OP_GATE_UP = 0, OP_DOWN = 1, OP_DACT = 2, OP_DX = 3, OP_DW = 4, OP_DW_SPLIT = 5, OP_DW_TAIL = 6, OP_HEAD_LOGITS = 7, OP_HEAD_DX = 8, OP_HEAD_DX_SPLIT = 9, OP_HEAD_DW = 10 };
 
 // fp32 contraction on the matrix cores, any shape.
 int gemm_f32(const GemmDesc& g, hipStream_t s);
@@ -199,6 +200,30 @@ int gemm_f32(const GemmDesc& g, hipStream_t s);
 // with depth-major right operands, none of whose outputs shares memory with an operand, as one launch.  SDP_ERR_UNSUPPORTED: not
 // these; nothing was launched.
 int gemm_f32_group(const GemmDesc* d, int n, const char* name, hipStream_t s);
+// ---- the output head's contractions (bf16), of `rows` tokens, of whom those from number `base` on have a target: min(rows, *live - base) -----
+struct HeadGemm {
+    const void* X = nullptr; // [rows][d], theirs without gaps
+    const void* W = nullptr; // [V][d]
+    void* P = nullptr;       // [rows][ldp]: codes of their logits, then the logits' gradient
+    int64_t ldp = 0;
+    int rows = 0, V = 0, d = 0;
+    const int32_t* live = nullptr;
+    int base = 0;
+};
+// A logit is kept as its distance from the largest of its block of columns: 16 bits for 0 .. kCodeRange in powers of two, after the division
+// by the temperature.  A step is 0.0015, so that a probability made from it is 5.1e-4 off at most and 2.9e-4 in the mean square: a sixth of what
+// its rounding to bf16 for the products costs next, which is thus the only one that counts (the probability itself as bf16, and again
+// as bf16 after its row's sum is known: twice).  From kCodeRange on, 2^-96 of the block's largest, it is 0.
+constexpr float kCodeRange = 96.f;
+// columns of a block: (largest logit, sum of the powers of their differences) of each go into stats [rows][nblk]
+int head_block(int rows, int V, int d);
+int gemm_head_logits(const HeadGemm& h, float inv_tau, bool codes, float2* stats, int nblk, const int32_t* labels, float* at_label, hipStream_t s);
+// dX[list[row]] = P W, with scratch of head_dx_ws_bytes
+size_t head_dx_ws_bytes(int rows, int V, int d);
+int gemm_head_dx(const HeadGemm& h, const int32_t* list, void* dX, float* split_ws, hipStream_t s);
+// dW = P^T X over pieces of tokens (piece: 0 the only one, 1 first, 2 between, 3 last), which share sums of head_sums_bytes
+size_t head_sums_bytes(int V, int d);
+int gemm_head_dw(const HeadGemm& h, void* dW, float* sums, int piece, hipStream_t s);
 // Plain LDS-tiled bf16 contraction, any shape: what the MFMA kernel's address ranges do not take.
 int gemm_simple(const GemmDesc& g, hipStream_t s);
 // bf16 MFMA contraction; returns SDP_ERR_UNSUPPORTED when the shape / alignment does not fit.
@@ -287,5 +312,30 @@ int copy_rows_f32(const float* in, const int32_t* rows, int R, int C, float* out
 // crank[n] for n < N from the ascending list cidx[0 .. pc): the number of listed columns below n if n is listed,
 // else -1 - that number
 int column_ranks(const int32_t* cidx, int pc, int N, int32_t* crank, hipStream_t s);
+
+// ---- losses --------------------------------------------------------------------------------------
+// *loss = scale scale_dev[0] sum of T values, in fp64 in a fixed order
+int loss_sum(const float* of, int T, float scale, const float* scale_dev, float* loss, hipStream_t s);
+
+// What rows of logits are held against: k entries a token of a teacher, or (top null, k = 1) its label.
+struct Targets {
+    const void *ids = nullptr, *top = nullptr; // [T][k]
+    const float* top_lse = nullptr;            // [T], optional
+    int k = 1, wide = 0, top_bf16 = 0;         // wide: 64-bit ids
+    float inv_tau = 1.f;
+    float scale = 1.f;
+    const float* scale_dev = nullptr;
+};
+// Rows of logits in memory against their targets: the divergence (or the label's nll), lse and gradient of each.
+struct TargetRows {
+    const void* Z = nullptr;
+    void* dZ = nullptr; // may be null
+    int64_t ldz = 0;
+    Targets t;
+    float *kl = nullptr, *lse = nullptr; // [token]; lse may be null
+    int rows = 0, V = 0;
+    const int32_t* list = nullptr; // token of every row, -1 - token where it has no target; null: row r is token r's, which may have none
+};
+int target_rows(int dtype, const TargetRows& r, const char* name, hipStream_t s);
 
 } // namespace sdp

@@ -15,14 +15,16 @@
 #include <type_traits>
 
 #include "sdp_internal.h"
+#include "sdp_loss_rows.h"
 #include "sdp_rows.h"
 
 namespace {
 
+using sdp::group_all;
+using sdp::kLog2e;
+using sdp::minus_inf;
 using sdp::Row;
 using sdp::u32x4;
-
-constexpr float kLog2e = 1.44269504088896340736f;
 
 struct Loss {
     const void *Z, *labels;
@@ -33,24 +35,6 @@ struct Loss {
     int64_t ldz;
     float scale;
 };
-
-// maximum / sum over a workgroup, in a fixed order; every thread has the result
-template <int WAVES, bool MAX>
-__device__ inline float group_all(float x, float* lds) {
-    x = MAX ? sdp::wave_max(x) : sdp::wave_sum(x);
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
-    __syncthreads();
-    x = lds[0];
-#pragma unroll
-    for (int i = 1; i < WAVES; ++i) x = MAX ? fmaxf(x, lds[i]) : x + lds[i];
-    return x;
-}
-
-// value of a piece's word behind the row's end: -inf
-template <int BF16>
-constexpr uint32_t minus_inf() {
-    return BF16 ? 0xFF80FF80u : 0xFF800000u;
-}
 
 // PIECES > 0: pieces a lane holds, the row has no more; 0: the row is read again for the sum, and again for the gradient
 template <int BF16, int WAVES, int PIECES, int ONCE>
@@ -209,41 +193,12 @@ __global__ __launch_bounds__(1024) void label_scale_kernel(const void* __restric
     if (threadIdx.x == 0) *scale = 1.0f / (float)(n > 1 ? n : 1);
 }
 
-// Waves of a row and pieces of a lane: the first pair in this order that holds the row.  Few waves leave no lane idle and wait for
-// each other less, many keep the registers few enough for two workgroups on a CU, so that one loads while the other computes or stores.  bf16,
-// us: 8192 x 1024 two waves of one piece 7, four 12.6; 8192 x 4000 4 x 2 23.3, 8 x 1 30.8; 8192 x 8000 4 x 4 45.7, 8 x 2 48.1, 16 x 1 65.8; 4096 x 16000
-// 8 x 4 47.4, 16 x 2 50.9; 8192 x 32000 16 x 4 172, 8 x 8 178, 4 x 16 181; 1000 x 50001 16 x 7 40.5, 8 x 16 43; 1000 x 65536 8 x 16 53.1, 16 x 8 (66
-// registers, one workgroup) 59.6.
-template <class F>
-void by_row(int bf16, int V, F&& launch) {
-    const int n = bf16 ? 8 : 4;
-    auto with = [&](auto b) {
-        const int64_t pieces = ((int64_t)V + n - 1) / n;
-#define SDP_LOSS_ROW(WAVES, PIECES) \
-    if (pieces <= WAVES * 64 * PIECES) return launch(b, std::integral_constant<int, WAVES>{}, std::integral_constant<int, PIECES>{})
-        SDP_LOSS_ROW(1, 1);
-        SDP_LOSS_ROW(2, 1);
-        SDP_LOSS_ROW(4, 1);
-        SDP_LOSS_ROW(4, 2);
-        SDP_LOSS_ROW(4, 4);
-        SDP_LOSS_ROW(8, 3);
-        SDP_LOSS_ROW(8, 4);
-        SDP_LOSS_ROW(8, 6);
-        SDP_LOSS_ROW(16, 4);
-        SDP_LOSS_ROW(16, 5);
-        SDP_LOSS_ROW(16, 6);
-        SDP_LOSS_ROW(16, 7);
-        SDP_LOSS_ROW(8, 16);
-        SDP_LOSS_ROW(16, 12);
-        SDP_LOSS_ROW(16, 16);
-#undef SDP_LOSS_ROW
-        launch(b, std::integral_constant<int, 16>{}, std::integral_constant<int, 0>{});
-    };
-    if (bf16) with(std::integral_constant<int, 1>{});
-    else with(std::integral_constant<int, 0>{});
-}
-
 } // namespace
+
+int sdp::loss_sum(const float* of, int T, float scale, const float* scale_dev, float* loss, hipStream_t s) {
+    loss_sum_kernel<<<1, 1024, 0, s>>>(of, T, scale, scale_dev, loss);
+    return launch_status();
+}
 
 extern "C" int sdp_token_loss(int dtype, int id_type, int T, int V, int64_t ldz, float scale, const void* Z, const void* labels,
                               const float* scale_dev, float* nll, float* lse, void* dZ, float* loss, void* stream) {
@@ -268,15 +223,14 @@ extern "C" int sdp_token_loss(int dtype, int id_type, int T, int V, int64_t ldz,
     if (T > 0) {
         const Loss a{Z, labels, scale_dev, nll, lse, dZ, T, V, id_type == SDP_I64, ldz, scale};
         const bool once = sdp::read_once({eZ}, (size_t)ldz * es);
-        by_row(dtype == SDP_BF16, V, [&](auto b, auto waves, auto p) {
+        sdp::by_row(dtype == SDP_BF16, V, [&](auto b, auto waves, auto p) {
             if (p.value && once) token_loss_kernel<b.value, waves.value, p.value, p.value != 0><<<sdp::grid_of(T), waves.value * 64, 0, s>>>(a);
             else token_loss_kernel<b.value, waves.value, p.value, 0><<<sdp::grid_of(T), waves.value * 64, 0, s>>>(a);
         });
         rc = sdp::launch_status();
     }
     if (rc != SDP_OK || !loss) return rc;
-    loss_sum_kernel<<<1, 1024, 0, s>>>(nll, T, scale, scale_dev, loss);
-    return sdp::launch_status();
+    return sdp::loss_sum(nll, T, scale, scale_dev, loss, s);
 }
 
 extern "C" int sdp_label_scale(int id_type, int T, int V, const void* labels, float* scale, void* stream) {

@@ -17,7 +17,7 @@
 namespace {
 
 // A pointer parameter: its name in messages and what it points to: 'a' the type given by the call's dtype argument,
-// 'i' int32, 'f' float32, 't' int32 or int64, 'w' bytes, 'z' as 'a' but a
+// 'i' int32, 'f' float32, 't' int32 or int64, 'v' float32 or bfloat16, 'w' bytes, 'z' as 'a' but a
 // matrix whose rows may lie apart (the caller passes their distance), in capitals where None stands for a null pointer; 0 for parameters
 // passed as they are (numbers, workspace and stream addresses).
 // For calls that state their shapes: d0, d1 are the places of the integer arguments that are the tensor's sizes (kOne: size 1), ld that of
@@ -67,10 +67,11 @@ bool take(PyObject* o, const Param& p, c10::ScalarType act, int device, A& out) 
             out = nullptr;
             return true;
         }
-        c10::ScalarType want = kind == 'f' ? c10::kFloat : kind == 'i' || kind == 't' ? c10::kInt : kind == 'w' ? c10::kByte : act;
+        c10::ScalarType want = kind == 'f' || kind == 'v' ? c10::kFloat : kind == 'i' || kind == 't' ? c10::kInt : kind == 'w' ? c10::kByte : act;
         if (!THPVariable_Check(o)) return type_error(p, want);
         const at::Tensor& t = THPVariable_Unpack(o);
         if (kind == 't' && t.scalar_type() == c10::kLong) want = c10::kLong;
+        if (kind == 'v' && t.scalar_type() == c10::kBFloat16) want = c10::kBFloat16;
         const bool rows_apart = kind == 'z' && t.dim() == 2 && (t.size(1) <= 1 || t.stride(1) == 1);
         if (!t.is_cuda() || !(rows_apart || t.is_contiguous()) || t.scalar_type() != want) return type_error(p, want);
         if (device >= 0 && t.get_device() != device) {
@@ -169,13 +170,21 @@ SDP_ENTRY_HERE(embed_fwd, sdp_embed_fwd, 0, {}, {}, {}, {}, {}, {}, {"E", 'a', 3
 SDP_ENTRY_HERE(embed_bwd, sdp_embed_bwd, 0, {}, {}, {}, {}, {}, {}, {"dY", 'a', 2, 4}, {"ids", 't', 2}, {"dE", 'a', 3, 4}, {"ws", 'w'}, {}, {})
 SDP_ENTRY_HERE(token_loss, sdp_token_loss, 0, {}, {}, {}, {}, {}, {}, {"Z", 'z', 2, 3, 4}, {"labels", 't', 2}, {"scale_dev", 'F', kOne}, {"nll", 'f', 2},
                {"lse", 'F', 2}, {"dZ", 'Z', 2, 3, 4}, {"loss", 'F', kOne}, {})
+SDP_ENTRY_HERE(distill_loss, sdp_distill_loss, 0, {}, {}, {}, {}, {}, {}, {}, {}, {}, {"Z", 'z', 3, 4, 6}, {"ids", 't', 3, 5}, {"top", 'v', 3, 5},
+               {"top_lse", 'F', 3}, {"scale_dev", 'F', kOne}, {"kl", 'f', 3}, {"lse", 'F', 3}, {"dZ", 'Z', 3, 4, 6}, {"loss", 'F', kOne}, {})
+SDP_ENTRY_HERE(head_loss, sdp_head_loss, 0, {}, {}, {}, {}, {}, {}, {"X", 'a', 2, 4}, {"W", 'a', 3, 4}, {"labels", 't', 2}, {"scale_dev", 'F', kOne},
+               {"nll", 'f', 2}, {"lse", 'F', 2}, {"dX", 'A', 2, 4}, {"dW", 'A', 3, 4}, {"loss", 'F', kOne}, {"ws", 'w'}, {}, {})
+SDP_ENTRY_HERE(head_distill, sdp_head_distill, 0, {}, {}, {}, {}, {}, {}, {}, {}, {}, {"X", 'a', 3, 5}, {"W", 'a', 4, 5}, {"ids", 't', 3, 6},
+               {"top", 'v', 3, 6}, {"top_lse", 'F', 3}, {"scale_dev", 'F', kOne}, {"kl", 'f', 3}, {"lse", 'F', 3}, {"dX", 'A', 3, 5}, {"dW", 'A', 4, 5},
+               {"loss", 'F', kOne}, {"ws", 'w'}, {}, {})
 SDP_ENTRY_HERE(label_scale, sdp_label_scale, 0, {}, {}, {}, {"labels", 't'}, {"scale", 'f', kOne}, {})
 
 #define SDP_METHOD(py) {#py, (PyCFunction)(void (*)(void))py, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {SDP_METHOD(mlp_fwd),   SDP_METHOD(mlp_bwd),   SDP_METHOD(attn_fwd), SDP_METHOD(attn_bwd),
                          SDP_METHOD(block_fwd), SDP_METHOD(block_bwd),
                          SDP_METHOD(norm_fwd),  SDP_METHOD(norm_bwd),  SDP_METHOD(embed_fwd), SDP_METHOD(embed_bwd),
-                         SDP_METHOD(token_loss), SDP_METHOD(label_scale), {nullptr, nullptr, 0, nullptr}};
+                         SDP_METHOD(token_loss), SDP_METHOD(label_scale),
+                         SDP_METHOD(distill_loss), SDP_METHOD(head_loss), SDP_METHOD(head_distill), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_sdp_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 } // namespace
