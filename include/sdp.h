@@ -470,16 +470,16 @@ int sdp_distill_loss(int dtype, int id_type, int top_dtype, int T, int V, int k,
  * The output head and its loss in one: sdp_token_loss on the logits Z = X W^T, with the gradients of the tokens and of the head,
  * without the logits in memory.
  *   nll, lse, loss as there (Z in fp32);   dX = dZ W  [T][d];   dW = dZ^T X  [V][d]
- * It works on as many tokens at a time as keep what it holds of their logits within SDP_HEAD_PIECE_BYTES (2 bytes a logit with SDP_BF16, 4
- * with SDP_F32).  Tokens without a label cost nothing but the zeros of their dX: with SDP_BF16 their products are not computed.  Their X is not
+ * It works on as many tokens at a time (64 at least) as keep what it holds of their logits within SDP_HEAD_PIECE_BYTES (2 bytes a logit with
+ * SDP_BF16, 4 with SDP_F32), and their X likewise.  Tokens without a label cost nothing but the zeros of their dX: with SDP_BF16 their products are not computed.  Their X is not
  * looked at.
  *   X [T][d], W [V][d] (row-major by token of the vocabulary, like an embedding, which it may be), labels [T] in
  *   nll [T] fp32 out;  lse [T] fp32, may be NULL;  loss [1] fp32, may be NULL
  *   dX [T][d], dW [V][d] out, either may be NULL (not wanted); dX may take the place of X.  dW has every row; sums over tokens are
  *   fp32 and rounded once.
  *   ws: sdp_head_loss_workspace_bytes(dtype, T, V, d, want_dx, want_dw), 256-byte aligned
- * With SDP_BF16 dZ is rounded once to bf16 where it enters the two products, as the logits' gradient that sdp_token_loss stores.
- * Limits: for SDP_BF16 d a multiple of 8, X, W, dX, dW 16-byte aligned, V < 2^22, V d < 2^31; T <= SDP_EMBED_MAX_TOKENS.
+ * With SDP_BF16 dZ / c is rounded once to bf16 where it enters the two products; c follows in fp32.
+ * Limits: for SDP_BF16 d a multiple of 8, X, W, dX, dW 16-byte aligned;  V < 2^22, d <= 2^20, V d < 2^31, T <= SDP_EMBED_MAX_TOKENS.
  * Errors: as for sdp_token_loss, SHAPE where a limit is exceeded, WORKSPACE.
  *
  * sdp_head_distill: the same for sdp_distill_loss on Z = X W^T.

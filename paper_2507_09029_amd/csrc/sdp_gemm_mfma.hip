@@ -119,6 +119,9 @@ struct HeadArgs {
     int nblk;
     const int32_t* labels; // [row], optional
     float* at_label;       // [row]
+    // OP_HEAD_DX, OP_HEAD_DW: the factor of the sums, scale scale_dev[0]
+    float scale;
+    const float* scale_dev;
     // OP_HEAD_DX_SPLIT, OP_HEAD_DW: rows of the outputs (of one range's partial sums; that are stored)
     int out_rows;
     // OP_HEAD_DW: sums of the pieces of tokens before this one, fp32 as the accumulators lie; 0: there are no others, 1: the first of
@@ -397,7 +400,6 @@ __device__ __attribute__((always_inline)) inline void gemm_tile(const Dev& g, co
         gC = batch == 0 ? g.Cb[0] : (batch == 1 ? g.Cb[1] : (batch == 2 ? g.Cb[2] : g.Cb[3]));
     }
     const int m0 = tile_m * BM;
-    if (is_head(OP) && m0 >= g.M) return; // no token there
     const int n0 = kFwd ? tile_n * (BN / 2) : tile_n * BN; // SWIGLU_FWD: BN columns = BN/2 neurons x {gate, up}
     // SWIGLU_BWD with neuron-major copies: the encoded rank of each of this wave's output columns (at most two
     // per lane), fetched now so that the epilogue does not wait for it; a column outside the matrix counts as
@@ -1129,8 +1131,17 @@ __device__ __attribute__((always_inline)) inline void gemm_tile(const Dev& g, co
                         if (head.piece > 1) acc[i][j][q] += *at;
                         if (head.piece < 3) *at = acc[i][j][q];
                     }
-            if (head.piece < 3) return;
+            if (head.piece == 1 || head.piece == 2) return;
         }
+    }
+    if constexpr (is_head(OP)) {
+        const float c = head.scale * (head.scale_dev ? *head.scale_dev : 1.f);
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) acc[i][j][q] *= c;
     }
 
     // residual of a single-problem store (the skip connection of a block): fetched one fragment row ahead like G, U
@@ -1986,8 +1997,12 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, BM == 64 && BN == 64 ? 2 : 1
         g.K = n < 0 ? 0 : n < g.K ? n : g.K;
         if (g.K == 0 && head.piece == 2) return; // the sums stay
     } else {
+        // the tiles of the tokens that there are, dealt out anew: with those of all tokens in place, the XCDs that hold the last ones would have none
         if (n <= 0) return;
         g.M = n < g.M ? n : g.M;
+        g.tiles_m = (g.M + BM - 1) / BM;
+        g.ntot = g.tiles_m * g.tiles_n * (is_split(OP) ? g.ksplit : 1);
+        if ((int)blockIdx.x >= g.ntot) return;
     }
     gemm_tile<BM, BN, WAVES_M, WAVES_N, EPI, OP, KM>(g, (int)blockIdx.x, smem, head);
 }
@@ -2043,17 +2058,18 @@ int head_dx_ranges(int rows, int V, int d) {
 }
 
 // sums of the ranges of dX, in their order -> bf16 rows of the tokens; one thread per 8 columns
-__global__ __launch_bounds__(256) void head_dx_reduce_kernel(const float* partial, int ranges, int rows, int d, const int32_t* list, const int32_t* live, int base,
-                                                             uint16_t* dX) {
+__global__ __launch_bounds__(256) void head_dx_reduce_kernel(const float* partial, int ranges, int rows, int d, const int32_t* list, HeadArgs head, uint16_t* dX) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int m = (int)(i / (d / 8)), n = (int)(i % (d / 8)) * 8;
-    if (m >= rows || m >= *live - base) return;
+    if (m >= rows || m >= *head.live - head.base) return;
     f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
     for (int k = 0; k < ranges; ++k) {
         const float* p = partial + ((int64_t)k * rows + m) * d + n;
         a += *(const f32x4*)p;
         b += *(const f32x4*)(p + 4);
     }
+    const float c = head.scale * (head.scale_dev ? *head.scale_dev : 1.f);
+    a *= c, b *= c;
     *(u32x4*)(dX + (int64_t)list[m] * d + n) = u32x4{pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3]), pack_bf16(b[0], b[1]), pack_bf16(b[2], b[3])};
 }
 
@@ -2079,7 +2095,7 @@ int gemm_head_dx(const HeadGemm& h, const int32_t* list, void* dX, float* split_
     GemmDesc d = extents(h.rows, h.d, h.V);
     d.A = h.P, d.lda = h.ldp, d.B = h.W, d.ldb = h.d, d.b_km = 1, d.C = dX, d.ldc = h.d, d.c_scatter = list, d.name = "head_dx";
     HeadArgs a{};
-    a.live = h.live, a.base = h.base, a.out_rows = h.rows;
+    a.live = h.live, a.base = h.base, a.scale = h.scale, a.scale_dev = h.scale_dev, a.out_rows = h.rows;
     const int r = head_dx_ranges(h.rows, h.V, h.d);
     if (r < 2) return launch_head<EPI_STORE, OP_HEAD_DX, 2>(d, a, choose_shape<EPI_STORE>(d, 1, 1), s);
     d.ksplit = r, d.split_ws = split_ws;
@@ -2087,7 +2103,7 @@ int gemm_head_dx(const HeadGemm& h, const int32_t* list, void* dX, float* split_
     if (rc != SDP_OK) return rc;
     const int64_t threads = (int64_t)h.rows * (h.d / 8);
     ProfileScope ps("head_dx_reduce", s);
-    head_dx_reduce_kernel<<<(unsigned)((threads + 255) / 256), 256, 0, s>>>(split_ws, r, h.rows, h.d, list, h.live, h.base, (uint16_t*)dX);
+    head_dx_reduce_kernel<<<(unsigned)((threads + 255) / 256), 256, 0, s>>>(split_ws, r, h.rows, h.d, list, a, (uint16_t*)dX);
     return launch_status();
 }
 
@@ -2095,10 +2111,10 @@ size_t head_sums_bytes(int V, int d) { return (size_t)((V + 255) / 256 * 256) * 
 
 int gemm_head_dw(const HeadGemm& h, void* dW, float* sums, int piece, hipStream_t s) {
     GemmDesc d = extents((h.V + 7) / 8 * 8, h.d, h.rows); // columns of the logits' rows in whole chunks: the last ones are zeros
-    d.A = h.P, d.lda = h.ldp, d.a_km = 1, d.B = h.X, d.ldb = h.d, d.b_km = 1, d.C = dW, d.ldc = h.d, d.name = "head_dw";
+    d.A = h.P, d.lda = h.ldp, d.a_km = 1, d.B = h.Xt, d.ldb = h.ldt, d.C = dW, d.ldc = h.d, d.name = "head_dw";
     HeadArgs a{};
-    a.live = h.live, a.base = h.base, a.out_rows = h.V, a.sums = sums, a.piece = piece;
-    return launch_head<EPI_STORE, OP_HEAD_DW, 3>(d, a, choose_shape<EPI_STORE>(d, 1, 1), s);
+    a.live = h.live, a.base = h.base, a.scale = h.scale, a.scale_dev = h.scale_dev, a.out_rows = h.V, a.sums = sums, a.piece = piece;
+    return launch_head<EPI_STORE, OP_HEAD_DW, 1>(d, a, choose_shape<EPI_STORE>(d, 1, 1), s);
 }
 
 } // namespace sdp

@@ -79,74 +79,112 @@ __global__ __launch_bounds__(1024) void list_kernel(const void* __restrict__ lab
 }
 
 struct Gather {
-    const void *X, *W;
-    void *Xc, *dX; // dX: zeros for tokens without a target, may be null
+    const void* X;
+    void *Xc, *Xt, *dX; // Xt: may be null; dX: zeros for tokens without a target, may be null
+    int64_t ldt;
     const int32_t* list;
-    Targets t;
-    int32_t* labels; // [row], -1 for none; or
-    float* z;        // [row][k]: the entries' logits
+    const void* labels_in;
+    int wide;
+    int32_t* labels; // [row], -1 for none; may be null
     int rows, V, d;
 };
 
-// A workgroup a row.  bf16: of d a multiple of 8 and 16-byte aligned.
-template <int BF16, int TH>
-__global__ __launch_bounds__(TH) void gather_kernel(Gather a) {
-    typedef Row<BF16> Rw;
-    typedef typename Rw::Elem Elem;
+// Rows of X in the list's order, and (bf16) the same column by column for dW, whose depth they are: read along it, they need one LDS read a
+// fragment where rows need two (a depth step of 256 x 256 1.67 -> 1.40 us with one transposed operand instead of two).  A workgroup takes
+// 64 tokens x 64 columns; tokens without a target are zeros.  bf16: d a multiple of 8, 16-byte aligned.
+__global__ __launch_bounds__(256) void gather_kernel(Gather a) {
+    __shared__ uint16_t tile[64][72]; // rows of 144 bytes: 16 of them start on different banks
+    const int tid = threadIdx.x, r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int r = 32 * h + tid / 8, c = c0 + tid % 8 * 8;
+        const int listed = r0 + r < a.rows ? a.list[r0 + r] : -1;
+        u32x4 w = {0, 0, 0, 0};
+        if (c < a.d && r0 + r < a.rows) {
+            if (listed >= 0) {
+                w = *(const u32x4*)((const uint16_t*)a.X + (int64_t)listed * a.d + c);
+                *(u32x4*)((uint16_t*)a.Xc + (int64_t)(r0 + r) * a.d + c) = w; // read next
+            } else if (a.dX) {
+                *(u32x4*)((uint16_t*)a.dX + (int64_t)(-1 - listed) * a.d + c) = w;
+            }
+        }
+        if (a.labels && c0 == 0 && tid % 8 == 0 && r0 + r < a.rows) a.labels[r0 + r] = listed < 0 ? -1 : sdp::token_id(a.labels_in, a.wide, listed, a.V);
+        if (a.Xt) *(u32x4*)&tile[r][tid % 8 * 8] = w;
+    }
+    if (!a.Xt) return;
+    __syncthreads();
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int c = 32 * h + tid / 8, r = tid % 8 * 8;
+        if (c0 + c >= a.d) continue;
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = tile[r + 2 * i][c] | (uint32_t)tile[r + 2 * i + 1][c] << 16;
+        *(u32x4*)((uint16_t*)a.Xt + (int64_t)(c0 + c) * a.ldt + r0 + r) = u32x4{w[0], w[1], w[2], w[3]};
+    }
+}
+
+// fp32: a wave a row, of any width and alignment
+__global__ __launch_bounds__(64) void gather_f32_kernel(Gather a) {
+    typedef Row<0> Rw;
     constexpr int N = Rw::N;
     const int64_t row = sdp::group_id();
     if (row >= a.rows) return;
-    const int listed = a.list[row], tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, d = a.d, whole = Rw::whole(d);
-    const bool live = listed >= 0;
-    const int64_t token = live ? listed : -1 - listed;
-    const Elem* x = (const Elem*)a.X + token * d;
-    Elem* xc = (Elem*)a.Xc + row * d;
-    Elem* dx = (Elem*)a.dX + token * d;
-    if (!live) {
-        for (int e = tid * N; e < whole; e += TH * N) {
-            if (!BF16) Rw::store(xc, e, whole, u32x4{0, 0, 0, 0}); // the fp32 contractions go over all rows
-            if (a.dX) Rw::store(dx, e, whole, u32x4{0, 0, 0, 0});
-        }
-        if (whole + tid < d) {
-            if (!BF16) Rw::put(xc + whole + tid, 0.f);
-            if (a.dX) Rw::put(dx + whole + tid, 0.f);
-        }
-        if (a.labels && tid == 0) a.labels[row] = -1;
-        return;
+    const int listed = a.list[row], tid = threadIdx.x, d = a.d, whole = Rw::whole(d);
+    const float* x = (const float*)a.X + (int64_t)(listed < 0 ? 0 : listed) * d;
+    float* xc = (float*)a.Xc + row * d;
+    float* dx = (float*)a.dX + (int64_t)(listed < 0 ? -1 - listed : 0) * d;
+    const u32x4 none = {0, 0, 0, 0};
+    for (int e = tid * N; e < whole; e += 64 * N) {
+        *(Rw::Piece*)(xc + e) = listed < 0 ? none : Rw::load_some(x, e, whole); // the contractions go over all rows
+        if (listed < 0 && a.dX) *(Rw::Piece*)(dx + e) = none;
     }
-    if (a.labels && tid == 0) a.labels[row] = sdp::token_id(a.t.ids, a.t.wide, token, a.V);
-    for (int e = tid * N; e < whole; e += TH * N) *(typename Rw::Piece*)(xc + e) = Rw::load_some(x, e, whole); // read next
-    if (whole + tid < d) xc[whole + tid] = x[whole + tid];
-    if constexpr (BF16) {
-        if (!a.z) return;
-        // the entries' logits in fp32, a wave four entries at a time
-        constexpr int WAVES = TH / 64, M = 4;
-        for (int i0 = wave * M; i0 < a.t.k; i0 += WAVES * M) {
-            const Elem* w[M];
-            float sum[M];
-            int id[M];
+    if (whole + tid < d) {
+        xc[whole + tid] = listed < 0 ? 0.f : x[whole + tid];
+        if (listed < 0 && a.dX) dx[whole + tid] = 0.f;
+    }
+}
+
+struct EntryLogits {
+    const uint16_t *X, *W; // [row][d], [V][d]
+    const int32_t* list;
+    Targets t;
+    float* z; // [row][k]
+    int rows, V, d;
+};
+// The entries' logits in fp32: a workgroup a row, a wave four entries at a time.
+__global__ __launch_bounds__(256) void entry_logits_kernel(EntryLogits a) {
+    typedef Row<1> Rw;
+    constexpr int WAVES = 4, M = 4;
+    const int64_t row = sdp::group_id();
+    if (row >= a.rows) return;
+    const int listed = a.list[row], lane = threadIdx.x & 63, wave = threadIdx.x >> 6, k = a.t.k;
+    if (listed < 0) return;
+    const uint16_t* x = a.X + row * a.d;
+    for (int i0 = wave * M; i0 < k; i0 += WAVES * M) {
+        const uint16_t* w[M];
+        float sum[M];
+#pragma unroll
+        for (int j = 0; j < M; ++j) {
+            const int id = i0 + j < k ? sdp::token_id(a.t.ids, a.t.wide, (int64_t)listed * k + i0 + j, a.V) : -1;
+            w[j] = a.W + (int64_t)(id < 0 ? 0 : id) * a.d;
+            sum[j] = 0.f;
+        }
+        for (int e = lane * 8; e < a.d; e += 64 * 8) {
+            float xv[8];
+            Rw::unpack(*(const u32x4*)(x + e), xv);
 #pragma unroll
             for (int j = 0; j < M; ++j) {
-                id[j] = i0 + j < a.t.k ? sdp::token_id(a.t.ids, a.t.wide, token * a.t.k + i0 + j, a.V) : -1;
-                w[j] = (const Elem*)a.W + (int64_t)(id[j] < 0 ? 0 : id[j]) * d;
-                sum[j] = 0.f;
-            }
-            for (int e = lane * N; e < d; e += 64 * N) {
-                float xv[N];
-                Rw::unpack(Rw::load_some(x, e, whole), xv);
+                float wv[8];
+                Rw::unpack(*(const u32x4*)(w[j] + e), wv);
 #pragma unroll
-                for (int j = 0; j < M; ++j) {
-                    float wv[N];
-                    Rw::unpack(Rw::load_some(w[j], e, whole), wv);
-#pragma unroll
-                    for (int n = 0; n < N; ++n) sum[j] = fmaf(xv[n], wv[n], sum[j]);
-                }
+                for (int n = 0; n < 8; ++n) sum[j] = fmaf(xv[n], wv[n], sum[j]);
             }
+        }
 #pragma unroll
-            for (int j = 0; j < M; ++j) {
-                const float z = sdp::wave_sum(sum[j]);
-                if (lane == 0 && i0 + j < a.t.k) a.z[row * a.t.k + i0 + j] = z;
-            }
+        for (int j = 0; j < M; ++j) {
+            const float z = sdp::wave_sum(sum[j]);
+            if (lane == 0 && i0 + j < k) a.z[row * k + i0 + j] = z;
         }
     }
 }
@@ -211,7 +249,10 @@ __global__ __launch_bounds__(kCodeThreads) void code_rows_kernel(CodeRows a) {
         if (a.lse) a.lse[listed] = m * a.t.inv_tau + log_sum;
     }
     if (!a.P) return;
-    const float c = a.t.scale * (a.t.scale_dev ? *a.t.scale_dev : 1.f) * a.t.inv_tau, inv = c * mass / sum;
+    // The gradient's factor c / tau comes in fp32 with the products' results: mass p - q is rounded by itself, which keeps a label's 1 - p, that most of a
+    // row's length lies in, at the fine end of bf16's steps where p is small (1 / 3350 of it may lie anywhere: dX 2.5e-3 off instead of 2.0e-3),
+    // and keeps a small factor out of bf16's range.
+    const float inv = mass / sum;
     uint16_t* p = a.P + row * a.ldp;
     constexpr float kStep = sdp::kCodeRange / 65535.f;
     const int end = (a.V + 7) / 8 * 8; // codes of columns behind V say 0
@@ -241,7 +282,7 @@ __global__ __launch_bounds__(kCodeThreads) void code_rows_kernel(CodeRows a) {
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
     for (int i = tid; i < k; i += TH)
-        if (en.id[i] >= 0) Rw::put(p + en.id[i], __builtin_amdgcn_exp2f((en.z[i] - m) * rate) * inv - c * en.all_of(i, k));
+        if (en.id[i] >= 0) Rw::put(p + en.id[i], __builtin_amdgcn_exp2f((en.z[i] - m) * rate) * inv - en.all_of(i, k));
 }
 
 __global__ __launch_bounds__(256) void zero_kernel(uint16_t* p, int64_t n) {
@@ -252,14 +293,15 @@ __global__ __launch_bounds__(256) void zero_kernel(uint16_t* p, int64_t n) {
 struct Plan {
     int rows = 0, pieces = 0, block = 0, nblk = 0; // tokens of a piece; columns of a statistic's block
     int64_t ldz = 0;                               // of the codes, or of the fp32 logits
-    size_t list = 0, live = 0, has = 0, X = 0, Z = 0, stats = 0, labels = 0, z = 0, sums = 0, split = 0, bytes = 0;
+    int64_t ldt = 0;
+    size_t list = 0, live = 0, has = 0, X = 0, Xt = 0, Z = 0, stats = 0, labels = 0, z = 0, sums = 0, split = 0, bytes = 0;
 };
 Plan plan(int dtype, int T, int V, int d, int k, bool teacher, bool dx, bool dw) {
     Plan p;
     const bool bf16 = dtype == SDP_BF16, grads = dx || dw;
-    // per token: codes and statistics, or logits
-    const size_t row = bf16 ? (grads ? ((size_t)V + 191) * 2 : 0) + ((size_t)V + 31) / 32 * 8 : ((size_t)V + 3) * 4;
-    const int64_t most = (int64_t)(SDP_HEAD_PIECE_BYTES / row) / 64 * 64;
+    const size_t row = bf16 ? (grads ? (size_t)sdp::line_ld(V, 1) * 2 : ((size_t)V + 31) / 32 * 8) : ((size_t)V + 3) * 4;
+    const size_t wide = (size_t)d * (bf16 ? 2 : 4);
+    const int64_t most = (int64_t)(SDP_HEAD_PIECE_BYTES / (row > wide ? row : wide)) / 64 * 64;
     const int64_t rows_max = most < 64 ? 64 : most;
     p.pieces = (int)((T + rows_max - 1) / rows_max);
     p.rows = T;
@@ -279,6 +321,8 @@ Plan plan(int dtype, int T, int V, int d, int k, bool teacher, bool dx, bool dw)
     p.X = take(rows * d * (bf16 ? 2 : 4));
     if (bf16) {
         p.ldz = sdp::line_ld(V, p.rows);
+        p.ldt = sdp::line_ld(p.rows, d);
+        if (dw) p.Xt = take((size_t)p.ldt * d * 2);
         p.block = sdp::head_block(p.rows, V, d), p.nblk = (V + p.block - 1) / p.block;
         if (grads) p.Z = take(rows * p.ldz * 2);
         p.stats = take(rows * p.nblk * 8);
@@ -319,22 +363,26 @@ int run(const Call& c, unsigned char* ws, hipStream_t s) {
     int rc = sdp::launch_status();
     for (int i = 0; i < p.pieces && rc == SDP_OK; ++i) {
         const int base = i * p.rows, rows = c.T - base < p.rows ? c.T - base : p.rows;
-        Gather g{c.X, c.W, ws + p.X, c.dX, list + base, c.t, nullptr, nullptr, rows, c.V, c.d};
+        Gather g{c.X, ws + p.X, c.dW && bf16 ? ws + p.Xt : nullptr, c.dX, p.ldt, list + base, c.t.ids, c.t.wide, nullptr, rows, c.V, c.d};
         if (bf16 && !teacher) g.labels = (int32_t*)(ws + p.labels);
-        if (bf16 && teacher) g.z = (float*)(ws + p.z);
         {
             sdp::ProfileScope ps("head_gather", s);
-            if (!bf16) gather_kernel<0, 64><<<sdp::grid_of(rows), 64, 0, s>>>(g);
-            else if (teacher) gather_kernel<1, 256><<<sdp::grid_of(rows), 256, 0, s>>>(g);
-            else gather_kernel<1, 64><<<sdp::grid_of(rows), 64, 0, s>>>(g);
+            if (bf16) gather_kernel<<<dim3((rows + 63) / 64, (c.d + 63) / 64), 256, 0, s>>>(g);
+            else gather_f32_kernel<<<sdp::grid_of(rows), 64, 0, s>>>(g);
         }
         rc = sdp::launch_status();
         if (rc != SDP_OK) return rc;
         if (bf16) {
             sdp::HeadGemm h;
             h.X = ws + p.X, h.W = c.W, h.P = ws + p.Z, h.ldp = p.ldz, h.rows = p.rows, h.V = c.V, h.d = c.d, h.live = live, h.base = base;
+            h.Xt = ws + p.Xt, h.ldt = p.ldt;
+            h.scale = c.t.scale * c.t.inv_tau, h.scale_dev = c.t.scale_dev;
             float2* stats = (float2*)(ws + p.stats);
             float* z = (float*)(ws + p.z);
+            if (teacher) {
+                sdp::ProfileScope ps("head_entry_logits", s);
+                entry_logits_kernel<<<sdp::grid_of(rows), 256, 0, s>>>({(const uint16_t*)h.X, (const uint16_t*)c.W, list + base, c.t, z, rows, c.V, c.d});
+            }
             rc = sdp::gemm_head_logits(h, c.t.inv_tau, grads, stats, p.nblk, g.labels, z, s);
             if (rc != SDP_OK) return rc;
             const CodeRows r{grads ? (uint16_t*)h.P : nullptr, p.ldz, stats, p.nblk, p.block == 64 ? 6 : 5, z, c.t, list + base, c.kl, c.lse, rows, c.V};
@@ -374,9 +422,9 @@ int run(const Call& c, unsigned char* ws, hipStream_t s) {
 }
 
 bool sizes_ok(int dtype, int T, int V, int d, int k) {
-    if (T > SDP_EMBED_MAX_TOKENS || V >= 1 << 22 || d > SDP_MAX_EXTENT || k > SDP_MAX_ENTRIES) return false;
+    if (T > SDP_EMBED_MAX_TOKENS || V >= 1 << 22 || d > 1 << 20 || k > SDP_MAX_ENTRIES) return false;
     if ((int64_t)V * d >= (int64_t)1 << 31) return false;
-    return dtype != SDP_BF16 || (d % 8 == 0 && d < 1 << 22);
+    return dtype != SDP_BF16 || d % 8 == 0;
 }
 size_t workspace(int dtype, int T, int V, int d, int k, bool teacher, bool dx, bool dw) {
     if ((dtype != SDP_F32 && dtype != SDP_BF16) || T < 1 || V < 1 || d < 1 || k < 1 || !sizes_ok(dtype, T, V, d, k)) return 0;

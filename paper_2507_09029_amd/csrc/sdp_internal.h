@@ -202,13 +202,17 @@ int gemm_f32(const GemmDesc& g, hipStream_t s);
 int gemm_f32_group(const GemmDesc* d, int n, const char* name, hipStream_t s);
 // ---- the output head's contractions (bf16), of `rows` tokens, of whom those from number `base` on have a target: min(rows, *live - base) -----
 struct HeadGemm {
-    const void* X = nullptr; // [rows][d], theirs without gaps
+    const void* X = nullptr;  // [rows][d], theirs without gaps
+    const void* Xt = nullptr; // [d][ldt]: the same columns by columns, zeros behind the last token to a multiple of 8
+    int64_t ldt = 0;
     const void* W = nullptr; // [V][d]
-    void* P = nullptr;       // [rows][ldp]: codes of their logits, then the logits' gradient
+    void* P = nullptr;       // [rows][ldp]: codes of their logits, then mass p - q: their gradient without its factor
     int64_t ldp = 0;
     int rows = 0, V = 0, d = 0;
     const int32_t* live = nullptr;
     int base = 0;
+    float scale = 1.f; // of dX and dW: scale scale_dev[0], in fp32 before they are rounded
+    const float* scale_dev = nullptr;
 };
 // A logit is kept as its distance from the largest of its block of columns: 16 bits for 0 .. kCodeRange in powers of two, after the division
 // by the temperature.  A step is 0.0015, so that a probability made from it is 5.1e-4 off at most and 2.9e-4 in the mean square: a sixth of what

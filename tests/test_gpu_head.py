@@ -116,9 +116,10 @@ def test_large_tiles(sdp, T, V, d):
     _reference(X, W, labels.cuda()[:, None], None, 1.0 / T).check(sdp.head_loss(X, W, labels.cuda(), scale=1.0 / T))
 
 
-@pytest.mark.parametrize("dtype,T,V,d,live", [("bf16", 10000, 60000, 64, 1.0), ("bf16", 20000, 60000, 48, 0.7), ("bf16", 20000, 60000, 48, 0.02), ("f32", 10000, 30001, 33, 0.6)])
+@pytest.mark.parametrize("dtype,T,V,d,live", [("bf16", 10000, 60000, 64, 1.0), ("bf16", 20000, 60000, 48, 0.7), ("bf16", 20000, 60000, 48, 0.02), ("f32", 10000, 30001, 33, 0.6),
+                                                ("bf16", 600000, 5, 1000, 0.8)])
 def test_more_tokens_than_a_piece(sdp, dtype, T, V, d, live):
-    """Two to three pieces, the later ones without a token that has a label in the third case."""
+    """Two to three pieces, the later ones without a token that has a label in the third case; tokens of more bytes than their logits."""
     dt = DT[dtype]
     labels = some_labels(T, V, 2, 1.0 - live)
     X, W = (t.cuda() for t in head(T, V, d, dt, labels))

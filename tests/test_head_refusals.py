@@ -53,7 +53,7 @@ def test_head_loss(L):
                 dict(loss=at(3)), dict(lse=at(2)), dict(nll=at(0)), dict(ws=at(0)), dict(ws=at(6)), dict(ws=at(8))):
         assert f(**bad) == INVALID, bad
     assert f(d=12) == SHAPE and f(V=1 << 22) == SHAPE and f(V=1 << 20, d=1 << 11) == SHAPE and f(T=(1 << 26) + 1) == SHAPE
-    assert f(dtype=0, V=1 << 22) == SHAPE
+    assert f(dtype=0, V=1 << 22) == SHAPE and f(V=5, d=(1 << 20) + 8) == SHAPE
     assert f(ws=None) == WORKSPACE and f(ws_bytes=64) == WORKSPACE and f(ws=odd(0x80)) == WORKSPACE
     w = L.sdp_head_loss_workspace_bytes
     assert f(ws_bytes=w(1, 4, 10, 16, 1, 1) - 1) == WORKSPACE
