@@ -113,9 +113,9 @@ struct HeadArgs {
     const int32_t* live; // rows of all pieces together; this launch has min(its rows, *live - base) of them
     int base;
     // EPI_CODES
-    float rate, to_code; // log2(e) / tau; rate / kCodeRange
-    int codes;           // whether they are wanted, or the statistics alone
-    float2* stats;       // [row][nblk]
+    float rate;    // log2(e) / tau
+    int codes;     // whether they are wanted, or the statistics alone
+    float2* stats; // [row][nblk]
     int nblk;
     const int32_t* labels; // [row], optional
     float* at_label;       // [row]
@@ -1057,8 +1057,21 @@ __device__ __attribute__((always_inline)) inline void gemm_tile(const Dev& g, co
     };
 
     if constexpr (EPI == EPI_CODES) {
-        // A row's WN columns lie with the four lanes l16, l16 + 16, ..: their largest logit and the sum of the others' powers beside it, in
-        // fp32, and every logit's distance from it as 16 bits (kCodeRange).
+        // A row's WN columns lie with the four lanes l16, l16 + 16, ..: their largest logit m, the sum of 2^(rate z - rate m), and every logit's
+        // distance from m in 16 bits (kCodeRange).  rate m is rounded once and is what all of the row goes by, here and later, so that a
+        // difference has the rounding of one fused multiply-add.  128 powers a lane, an eighth of the vector unit's work here each, and the stores are what a tile
+        // takes beyond its depth steps.
+        if (wcol0 + WN > g.N) {
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (wcol0 + 32 * j + 16 * (q & 1) + 4 * lq + r >= g.N)
+#pragma unroll
+                            for (int i = 0; i < FM; ++i) acc[i][j][q][r] = -INFINITY;
+        }
         int label[FM][2];
 #pragma unroll
         for (int i = 0; i < FM; ++i)
@@ -1067,55 +1080,53 @@ __device__ __attribute__((always_inline)) inline void gemm_tile(const Dev& g, co
                 const int r = 32 * i + 16 * h + l16;
                 label[i][h] = head.labels && r < wrows ? head.labels[wrow0 + r] - wcol0 : -1;
             }
-        const bool edge = wcol0 + WN > g.N;
+        auto blocks = [&](auto codes_c) __attribute__((always_inline)) {
+            constexpr bool kCodes = decltype(codes_c)::value;
 #pragma unroll
-        for (int i = 0; i < FM; ++i) {
-            __builtin_amdgcn_sched_barrier(0);
+            for (int i = 0; i < FM; ++i) {
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                float v[FN][2][4], m = -INFINITY, sum = 0.f;
-#pragma unroll
-                for (int j = 0; j < FN; ++j)
-#pragma unroll
-                    for (int c = 0; c < 2; ++c)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            const float x = acc[i][j][2 * h + c][r];
-                            v[j][c][r] = edge && wcol0 + 32 * j + 16 * c + 4 * lq + r >= g.N ? -INFINITY : x;
-                            m = fmaxf(m, v[j][c][r]);
-                        }
-                m = across_rows<true>(m);
-                const float from = m == -INFINITY ? 0.f : m; // nothing but -inf: a sum of 0
-#pragma unroll
-                for (int j = 0; j < FN; ++j)
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        float t[4];
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            t[r] = from - v[j][c][r];
-                            sum += __builtin_amdgcn_exp2f(t[r] * -head.rate);
-                        }
-                        if (head.codes)
-                            strip_put(strip0, 32 * j, 2 * h + c,
-                                      u32x2{code_pair(t[0] * head.to_code, t[1] * head.to_code), code_pair(t[2] * head.to_code, t[3] * head.to_code)});
-                    }
-                sum = across_rows<false>(sum);
-                const int row = 32 * i + 16 * h + l16;
-                if (lq == 0 && row < wrows && wcol0 < g.N) head.stats[(int64_t)(wrow0 + row) * head.nblk + wcol0 / WN] = float2{m, sum};
-                const int at = label[i][h];
-                if ((uint32_t)at < (uint32_t)WN && ((at >> 2) & 3) == lq) {
+                for (int h = 0; h < 2; ++h) {
+                    float m = -INFINITY, sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int j = 0; j < FN; ++j)
 #pragma unroll
                         for (int c = 0; c < 2; ++c)
 #pragma unroll
-                            for (int r = 0; r < 4; ++r)
-                                if (at == 32 * j + 16 * c + 4 * lq + r) head.at_label[wrow0 + row] = v[j][c][r];
+                            for (int r = 0; r < 4; ++r) m = fmaxf(m, acc[i][j][2 * h + c][r]);
+                    m = across_rows<true>(m) * head.rate;
+                    const float from = m == -INFINITY ? 0.f : m; // nothing but -inf: a sum of 0
+#pragma unroll
+                    for (int j = 0; j < FN; ++j)
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+                            float y[4];
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) {
+                                y[r] = fmaf(acc[i][j][2 * h + c][r], head.rate, -from);
+                                sum[r] += __builtin_amdgcn_exp2f(y[r]);
+                            }
+                            constexpr float kToCode = -1.f / kCodeRange;
+                            if (kCodes) strip_put(strip0, 32 * j, 2 * h + c, u32x2{code_pair(y[0] * kToCode, y[1] * kToCode), code_pair(y[2] * kToCode, y[3] * kToCode)});
+                        }
+                    const float total = across_rows<false>((sum[0] + sum[1]) + (sum[2] + sum[3]));
+                    const int row = 32 * i + 16 * h + l16;
+                    if (lq == 0 && row < wrows && wcol0 < g.N) head.stats[(int64_t)(wrow0 + row) * head.nblk + wcol0 / WN] = float2{m, total};
+                    const int at = label[i][h];
+                    if ((uint32_t)at < (uint32_t)WN && ((at >> 2) & 3) == lq) {
+#pragma unroll
+                        for (int j = 0; j < FN; ++j)
+#pragma unroll
+                            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                                for (int r = 0; r < 4; ++r)
+                                    if (at == 32 * j + 16 * c + 4 * lq + r) head.at_label[wrow0 + row] = acc[i][j][2 * h + c][r];
+                    }
                 }
+                if (kCodes) strip_store(strip0, g.C, g.ldc, i, std::integral_constant<int, kKeep>{});
             }
-            if (head.codes) strip_store(strip0, g.C, g.ldc, i, std::integral_constant<int, kKeep>{});
-        }
+        };
+        if (head.codes) blocks(std::true_type{}); else blocks(std::false_type{});
         return;
     }
     if constexpr (kHeadDw) {
@@ -2077,11 +2088,11 @@ __global__ __launch_bounds__(256) void head_dx_reduce_kernel(const float* partia
 
 int head_block(int rows, int V, int d) { return choose_shape<EPI_CODES>(extents(rows, V, d), 1, 1) == T64x64 ? 32 : 64; }
 
-int gemm_head_logits(const HeadGemm& h, float inv_tau, bool codes, float2* stats, int nblk, const int32_t* labels, float* at_label, hipStream_t s) {
+int gemm_head_logits(const HeadGemm& h, float rate, bool codes, float2* stats, int nblk, const int32_t* labels, float* at_label, hipStream_t s) {
     GemmDesc d = extents(h.rows, h.V, h.d);
     d.A = h.X, d.lda = h.d, d.B = h.W, d.ldb = h.d, d.epilogue = EPI_CODES, d.C = h.P, d.ldc = h.ldp, d.name = "head_logits";
     HeadArgs a{};
-    a.live = h.live, a.base = h.base, a.rate = inv_tau * 1.44269504088896340736f, a.to_code = a.rate / kCodeRange;
+    a.live = h.live, a.base = h.base, a.rate = rate;
     a.codes = codes, a.stats = stats, a.nblk = nblk, a.labels = labels, a.at_label = at_label;
     return launch_head<EPI_CODES, OP_HEAD_LOGITS, 0>(d, a, choose_shape<EPI_CODES>(d, 1, 1), s);
 }

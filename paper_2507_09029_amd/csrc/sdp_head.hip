@@ -223,30 +223,31 @@ __global__ __launch_bounds__(kCodeThreads) void code_rows_kernel(CodeRows a) {
     float vmax = en.load<TH>(a.t, listed, a.V);
     for (int i = tid; i < k; i += TH) en.z[i] = en.id[i] >= 0 ? a.z[row * k + i] : 0.f;
     const float rate = sdp::kLog2e * a.t.inv_tau;
-    float m = -INFINITY, sum = 0.f;
+    constexpr float kLn2 = 0.69314718055994530942f;
+    float m = -INFINITY, sum = 0.f; // powers of two from here on
     for (int b = tid; b < a.nblk; b += TH) {
         const float2 s = stats[b];
         const float top = fmaxf(m, s.x), from = top == -INFINITY ? 0.f : top;
-        sum = sum * __builtin_amdgcn_exp2f((m - from) * rate) + s.y * __builtin_amdgcn_exp2f((s.x - from) * rate);
+        sum = sum * __builtin_amdgcn_exp2f(m - from) + s.y * __builtin_amdgcn_exp2f(s.x - from);
         m = top;
     }
     const float mine = m;
     sdp::group_both<WAVES, true>(m, vmax, lds[0]);
     // a thread without blocks, or with nothing but -inf: 0; nothing but -inf in the whole row: NaN
-    sum *= __builtin_amdgcn_exp2f((mine - m) * rate);
+    sum *= __builtin_amdgcn_exp2f(mine - m);
     float of_entries = en.sum<TH>(a.t, vmax);
     sdp::group_both<WAVES, false>(sum, of_entries, lds[1]);
     const float log_sum = logf(sum);
     float mass = 0.f, kl = 0.f;
     en.masses<TH>(a.t, listed, vmax, of_entries, [&](int i, float q, float log_q) {
         mass += q;
-        if (q != 0.f) kl += q * ((log_q - (en.z[i] - m) * a.t.inv_tau) + log_sum);
+        if (q != 0.f) kl += q * ((log_q - fmaf(en.z[i], rate, -m) * kLn2) + log_sum);
     });
     sdp::group_both<WAVES, false>(mass, kl, lds[2]);
     if (!a.t.top_lse && mass == mass) mass = 1.f;
     if (tid == 0) {
         a.kl[listed] = !a.t.top && kl < 0.f ? 0.f : kl; // a label's logit that is all of its row's sum, but for roundings
-        if (a.lse) a.lse[listed] = m * a.t.inv_tau + log_sum;
+        if (a.lse) a.lse[listed] = fmaf(m, kLn2, log_sum);
     }
     if (!a.P) return;
     // The gradient's factor c / tau comes in fp32 with the products' results: mass p - q is rounded by itself, which keeps a label's 1 - p, that most of a
@@ -258,7 +259,7 @@ __global__ __launch_bounds__(kCodeThreads) void code_rows_kernel(CodeRows a) {
     const int end = (a.V + 7) / 8 * 8; // codes of columns behind V say 0
     auto value = [&](uint32_t code, float from) { return code == 65535u ? 0.f : __builtin_amdgcn_exp2f(fmaf((float)code, -kStep, from)) * inv; };
     auto turn = [&](int e, const u32x4& w, float block) {
-        const float from = (block - m) * rate;
+        const float from = block - m;
         float v[8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[2 * i] = value(w[i] & 0xFFFFu, from), v[2 * i + 1] = value(w[i] >> 16, from);
@@ -282,7 +283,7 @@ __global__ __launch_bounds__(kCodeThreads) void code_rows_kernel(CodeRows a) {
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
     for (int i = tid; i < k; i += TH)
-        if (en.id[i] >= 0) Rw::put(p + en.id[i], __builtin_amdgcn_exp2f((en.z[i] - m) * rate) * inv - en.all_of(i, k));
+        if (en.id[i] >= 0) Rw::put(p + en.id[i], __builtin_amdgcn_exp2f(fmaf(en.z[i], rate, -m)) * inv - en.all_of(i, k));
 }
 
 __global__ __launch_bounds__(256) void zero_kernel(uint16_t* p, int64_t n) {
@@ -383,7 +384,7 @@ int run(const Call& c, unsigned char* ws, hipStream_t s) {
                 sdp::ProfileScope ps("head_entry_logits", s);
                 entry_logits_kernel<<<sdp::grid_of(rows), 256, 0, s>>>({(const uint16_t*)h.X, (const uint16_t*)c.W, list + base, c.t, z, rows, c.V, c.d});
             }
-            rc = sdp::gemm_head_logits(h, c.t.inv_tau, grads, stats, p.nblk, g.labels, z, s);
+            rc = sdp::gemm_head_logits(h, sdp::kLog2e * c.t.inv_tau, grads, stats, p.nblk, g.labels, z, s);
             if (rc != SDP_OK) return rc;
             const CodeRows r{grads ? (uint16_t*)h.P : nullptr, p.ldz, stats, p.nblk, p.block == 64 ? 6 : 5, z, c.t, list + base, c.kl, c.lse, rows, c.V};
             {

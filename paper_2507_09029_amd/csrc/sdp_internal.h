@@ -219,9 +219,9 @@ struct HeadGemm {
 // its rounding to bf16 for the products costs next, which is thus the only one that counts (the probability itself as bf16, and again
 // as bf16 after its row's sum is known: twice).  From kCodeRange on, 2^-96 of the block's largest, it is 0.
 constexpr float kCodeRange = 96.f;
-// columns of a block: (largest logit, sum of the powers of their differences) of each go into stats [rows][nblk]
+// Columns of a block; rate = log2(e) / tau.  (m = rate x largest logit, sum of 2^(rate z - m)) of each go into stats [rows][nblk].
 int head_block(int rows, int V, int d);
-int gemm_head_logits(const HeadGemm& h, float inv_tau, bool codes, float2* stats, int nblk, const int32_t* labels, float* at_label, hipStream_t s);
+int gemm_head_logits(const HeadGemm& h, float rate, bool codes, float2* stats, int nblk, const int32_t* labels, float* at_label, hipStream_t s);
 // dX[list[row]] = P W, with scratch of head_dx_ws_bytes
 size_t head_dx_ws_bytes(int rows, int V, int d);
 int gemm_head_dx(const HeadGemm& h, const int32_t* list, void* dX, float* split_ws, hipStream_t s);
