@@ -2033,7 +2033,8 @@ int launch_head_cfg(const GemmDesc& d, const HeadArgs& head, hipStream_t s) {
 }
 template <int EPI, int OP, int KM>
 int launch_head(const GemmDesc& d, const HeadArgs& head, Shape shape, hipStream_t s) {
-    if (shape == T256x256) return launch_head_cfg<256, 256, 2, 4, EPI, OP, KM>(d, head, s);
+    // waves high and narrow where the left operand is the one of two LDS reads a fragment: 16 reads a half step instead of 20
+    if (shape == T256x256) return launch_head_cfg<256, 256, KM == 1 ? 4 : 2, KM == 1 ? 2 : 4, EPI, OP, KM>(d, head, s);
     if (shape == T128x256) return launch_head_cfg<128, 256, 2, 4, EPI, OP, KM>(d, head, s);
     if (shape == T128x128) return launch_head_cfg<128, 128, 4, 2, EPI, OP, KM>(d, head, s);
     if (shape == T64x64) return launch_head_cfg<64, 64, 2, 2, EPI, OP, KM>(d, head, s);

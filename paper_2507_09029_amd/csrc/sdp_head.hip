@@ -23,7 +23,7 @@ using sdp::Row;
 using sdp::Targets;
 using sdp::u32x4;
 
-// tokens of 1024 threads' turn in the list's kernel: 16 a thread
+// tokens of a turn in the list's kernel: 16 a thread
 constexpr int kListTurn = 1024 * 16;
 
 // whether a token has an entry; a wave a token
@@ -41,36 +41,43 @@ __global__ __launch_bounds__(256) void entries_kernel(Targets t, int T, int V, u
 }
 
 // list: the tokens with a target in order, from its front; the others as -1 - token, from its end.  *live: how many the first are.  One
-// workgroup: 16384 tokens are one turn.
-__global__ __launch_bounds__(1024) void list_kernel(const void* __restrict__ labels, int wide, const uint8_t* __restrict__ has, int T, int V,
-                                                    int32_t* __restrict__ list, int32_t* live) {
+// workgroup: 16384 tokens are one turn.  `from`: 0, 1 labels of 32, 64 bits, 2 what entries_kernel wrote.
+template <int FROM>
+__global__ __launch_bounds__(1024) void list_kernel(const void* __restrict__ from, int T, int V, int32_t* __restrict__ list, int32_t* live) {
     __shared__ int wave_sums[16];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     int before = 0; // tokens with a target in earlier turns
     for (int64_t t0 = 0; t0 < T; t0 += kListTurn) {
-        const int64_t first = t0 + tid * 16;
-        uint32_t mask = 0;
+        // a wave's 1024 tokens, 64 at a time: loads without conditions
+        const int64_t first = t0 + wave * 1024 + lane;
+        bool has[16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-            if (first + i < T && (has ? has[first + i] != 0 : sdp::token_id(labels, wide, first + i, V) >= 0)) mask |= 1u << i;
-        const int n = __popc(mask);
-        int upto = n; // over the wave, then the waves
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int x = __shfl_up(upto, d, 64);
-            if (lane >= d) upto += x;
+        for (int i = 0; i < 16; ++i) {
+            const int64_t t = first + 64 * i < T ? first + 64 * i : T - 1;
+            if constexpr (FROM == 2) has[i] = ((const uint8_t*)from)[t] != 0;
+            else has[i] = sdp::token_id<FROM>(from, t, V) >= 0;
         }
-        if (lane == 63) wave_sums[wave] = upto;
+        uint64_t mask[16];
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mask[i] = __ballot(has[i] && first + 64 * i < T), n += __popcll(mask[i]);
+        if (lane == 0) wave_sums[wave] = n;
         __syncthreads();
-        int at = before + upto - n, all = 0;
+        int at = before, all = 0;
 #pragma unroll
         for (int w = 0; w < 16; ++w) {
             if (w < wave) at += wave_sums[w];
             all += wave_sums[w];
         }
-        for (int i = 0; i < 16 && first + i < T; ++i) {
-            if (mask >> i & 1) list[at++] = (int32_t)(first + i);
-            else list[T - 1 - (first + i - at)] = -1 - (int32_t)(first + i); // first + i - at: those without before it
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int64_t t = first + 64 * i;
+            const int mine = at + __popcll(mask[i] & ((1ull << lane) - 1)); // those with a target before token t
+            if (t < T) {
+                if (mask[i] >> lane & 1) list[mine] = (int32_t)t;
+                else list[T - 1 - (t - mine)] = -1 - (int32_t)t;
+            }
+            at += __popcll(mask[i]);
         }
         before += all;
         __syncthreads();
@@ -201,8 +208,10 @@ struct CodeRows {
     int rows, V;
 };
 
-// A row of codes and its blocks' statistics -> its loss, lse and gradient.  One workgroup a row.
+// A row of codes and its blocks' statistics -> its loss, lse and gradient.  One workgroup a row.  ONCE: around the caches, where the codes are far
+// more than the 256 MB behind the L2s hold: 16384 x 32000 444 -> 396 us, but 3350 x 50001 123 -> 136.
 constexpr int kCodeThreads = 256;
+template <int ONCE>
 __global__ __launch_bounds__(kCodeThreads) void code_rows_kernel(CodeRows a) {
     typedef Row<1> Rw;
     constexpr int TH = kCodeThreads, WAVES = TH / 64;
@@ -263,7 +272,8 @@ __global__ __launch_bounds__(kCodeThreads) void code_rows_kernel(CodeRows a) {
         float v[8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[2 * i] = value(w[i] & 0xFFFFu, from), v[2 * i + 1] = value(w[i] >> 16, from);
-        *(u32x4*)(p + e) = Rw::pack(v); // read next
+        if (ONCE) __builtin_nontemporal_store(Rw::pack(v), (u32x4*)(p + e));
+        else *(u32x4*)(p + e) = Rw::pack(v); // read next
     };
     constexpr int U = 4;
     for (int e0 = tid * 8; e0 < end; e0 += U * TH * 8) {
@@ -272,7 +282,7 @@ __global__ __launch_bounds__(kCodeThreads) void code_rows_kernel(CodeRows a) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int e = min(e0 + u * TH * 8, end - 8);
-            w[u] = *(const u32x4*)(p + e);
+            w[u] = ONCE ? __builtin_nontemporal_load((const u32x4*)(p + e)) : *(const u32x4*)(p + e);
             block[u] = stats[e >> a.shift].x;
         }
 #pragma unroll
@@ -359,7 +369,9 @@ int run(const Call& c, unsigned char* ws, hipStream_t s) {
     }
     {
         sdp::ProfileScope ps("head_list", s);
-        list_kernel<<<1, 1024, 0, s>>>(c.t.ids, c.t.wide, has, c.T, c.V, list, live);
+        if (teacher) list_kernel<2><<<1, 1024, 0, s>>>(has, c.T, c.V, list, live);
+        else if (c.t.wide) list_kernel<1><<<1, 1024, 0, s>>>(c.t.ids, c.T, c.V, list, live);
+        else list_kernel<0><<<1, 1024, 0, s>>>(c.t.ids, c.T, c.V, list, live);
     }
     int rc = sdp::launch_status();
     for (int i = 0; i < p.pieces && rc == SDP_OK; ++i) {
@@ -389,7 +401,9 @@ int run(const Call& c, unsigned char* ws, hipStream_t s) {
             const CodeRows r{grads ? (uint16_t*)h.P : nullptr, p.ldz, stats, p.nblk, p.block == 64 ? 6 : 5, z, c.t, list + base, c.kl, c.lse, rows, c.V};
             {
                 sdp::ProfileScope ps("head_rows", s);
-                code_rows_kernel<<<sdp::grid_of(rows), kCodeThreads, sdp::Entries::bytes(c.t.k), s>>>(r);
+                const size_t lds = sdp::Entries::bytes(c.t.k);
+                if (grads && (size_t)rows * p.ldz * 2 >= (size_t)1 << 29) code_rows_kernel<1><<<sdp::grid_of(rows), kCodeThreads, lds, s>>>(r);
+                else code_rows_kernel<0><<<sdp::grid_of(rows), kCodeThreads, lds, s>>>(r);
             }
             rc = sdp::launch_status();
             if (rc == SDP_OK && c.dX) rc = sdp::gemm_head_dx(h, list + base, c.dX, (float*)(ws + p.split), s);
