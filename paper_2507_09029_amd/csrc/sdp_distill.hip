@@ -38,9 +38,7 @@ __global__ __launch_bounds__(WAVES * 64) void target_rows_kernel(TargetRows a) {
     const int listed = a.list ? a.list[row] : (int)row;
     const int token = listed < 0 ? -1 - listed : listed;
     const sdp::Entries en(entry_lds, k);
-    float vmax = en.load<TH>(a.t, listed < 0 ? -1 : token, V);
-    const bool some = __syncthreads_or(vmax > -INFINITY || vmax != vmax);
-    if (!some) {
+    if (listed < 0 || !sdp::has_entry(a.t, token, V)) { // every wave finds out for itself: a barrier less before the row is requested
         if (tid == 0) {
             a.kl[token] = 0.f;
             if (a.lse) a.lse[token] = 0.f;
@@ -57,6 +55,7 @@ __global__ __launch_bounds__(WAVES * 64) void target_rows_kernel(TargetRows a) {
 #pragma unroll
         for (int i = 0; i < P; ++i) w[i] = Rw::template load<ONCE>(z, (tid + i * TH) * N, whole);
     const float zt = tail ? Rw::one(z + whole + tid) : -INFINITY;
+    float vmax = en.load<TH>(a.t, token, V);
     for (int i = tid; i < k; i += TH) en.z[i] = en.id[i] >= 0 ? Rw::one(z + en.id[i]) : 0.f; // before anything is written: dZ may be Z
     float m = zt, sum = 0.f;
     if (PIECES) {
@@ -120,15 +119,15 @@ __global__ __launch_bounds__(WAVES * 64) void target_rows_kernel(TargetRows a) {
     const float c = a.t.scale * (a.t.scale_dev ? *a.t.scale_dev : 1.f) * a.t.inv_tau, inv = c * mass / sum;
     // A lane looks at one entry in 64 of them; those of the 64 pieces that the wave is about to store are found by a vote and taken off by their lanes.
     const int lane = tid & 63;
+    const int id0 = lane < k ? en.id[lane] : -1;
+    const float q0 = lane < k ? en.q[lane] * c : 0.f;
     auto gradient = [&](int64_t e, const u32x4& x) { // e: this lane's, the wave's others side by side
         float v[N];
         Rw::unpack(x, v);
 #pragma unroll
         for (int j = 0; j < N; ++j) v[j] = power(v[j]) * inv;
         const int64_t first = e - (int64_t)lane * N;
-        for (int c0 = 0; c0 < k; c0 += 64) {
-            const int id = c0 + lane < k ? en.id[c0 + lane] : -1;
-            const float q = c0 + lane < k ? en.q[c0 + lane] * c : 0.f;
+        auto take_off = [&](int id, float q) {
             uint64_t hits = __ballot(id >= first && id < first + 64 * N);
             while (hits) {
                 const int from = __builtin_ctzll(hits);
@@ -138,7 +137,9 @@ __global__ __launch_bounds__(WAVES * 64) void target_rows_kernel(TargetRows a) {
 #pragma unroll
                 for (int j = 0; j < N; ++j) v[j] -= at == j ? off : 0.f;
             }
-        }
+        };
+        take_off(id0, q0);
+        for (int i = 64 + lane; i - lane < k; i += 64) take_off(i < k ? en.id[i] : -1, i < k ? en.q[i] * c : 0.f);
         Rw::store(dz, (int)e, whole, Rw::pack(v));
     };
     if (PIECES) {

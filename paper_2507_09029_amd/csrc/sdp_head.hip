@@ -30,13 +30,7 @@ constexpr int kListTurn = 1024 * 16;
 __global__ __launch_bounds__(256) void entries_kernel(Targets t, int T, int V, uint8_t* __restrict__ has) {
     const int64_t token = (int64_t)sdp::group_id() * 4 + (threadIdx.x >> 6);
     if (token >= T) return;
-    bool any = false;
-    for (int i = threadIdx.x & 63; i < t.k; i += 64) {
-        const int64_t at = token * t.k + i;
-        const float v = t.top_bf16 ? Row<1>::one((const uint16_t*)t.top + at) : ((const float*)t.top)[at];
-        any |= sdp::token_id(t.ids, t.wide, at, V) >= 0 && !(v == -INFINITY);
-    }
-    any = __any(any);
+    const bool any = sdp::has_entry(t, token, V);
     if ((threadIdx.x & 63) == 0) has[token] = any;
 }
 

@@ -25,6 +25,20 @@ __device__ inline void group_both(float& x, float& y, float (*lds)[WAVES]) {
     }
 }
 
+// Whether a token has an entry; the same in all lanes of a wave.
+__device__ inline bool has_entry(const Targets& t, int64_t token, int V) {
+    for (int i = threadIdx.x & 63; i - (int)(threadIdx.x & 63) < t.k; i += 64) {
+        bool any = false;
+        if (i < t.k) {
+            const int64_t at = token * t.k + i;
+            const float v = !t.top ? 0.f : t.top_bf16 ? Row<1>::one((const uint16_t*)t.top + at) : ((const float*)t.top)[at];
+            any = token_id(t.ids, t.wide, at, V) >= 0 && !(v == -INFINITY);
+        }
+        if (__any(any)) return true;
+    }
+    return false;
+}
+
 // The entries of one token in LDS; thread t of TH has entries t, t + TH, ..  All but all_of look at a thread's own alone.
 struct Entries {
     int* id;     // -1: none
@@ -32,19 +46,15 @@ struct Entries {
     static constexpr size_t bytes(int k) { return (size_t)k * 12; }
     __device__ Entries(unsigned char* lds, int k) : id((int*)lds), q((float*)lds + k), z((float*)lds + 2 * k) {}
 
-    // fetches them (token -1: there are none); this thread's largest logit, NaN where one is, -inf where it has no entry
+    // fetches them; this thread's largest logit, NaN where one is, -inf where it has no entry
     template <int TH>
     __device__ float load(const Targets& t, int token, int V) const {
         float top = -INFINITY;
         for (int i = threadIdx.x; i < t.k; i += TH) {
-            int j = -1;
-            float v = 0.f;
-            if (token >= 0) {
-                const int64_t at = (int64_t)token * t.k + i;
-                j = token_id(t.ids, t.wide, at, V);
-                if (t.top) v = t.top_bf16 ? Row<1>::one((const uint16_t*)t.top + at) : ((const float*)t.top)[at];
-                if (v == -INFINITY) j = -1;
-            }
+            const int64_t at = (int64_t)token * t.k + i;
+            int j = token_id(t.ids, t.wide, at, V);
+            const float v = !t.top ? 0.f : t.top_bf16 ? Row<1>::one((const uint16_t*)t.top + at) : ((const float*)t.top)[at];
+            if (v == -INFINITY) j = -1;
             id[i] = j, q[i] = v;
             if (j >= 0) top = v != v || top != top ? NAN : fmaxf(top, v);
         }
