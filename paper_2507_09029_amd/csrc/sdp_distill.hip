@@ -162,7 +162,7 @@ int sdp::target_rows(int dtype, const TargetRows& r, const char* name, hipStream
     ProfileScope ps(name, s);
     const bool bf16 = dtype == SDP_BF16, once = read_once({{r.Z, ((size_t)(r.rows - 1) * r.ldz + r.V) * (bf16 ? 2 : 4)}}, (size_t)r.ldz * (bf16 ? 2 : 4));
     const size_t lds = Entries::bytes(r.t.k);
-    by_row(bf16, r.V, [&](auto b, auto waves, auto p) {
+    by_row<false>(bf16, r.V, [&](auto b, auto waves, auto p) {
         if (p.value && once) target_rows_kernel<b.value, waves.value, p.value, p.value != 0><<<grid_of(r.rows), waves.value * 64, lds, s>>>(r);
         else target_rows_kernel<b.value, waves.value, p.value, 0><<<grid_of(r.rows), waves.value * 64, lds, s>>>(r);
     });

@@ -107,11 +107,9 @@ struct Dev {
     int n_head, tail;
 };
 
-// The output head's contractions (kHead* below), beside Dev.  Rows of X and of the logits are those of tokens that have a target, first
-// to last; how many they are is known on the device alone.
+// The output head's contractions, beside Dev.  Rows of X and of the logits are those of tokens that have a target, first to last.
 struct HeadArgs {
-    const int32_t* live; // rows of all pieces together; this launch has min(its rows, *live - base) of them
-    int base;
+    const HeadPiece* piece;
     // EPI_CODES
     float rate;    // log2(e) / tau
     int codes;     // whether they are wanted, or the statistics alone
@@ -122,12 +120,12 @@ struct HeadArgs {
     // OP_HEAD_DX, OP_HEAD_DW: the factor of the sums, scale scale_dev[0]
     float scale;
     const float* scale_dev;
-    // OP_HEAD_DX_SPLIT, OP_HEAD_DW: rows of the outputs (of one range's partial sums; that are stored)
+    // OP_HEAD_DW: rows that are stored
     int out_rows;
     // OP_HEAD_DW: sums of the pieces of tokens before this one, fp32 as the accumulators lie; 0: there are no others, 1: the first of
     // several, 2: neither first nor last, 3: the last
     float* sums;
-    int piece;
+    int of;
 };
 
 // two fp32 -> packed bf16, round to nearest even (the hardware's v_cvt_pk_bf16_f32)
@@ -317,7 +315,7 @@ struct Geometry {
 struct NoSide {};
 constexpr bool carries_side(int op) { return op == OP_GATE_UP || op == OP_DACT || op == OP_DW; }
 constexpr bool is_batched(int op) { return op == OP_DW || op == OP_DW_SPLIT || op == OP_DW_TAIL; }
-constexpr bool is_split(int op) { return op == OP_DW_SPLIT || op == OP_HEAD_DX_SPLIT; }
+constexpr bool is_tail(int op) { return op == OP_DW_TAIL || op == OP_HEAD_DX || op == OP_HEAD_DW; }
 constexpr bool is_head(int op) { return op >= OP_HEAD_LOGITS; }
 // the launches of the attention block, whose lists may be of heads
 constexpr bool takes_heads(int op) { return op == OP_DOWN || op == OP_DW || op == OP_DW_SPLIT; }
@@ -355,7 +353,7 @@ __device__ __attribute__((always_inline)) inline void gemm_tile(const Dev& g, co
     // of a linear order in which the problems of a batch vary fastest, then group_m tile-rows, then the
     // tile-columns: the tiles that run together on one XCD then form a compact block of (problems x
     // tile-rows x tile-columns) whose operand rows are fetched into that XCD's L2 once.
-    constexpr bool kTail = OP == OP_DW_TAIL;
+    constexpr bool kTail = is_tail(OP);
     int bid = block;
     bool cut = false;  // OP_DW_TAIL: this workgroup computes one depth range of a tile of the last round
     int tail_part = 0, tail_q = 0;
@@ -367,9 +365,9 @@ __device__ __attribute__((always_inline)) inline void gemm_tile(const Dev& g, co
         bid = head_position(bid, g.ntot);
     }
     constexpr bool kBatched = is_batched(OP);
-    constexpr bool kSplit = is_split(OP);
+    constexpr bool kSplit = OP == OP_DW_SPLIT;
     constexpr bool kHeadDw = OP == OP_HEAD_DW;
-    const int nb = (kBatched ? g.nbatch : 1) * (kSplit ? g.ksplit : 1);
+    const int nb = kBatched ? g.nbatch * (kSplit ? g.ksplit : 1) : 1;
     int tile_m, tile_n, batch;
     if (kBatched && g.np0 > 0) {
         tile_of_shared(bid, g.tiles_m, g.tiles_n, g.np0, g.nbatch, g.ksplit, g.group_m, batch, tile_m, tile_n);
@@ -389,7 +387,7 @@ __device__ __attribute__((always_inline)) inline void gemm_tile(const Dev& g, co
     uint16_t* gC = g.C;
     int64_t lda = g.lda;
     int kpart = 0; // depth range of this workgroup (OP_DW_SPLIT, and the cut tiles of OP_DW_TAIL)
-    if (kSplit) kpart = kBatched ? batch / g.nbatch : batch, batch -= kpart * (kBatched ? g.nbatch : 1);
+    if (kSplit) kpart = batch / g.nbatch, batch -= kpart * g.nbatch;
     if (kTail) kpart = tail_part;
     if (kBatched) {
         // selected by comparisons: a runtime index into a by-value kernel argument would go through scratch
@@ -900,7 +898,7 @@ __device__ __attribute__((always_inline)) inline void gemm_tile(const Dev& g, co
     //                             n = n0 + (column base of block j) + 16 (q & 1) + 4 lq + r.
     if constexpr (kSplit) {
         // fp32 partial sums of this depth range, 16 bytes (4 columns) per store; N % 8 == 0
-        float* P = g.partial + (is_head(OP) ? (int64_t)kpart * head.out_rows : ((int64_t)kpart * g.nbatch + batch) * g.M) * g.N;
+        float* P = g.partial + ((int64_t)kpart * g.nbatch + batch) * g.M * g.N;
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
 #pragma unroll
@@ -1130,7 +1128,7 @@ __device__ __attribute__((always_inline)) inline void gemm_tile(const Dev& g, co
         return;
     }
     if constexpr (kHeadDw) {
-        if (head.piece > 0) { // this lane's accumulators of the tile, 16 bytes a lane side by side
+        if (head.of > 0) { // this lane's accumulators of the tile, 16 bytes a lane side by side
             f32x4* const sums = (f32x4*)head.sums + ((int64_t)(tile_m * g.tiles_n + tile_n) * NW + wave) * (FM * FN * 4 * 64) + lane;
 #pragma unroll
             for (int i = 0; i < FM; ++i)
@@ -1139,10 +1137,10 @@ __device__ __attribute__((always_inline)) inline void gemm_tile(const Dev& g, co
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         f32x4* const at = sums + ((i * FN + j) * 4 + q) * 64;
-                        if (head.piece > 1) acc[i][j][q] += *at;
-                        if (head.piece < 3) *at = acc[i][j][q];
+                        if (head.of > 1) acc[i][j][q] += *at;
+                        if (head.of < 3) *at = acc[i][j][q];
                     }
-            if (head.piece == 1 || head.piece == 2) return;
+            if (head.of == 1 || head.of == 2) return;
         }
     }
     if constexpr (is_head(OP)) {
@@ -1493,14 +1491,14 @@ int describe(const GemmDesc& d, Dev& g) {
     g.tiles_n = (d.N + ncols - 1) / ncols;
     const int64_t ntiles = (int64_t)g.tiles_m * g.tiles_n;
     constexpr bool kBatched = is_batched(OP);
-    const int ksplit = is_split(OP) ? d.ksplit : 1;
+    const int ksplit = OP == OP_DW_SPLIT ? d.ksplit : 1;
     const int nbatch = (kBatched ? d.nbatch : 1) * ksplit; // problems of the launch
     if (ntiles * nbatch > 0x7FFFFFFF) return SDP_ERR_SHAPE;
     g.ntot = (int)(ntiles * nbatch);
     g.nbatch = kBatched ? d.nbatch : 1;
     g.ksplit = OP == OP_DW_TAIL ? d.ksplit : ksplit;
     g.ksteps = ((d.K + BK - 1) / BK + g.ksplit - 1) / g.ksplit;
-    g.partial = (float*)(OP == OP_DW_TAIL ? d.tail_ws : d.split_ws);
+    g.partial = (float*)(is_tail(OP) ? d.tail_ws : d.split_ws);
     g.n_head = g.ntot, g.tail = 0;
     int na = 1, nbo = 1; // distinct A / B operands among the problems of a batch
     for (int z = 0; z < kMaxBatch; ++z) {
@@ -2000,26 +1998,64 @@ int gemm_mfma_bf16(const GemmDesc& d, hipStream_t s) {
 // ---- the output head's contractions -----------------------------------------------------------------------------------
 namespace {
 
-template <int BM, int BN, int WAVES_M, int WAVES_N, int EPI, int OP, int KM>
-__global__ __launch_bounds__(WAVES_M* WAVES_N * 64, BM == 64 && BN == 64 ? 2 : 1) void sdp_head_gemm_kernel(Dev g, HeadArgs head) {
-    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    const int n = *head.live - head.base;
+// The device's view of a launch: its tokens, its cut; false where this workgroup has nothing to do.  The tiles are those of the tokens that there
+// are, dealt out anew: with those of all tokens in place, the XCDs that hold the last ones would have none.
+template <int BM, int OP>
+__device__ inline bool head_view(Dev& g, const HeadArgs& head, const HeadPiece& piece) {
     if constexpr (OP == OP_HEAD_DW) {
-        g.K = n < 0 ? 0 : n < g.K ? n : g.K;
-        if (g.K == 0 && head.piece == 2) return; // the sums stay
+        g.K = piece.rows;
+        if (g.K == 0 && head.of == 2) return false; // the sums stay
     } else {
-        // the tiles of the tokens that there are, dealt out anew: with those of all tokens in place, the XCDs that hold the last ones would have none
-        if (n <= 0) return;
-        g.M = n < g.M ? n : g.M;
+        g.M = piece.rows;
+        if (g.M == 0) return false;
         g.tiles_m = (g.M + BM - 1) / BM;
-        g.ntot = g.tiles_m * g.tiles_n * (is_split(OP) ? g.ksplit : 1);
-        if ((int)blockIdx.x >= g.ntot) return;
+        g.ntot = g.tiles_m * g.tiles_n;
     }
-    gemm_tile<BM, BN, WAVES_M, WAVES_N, EPI, OP, KM>(g, (int)blockIdx.x, smem, head);
+    g.n_head = g.ntot;
+    if constexpr (is_tail(OP)) {
+        const HeadCut& cut = OP == OP_HEAD_DX ? piece.dx : piece.dw;
+        g.n_head = cut.head, g.tail = cut.tail, g.ksplit = cut.parts, g.ksteps = cut.steps;
+    }
+    return true;
 }
 
 template <int BM, int BN, int WAVES_M, int WAVES_N, int EPI, int OP, int KM>
-int launch_head_cfg(const GemmDesc& d, const HeadArgs& head, hipStream_t s) {
+__global__ __launch_bounds__(WAVES_M* WAVES_N * 64, BM == 64 && BN == 64 ? 2 : 1) void sdp_head_gemm_kernel(Dev g, HeadArgs head) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    const HeadPiece piece = *head.piece;
+    if (!head_view<BM, OP>(g, head, piece)) return;
+    if ((int)blockIdx.x >= g.n_head + (is_tail(OP) ? g.tail * g.ksplit : 0)) return;
+    gemm_tile<BM, BN, WAVES_M, WAVES_N, EPI, OP, KM>(g, (int)blockIdx.x, smem, head);
+}
+
+// the ranges of every cut tile, in depth order -> its rows; a thread per 8 columns
+template <int BM, int BN, int OP>
+__global__ __launch_bounds__(256) void head_cut_kernel(Dev g, HeadArgs head) {
+    const HeadPiece piece = *head.piece;
+    if (!head_view<BM, OP>(g, head, piece)) return;
+    const float c = head.scale * (head.scale_dev ? *head.scale_dev : 1.f);
+    const int rows = OP == OP_HEAD_DW ? head.out_rows : g.M;
+    const int64_t all = (int64_t)g.tail * (BM * BN / 8);
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        const int q = (int)(i / (BM * BN / 8)), e = (int)(i % (BM * BN / 8)), row = e / (BN / 8), col = e % (BN / 8) * 8;
+        const int bid = tail_position(q, g.ntot, g.n_head), per_group = g.group_m * g.tiles_n, grp = bid / per_group, first_m = grp * g.group_m;
+        const int gm = g.tiles_m - first_m < g.group_m ? g.tiles_m - first_m : g.group_m, in = bid - grp * per_group;
+        const int m = (first_m + in % gm) * BM + row, n = in / gm * BN + col;
+        if (m >= rows || n >= g.N) continue;
+        f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
+        for (int k = 0; k < g.ksplit; ++k) {
+            const float* p = g.partial + ((int64_t)k * g.tail + q) * (BM * BN) + row * BN + col;
+            a += *(const f32x4*)p;
+            b += *(const f32x4*)(p + 4);
+        }
+        a *= c, b *= c;
+        const int64_t to = g.cs ? g.cs[m] : m;
+        *(u32x4*)(g.C + to * g.ldc + n) = u32x4{pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3]), pack_bf16(b[0], b[1]), pack_bf16(b[2], b[3])};
+    }
+}
+
+template <int BM, int BN, int WAVES_M, int WAVES_N, int EPI, int OP, int KM>
+int launch_head_cfg(const GemmDesc& d, const HeadArgs& head, int most, hipStream_t s) {
     constexpr int LDS = Geometry<BM, BN, WAVES_M, WAVES_N, EPI, KM>::LDS;
     Dev g;
     const int drc = describe<BM, BN, EPI, OP>(d, g);
@@ -2027,22 +2063,34 @@ int launch_head_cfg(const GemmDesc& d, const HeadArgs& head, hipStream_t s) {
     auto kern = sdp_head_gemm_kernel<BM, BN, WAVES_M, WAVES_N, EPI, OP, KM>;
     static const hipError_t attr = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
     if (attr != hipSuccess) return SDP_ERR_HIP;
-    ProfileScope ps(d.name, s);
-    kern<<<dim3((unsigned)g.ntot), WAVES_M * WAVES_N * 64, LDS, s>>>(g, head);
+    // as many workgroups as the tiles of any number of tokens, and their cut, may be
+    const int64_t cut = most > 0 ? (int64_t)g.ntot / kHeadRound * kHeadRound + most : 0, grid = cut > g.ntot ? cut : g.ntot;
+    if (grid > 0x7FFFFFFF) return SDP_ERR_SHAPE;
+    {
+        ProfileScope ps(d.name, s);
+        kern<<<dim3((unsigned)grid), WAVES_M * WAVES_N * 64, LDS, s>>>(g, head);
+    }
+    const int rc = launch_status();
+    if (rc != SDP_OK || most == 0) return rc;
+    if constexpr (is_tail(OP)) {
+        ProfileScope ps("head_cut", s);
+        const int64_t groups = (int64_t)(g.ntot < kHeadRound ? g.ntot : kHeadRound - 1) * (BM * BN / 8 / 256);
+        head_cut_kernel<BM, BN, OP><<<(unsigned)(groups < 2048 ? groups : 2048), 256, 0, s>>>(g, head);
+    }
     return launch_status();
 }
 template <int EPI, int OP, int KM>
-int launch_head(const GemmDesc& d, const HeadArgs& head, Shape shape, hipStream_t s) {
+int launch_head(const GemmDesc& d, const HeadArgs& head, int bm, int bn, int most, hipStream_t s) {
     // waves high and narrow where the left operand is the one of two LDS reads a fragment: 16 reads a half step instead of 20
-    if (shape == T256x256) return launch_head_cfg<256, 256, KM == 1 ? 4 : 2, KM == 1 ? 2 : 4, EPI, OP, KM>(d, head, s);
-    if (shape == T128x256) return launch_head_cfg<128, 256, 2, 4, EPI, OP, KM>(d, head, s);
-    if (shape == T128x128) return launch_head_cfg<128, 128, 4, 2, EPI, OP, KM>(d, head, s);
-    if (shape == T64x64) return launch_head_cfg<64, 64, 2, 2, EPI, OP, KM>(d, head, s);
+    if (bm == 256 && bn == 256) return launch_head_cfg<256, 256, KM == 1 ? 4 : 2, KM == 1 ? 2 : 4, EPI, OP, KM>(d, head, most, s);
+    if (bm == 128 && bn == 256) return launch_head_cfg<128, 256, 2, 4, EPI, OP, KM>(d, head, most, s);
+    if (bm == 128 && bn == 128) return launch_head_cfg<128, 128, 4, 2, EPI, OP, KM>(d, head, most, s);
+    if (bm == 64 && bn == 64) return launch_head_cfg<64, 64, 2, 2, EPI, OP, KM>(d, head, most, s);
     if constexpr (EPI != EPI_CODES) {
-        if (shape == T256x192) return launch_head_cfg<256, 192, 4, 2, EPI, OP, KM>(d, head, s);
-        if (shape == T128x192) return launch_head_cfg<128, 192, 4, 2, EPI, OP, KM>(d, head, s);
+        if (bm == 256 && bn == 192) return launch_head_cfg<256, 192, 4, 2, EPI, OP, KM>(d, head, most, s);
+        if (bm == 128 && bn == 192) return launch_head_cfg<128, 192, 4, 2, EPI, OP, KM>(d, head, most, s);
     }
-    return SDP_ERR_INVALID_ARG; // not reached: the shapes that choose_shape has for EPI
+    return SDP_ERR_INVALID_ARG; // not reached: the shapes that there are
 }
 
 GemmDesc extents(int M, int N, int K) {
@@ -2051,38 +2099,27 @@ GemmDesc extents(int M, int N, int K) {
     return d;
 }
 
-// Depth ranges of dX: its outputs are few and its depth is the vocabulary.  As many as the tiles' model, the traffic of the partial sums at 4 TB/s
-// and a launch more make worth it, each of 4 steps at least.
-int head_dx_ranges(int rows, int V, int d) {
-    const GemmDesc g = extents(rows, d, V);
-    const int nk = (V + BK - 1) / BK;
-    int best = 1;
+// Tiles of a contraction whose last round is cut (head_cut): those that take least when all tokens have a target
+HeadTiles cut_tiles(int M, int N, int K, bool cuts) {
+    const int nk = (K + BK - 1) / BK;
+    HeadTiles best{};
     double least = -1;
-    for (int r = 1; r <= 64; r += r < 4 ? 1 : r / 4) {
-        const int steps = (nk + r - 1) / r;
-        if (r > 1 && (steps < 4 || (nk + steps - 1) / steps != r)) continue; // no empty range
-        double cost = 0;
-        choose_shape<EPI_STORE>(g, 1, r, nullptr, &cost);
-        if (r > 1) cost += 3.0 + (double)r * rows * d * 8.0 / 4e6;
-        if (least < 0 || cost < least) least = cost, best = r;
+    for (int i = 0; i < NUM_SHAPES; ++i) {
+        const ShapeInfo& h = kShapes[i];
+        const EpilogueCost e = epilogue_cost(EPI_STORE);
+        const HeadTiles t{h.bm, h.bn, (float)h.step1, (float)(e.e0 + e.e1 * h.bm * h.bn / 1024), cuts && nk >= 8 ? (i == T64x64 ? 1024 : 512) : 0};
+        const int64_t tiles = (int64_t)((M + h.bm - 1) / h.bm) * ((N + h.bn - 1) / h.bn), full = tiles / kHeadRound;
+        const int tail = (int)(tiles % kHeadRound);
+        const double one = nk * t.step + t.epilogue;
+        double last = tail ? one : 0.0;
+        for (int p = 2; p <= 64 && tail * p <= t.most && (nk + p - 1) / p >= 4; ++p) {
+            const double cost = 1.05 * ((tail * p + kHeadRound - 1) / kHeadRound) * ((nk + p - 1) / p * t.step + t.epilogue) + (double)tail * p * h.bm * h.bn * 2e-6 + 3.0;
+            last = cost < last ? cost : last;
+        }
+        const double cost = (double)full * one + last;
+        if (least < 0 || cost < least) least = cost, best = t;
     }
     return best;
-}
-
-// sums of the ranges of dX, in their order -> bf16 rows of the tokens; one thread per 8 columns
-__global__ __launch_bounds__(256) void head_dx_reduce_kernel(const float* partial, int ranges, int rows, int d, const int32_t* list, HeadArgs head, uint16_t* dX) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int m = (int)(i / (d / 8)), n = (int)(i % (d / 8)) * 8;
-    if (m >= rows || m >= *head.live - head.base) return;
-    f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
-    for (int k = 0; k < ranges; ++k) {
-        const float* p = partial + ((int64_t)k * rows + m) * d + n;
-        a += *(const f32x4*)p;
-        b += *(const f32x4*)(p + 4);
-    }
-    const float c = head.scale * (head.scale_dev ? *head.scale_dev : 1.f);
-    a *= c, b *= c;
-    *(u32x4*)(dX + (int64_t)list[m] * d + n) = u32x4{pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3]), pack_bf16(b[0], b[1]), pack_bf16(b[2], b[3])};
 }
 
 } // namespace
@@ -2093,40 +2130,32 @@ int gemm_head_logits(const HeadGemm& h, float rate, bool codes, float2* stats, i
     GemmDesc d = extents(h.rows, h.V, h.d);
     d.A = h.X, d.lda = h.d, d.B = h.W, d.ldb = h.d, d.epilogue = EPI_CODES, d.C = h.P, d.ldc = h.ldp, d.name = "head_logits";
     HeadArgs a{};
-    a.live = h.live, a.base = h.base, a.rate = rate;
-    a.codes = codes, a.stats = stats, a.nblk = nblk, a.labels = labels, a.at_label = at_label;
-    return launch_head<EPI_CODES, OP_HEAD_LOGITS, 0>(d, a, choose_shape<EPI_CODES>(d, 1, 1), s);
+    a.piece = h.piece, a.rate = rate, a.codes = codes, a.stats = stats, a.nblk = nblk, a.labels = labels, a.at_label = at_label;
+    const ShapeInfo& t = kShapes[choose_shape<EPI_CODES>(d, 1, 1)];
+    return launch_head<EPI_CODES, OP_HEAD_LOGITS, 0>(d, a, t.bm, t.bn, 0, s);
 }
 
-size_t head_dx_ws_bytes(int rows, int V, int d) {
-    const int r = head_dx_ranges(rows, V, d);
-    return r > 1 ? (size_t)r * rows * d * 4 : 0;
-}
+HeadTiles head_dx_tiles(int rows, int V, int d) { return cut_tiles(rows, d, V, true); }
+HeadTiles head_dw_tiles(int rows, int V, int d, int pieces) { return cut_tiles(V, d, rows, pieces == 1); }
 
-int gemm_head_dx(const HeadGemm& h, const int32_t* list, void* dX, float* split_ws, hipStream_t s) {
+int gemm_head_dx(const HeadGemm& h, const int32_t* list, void* dX, float* cut_ws, hipStream_t s) {
     GemmDesc d = extents(h.rows, h.d, h.V);
-    d.A = h.P, d.lda = h.ldp, d.B = h.W, d.ldb = h.d, d.b_km = 1, d.C = dX, d.ldc = h.d, d.c_scatter = list, d.name = "head_dx";
+    d.A = h.P, d.lda = h.ldp, d.B = h.W, d.ldb = h.d, d.b_km = 1, d.C = dX, d.ldc = h.d, d.c_scatter = list, d.tail_ws = cut_ws, d.name = "head_dx";
     HeadArgs a{};
-    a.live = h.live, a.base = h.base, a.scale = h.scale, a.scale_dev = h.scale_dev, a.out_rows = h.rows;
-    const int r = head_dx_ranges(h.rows, h.V, h.d);
-    if (r < 2) return launch_head<EPI_STORE, OP_HEAD_DX, 2>(d, a, choose_shape<EPI_STORE>(d, 1, 1), s);
-    d.ksplit = r, d.split_ws = split_ws;
-    const int rc = launch_head<EPI_STORE, OP_HEAD_DX_SPLIT, 2>(d, a, choose_shape<EPI_STORE>(d, 1, r), s);
-    if (rc != SDP_OK) return rc;
-    const int64_t threads = (int64_t)h.rows * (h.d / 8);
-    ProfileScope ps("head_dx_reduce", s);
-    head_dx_reduce_kernel<<<(unsigned)((threads + 255) / 256), 256, 0, s>>>(split_ws, r, h.rows, h.d, list, a, (uint16_t*)dX);
-    return launch_status();
+    a.piece = h.piece, a.scale = h.scale, a.scale_dev = h.scale_dev;
+    const HeadTiles t = head_dx_tiles(h.rows, h.V, h.d);
+    return launch_head<EPI_STORE, OP_HEAD_DX, 2>(d, a, t.bm, t.bn, t.most, s);
 }
 
 size_t head_sums_bytes(int V, int d) { return (size_t)((V + 255) / 256 * 256) * ((d + 767) / 768 * 768) * 4; } // whole tiles of any shape
 
-int gemm_head_dw(const HeadGemm& h, void* dW, float* sums, int piece, hipStream_t s) {
+int gemm_head_dw(const HeadGemm& h, void* dW, float* sums, int of, float* cut_ws, hipStream_t s) {
     GemmDesc d = extents((h.V + 7) / 8 * 8, h.d, h.rows); // columns of the logits' rows in whole chunks: the last ones are zeros
-    d.A = h.P, d.lda = h.ldp, d.a_km = 1, d.B = h.Xt, d.ldb = h.ldt, d.C = dW, d.ldc = h.d, d.name = "head_dw";
+    d.A = h.P, d.lda = h.ldp, d.a_km = 1, d.B = h.Xt, d.ldb = h.ldt, d.C = dW, d.ldc = h.d, d.tail_ws = cut_ws, d.name = "head_dw";
     HeadArgs a{};
-    a.live = h.live, a.base = h.base, a.scale = h.scale, a.scale_dev = h.scale_dev, a.out_rows = h.V, a.sums = sums, a.piece = piece;
-    return launch_head<EPI_STORE, OP_HEAD_DW, 1>(d, a, choose_shape<EPI_STORE>(d, 1, 1), s);
+    a.piece = h.piece, a.scale = h.scale, a.scale_dev = h.scale_dev, a.out_rows = h.V, a.sums = sums, a.of = of;
+    const HeadTiles t = head_dw_tiles(h.rows, h.V, h.d, of ? 2 : 1);
+    return launch_head<EPI_STORE, OP_HEAD_DW, 1>(d, a, t.bm, t.bn, t.most, s);
 }
 
 } // namespace sdp

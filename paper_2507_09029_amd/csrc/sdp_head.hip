@@ -34,10 +34,16 @@ __global__ __launch_bounds__(256) void entries_kernel(Targets t, int T, int V, u
     if ((threadIdx.x & 63) == 0) has[token] = any;
 }
 
-// list: the tokens with a target in order, from its front; the others as -1 - token, from its end.  *live: how many the first are.  One
-// workgroup: 16384 tokens are one turn.  `from`: 0, 1 labels of 32, 64 bits, 2 what entries_kernel wrote.
+// The sizes that the pieces' contractions are planned from
+struct Shapes {
+    sdp::HeadTiles dx, dw;
+    int rows, pieces, V, d;
+};
+
+// list: the tokens with a target in order, from its front; the others as -1 - token, from its end.  pieces: what each of them has of the former
+// (bf16).  One workgroup: 16384 tokens are one turn.  FROM: 0, 1 labels of 32, 64 bits, 2 what entries_kernel wrote.
 template <int FROM>
-__global__ __launch_bounds__(1024) void list_kernel(const void* __restrict__ from, int T, int V, int32_t* __restrict__ list, int32_t* live) {
+__global__ __launch_bounds__(1024) void list_kernel(const void* __restrict__ from, int T, int V, int32_t* __restrict__ list, sdp::HeadPiece* pieces, Shapes g) {
     __shared__ int wave_sums[16];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     int before = 0; // tokens with a target in earlier turns
@@ -76,7 +82,13 @@ __global__ __launch_bounds__(1024) void list_kernel(const void* __restrict__ fro
         before += all;
         __syncthreads();
     }
-    if (tid == 0) *live = before;
+    if (!pieces) return;
+    for (int p = wave; p < g.pieces; p += 16) {
+        const int left = before - p * g.rows, rows = left < 0 ? 0 : left < g.rows ? left : g.rows;
+        const sdp::HeadCut dx = sdp::head_cut(g.dx, ((rows + g.dx.bm - 1) / g.dx.bm) * ((g.d + g.dx.bn - 1) / g.dx.bn), (g.V + 63) / 64);
+        const sdp::HeadCut dw = sdp::head_cut(g.dw, ((g.V + g.dw.bm - 1) / g.dw.bm) * ((g.d + g.dw.bn - 1) / g.dw.bn), (rows + 63) / 64);
+        if (lane == 0) pieces[p] = {rows, {}, dx, dw};
+    }
 }
 
 struct Gather {
@@ -299,7 +311,8 @@ struct Plan {
     int rows = 0, pieces = 0, block = 0, nblk = 0; // tokens of a piece; columns of a statistic's block
     int64_t ldz = 0;                               // of the codes, or of the fp32 logits
     int64_t ldt = 0;
-    size_t list = 0, live = 0, has = 0, X = 0, Xt = 0, Z = 0, stats = 0, labels = 0, z = 0, sums = 0, split = 0, bytes = 0;
+    sdp::HeadTiles tx{}, tw{};
+    size_t list = 0, piece = 0, has = 0, X = 0, Xt = 0, Z = 0, stats = 0, labels = 0, z = 0, sums = 0, cut = 0, bytes = 0;
 };
 Plan plan(int dtype, int T, int V, int d, int k, bool teacher, bool dx, bool dw) {
     Plan p;
@@ -321,7 +334,7 @@ Plan plan(int dtype, int T, int V, int d, int k, bool teacher, bool dx, bool dw)
         return here;
     };
     const size_t rows = (size_t)p.rows;
-    p.list = take((size_t)T * 4), p.live = take(4);
+    p.list = take((size_t)T * 4);
     if (teacher) p.has = take((size_t)T);
     p.X = take(rows * d * (bf16 ? 2 : 4));
     if (bf16) {
@@ -334,7 +347,11 @@ Plan plan(int dtype, int T, int V, int d, int k, bool teacher, bool dx, bool dw)
         if (!teacher) p.labels = take(rows * 4);
         p.z = take(rows * k * 4);
         if (dw && p.pieces > 1) p.sums = take(sdp::head_sums_bytes(V, d));
-        if (dx) p.split = take(sdp::head_dx_ws_bytes(p.rows, V, d));
+        p.piece = take((size_t)p.pieces * sizeof(sdp::HeadPiece));
+        p.tx = sdp::head_dx_tiles(p.rows, V, d), p.tw = sdp::head_dw_tiles(p.rows, V, d, p.pieces);
+        // both contractions' cut tiles, one after the other
+        const size_t bx = dx ? sdp::head_cut_bytes(p.tx) : 0, bw = dw ? sdp::head_cut_bytes(p.tw) : 0;
+        p.cut = take(bx > bw ? bx : bw);
     } else {
         p.ldz = (V + 3) / 4 * 4;
         p.Z = take(rows * p.ldz * 4);
@@ -355,7 +372,9 @@ struct Call {
 int run(const Call& c, unsigned char* ws, hipStream_t s) {
     const bool bf16 = c.dtype == SDP_BF16, teacher = c.t.top != nullptr, grads = c.dX || c.dW;
     const Plan p = plan(c.dtype, c.T, c.V, c.d, c.t.k, teacher, c.dX, c.dW);
-    int32_t *list = (int32_t*)(ws + p.list), *live = (int32_t*)(ws + p.live);
+    int32_t* list = (int32_t*)(ws + p.list);
+    sdp::HeadPiece* pieces = bf16 ? (sdp::HeadPiece*)(ws + p.piece) : nullptr;
+    const Shapes shapes{p.tx, p.tw, p.rows, p.pieces, c.V, c.d};
     uint8_t* has = teacher ? ws + p.has : nullptr;
     if (teacher) {
         sdp::ProfileScope ps("head_entries", s);
@@ -363,9 +382,9 @@ int run(const Call& c, unsigned char* ws, hipStream_t s) {
     }
     {
         sdp::ProfileScope ps("head_list", s);
-        if (teacher) list_kernel<2><<<1, 1024, 0, s>>>(has, c.T, c.V, list, live);
-        else if (c.t.wide) list_kernel<1><<<1, 1024, 0, s>>>(c.t.ids, c.T, c.V, list, live);
-        else list_kernel<0><<<1, 1024, 0, s>>>(c.t.ids, c.T, c.V, list, live);
+        if (teacher) list_kernel<2><<<1, 1024, 0, s>>>(has, c.T, c.V, list, pieces, shapes);
+        else if (c.t.wide) list_kernel<1><<<1, 1024, 0, s>>>(c.t.ids, c.T, c.V, list, pieces, shapes);
+        else list_kernel<0><<<1, 1024, 0, s>>>(c.t.ids, c.T, c.V, list, pieces, shapes);
     }
     int rc = sdp::launch_status();
     for (int i = 0; i < p.pieces && rc == SDP_OK; ++i) {
@@ -381,7 +400,7 @@ int run(const Call& c, unsigned char* ws, hipStream_t s) {
         if (rc != SDP_OK) return rc;
         if (bf16) {
             sdp::HeadGemm h;
-            h.X = ws + p.X, h.W = c.W, h.P = ws + p.Z, h.ldp = p.ldz, h.rows = p.rows, h.V = c.V, h.d = c.d, h.live = live, h.base = base;
+            h.X = ws + p.X, h.W = c.W, h.P = ws + p.Z, h.ldp = p.ldz, h.rows = p.rows, h.V = c.V, h.d = c.d, h.piece = pieces + i;
             h.Xt = ws + p.Xt, h.ldt = p.ldt;
             h.scale = c.t.scale * c.t.inv_tau, h.scale_dev = c.t.scale_dev;
             float2* stats = (float2*)(ws + p.stats);
@@ -400,9 +419,9 @@ int run(const Call& c, unsigned char* ws, hipStream_t s) {
                 else code_rows_kernel<0><<<sdp::grid_of(rows), kCodeThreads, lds, s>>>(r);
             }
             rc = sdp::launch_status();
-            if (rc == SDP_OK && c.dX) rc = sdp::gemm_head_dx(h, list + base, c.dX, (float*)(ws + p.split), s);
+            if (rc == SDP_OK && c.dX) rc = sdp::gemm_head_dx(h, list + base, c.dX, (float*)(ws + p.cut), s);
             if (rc == SDP_OK && c.dW)
-                rc = sdp::gemm_head_dw(h, c.dW, (float*)(ws + p.sums), p.pieces == 1 ? 0 : i == 0 ? 1 : i == p.pieces - 1 ? 3 : 2, s);
+                rc = sdp::gemm_head_dw(h, c.dW, (float*)(ws + p.sums), p.pieces == 1 ? 0 : i == 0 ? 1 : i == p.pieces - 1 ? 3 : 2, (float*)(ws + p.cut), s);
             continue;
         }
         sdp::GemmDesc d;

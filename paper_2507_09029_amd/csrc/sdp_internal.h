@@ -192,7 +192,7 @@ struct GemmDesc {
 };
 
 // tags that give each call site of the MFMA contraction its own kernel symbol
-enum GemmOp { OP_GATE_UP = 0, OP_DOWN = 1, OP_DACT = 2, OP_DX = 3, OP_DW = 4, OP_DW_SPLIT = 5, OP_DW_TAIL = 6, OP_HEAD_LOGITS = 7, OP_HEAD_DX = 8, OP_HEAD_DX_SPLIT = 9, OP_HEAD_DW = 10 };
+enum GemmOp { OP_GATE_UP = 0, OP_DOWN = 1, OP_DACT = 2, OP_DX = 3, OP_DW = 4, OP_DW_SPLIT = 5, OP_DW_TAIL = 6, OP_HEAD_LOGITS = 7, OP_HEAD_DX = 8, OP_HEAD_DW = 9 };
 
 // fp32 contraction on the matrix cores, any shape.
 int gemm_f32(const GemmDesc& g, hipStream_t s);
@@ -200,7 +200,48 @@ int gemm_f32(const GemmDesc& g, hipStream_t s);
 // with depth-major right operands, none of whose outputs shares memory with an operand, as one launch.  SDP_ERR_UNSUPPORTED: not
 // these; nothing was launched.
 int gemm_f32_group(const GemmDesc* d, int n, const char* name, hipStream_t s);
-// ---- the output head's contractions (bf16), of `rows` tokens, of whom those from number `base` on have a target: min(rows, *live - base) -----
+// ---- the output head's contractions (bf16) of a piece of at most `rows` tokens; how many of them have a target the device knows ----------------
+// Of a contraction of `tiles` tiles, workgroups below `head` take a whole one; the tiles of the last round are cut into `parts` ranges of
+// `steps` depth steps, which a second kernel adds up.
+constexpr int kHeadRound = 256; // workgroups of a full round: the CUs
+struct HeadCut {
+    int head, tail, parts, steps;
+};
+// what the device says of a piece
+struct HeadPiece {
+    int rows; // its tokens
+    int pad[3];
+    HeadCut dx, dw;
+};
+// What it needs for that: the tiles' sizes, a depth step's and an epilogue's us, and the most that the cut tiles may become (0: no cut)
+struct HeadTiles {
+    int bm, bn;
+    float step, epilogue;
+    int most;
+};
+HeadTiles head_dx_tiles(int rows, int V, int d), head_dw_tiles(int rows, int V, int d, int pieces);
+// scratch of the cut tiles
+inline size_t head_cut_bytes(const HeadTiles& t) { return (size_t)t.most * t.bm * t.bn * 4; }
+#ifdef __HIPCC__
+// The cut of `tiles` tiles of nk steps, by a whole wave (lane p - 1 looks at p parts): whole tiles for the full rounds, and for the last one as
+// many ranges as make it shortest, with what the partial sums move at 4 TB/s and a launch counted.
+__device__ inline HeadCut head_cut(const HeadTiles& t, int tiles, int nk) {
+    const int p = (int)(threadIdx.x & 63) + 1, head = tiles / kHeadRound * kHeadRound, tail = tiles - head;
+    const int steps = (nk + p - 1) / p, rounds = (tail * p + kHeadRound - 1) / kHeadRound;
+    float cost = (float)rounds * ((float)steps * t.step + t.epilogue);
+    if (p > 1) cost = cost * 1.05f + (float)(tail * p) * (float)(t.bm * t.bn) * 2e-6f + 3.f;
+    if (p > 1 && (tail * p > t.most || steps < 4 || (nk + steps - 1) / steps != p)) cost = INFINITY; // (no empty range)
+    int best = p;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const float c = __shfl_xor(cost, d, 64);
+        const int b = __shfl_xor(best, d, 64);
+        if (c < cost || (c == cost && b < best)) cost = c, best = b;
+    }
+    if (best < 2 || tail == 0) return {tiles, 0, 1, nk};
+    return {head, tail, best, (nk + best - 1) / best};
+}
+#endif
 struct HeadGemm {
     const void* X = nullptr;  // [rows][d], theirs without gaps
     const void* Xt = nullptr; // [d][ldt]: the same columns by columns, zeros behind the last token to a multiple of 8
@@ -209,8 +250,7 @@ struct HeadGemm {
     void* P = nullptr;       // [rows][ldp]: codes of their logits, then mass p - q: their gradient without its factor
     int64_t ldp = 0;
     int rows = 0, V = 0, d = 0;
-    const int32_t* live = nullptr;
-    int base = 0;
+    const HeadPiece* piece = nullptr;
     float scale = 1.f; // of dX and dW: scale scale_dev[0], in fp32 before they are rounded
     const float* scale_dev = nullptr;
 };
@@ -222,12 +262,12 @@ constexpr float kCodeRange = 96.f;
 // Columns of a block; rate = log2(e) / tau.  (m = rate x largest logit, sum of 2^(rate z - m)) of each go into stats [rows][nblk].
 int head_block(int rows, int V, int d);
 int gemm_head_logits(const HeadGemm& h, float rate, bool codes, float2* stats, int nblk, const int32_t* labels, float* at_label, hipStream_t s);
-// dX[list[row]] = P W, with scratch of head_dx_ws_bytes
-size_t head_dx_ws_bytes(int rows, int V, int d);
-int gemm_head_dx(const HeadGemm& h, const int32_t* list, void* dX, float* split_ws, hipStream_t s);
-// dW = P^T X over pieces of tokens (piece: 0 the only one, 1 first, 2 between, 3 last), which share sums of head_sums_bytes
+// dX[list[row]] = P W, with scratch of head_cut_bytes
+int gemm_head_dx(const HeadGemm& h, const int32_t* list, void* dX, float* cut_ws, hipStream_t s);
+// dW = P^T X over pieces of tokens (of: 0 the only one, 1 first, 2 between, 3 last), which share sums of head_sums_bytes; the only one takes
+// scratch of head_cut_bytes instead
 size_t head_sums_bytes(int V, int d);
-int gemm_head_dw(const HeadGemm& h, void* dW, float* sums, int piece, hipStream_t s);
+int gemm_head_dw(const HeadGemm& h, void* dW, float* sums, int of, float* cut_ws, hipStream_t s);
 // Plain LDS-tiled bf16 contraction, any shape: what the MFMA kernel's address ranges do not take.
 int gemm_simple(const GemmDesc& g, hipStream_t s);
 // bf16 MFMA contraction; returns SDP_ERR_UNSUPPORTED when the shape / alignment does not fit.
