@@ -128,6 +128,14 @@ struct HeadArgs {
     int of;
 };
 
+// q of tail_position(q, ntiles, 0) = position
+__host__ __device__ inline int tail_number(int position, int ntiles) {
+    const int base = ntiles / NUM_XCD, rem = ntiles % NUM_XCD, longer = rem * (base + 1);
+    const int x = position < longer ? position / (base + 1) : rem + (position - longer) / base;
+    const int i = position - x * base - (x < rem ? x : rem);
+    return i < base ? i * NUM_XCD + x : NUM_XCD * base + x;
+}
+
 // two fp32 -> packed bf16, round to nearest even (the hardware's v_cvt_pk_bf16_f32)
 __device__ inline uint32_t pack_bf16(float lo, float hi) {
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -917,13 +925,15 @@ __device__ __attribute__((always_inline)) inline void gemm_tile(const Dev& g, co
             // fp32 partial tile of this depth range, tile-local [BM][BN]; rows and columns outside the matrix hold
             // what the clamped operand rows gave and are never read back
             float* P = g.partial + ((int64_t)tail_part * g.tail + tail_q) * (BM * BN);
+            if constexpr (is_head(OP)) P += (wave * (FM * FN * 4) * 64 + lane) * 4; // as the accumulators lie: 1 KB a store
 #pragma unroll
             for (int i = 0; i < FM; ++i)
 #pragma unroll
                 for (int j = 0; j < FN; ++j)
 #pragma unroll
                     for (int q = 0; q < 4; ++q)
-                        *(f32x4*)(P + (WM * wm + 32 * i + 16 * (q >> 1) + l16) * BN + WN * wn + 32 * j + 16 * (q & 1) + 4 * lq) =
+                        if constexpr (is_head(OP)) *(f32x4*)(P + ((i * FN + j) * 4 + q) * 256) = acc[i][j][q];
+                        else *(f32x4*)(P + (WM * wm + 32 * i + 16 * (q >> 1) + l16) * BN + WN * wn + 32 * j + 16 * (q & 1) + 4 * lq) =
                             acc[i][j][q];
             return;
         }
@@ -1202,7 +1212,7 @@ __device__ __attribute__((always_inline)) inline void gemm_tile(const Dev& g, co
                     for (int q = 0; q < 4; ++q)
                         strip_put(strip0, 32 * j, q,
                                   pack4(acc[i][j][q][0], acc[i][j][q][1], acc[i][j][q][2], acc[i][j][q][3]));
-                if (g.cs) strip_store_scatter(strip0, gC, g.ldc, g.cs, i); else strip_store(strip0, gC, g.ldc, i, std::integral_constant<int, kKeep>{});
+                if (g.cs) strip_store_scatter(strip0, gC, g.ldc, g.cs, i); else strip_store(strip0, gC, g.ldc, i, std::integral_constant<int, kHeadDw ? kStream : kKeep>{});
             } else if (EPI == EPI_SWIGLU_FWD) {
                 // fragments 2 jj (gate) and 2 jj + 1 (up) cover the same 32 neurons
 #pragma unroll
@@ -2003,10 +2013,10 @@ namespace {
 template <int BM, int OP>
 __device__ inline bool head_view(Dev& g, const HeadArgs& head, const HeadPiece& piece) {
     if constexpr (OP == OP_HEAD_DW) {
-        g.K = piece.rows;
+        g.K = piece.rows * piece.terms;
         if (g.K == 0 && head.of == 2) return false; // the sums stay
     } else {
-        g.M = piece.rows;
+        g.M = piece.rows * (OP == OP_HEAD_DX ? piece.terms : 1);
         if (g.M == 0) return false;
         g.tiles_m = (g.M + BM - 1) / BM;
         g.ntot = g.tiles_m * g.tiles_n;
@@ -2028,29 +2038,47 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, BM == 64 && BN == 64 ? 2 : 1
     gemm_tile<BM, BN, WAVES_M, WAVES_N, EPI, OP, KM>(g, (int)blockIdx.x, smem, head);
 }
 
-// the ranges of every cut tile, in depth order -> its rows; a thread per 8 columns
-template <int BM, int BN, int OP>
+// The ranges of every cut tile, in depth order -> its rows; a thread per 4 columns, in the order of the accumulators
+template <int BM, int BN, int WAVES_M, int WAVES_N, int OP>
 __global__ __launch_bounds__(256) void head_cut_kernel(Dev g, HeadArgs head) {
+    constexpr int WM = BM / WAVES_M, WN = BN / WAVES_N, FN = WN / 32, PER_WAVE = WM * WN / 4;
     const HeadPiece piece = *head.piece;
     if (!head_view<BM, OP>(g, head, piece)) return;
     const float c = head.scale * (head.scale_dev ? *head.scale_dev : 1.f);
+    auto put = [&](int m, int n, const f32x4& a) {
+        const int64_t to = g.cs ? g.cs[m] : m;
+        *(u32x2*)(g.C + to * g.ldc + n) = pack4(a[0] * c, a[1] * c, a[2] * c, a[3] * c);
+    };
+    if (OP == OP_HEAD_DX && piece.terms == 2) { // all tiles are here; a token's two rows
+        auto part = [&](int m, int n) {
+            const int tile_m = m / BM, first_m = tile_m / g.group_m * g.group_m, gm = g.tiles_m - first_m < g.group_m ? g.tiles_m - first_m : g.group_m;
+            const int q = tail_number(first_m * g.tiles_n + tile_m - first_m + n / BN * gm, g.ntot);
+            const int r = m % BM, col = n % BN, wave = r / WM * WAVES_N + col / WN, i = r % WM / 32, j = col % WN / 32;
+            const int unit = wave * PER_WAVE + ((i * FN + j) * 4 + r % 32 / 16 * 2 + col % 32 / 16) * 64 + col % 16 / 4 * 16 + r % 16;
+            return g.partial + (int64_t)q * (BM * BN) + unit * 4;
+        };
+        for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)piece.rows * (g.N / 4); i += (int64_t)gridDim.x * 256) {
+            const int m = (int)(i / (g.N / 4)), n = (int)(i % (g.N / 4)) * 4;
+            const float *p = part(m, n), *second = part(m + piece.rows, n);
+            f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
+            for (int k = 0; k < g.ksplit; ++k, p += (int64_t)g.tail * (BM * BN), second += (int64_t)g.tail * (BM * BN)) a += *(const f32x4*)p, b += *(const f32x4*)second;
+            put(m, n, a + b);
+        }
+        return;
+    }
     const int rows = OP == OP_HEAD_DW ? head.out_rows : g.M;
-    const int64_t all = (int64_t)g.tail * (BM * BN / 8);
+    const int64_t all = (int64_t)g.tail * (BM * BN / 4);
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
-        const int q = (int)(i / (BM * BN / 8)), e = (int)(i % (BM * BN / 8)), row = e / (BN / 8), col = e % (BN / 8) * 8;
+        const int q = (int)(i / (BM * BN / 4)), unit = (int)(i % (BM * BN / 4)), wave = unit / PER_WAVE, f = unit % PER_WAVE / 64, lane = unit % 64;
         const int bid = tail_position(q, g.ntot, g.n_head), per_group = g.group_m * g.tiles_n, grp = bid / per_group, first_m = grp * g.group_m;
         const int gm = g.tiles_m - first_m < g.group_m ? g.tiles_m - first_m : g.group_m, in = bid - grp * per_group;
-        const int m = (first_m + in % gm) * BM + row, n = in / gm * BN + col;
+        const int m = (first_m + in % gm) * BM + wave / WAVES_N * WM + f / 4 / FN * 32 + f % 4 / 2 * 16 + lane % 16;
+        const int n = in / gm * BN + wave % WAVES_N * WN + f / 4 % FN * 32 + f % 2 * 16 + lane / 16 * 4;
         if (m >= rows || n >= g.N) continue;
-        f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
-        for (int k = 0; k < g.ksplit; ++k) {
-            const float* p = g.partial + ((int64_t)k * g.tail + q) * (BM * BN) + row * BN + col;
-            a += *(const f32x4*)p;
-            b += *(const f32x4*)(p + 4);
-        }
-        a *= c, b *= c;
-        const int64_t to = g.cs ? g.cs[m] : m;
-        *(u32x4*)(g.C + to * g.ldc + n) = u32x4{pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3]), pack_bf16(b[0], b[1]), pack_bf16(b[2], b[3])};
+        f32x4 a = {0.f, 0.f, 0.f, 0.f};
+        const float* p = g.partial + (int64_t)q * (BM * BN) + unit * 4;
+        for (int k = 0; k < g.ksplit; ++k, p += (int64_t)g.tail * (BM * BN)) a += *(const f32x4*)p;
+        put(m, n, a);
     }
 }
 
@@ -2074,8 +2102,8 @@ int launch_head_cfg(const GemmDesc& d, const HeadArgs& head, int most, hipStream
     if (rc != SDP_OK || most == 0) return rc;
     if constexpr (is_tail(OP)) {
         ProfileScope ps("head_cut", s);
-        const int64_t groups = (int64_t)(g.ntot < kHeadRound ? g.ntot : kHeadRound - 1) * (BM * BN / 8 / 256);
-        head_cut_kernel<BM, BN, OP><<<(unsigned)(groups < 2048 ? groups : 2048), 256, 0, s>>>(g, head);
+        const int64_t groups = (int64_t)(g.ntot < kHeadRound ? g.ntot : kHeadRound - 1) * (BM * BN / 4 / 256);
+        head_cut_kernel<BM, BN, WAVES_M, WAVES_N, OP><<<(unsigned)(groups < 2048 ? groups : 2048), 256, 0, s>>>(g, head);
     }
     return launch_status();
 }
@@ -2099,24 +2127,31 @@ GemmDesc extents(int M, int N, int K) {
     return d;
 }
 
-// Tiles of a contraction whose last round is cut (head_cut): those that take least when all tokens have a target
-HeadTiles cut_tiles(int M, int N, int K, bool cuts) {
-    const int nk = (K + BK - 1) / BK;
+// us of M x N outputs, nk steps deep, in tiles whose last round is cut as head_cut does it
+double cut_us(const HeadTiles& t, int M, int N, int nk) {
+    const int64_t tiles = (int64_t)((M + t.bm - 1) / t.bm) * ((N + t.bn - 1) / t.bn);
+    const int tail = (int)(tiles % kHeadRound);
+    const double one = (double)nk * t.step + t.epilogue;
+    double last = tail ? one : 0.0;
+    for (int p = 2; p <= 64 && tail * p <= t.most && (nk + p - 1) / p >= 4; ++p) {
+        const double rounds = (tail * p + kHeadRound - 1) / kHeadRound;
+        const double cost = 1.05 * rounds * ((nk + p - 1) / p * t.step + t.epilogue) + (double)tail * p * t.bm * t.bn * 2e-6 + 3.0;
+        last = cost < last ? cost : last;
+    }
+    return (double)(tiles / kHeadRound) * one + last;
+}
+// The tiles that take least, on the mean of five numbers of tokens, from all that there may be to half of them: those of dX chosen for all
+// tokens took 715 us where a third of 5000 had no label (128 x 256, d = 1600, V = 50001), now 445.
+template <class F>
+HeadTiles cut_tiles(bool cuts, int rows, F&& us) {
     HeadTiles best{};
     double least = -1;
     for (int i = 0; i < NUM_SHAPES; ++i) {
         const ShapeInfo& h = kShapes[i];
         const EpilogueCost e = epilogue_cost(EPI_STORE);
-        const HeadTiles t{h.bm, h.bn, (float)h.step1, (float)(e.e0 + e.e1 * h.bm * h.bn / 1024), cuts && nk >= 8 ? (i == T64x64 ? 1024 : 512) : 0};
-        const int64_t tiles = (int64_t)((M + h.bm - 1) / h.bm) * ((N + h.bn - 1) / h.bn), full = tiles / kHeadRound;
-        const int tail = (int)(tiles % kHeadRound);
-        const double one = nk * t.step + t.epilogue;
-        double last = tail ? one : 0.0;
-        for (int p = 2; p <= 64 && tail * p <= t.most && (nk + p - 1) / p >= 4; ++p) {
-            const double cost = 1.05 * ((tail * p + kHeadRound - 1) / kHeadRound) * ((nk + p - 1) / p * t.step + t.epilogue) + (double)tail * p * h.bm * h.bn * 2e-6 + 3.0;
-            last = cost < last ? cost : last;
-        }
-        const double cost = (double)full * one + last;
+        const HeadTiles t{h.bm, h.bn, (float)h.step1, (float)(e.e0 + e.e1 * h.bm * h.bn / 1024), cuts ? (i == T64x64 ? 1024 : 512) : 0};
+        double cost = 0;
+        for (int eighths = 8; eighths >= 4; --eighths) cost += us(t, head_held((int)(((int64_t)rows * eighths + 7) / 8)));
         if (least < 0 || cost < least) least = cost, best = t;
     }
     return best;
@@ -2135,11 +2170,15 @@ int gemm_head_logits(const HeadGemm& h, float rate, bool codes, float2* stats, i
     return launch_head<EPI_CODES, OP_HEAD_LOGITS, 0>(d, a, t.bm, t.bn, 0, s);
 }
 
-HeadTiles head_dx_tiles(int rows, int V, int d) { return cut_tiles(rows, d, V, true); }
-HeadTiles head_dw_tiles(int rows, int V, int d, int pieces) { return cut_tiles(V, d, rows, pieces == 1); }
+HeadTiles head_dx_tiles(int rows, int V, int d) {
+    return cut_tiles(true, rows, [&](const HeadTiles& t, int held) { return cut_us(t, held, d, (V + BK - 1) / BK); });
+}
+HeadTiles head_dw_tiles(int rows, int V, int d, int pieces) {
+    return cut_tiles(pieces == 1 && head_held(rows) >= 512, rows, [&](const HeadTiles& t, int held) { return cut_us(t, V, d, (held + BK - 1) / BK); });
+}
 
 int gemm_head_dx(const HeadGemm& h, const int32_t* list, void* dX, float* cut_ws, hipStream_t s) {
-    GemmDesc d = extents(h.rows, h.d, h.V);
+    GemmDesc d = extents(head_held(h.rows), h.d, h.V);
     d.A = h.P, d.lda = h.ldp, d.B = h.W, d.ldb = h.d, d.b_km = 1, d.C = dX, d.ldc = h.d, d.c_scatter = list, d.tail_ws = cut_ws, d.name = "head_dx";
     HeadArgs a{};
     a.piece = h.piece, a.scale = h.scale, a.scale_dev = h.scale_dev;
@@ -2150,7 +2189,7 @@ int gemm_head_dx(const HeadGemm& h, const int32_t* list, void* dX, float* cut_ws
 size_t head_sums_bytes(int V, int d) { return (size_t)((V + 255) / 256 * 256) * ((d + 767) / 768 * 768) * 4; } // whole tiles of any shape
 
 int gemm_head_dw(const HeadGemm& h, void* dW, float* sums, int of, float* cut_ws, hipStream_t s) {
-    GemmDesc d = extents((h.V + 7) / 8 * 8, h.d, h.rows); // columns of the logits' rows in whole chunks: the last ones are zeros
+    GemmDesc d = extents((h.V + 7) / 8 * 8, h.d, head_held(h.rows)); // columns of the logits' rows in whole chunks: the last ones are zeros
     d.A = h.P, d.lda = h.ldp, d.a_km = 1, d.B = h.Xt, d.ldb = h.ldt, d.C = dW, d.ldc = h.d, d.tail_ws = cut_ws, d.name = "head_dw";
     HeadArgs a{};
     a.piece = h.piece, a.scale = h.scale, a.scale_dev = h.scale_dev, a.out_rows = h.V, a.sums = sums, a.of = of;

@@ -40,6 +40,16 @@ struct Shapes {
     int rows, pieces, V, d;
 };
 
+// by a whole wave
+__device__ inline void plan_piece(const Shapes& g, int rows, sdp::HeadPiece* to) {
+    auto tiles = [](const sdp::HeadTiles& t, int m, int n) { return ((m + t.bm - 1) / t.bm) * ((n + t.bn - 1) / t.bn); };
+    const bool two = rows <= sdp::kTwoTermRows && tiles(g.dx, 2 * rows, g.d) <= g.dx.most;
+    const int held = two ? 2 * rows : rows;
+    const sdp::HeadCut dx = sdp::head_cut(g.dx, tiles(g.dx, held, g.d), (g.V + 63) / 64, two);
+    const sdp::HeadCut dw = sdp::head_cut(g.dw, tiles(g.dw, g.V, g.d), (held + 63) / 64);
+    if ((threadIdx.x & 63) == 0) *to = {rows, two ? 2 : 1, {}, dx, dw};
+}
+
 // list: the tokens with a target in order, from its front; the others as -1 - token, from its end.  pieces: what each of them has of the former
 // (bf16).  One workgroup: 16384 tokens are one turn.  FROM: 0, 1 labels of 32, 64 bits, 2 what entries_kernel wrote.
 template <int FROM>
@@ -84,18 +94,44 @@ __global__ __launch_bounds__(1024) void list_kernel(const void* __restrict__ fro
     }
     if (!pieces) return;
     for (int p = wave; p < g.pieces; p += 16) {
-        const int left = before - p * g.rows, rows = left < 0 ? 0 : left < g.rows ? left : g.rows;
-        const sdp::HeadCut dx = sdp::head_cut(g.dx, ((rows + g.dx.bm - 1) / g.dx.bm) * ((g.d + g.dx.bn - 1) / g.dx.bn), (g.V + 63) / 64);
-        const sdp::HeadCut dw = sdp::head_cut(g.dw, ((g.V + g.dw.bm - 1) / g.dw.bm) * ((g.d + g.dw.bn - 1) / g.dw.bn), (rows + 63) / 64);
-        if (lane == 0) pieces[p] = {rows, {}, dx, dw};
+        const int left = before - p * g.rows;
+        plan_piece(g, left < 0 ? 0 : left < g.rows ? left : g.rows, pieces + p);
     }
+}
+
+// The list of at most kSmallList tokens with labels, by every workgroup of TH threads that needs it, in its own LDS; returns how many have one.
+constexpr int kSmallList = 1024;
+template <int TH>
+__device__ int small_list(const void* labels, int wide, int T, int V, int32_t* list) {
+    __shared__ uint64_t masks[kSmallList / 64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int c = 0; c < kSmallList / 64; c += TH / 64) {
+        const int t = (c + wave) * 64 + lane;
+        const uint64_t mask = __ballot(sdp::token_id(labels, wide, t < T ? t : T - 1, V) >= 0 && t < T);
+        if (lane == 0) masks[c + wave] = mask;
+    }
+    __syncthreads();
+    int before = 0;
+    for (int c = 0; c * 64 < T; ++c) {
+        const uint64_t mask = masks[c];
+        if (c % (TH / 64) == wave) {
+            const int t = c * 64 + lane, mine = before + __popcll(mask & ((1ull << lane) - 1));
+            if (t < T) list[mask >> lane & 1 ? mine : T - 1 - (t - mine)] = mask >> lane & 1 ? t : -1 - t;
+        }
+        before += __popcll(mask);
+    }
+    __syncthreads();
+    return before;
 }
 
 struct Gather {
     const void* X;
     void *Xc, *Xt, *dX; // Xt: may be null; dX: zeros for tokens without a target, may be null
     int64_t ldt;
-    const int32_t* list;
+    int32_t* list; // SMALL: made here, of T = rows tokens
+    sdp::HeadPiece* piece;
+    Shapes shapes;
     const void* labels_in;
     int wide;
     int32_t* labels; // [row], -1 for none; may be null
@@ -104,21 +140,38 @@ struct Gather {
 
 // Rows of X in the list's order, and (bf16) the same column by column for dW, whose depth they are: read along it, they need one LDS read a
 // fragment where rows need two (a depth step of 256 x 256 1.67 -> 1.40 us with one transposed operand instead of two).  A workgroup takes
-// 64 tokens x 64 columns; tokens without a target are zeros.  bf16: d a multiple of 8, 16-byte aligned.
+// 64 tokens x 64 columns; tokens without a target are zeros.  d a multiple of 8, 16-byte aligned.  With two terms (HeadPiece) the columns behind
+// the last token are those of all tokens again.  SMALL: the list and the plan of the other kernels are made here as well, a launch less.
+template <int SMALL>
 __global__ __launch_bounds__(256) void gather_kernel(Gather a) {
     __shared__ uint16_t tile[64][72]; // rows of 144 bytes: 16 of them start on different banks
+    __shared__ int32_t small[SMALL ? kSmallList : 1];
     const int tid = threadIdx.x, r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;
+    const int32_t* list = a.list;
+    int live, terms;
+    if constexpr (SMALL) {
+        live = small_list<256>(a.labels_in, a.wide, a.rows, a.V, small);
+        list = small;
+        if (r0 == 0 && c0 == 0) {
+            for (int i = tid; i < a.rows; i += 256) a.list[i] = small[i];
+            if (tid < 64) plan_piece(a.shapes, live, a.piece);
+        }
+        terms = live <= sdp::kTwoTermRows ? 2 : 1; // columns of more than the plan has do no harm
+    } else {
+        live = a.piece->rows, terms = a.piece->terms;
+    }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const int r = 32 * h + tid / 8, c = c0 + tid % 8 * 8;
-        const int listed = r0 + r < a.rows ? a.list[r0 + r] : -1;
+        const int listed = r0 + r < a.rows ? list[r0 + r] : -1;
         u32x4 w = {0, 0, 0, 0};
-        if (c < a.d && r0 + r < a.rows) {
-            if (listed >= 0) {
+        if (c < a.d) {
+            if (r0 + r < a.rows && listed >= 0) {
                 w = *(const u32x4*)((const uint16_t*)a.X + (int64_t)listed * a.d + c);
                 *(u32x4*)((uint16_t*)a.Xc + (int64_t)(r0 + r) * a.d + c) = w; // read next
-            } else if (a.dX) {
-                *(u32x4*)((uint16_t*)a.dX + (int64_t)(-1 - listed) * a.d + c) = w;
+            } else {
+                if (r0 + r < a.rows && a.dX) *(u32x4*)((uint16_t*)a.dX + (int64_t)(-1 - listed) * a.d + c) = w;
+                if (r0 + r < live * terms) w = *(const u32x4*)((const uint16_t*)a.X + (int64_t)list[r0 + r - live] * a.d + c);
             }
         }
         if (a.labels && c0 == 0 && tid % 8 == 0 && r0 + r < a.rows) a.labels[r0 + r] = listed < 0 ? -1 : sdp::token_id(a.labels_in, a.wide, listed, a.V);
@@ -138,12 +191,19 @@ __global__ __launch_bounds__(256) void gather_kernel(Gather a) {
 }
 
 // fp32: a wave a row, of any width and alignment
+template <int SMALL>
 __global__ __launch_bounds__(64) void gather_f32_kernel(Gather a) {
     typedef Row<0> Rw;
     constexpr int N = Rw::N;
+    __shared__ int32_t small[SMALL ? kSmallList : 1];
     const int64_t row = sdp::group_id();
     if (row >= a.rows) return;
-    const int listed = a.list[row], tid = threadIdx.x, d = a.d, whole = Rw::whole(d);
+    if constexpr (SMALL) {
+        small_list<64>(a.labels_in, a.wide, a.rows, a.V, small);
+        if (row == 0)
+            for (int i = threadIdx.x; i < a.rows; i += 64) a.list[i] = small[i];
+    }
+    const int listed = SMALL ? small[row] : a.list[row], tid = threadIdx.x, d = a.d, whole = Rw::whole(d);
     const float* x = (const float*)a.X + (int64_t)(listed < 0 ? 0 : listed) * d;
     float* xc = (float*)a.Xc + row * d;
     float* dx = (float*)a.dX + (int64_t)(listed < 0 ? -1 - listed : 0) * d;
@@ -210,17 +270,18 @@ struct CodeRows {
     const float* z;  // [row][k]
     Targets t;
     const int32_t* list;
+    const sdp::HeadPiece* piece;
     float *kl, *lse;
     int rows, V;
 };
 
 // A row of codes and its blocks' statistics -> its loss, lse and gradient.  One workgroup a row.  ONCE: around the caches, where the codes are far
 // more than the 256 MB behind the L2s hold: 16384 x 32000 444 -> 396 us, but 3350 x 50001 123 -> 136.
-constexpr int kCodeThreads = 256;
-template <int ONCE>
-__global__ __launch_bounds__(kCodeThreads) void code_rows_kernel(CodeRows a) {
+// Few rows: 16 waves each.
+template <int ONCE, int TH>
+__global__ __launch_bounds__(TH) void code_rows_kernel(CodeRows a) {
     typedef Row<1> Rw;
-    constexpr int TH = kCodeThreads, WAVES = TH / 64;
+    constexpr int WAVES = TH / 64;
     __shared__ float lds[3][2][WAVES];
     extern __shared__ unsigned char entry_lds[];
     const int64_t row = sdp::group_id();
@@ -270,6 +331,8 @@ __global__ __launch_bounds__(kCodeThreads) void code_rows_kernel(CodeRows a) {
     // and keeps a small factor out of bf16's range.
     const float inv = mass / sum;
     uint16_t* p = a.P + row * a.ldp;
+    const sdp::HeadPiece* piece = a.piece;
+    uint16_t* second = piece->terms == 2 ? p + piece->rows * a.ldp : nullptr; // the second term's row
     constexpr float kStep = sdp::kCodeRange / 65535.f;
     const int end = (a.V + 7) / 8 * 8; // codes of columns behind V say 0
     auto value = [&](uint32_t code, float from) { return code == 65535u ? 0.f : __builtin_amdgcn_exp2f(fmaf((float)code, -kStep, from)) * inv; };
@@ -280,6 +343,10 @@ __global__ __launch_bounds__(kCodeThreads) void code_rows_kernel(CodeRows a) {
         for (int i = 0; i < 4; ++i) v[2 * i] = value(w[i] & 0xFFFFu, from), v[2 * i + 1] = value(w[i] >> 16, from);
         if (ONCE) __builtin_nontemporal_store(Rw::pack(v), (u32x4*)(p + e));
         else *(u32x4*)(p + e) = Rw::pack(v); // read next
+        if (!second) return;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] -= Rw::rounded(v[i]);
+        *(u32x4*)(second + e) = Rw::pack(v);
     };
     constexpr int U = 4;
     for (int e0 = tid * 8; e0 < end; e0 += U * TH * 8) {
@@ -298,8 +365,12 @@ __global__ __launch_bounds__(kCodeThreads) void code_rows_kernel(CodeRows a) {
     // The entries' elements are written twice: the first time has to have reached memory, whichever wave it came from.
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
-    for (int i = tid; i < k; i += TH)
-        if (en.id[i] >= 0) Rw::put(p + en.id[i], __builtin_amdgcn_exp2f(fmaf(en.z[i], rate, -m)) * inv - en.all_of(i, k));
+    for (int i = tid; i < k; i += TH) {
+        if (en.id[i] < 0) continue;
+        const float v = __builtin_amdgcn_exp2f(fmaf(en.z[i], rate, -m)) * inv - en.all_of(i, k);
+        Rw::put(p + en.id[i], v);
+        if (second) Rw::put(second + en.id[i], v - Rw::rounded(v));
+    }
 }
 
 __global__ __launch_bounds__(256) void zero_kernel(uint16_t* p, int64_t n) {
@@ -339,10 +410,11 @@ Plan plan(int dtype, int T, int V, int d, int k, bool teacher, bool dx, bool dw)
     p.X = take(rows * d * (bf16 ? 2 : 4));
     if (bf16) {
         p.ldz = sdp::line_ld(V, p.rows);
-        p.ldt = sdp::line_ld(p.rows, d);
+        const size_t held = (size_t)sdp::head_held(p.rows);
+        p.ldt = sdp::line_ld((int64_t)held, d);
         if (dw) p.Xt = take((size_t)p.ldt * d * 2);
         p.block = sdp::head_block(p.rows, V, d), p.nblk = (V + p.block - 1) / p.block;
-        if (grads) p.Z = take(rows * p.ldz * 2);
+        if (grads) p.Z = take(held * p.ldz * 2);
         p.stats = take(rows * p.nblk * 8);
         if (!teacher) p.labels = take(rows * 4);
         p.z = take(rows * k * 4);
@@ -375,12 +447,13 @@ int run(const Call& c, unsigned char* ws, hipStream_t s) {
     int32_t* list = (int32_t*)(ws + p.list);
     sdp::HeadPiece* pieces = bf16 ? (sdp::HeadPiece*)(ws + p.piece) : nullptr;
     const Shapes shapes{p.tx, p.tw, p.rows, p.pieces, c.V, c.d};
+    const bool small = !teacher && p.pieces == 1 && c.T <= (bf16 ? kSmallList : 256); // listed by what gathers
     uint8_t* has = teacher ? ws + p.has : nullptr;
     if (teacher) {
         sdp::ProfileScope ps("head_entries", s);
         entries_kernel<<<sdp::grid_of((c.T + 3) / 4), 256, 0, s>>>(c.t, c.T, c.V, has);
     }
-    {
+    if (!small) {
         sdp::ProfileScope ps("head_list", s);
         if (teacher) list_kernel<2><<<1, 1024, 0, s>>>(has, c.T, c.V, list, pieces, shapes);
         else if (c.t.wide) list_kernel<1><<<1, 1024, 0, s>>>(c.t.ids, c.T, c.V, list, pieces, shapes);
@@ -389,12 +462,15 @@ int run(const Call& c, unsigned char* ws, hipStream_t s) {
     int rc = sdp::launch_status();
     for (int i = 0; i < p.pieces && rc == SDP_OK; ++i) {
         const int base = i * p.rows, rows = c.T - base < p.rows ? c.T - base : p.rows;
-        Gather g{c.X, ws + p.X, c.dW && bf16 ? ws + p.Xt : nullptr, c.dX, p.ldt, list + base, c.t.ids, c.t.wide, nullptr, rows, c.V, c.d};
+        Gather g{c.X, ws + p.X, c.dW && bf16 ? ws + p.Xt : nullptr, c.dX, p.ldt, list + base, pieces + i, shapes, c.t.ids, c.t.wide, nullptr, rows, c.V, c.d};
         if (bf16 && !teacher) g.labels = (int32_t*)(ws + p.labels);
         {
             sdp::ProfileScope ps("head_gather", s);
-            if (bf16) gather_kernel<<<dim3((rows + 63) / 64, (c.d + 63) / 64), 256, 0, s>>>(g);
-            else gather_f32_kernel<<<sdp::grid_of(rows), 64, 0, s>>>(g);
+            const dim3 grid((sdp::head_held(rows) + 63) / 64, (c.d + 63) / 64);
+            if (bf16 && small) gather_kernel<1><<<grid, 256, 0, s>>>(g);
+            else if (bf16) gather_kernel<0><<<grid, 256, 0, s>>>(g);
+            else if (small) gather_f32_kernel<1><<<sdp::grid_of(rows), 64, 0, s>>>(g);
+            else gather_f32_kernel<0><<<sdp::grid_of(rows), 64, 0, s>>>(g);
         }
         rc = sdp::launch_status();
         if (rc != SDP_OK) return rc;
@@ -411,12 +487,13 @@ int run(const Call& c, unsigned char* ws, hipStream_t s) {
             }
             rc = sdp::gemm_head_logits(h, sdp::kLog2e * c.t.inv_tau, grads, stats, p.nblk, g.labels, z, s);
             if (rc != SDP_OK) return rc;
-            const CodeRows r{grads ? (uint16_t*)h.P : nullptr, p.ldz, stats, p.nblk, p.block == 64 ? 6 : 5, z, c.t, list + base, c.kl, c.lse, rows, c.V};
+            const CodeRows r{grads ? (uint16_t*)h.P : nullptr, p.ldz, stats, p.nblk, p.block == 64 ? 6 : 5, z, c.t, list + base, pieces + i, c.kl, c.lse, rows, c.V};
             {
                 sdp::ProfileScope ps("head_rows", s);
                 const size_t lds = sdp::Entries::bytes(c.t.k);
-                if (grads && (size_t)rows * p.ldz * 2 >= (size_t)1 << 29) code_rows_kernel<1><<<sdp::grid_of(rows), kCodeThreads, lds, s>>>(r);
-                else code_rows_kernel<0><<<sdp::grid_of(rows), kCodeThreads, lds, s>>>(r);
+                if (grads && (size_t)rows * p.ldz * 2 >= (size_t)1 << 29) code_rows_kernel<1, 256><<<sdp::grid_of(rows), 256, lds, s>>>(r);
+                else if (rows > 512) code_rows_kernel<0, 256><<<sdp::grid_of(rows), 256, lds, s>>>(r);
+                else code_rows_kernel<0, 1024><<<sdp::grid_of(rows), 1024, lds, s>>>(r);
             }
             rc = sdp::launch_status();
             if (rc == SDP_OK && c.dX) rc = sdp::gemm_head_dx(h, list + base, c.dX, (float*)(ws + p.cut), s);
@@ -431,18 +508,18 @@ int run(const Call& c, unsigned char* ws, hipStream_t s) {
         sdp::TargetRows r;
         r.Z = ws + p.Z, r.dZ = grads ? ws + p.Z : nullptr, r.ldz = p.ldz, r.t = c.t, r.kl = c.kl, r.lse = c.lse, r.rows = rows, r.V = c.V, r.list = list + base;
         rc = sdp::target_rows(SDP_F32, r, "head_rows", s);
-        if (rc == SDP_OK && c.dX) {
-            sdp::GemmDesc x;
-            x.M = rows, x.N = c.d, x.K = c.V, x.A = ws + p.Z, x.lda = p.ldz, x.B = c.W, x.ldb = c.d, x.b_km = 1, x.C = c.dX, x.ldc = c.d;
-            x.c_scatter = list + base, x.name = "head_dx";
-            rc = sdp::gemm_f32(x, s);
-        }
-        if (rc == SDP_OK && c.dW) {
-            sdp::GemmDesc w;
-            w.M = c.V, w.N = c.d, w.K = rows, w.A = ws + p.Z, w.lda = p.ldz, w.a_km = 1, w.B = ws + p.X, w.ldb = c.d, w.b_km = 1, w.C = c.dW, w.ldc = c.d;
-            if (i > 0) w.R = c.dW, w.ldr = c.d; // the pieces before
-            w.name = "head_dw";
-            rc = sdp::gemm_f32(w, s);
+        sdp::GemmDesc both[2];
+        sdp::GemmDesc &x = both[0], &w = both[1];
+        x.M = rows, x.N = c.d, x.K = c.V, x.A = ws + p.Z, x.lda = p.ldz, x.B = c.W, x.ldb = c.d, x.b_km = 1, x.C = c.dX, x.ldc = c.d;
+        x.c_scatter = list + base, x.name = "head_dx";
+        w.M = c.V, w.N = c.d, w.K = rows, w.A = ws + p.Z, w.lda = p.ldz, w.a_km = 1, w.B = ws + p.X, w.ldb = c.d, w.b_km = 1, w.C = c.dW, w.ldc = c.d;
+        if (i > 0) w.R = c.dW, w.ldr = c.d; // the pieces before
+        w.name = "head_dw";
+        if (rc != SDP_OK) return rc;
+        rc = c.dX && c.dW ? sdp::gemm_f32_group(both, 2, "head_dx_dw", s) : SDP_ERR_UNSUPPORTED;
+        if (rc == SDP_ERR_UNSUPPORTED) {
+            rc = c.dX ? sdp::gemm_f32(x, s) : SDP_OK;
+            if (rc == SDP_OK && c.dW) rc = sdp::gemm_f32(w, s);
         }
     }
     if (rc != SDP_OK || !c.loss) return rc;

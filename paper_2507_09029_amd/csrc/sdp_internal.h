@@ -207,12 +207,17 @@ constexpr int kHeadRound = 256; // workgroups of a full round: the CUs
 struct HeadCut {
     int head, tail, parts, steps;
 };
-// what the device says of a piece
+// What the device says of a piece: its tokens, and in how many bf16 terms (1 or 2) the logits' gradient enters the products.  One costs a row's dX an error like
+// its own rounding's, but as a row's largest element by itself has it; over many rows these even out.  Of 128 tokens or fewer, whose products wait
+// for W and dW, the second term is a row of its own behind all first ones: dX adds the two rows, and dW's depth has every token twice.
+constexpr int kTwoTermRows = 128;
 struct HeadPiece {
-    int rows; // its tokens
-    int pad[3];
+    int rows, terms;
+    int pad[2];
     HeadCut dx, dw;
 };
+// rows of the gradient that a piece of at most `rows` tokens may have
+inline int head_held(int rows) { return rows >= 2 * kTwoTermRows ? rows : 2 * rows < 2 * kTwoTermRows ? 2 * rows : 2 * kTwoTermRows; }
 // What it needs for that: the tiles' sizes, a depth step's and an epilogue's us, and the most that the cut tiles may become (0: no cut)
 struct HeadTiles {
     int bm, bn;
@@ -225,8 +230,9 @@ inline size_t head_cut_bytes(const HeadTiles& t) { return (size_t)t.most * t.bm 
 #ifdef __HIPCC__
 // The cut of `tiles` tiles of nk steps, by a whole wave (lane p - 1 looks at p parts): whole tiles for the full rounds, and for the last one as
 // many ranges as make it shortest, with what the partial sums move at 4 TB/s and a launch counted.
-__device__ inline HeadCut head_cut(const HeadTiles& t, int tiles, int nk) {
-    const int p = (int)(threadIdx.x & 63) + 1, head = tiles / kHeadRound * kHeadRound, tail = tiles - head;
+// `all`: every tile is a cut one, of one part if need be.
+__device__ inline HeadCut head_cut(const HeadTiles& t, int tiles, int nk, bool all = false) {
+    const int p = (int)(threadIdx.x & 63) + 1, head = all ? 0 : tiles / kHeadRound * kHeadRound, tail = tiles - head;
     const int steps = (nk + p - 1) / p, rounds = (tail * p + kHeadRound - 1) / kHeadRound;
     float cost = (float)rounds * ((float)steps * t.step + t.epilogue);
     if (p > 1) cost = cost * 1.05f + (float)(tail * p) * (float)(t.bm * t.bn) * 2e-6f + 3.f;
@@ -238,7 +244,7 @@ __device__ inline HeadCut head_cut(const HeadTiles& t, int tiles, int nk) {
         const int b = __shfl_xor(best, d, 64);
         if (c < cost || (c == cost && b < best)) cost = c, best = b;
     }
-    if (best < 2 || tail == 0) return {tiles, 0, 1, nk};
+    if (!all && (best < 2 || tail == 0)) return {tiles, 0, 1, nk};
     return {head, tail, best, (nk + best - 1) / best};
 }
 #endif
