@@ -452,7 +452,7 @@ int sdp_label_scale(int id_type, int T, int V, const void* labels, float* scale,
  * top_lse is the teacher's log-sum-exp of all its logits over tau, for a teacher whose mass outside the entries counts as known to be
  * elsewhere: q then sums to less than 1.  An entry whose id lies outside [0, V), or whose logit is -inf, is none, so that shorter lists
  * are padded with either.  A token without entries has no teacher: kl = lse = 0, dZ = 0, its logits are not read.  Entries of
- * one id add up.  Logits Z of -inf are masked ones (probability 0; kl = +inf where an entry names one); a row of nothing else, or one with
+ * one id add up in dZ; kl counts each by itself.  Logits Z of -inf are masked ones (probability 0; kl = +inf where an entry names one); a row of nothing else, or one with
  * +inf or NaN, gives NaN, and so do a NaN among the entries or in top_lse; an entry of +inf gives what the formulas do.
  *   Z, dZ [T][ldz], ldz >= V: columns from V on are neither read nor written.  dZ may be NULL (loss alone) or Z.
  *   ids, top [T][k] in, top of top_dtype (SDP_F32 or SDP_BF16);  top_lse [T] fp32 in, may be NULL
@@ -471,7 +471,8 @@ int sdp_distill_loss(int dtype, int id_type, int top_dtype, int T, int V, int k,
  * without the logits in memory.
  *   nll, lse, loss as there (Z in fp32);   dX = dZ W  [T][d];   dW = dZ^T X  [V][d]
  * It works on as many tokens at a time (64 at least) as keep what it holds of their logits within SDP_HEAD_PIECE_BYTES (2 bytes a logit with
- * SDP_BF16, 4 with SDP_F32), and their X likewise.  Tokens without a label cost nothing but the zeros of their dX: with SDP_BF16 their products are not computed.  Their X is not
+ * SDP_BF16, 4 with SDP_F32), and their X likewise, and on no more than SDP_HEAD_PIECE_TOKENS, so that no sum of dW runs over more before it is
+ * added to the others (over 1.2 million tokens at once fp32 sums drifted by 1e-4).  Tokens without a label cost nothing but the zeros of their dX: with SDP_BF16 their products are not computed.  Their X is not
  * looked at.
  *   X [T][d], W [V][d] (row-major by token of the vocabulary, like an embedding, which it may be), labels [T] in
  *   nll [T] fp32 out;  lse [T] fp32, may be NULL;  loss [1] fp32, may be NULL
@@ -485,6 +486,7 @@ int sdp_distill_loss(int dtype, int id_type, int top_dtype, int T, int V, int k,
  * sdp_head_distill: the same for sdp_distill_loss on Z = X W^T.
  * ------------------------------------------------------------------------------------------- */
 #define SDP_HEAD_PIECE_BYTES (1 << 30)
+#define SDP_HEAD_PIECE_TOKENS (1 << 15)
 size_t sdp_head_loss_workspace_bytes(int dtype, int T, int V, int d, int want_dx, int want_dw);
 int sdp_head_loss(int dtype, int id_type, int T, int V, int d, float scale, const void* X, const void* W, const void* labels,
                   const float* scale_dev, float* nll, float* lse, void* dX, void* dW, float* loss, void* ws, size_t ws_bytes,

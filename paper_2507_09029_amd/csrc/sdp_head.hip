@@ -415,7 +415,7 @@ Plan plan(int dtype, int T, int V, int d, int k, bool teacher, bool dx, bool dw)
     const size_t row = bf16 ? (grads ? (size_t)sdp::line_ld(V, 1) * 2 : ((size_t)V + 31) / 32 * 8) : ((size_t)V + 3) * 4;
     const size_t wide = (size_t)d * (bf16 ? 2 : 4);
     const int64_t most = (int64_t)(SDP_HEAD_PIECE_BYTES / (row > wide ? row : wide)) / 64 * 64;
-    const int64_t rows_max = most < 64 ? 64 : most;
+    const int64_t rows_max = most < 64 ? 64 : most < SDP_HEAD_PIECE_TOKENS ? most : SDP_HEAD_PIECE_TOKENS;
     p.pieces = (int)((T + rows_max - 1) / rows_max);
     p.rows = T;
     if (p.pieces > 1) {

@@ -10,6 +10,7 @@ Bounds, elementwise (u = 2^-24; half = half a step of the stored type, 2^-8 rela
   dz     c / tau (mass p - q): c / tau (mass p (2e-5 + 2 z_err / tau) + q 2e-5), and its rounding to the stored type; in the head with bf16 beside it
          5.2e-4 c / tau mass p from the 16-bit distance to the block's largest logit (elements of entries do without), and mass 2^-95 c / tau
          for what is below that distance's range
+         Of 128 tokens with a target or fewer the head holds dz in two terms: 2^-17 of it instead of 2^-8 (`two`)
   dX, dW sums over dz's bound times |W|, |X|; the product's roundings, (depth / 8 + 8) u (fp32: depth / 2 + 16) times the sum of
          magnitudes; the result's rounding
 """
@@ -62,7 +63,7 @@ def targets64(ids, top, top_lse, V, tau):
 class Want:
     """The loss of logits z (64 bits) against targets, its gradient, and the bounds above; rows without a target are zeros whatever z holds."""
 
-    def __init__(self, z, ids, top, top_lse, tau, c, z_err=0.0, stored=torch.float32, codes=False):
+    def __init__(self, z, ids, top, top_lse, tau, c, z_err=0.0, stored=torch.float32, codes=False, half=None):
         T, V = z.shape
         dense, q, log_q, at, live = targets64(ids, top, top_lse, V, tau)
         z = torch.where(live[:, None], z, 0.0) / tau
@@ -87,7 +88,7 @@ class Want:
         if codes:
             room = room + abs(c) / tau * torch.where(dense > 0, 0.0, 5.2e-4 * p + mass[:, None] * 2.0 ** -95)
         self.dz_room = torch.where(live[:, None], room, 0.0)
-        self.dz_room += HALF[stored] * (self.dz.abs() + self.dz_room) + torch.where(live[:, None], 1e-37, 0.0)
+        self.dz_room += (half or HALF[stored]) * (self.dz.abs() + self.dz_room) + torch.where(live[:, None], 1e-37, 0.0)
         self.loss = self.kl.sum() * c
         self.loss_room = abs(c) * (self.kl_room.sum() + 4 * U * self.kl.abs().sum()) + 1e-30
 
@@ -113,8 +114,8 @@ def z_bound(X, W):
 
 
 def product_bound(A, B, room, stored, exact):
-    """Of A B where A is known within `room` and stored, B exactly."""
-    n = A.shape[1]
+    """Of A B where A is known within `room` and stored, B exactly.  A sum of dW runs over 32768 tokens at most, and then over these sums."""
+    n = min(A.shape[1], 32768 + A.shape[1] // 32768)
     f = (n / 8 + 8 if stored == torch.bfloat16 else n / 2 + 16) * U
     b = B.abs()
     return (room + f * (A.abs() + room)) @ b + HALF[stored] * exact.abs() + 1e-37
@@ -126,7 +127,8 @@ class HeadWant(Want):
         live = targets64(ids, top, top_lse, W.shape[0], tau)[4]
         x = torch.where(live[:, None], X.double(), 0.0)
         w = W.double()
-        super().__init__(x @ w.T, ids, top, top_lse, tau, c, z_bound(x.to(dt), W), dt, codes=dt == torch.bfloat16)
+        two = dt == torch.bfloat16 and int(live.sum()) <= 128
+        super().__init__(x @ w.T, ids, top, top_lse, tau, c, z_bound(x.to(dt), W), dt, codes=dt == torch.bfloat16, half=2.0 ** -17 if two else None)
         self.dX, self.dW = self.dz @ w, self.dz.T @ x
         self.dX_room = product_bound(self.dz, w, self.dz_room, dt, self.dX)
         self.dX_room = torch.where(live[:, None], self.dX_room, 1e-300)
