@@ -2254,7 +2254,9 @@ int gemm_head_dx(const HeadGemm& h, const int32_t* list, void* dX, float* cut_ws
     return launch_head<EPI_STORE, OP_HEAD_DX, 2>(d, a, t.bm, t.bn, t.most, s);
 }
 
-size_t head_sums_bytes(int V, int d) { return (size_t)((V + 255) / 256 * 256) * ((d + 767) / 768 * 768) * 4; } // whole tiles of any shape
+size_t head_sums_bytes(const HeadTiles& t, int V, int d) {
+    return (size_t)((V + t.bm - 1) / t.bm) * t.bm * ((d + t.bn - 1) / t.bn) * t.bn * 4;
+}
 
 int gemm_head_dw(const HeadGemm& h, void* dW, float* sums, int of, float* cut_ws, hipStream_t s) {
     if (of == 0 && h.rows <= kTwoTermRows) {

@@ -442,9 +442,9 @@ Plan plan(int dtype, int T, int V, int d, int k, bool teacher, bool dx, bool dw)
         p.stats = take(rows * p.nblk * 8);
         if (!teacher) p.labels = take(rows * 4);
         p.z = take(rows * k * 4);
-        if (dw && p.pieces > 1) p.sums = take(sdp::head_sums_bytes(V, d));
         p.piece = take((size_t)p.pieces * sizeof(sdp::HeadPiece));
         p.tx = sdp::head_dx_tiles(p.rows, V, d), p.tw = sdp::head_dw_tiles(p.rows, V, d, p.pieces);
+        if (dw && p.pieces > 1) p.sums = take(sdp::head_sums_bytes(p.tw, V, d));
         // both contractions' cut tiles, one after the other
         const size_t bx = dx ? sdp::head_cut_bytes(p.tx) : 0, bw = dw ? sdp::head_cut_bytes(p.tw) : 0;
         p.cut = take(bx > bw ? bx : bw);

@@ -272,7 +272,7 @@ int gemm_head_logits(const HeadGemm& h, float rate, bool codes, float2* stats, i
 int gemm_head_dx(const HeadGemm& h, const int32_t* list, void* dX, float* cut_ws, hipStream_t s);
 // dW = P^T X over pieces of tokens (of: 0 the only one, 1 first, 2 between, 3 last), which share sums of head_sums_bytes; the only one takes
 // scratch of head_cut_bytes instead
-size_t head_sums_bytes(int V, int d);
+size_t head_sums_bytes(const HeadTiles& dw, int V, int d);
 int gemm_head_dw(const HeadGemm& h, void* dW, float* sums, int of, float* cut_ws, hipStream_t s);
 // Plain LDS-tiled bf16 contraction, any shape: what the MFMA kernel's address ranges do not take.
 int gemm_simple(const GemmDesc& g, hipStream_t s);

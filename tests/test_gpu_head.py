@@ -117,9 +117,10 @@ def test_large_tiles(sdp, T, V, d):
 
 
 @pytest.mark.parametrize("dtype,T,V,d,live", [("bf16", 10000, 60000, 64, 1.0), ("bf16", 20000, 60000, 48, 0.7), ("bf16", 20000, 60000, 48, 0.02), ("f32", 10000, 30001, 33, 0.6),
-                                                ("bf16", 600000, 5, 1000, 0.8)])
+                                                ("bf16", 600000, 5, 1000, 0.8), ("bf16", 300, 3000001, 16, 0.9), ("f32", 600, 1000001, 9, 0.9)])
 def test_more_tokens_than_a_piece(sdp, dtype, T, V, d, live):
-    """Two to three pieces, the later ones without a token that has a label in the third case; tokens of more bytes than their logits."""
+    """Two to three pieces, the later ones without a token that has a label in the third case; tokens of more bytes than their logits; a
+    vocabulary that leaves a piece as few as are held in two terms."""
     dt = DT[dtype]
     labels = some_labels(T, V, 2, 1.0 - live)
     X, W = (t.cuda() for t in head(T, V, d, dt, labels))
