@@ -273,22 +273,25 @@ struct CodeRows {
     const sdp::HeadPiece* piece;
     float *kl, *lse;
     int rows, V;
+    int parts, columns; // a row is that many workgroups', of so many columns each
 };
 
 // A row of codes and its blocks' statistics -> its loss, lse and gradient.  One workgroup a row.  ONCE: around the caches, where the codes are far
 // more than the 256 MB behind the L2s hold: 16384 x 32000 444 -> 396 us, but 3350 x 50001 123 -> 136.
-// Few rows: 16 waves each.
-template <int ONCE, int TH>
-__global__ __launch_bounds__(TH) void code_rows_kernel(CodeRows a) {
+// Few rows are several workgroups' each, of which all find the row's sum.
+constexpr int kCodeThreads = 256;
+template <int ONCE>
+__global__ __launch_bounds__(kCodeThreads) void code_rows_kernel(CodeRows a) {
     typedef Row<1> Rw;
-    constexpr int WAVES = TH / 64;
+    constexpr int TH = kCodeThreads, WAVES = TH / 64;
     __shared__ float lds[3][2][WAVES];
     extern __shared__ unsigned char entry_lds[];
-    const int64_t row = sdp::group_id();
+    const uint32_t group = sdp::group_id();
+    const int64_t row = group / (uint32_t)a.parts;
     if (row >= a.rows) return;
-    const int tid = threadIdx.x, k = a.t.k, listed = a.list[row];
+    const int tid = threadIdx.x, k = a.t.k, listed = a.list[row], first = (int)(group % (uint32_t)a.parts) * a.columns;
     if (listed < 0) {
-        if (tid == 0) {
+        if (tid == 0 && first == 0) {
             a.kl[-1 - listed] = 0.f;
             if (a.lse) a.lse[-1 - listed] = 0.f;
         }
@@ -322,7 +325,7 @@ __global__ __launch_bounds__(TH) void code_rows_kernel(CodeRows a) {
     });
     sdp::group_both<WAVES, false>(mass, kl, lds[2]);
     if (!a.t.top_lse && mass == mass) mass = 1.f;
-    if (tid == 0) {
+    if (tid == 0 && first == 0) {
         a.kl[listed] = !a.t.top && kl < 0.f ? 0.f : kl; // a label's logit that is all of its row's sum, but for roundings
         if (a.lse) a.lse[listed] = fmaf(m, kLn2, log_sum);
     }
@@ -334,7 +337,7 @@ __global__ __launch_bounds__(TH) void code_rows_kernel(CodeRows a) {
     uint16_t* p = a.P + row * a.ldp;
     uint16_t* second = terms == 2 ? p + piece_rows * a.ldp : nullptr; // the second term's row
     constexpr float kStep = sdp::kCodeRange / 65535.f;
-    const int end = (a.V + 7) / 8 * 8; // codes of columns behind V say 0
+    const int all = (a.V + 7) / 8 * 8, end = min(first + a.columns, all); // codes of columns behind V say 0
     auto value = [&](uint32_t code, float from) { return code == 65535u ? 0.f : __builtin_amdgcn_exp2f(fmaf((float)code, -kStep, from)) * inv; };
     auto turn = [&](int e, const u32x4& w, float block) {
         const float from = block - m;
@@ -349,7 +352,7 @@ __global__ __launch_bounds__(TH) void code_rows_kernel(CodeRows a) {
         *(u32x4*)(second + e) = Rw::pack(v);
     };
     constexpr int U = 4;
-    for (int e0 = tid * 8; e0 < end; e0 += U * TH * 8) {
+    for (int e0 = first + tid * 8; e0 < end; e0 += U * TH * 8) {
         u32x4 w[U];
         float block[U];
 #pragma unroll
@@ -366,7 +369,7 @@ __global__ __launch_bounds__(TH) void code_rows_kernel(CodeRows a) {
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
     for (int i = tid; i < k; i += TH) {
-        if (en.id[i] < 0) continue;
+        if (en.id[i] < first || en.id[i] >= end) continue;
         const float v = __builtin_amdgcn_exp2f(fmaf(en.z[i], rate, -m)) * inv - en.all_of(i, k);
         Rw::put(p + en.id[i], v);
         if (second) Rw::put(second + en.id[i], v - Rw::rounded(v));
@@ -513,13 +516,14 @@ int run(const Call& c, unsigned char* ws, hipStream_t s) {
             }
             rc = sdp::gemm_head_logits(h, sdp::kLog2e * c.t.inv_tau, grads, stats, p.nblk, g.labels, z, s);
             if (rc != SDP_OK) return rc;
-            const CodeRows r{grads ? (uint16_t*)h.P : nullptr, p.ldz, stats, p.nblk, p.block == 64 ? 6 : 5, z, c.t, list + base, pieces + i, c.kl, c.lse, rows, c.V};
+            const int columns = rows < 512 ? 8192 : (c.V + 7) / 8 * 8, parts = grads ? (c.V + columns - 1) / columns : 1;
+            const CodeRows r{grads ? (uint16_t*)h.P : nullptr, p.ldz, stats, p.nblk, p.block == 64 ? 6 : 5, z, c.t, list + base, pieces + i, c.kl, c.lse, rows, c.V,
+                             parts, columns};
             {
                 sdp::ProfileScope ps("head_rows", s);
                 const size_t lds = sdp::Entries::bytes(c.t.k);
-                if (grads && (size_t)rows * p.ldz * 2 >= (size_t)1 << 29) code_rows_kernel<1, 256><<<sdp::grid_of(rows), 256, lds, s>>>(r);
-                else if (rows > 512) code_rows_kernel<0, 256><<<sdp::grid_of(rows), 256, lds, s>>>(r);
-                else code_rows_kernel<0, 1024><<<sdp::grid_of(rows), 1024, lds, s>>>(r);
+                if (grads && (size_t)rows * p.ldz * 2 >= (size_t)1 << 29) code_rows_kernel<1><<<sdp::grid_of((int64_t)rows * parts), kCodeThreads, lds, s>>>(r);
+                else code_rows_kernel<0><<<sdp::grid_of((int64_t)rows * parts), kCodeThreads, lds, s>>>(r);
             }
             rc = sdp::launch_status();
             if (rc == SDP_OK && c.dX) rc = sdp::gemm_head_dx(h, list + base, c.dX, (float*)(ws + p.cut), s);
