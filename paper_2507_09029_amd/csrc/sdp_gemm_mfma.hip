@@ -2154,12 +2154,25 @@ struct FewArgs {
     float scale;
     const float* scale_dev;
     uint16_t* dW;
+    float* loss; // may be null: by the last workgroup, which has nothing else to do
+    const float* kl;
+    int T;
+    float loss_scale;
 };
 __global__ __launch_bounds__(256) void head_dw_few_kernel(FewArgs g) {
     constexpr int kStripRow = 144; // bytes
     __shared__ __attribute__((aligned(16))) unsigned char stage[2 * kTwoTermRows * 128]; // [depth][64] as the depth-major stages above
     __shared__ __attribute__((aligned(16))) unsigned char strips[4 * 16 * kStripRow];
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, lq = lane >> 4, wave = tid >> 6;
+    if (blockIdx.x == gridDim.x - 1) { // at most kTwoTermRows terms: a wave's two each, in fp64 in one order
+        if (!g.loss || wave > 0) return;
+        static_assert(kTwoTermRows == 128, "two terms a lane");
+        double x = (lane < g.T ? (double)g.kl[lane] : 0.0) + (lane + 64 < g.T ? (double)g.kl[lane + 64] : 0.0);
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) x += __shfl_xor(x, d, 64);
+        if (lane == 0) *g.loss = (float)(x * ((double)g.loss_scale * (g.scale_dev ? (double)*g.scale_dev : 1.0)));
+        return;
+    }
     const int v0 = (int)(blockIdx.x / g.groups) * 64, n0 = (int)(blockIdx.x % g.groups) * 256 + wave * 64; // a row's parts one after the other
     const int K = g.piece->rows * g.piece->terms, steps = (K + 31) / 32;
     for (int q = tid; q < steps * 32 * 8; q += 256) {
@@ -2230,7 +2243,7 @@ double cut_us(const HeadTiles& t, int M, int N, int nk) {
     return (double)(tiles / kHeadRound) * one + last;
 }
 // The tiles that take least, on the mean of five numbers of tokens, from all that there may be to half of them: those of dX chosen for all
-// tokens took 715 us where a third of 5000 had no label (128 x 256, d = 1600, V = 50001), now 445.
+// tokens took 715 us where a third of 5000 had no label (128 x 256, d = 1600, V = 50001), now 525 and 27 for their ranges' sums.
 template <class F>
 HeadTiles cut_tiles(bool cuts, int rows, F&& us) {
     HeadTiles best{};
@@ -2280,11 +2293,11 @@ size_t head_sums_bytes(const HeadTiles& t, int V, int d) {
 }
 
 int gemm_head_dw(const HeadGemm& h, void* dW, float* sums, int of, float* cut_ws, hipStream_t s) {
-    if (of == 0 && h.rows <= kTwoTermRows) {
+    if (head_dw_sums_loss(h.rows, of ? 2 : 1)) {
         const uint32_t groups = (uint32_t)(h.d + 255) / 256;
         ProfileScope ps("head_dw", s);
-        const FewArgs f{(const uint16_t*)h.P, (const uint16_t*)h.Xt, h.ldp, h.ldt, h.piece, h.V, h.d, groups, h.scale, h.scale_dev, (uint16_t*)dW};
-        head_dw_few_kernel<<<(unsigned)((h.V + 63) / 64) * groups, 256, 0, s>>>(f);
+        const FewArgs f{(const uint16_t*)h.P, (const uint16_t*)h.Xt, h.ldp, h.ldt, h.piece, h.V, h.d, groups, h.scale, h.scale_dev, (uint16_t*)dW, h.loss, h.kl, h.T, h.loss_scale};
+        head_dw_few_kernel<<<(unsigned)((h.V + 63) / 64) * groups + 1, 256, 0, s>>>(f);
         return launch_status();
     }
     GemmDesc d = extents((h.V + 7) / 8 * 8, h.d, head_held(h.rows)); // columns of the logits' rows in whole chunks: the last ones are zeros

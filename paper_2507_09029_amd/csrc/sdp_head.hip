@@ -99,16 +99,18 @@ __global__ __launch_bounds__(1024) void list_kernel(const void* __restrict__ fro
     }
 }
 
-// The list of at most kSmallList tokens with labels, by every workgroup of TH threads that needs it, in its own LDS; returns how many have one.
+// The list of at most kSmallList tokens, by every workgroup of TH threads that needs it, in its own LDS; returns how many have a target.  `has`: what
+// entries_kernel wrote, null with labels.
 constexpr int kSmallList = 1024;
 template <int TH>
-__device__ int small_list(const void* labels, int wide, int T, int V, int32_t* list) {
+__device__ int small_list(const void* labels, int wide, const uint8_t* has, int T, int V, int32_t* list) {
     __shared__ uint64_t masks[kSmallList / 64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
     for (int c = 0; c < kSmallList / 64; c += TH / 64) {
         const int t = (c + wave) * 64 + lane;
-        const uint64_t mask = __ballot(sdp::token_id(labels, wide, t < T ? t : T - 1, V) >= 0 && t < T);
+        const int at = t < T ? t : T - 1;
+        const uint64_t mask = __ballot((has ? has[at] != 0 : sdp::token_id(labels, wide, at, V) >= 0) && t < T);
         if (lane == 0) masks[c + wave] = mask;
     }
     __syncthreads();
@@ -134,12 +136,13 @@ struct Gather {
     Shapes shapes;
     const void* labels_in;
     int wide;
+    const uint8_t* has;
     int32_t* labels; // [row], -1 for none; may be null
     int rows, V, d;
 };
 
 // Rows of X in the list's order, and (bf16) the same column by column for dW, whose depth they are: read along it, they need one LDS read a
-// fragment where rows need two (a depth step of 256 x 256 1.67 -> 1.40 us with one transposed operand instead of two).  A workgroup takes
+// fragment where rows need two (a depth step of 256 x 256 1.67 -> 1.45 us with one transposed operand instead of two).  A workgroup takes
 // 64 tokens x 64 columns; tokens without a target are zeros.  d a multiple of 8, 16-byte aligned.  With two terms (HeadPiece) the columns behind
 // the last token are those of all tokens again.  SMALL: the list and the plan of the other kernels are made here as well, a launch less.
 template <int SMALL>
@@ -150,7 +153,7 @@ __global__ __launch_bounds__(256) void gather_kernel(Gather a) {
     const int32_t* list = a.list;
     int live, terms;
     if constexpr (SMALL) {
-        live = small_list<256>(a.labels_in, a.wide, a.rows, a.V, small);
+        live = small_list<256>(a.labels_in, a.wide, a.has, a.rows, a.V, small);
         list = small;
         if (r0 == 0 && c0 == 0) {
             for (int i = tid; i < a.rows; i += 256) a.list[i] = small[i];
@@ -199,7 +202,7 @@ __global__ __launch_bounds__(64) void gather_f32_kernel(Gather a) {
     const int64_t row = sdp::group_id();
     if (row >= a.rows) return;
     if constexpr (SMALL) {
-        small_list<64>(a.labels_in, a.wide, a.rows, a.V, small);
+        small_list<64>(a.labels_in, a.wide, a.has, a.rows, a.V, small);
         if (row == 0)
             for (int i = threadIdx.x; i < a.rows; i += 64) a.list[i] = small[i];
     }
@@ -331,7 +334,7 @@ __global__ __launch_bounds__(kCodeThreads) void code_rows_kernel(CodeRows a) {
     }
     if (!a.P) return;
     // The gradient's factor c / tau comes in fp32 with the products' results: mass p - q is rounded by itself, which keeps a label's 1 - p, that most of a
-    // row's length lies in, at the fine end of bf16's steps where p is small (1 / 3350 of it may lie anywhere: dX 2.5e-3 off instead of 2.0e-3),
+    // row's length lies in, at the fine end of bf16's steps where p is small (1 / 3350 of it may lie anywhere: dX 2.5e-3 off instead of 2.1e-3),
     // and keeps a small factor out of bf16's range.
     const float inv = mass / sum;
     uint16_t* p = a.P + row * a.ldp;
@@ -377,7 +380,7 @@ __global__ __launch_bounds__(kCodeThreads) void code_rows_kernel(CodeRows a) {
 }
 
 // Depth ranges of fp32 dX, whose outputs are few and whose depth is the vocabulary: a launch of few tiles runs as up to four problems.  1023 x 511, 5003
-// deep 97 -> 60 us.
+// deep 97 -> 53 us, and 10 for their sums.
 int f32_dx_ranges(int rows, int V, int d) {
     const int64_t tiles = (int64_t)((rows + 63) / 64) * ((d + 63) / 64);
     int r = tiles > 0 && tiles <= 256 ? (int)(512 / tiles) : 1;
@@ -476,7 +479,7 @@ int run(const Call& c, unsigned char* ws, hipStream_t s) {
     int32_t* list = (int32_t*)(ws + p.list);
     sdp::HeadPiece* pieces = bf16 ? (sdp::HeadPiece*)(ws + p.piece) : nullptr;
     const Shapes shapes{p.tx, p.tw, p.rows, p.pieces, c.V, c.d};
-    const bool small = !teacher && p.pieces == 1 && c.T <= (bf16 ? kSmallList : 256); // listed by what gathers
+    const bool small = p.pieces == 1 && c.T <= (bf16 ? kSmallList : 256); // listed by what gathers
     uint8_t* has = teacher ? ws + p.has : nullptr;
     if (teacher) {
         sdp::ProfileScope ps("head_entries", s);
@@ -491,7 +494,7 @@ int run(const Call& c, unsigned char* ws, hipStream_t s) {
     int rc = sdp::launch_status();
     for (int i = 0; i < p.pieces && rc == SDP_OK; ++i) {
         const int base = i * p.rows, rows = c.T - base < p.rows ? c.T - base : p.rows;
-        Gather g{c.X, ws + p.X, c.dW && bf16 ? ws + p.Xt : nullptr, c.dX, p.ldt, list + base, pieces + i, shapes, c.t.ids, c.t.wide, nullptr, rows, c.V, c.d};
+        Gather g{c.X, ws + p.X, c.dW && bf16 ? ws + p.Xt : nullptr, c.dX, p.ldt, list + base, pieces + i, shapes, c.t.ids, c.t.wide, has, nullptr, rows, c.V, c.d};
         if (bf16 && !teacher) g.labels = (int32_t*)(ws + p.labels);
         {
             sdp::ProfileScope ps("head_gather", s);
@@ -527,6 +530,7 @@ int run(const Call& c, unsigned char* ws, hipStream_t s) {
             }
             rc = sdp::launch_status();
             if (rc == SDP_OK && c.dX) rc = sdp::gemm_head_dx(h, list + base, c.dX, (float*)(ws + p.cut), s);
+            h.loss = p.pieces == 1 ? c.loss : nullptr, h.kl = c.kl, h.T = c.T, h.loss_scale = c.t.scale;
             if (rc == SDP_OK && c.dW)
                 rc = sdp::gemm_head_dw(h, c.dW, (float*)(ws + p.sums), p.pieces == 1 ? 0 : i == 0 ? 1 : i == p.pieces - 1 ? 3 : 2, (float*)(ws + p.cut), s);
             continue;
@@ -567,7 +571,7 @@ int run(const Call& c, unsigned char* ws, hipStream_t s) {
             if (rc == SDP_OK && c.dW) rc = sdp::gemm_f32(w, s);
         }
     }
-    if (rc != SDP_OK || !c.loss) return rc;
+    if (rc != SDP_OK || !c.loss || (bf16 && c.dW && sdp::head_dw_sums_loss(p.rows, p.pieces))) return rc;
     return sdp::loss_sum(c.kl, c.T, c.t.scale, c.t.scale_dev, c.loss, s);
 }
 

@@ -259,6 +259,11 @@ struct HeadGemm {
     const HeadPiece* piece = nullptr;
     float scale = 1.f; // of dX and dW: scale scale_dev[0], in fp32 before they are rounded
     const float* scale_dev = nullptr;
+    // the loss, loss_scale scale_dev[0] sum kl[0 .. T), where head_dw_sums_loss says so
+    float* loss = nullptr;
+    const float* kl = nullptr;
+    int T = 0;
+    float loss_scale = 1.f;
 };
 // A logit is kept as its distance from the largest of its block of columns: 16 bits for 0 .. kCodeRange in powers of two, after the division
 // by the temperature.  A step is 0.0015, so that a probability made from it is 5.1e-4 off at most and 2.9e-4 in the mean square: a sixth of what
@@ -273,6 +278,8 @@ int gemm_head_dx(const HeadGemm& h, const int32_t* list, void* dX, float* cut_ws
 // dW = P^T X over pieces of tokens (of: 0 the only one, 1 first, 2 between, 3 last), which share sums of head_sums_bytes; the only one takes
 // scratch of head_cut_bytes instead
 size_t head_sums_bytes(const HeadTiles& dw, int V, int d);
+// whether gemm_head_dw also makes the loss, of the tokens of a call of one piece of `rows`
+inline bool head_dw_sums_loss(int rows, int pieces) { return pieces == 1 && rows <= kTwoTermRows; }
 int gemm_head_dw(const HeadGemm& h, void* dW, float* sums, int of, float* cut_ws, hipStream_t s);
 // Plain LDS-tiled bf16 contraction, any shape: what the MFMA kernel's address ranges do not take.
 int gemm_simple(const GemmDesc& g, hipStream_t s);
