@@ -479,7 +479,9 @@ int sdp_distill_loss(int dtype, int id_type, int top_dtype, int T, int V, int k,
  *   dX [T][d], dW [V][d] out, either may be NULL (not wanted); dX may take the place of X.  dW has every row; sums over tokens are
  *   fp32 and rounded once.
  *   ws: sdp_head_loss_workspace_bytes(dtype, T, V, d, want_dx, want_dw), 256-byte aligned
- * With SDP_BF16 dZ / c is rounded once to bf16 where it enters the two products; c follows in fp32.
+ * With SDP_BF16 a probability is held as 16 bits of its logarithm (within 5.2e-4 of it, 0 below 2^-95) while the row's sum is found, but for those of labels and
+ * entries; dZ / c is then rounded to bf16 where it enters the two products, as the sum of two bf16 numbers (2^-17) where at most 128 tokens
+ * of a piece have a target, and c follows in fp32.  nll, kl, lse and loss come from fp32 logits.
  * Limits: for SDP_BF16 d a multiple of 8, X, W, dX, dW 16-byte aligned;  V < 2^22, d <= 2^20, V d < 2^31, T <= SDP_EMBED_MAX_TOKENS.
  * Errors: as for sdp_token_loss, SHAPE where a limit is exceeded, WORKSPACE.
  *

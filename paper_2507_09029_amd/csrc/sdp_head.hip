@@ -508,6 +508,7 @@ int run(const Call& c, unsigned char* ws, hipStream_t s) {
         if (rc != SDP_OK) return rc;
         if (bf16) {
             sdp::HeadGemm h;
+            // p.rows, of the last piece as well: its tiles, statistics and sums lie as those that the plan is made for
             h.X = ws + p.X, h.W = c.W, h.P = ws + p.Z, h.ldp = p.ldz, h.rows = p.rows, h.V = c.V, h.d = c.d, h.piece = pieces + i;
             h.Xt = ws + p.Xt, h.ldt = p.ldt;
             h.scale = c.t.scale * c.t.inv_tau, h.scale_dev = c.t.scale_dev;

@@ -306,6 +306,17 @@ def test_offsets_past_32_bits(sdp):
         near(dW[v], w.dz[:, v] @ x, (w.dz_room[:, v] + 16 * 2.0 ** -24 * w.dz[:, v].abs()) @ x.abs() + 2.0 ** -8 * (w.dz[:, v] @ x).abs() + 1e-37, f"dW[{v}]")
 
 
+@pytest.mark.parametrize("T,V,d", [(2932, 348636, 88), (34417, 10808, 336), (38275, 2254, 1872), (130, 3000001, 16)])
+def test_a_last_piece_of_fewer_tokens(sdp, T, V, d):
+    """Two pieces, the second of so many tokens less that a call of as many would run in other tiles: 1460 after 1472, 17201 after 17216, 19075 after 19200, and
+    2 after 128."""
+    labels = (torch.arange(T, device="cuda") * 7919) % V
+    X, W = normal(T, d, dtype=torch.bfloat16, seed=3).cuda(), normal(V, d, dtype=torch.bfloat16, seed=4, std=1.5 / d ** 0.5).cuda()
+    print(f"head T={T} V={V} d={d}", flush=True)
+    got = sdp.head_loss(X, W, labels, scale=1.0 / T)
+    HeadWant(X, W, labels[:, None], None, None, 1.0, 1.0 / T).check(got)
+
+
 def test_more_workgroups_than_a_row_of_the_grid(sdp):
     T, V, d = 1200007, 8, 8
     g = torch.Generator(device="cuda").manual_seed(1)
