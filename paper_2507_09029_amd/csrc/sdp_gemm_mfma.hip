@@ -2043,7 +2043,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, BM == 64 && BN == 64 ? 2 : 1
 // The ranges of every cut tile -> its rows; 4 columns a thread, in the order of the accumulators.  Where ranges are many, outputs are few: the ranges of
 // one output are then dealt out to eight lanes (26 rows of 168, 64 ranges of two terms each: 27.9 us with one, 8.7 with eight), which is one order as well.
 template <int BM, int BN, int WAVES_M, int WAVES_N, int OP>
-__global__ __launch_bounds__(256) void head_cut_kernel(Dev g, HeadArgs head) {
+__device__ inline void add_ranges(Dev g, const HeadArgs& head, uint32_t group, uint32_t groups) {
     constexpr int WM = BM / WAVES_M, WN = BN / WAVES_N, FN = WN / 32, PER_WAVE = WM * WN / 4;
     const HeadPiece piece = *head.piece;
     if (!head_view<BM, OP>(g, head, piece)) return;
@@ -2073,7 +2073,7 @@ __global__ __launch_bounds__(256) void head_cut_kernel(Dev g, HeadArgs head) {
             return g.partial + (int64_t)q * (BM * BN) + unit * 4;
         };
         const int64_t all = (int64_t)piece.rows * (g.N / 4);
-        for (int64_t i0 = (int64_t)blockIdx.x * (256 / lanes); i0 < all; i0 += (int64_t)gridDim.x * (256 / lanes)) {
+        for (int64_t i0 = (int64_t)group * (256 / lanes); i0 < all; i0 += (int64_t)groups * (256 / lanes)) {
             const int64_t i = i0 + mine < all ? i0 + mine : all - 1;
             const int m = (int)(i / (g.N / 4)), n = (int)(i % (g.N / 4)) * 4;
             const float *p = part(m, n), *second = part(m + piece.rows, n);
@@ -2087,7 +2087,7 @@ __global__ __launch_bounds__(256) void head_cut_kernel(Dev g, HeadArgs head) {
     }
     const int rows = OP == OP_HEAD_DW ? head.out_rows : g.M;
     const int64_t all = (int64_t)g.tail * (BM * BN / 4);
-    for (int64_t i = (int64_t)blockIdx.x * (256 / lanes) + mine; i < all; i += (int64_t)gridDim.x * (256 / lanes)) { // (all: whole waves)
+    for (int64_t i = (int64_t)group * (256 / lanes) + mine; i < all; i += (int64_t)groups * (256 / lanes)) { // (all: whole waves)
         const int q = (int)(i / (BM * BN / 4)), unit = (int)(i % (BM * BN / 4)), wave = unit / PER_WAVE, f = unit % PER_WAVE / 64, lane = unit % 64;
         const int bid = tail_position(q, g.ntot, g.n_head), per_group = g.group_m * g.tiles_n, grp = bid / per_group, first_m = grp * g.group_m;
         const int gm = g.tiles_m - first_m < g.group_m ? g.tiles_m - first_m : g.group_m, in = bid - grp * per_group;
@@ -2101,44 +2101,9 @@ __global__ __launch_bounds__(256) void head_cut_kernel(Dev g, HeadArgs head) {
         if (range == 0 && m < rows && n < g.N) put(m, n, a);
     }
 }
-
-template <int BM, int BN, int WAVES_M, int WAVES_N, int EPI, int OP, int KM>
-int launch_head_cfg(const GemmDesc& d, const HeadArgs& head, int most, hipStream_t s) {
-    constexpr int LDS = Geometry<BM, BN, WAVES_M, WAVES_N, EPI, KM>::LDS;
-    Dev g;
-    const int drc = describe<BM, BN, EPI, OP>(d, g);
-    if (drc != SDP_OK) return drc;
-    auto kern = sdp_head_gemm_kernel<BM, BN, WAVES_M, WAVES_N, EPI, OP, KM>;
-    static const hipError_t attr = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
-    if (attr != hipSuccess) return SDP_ERR_HIP;
-    // as many workgroups as the tiles of any number of tokens, and their cut, may be
-    const int64_t cut = most > 0 ? (int64_t)g.ntot / kHeadRound * kHeadRound + most : 0, grid = cut > g.ntot ? cut : g.ntot;
-    if (grid > 0x7FFFFFFF) return SDP_ERR_SHAPE;
-    {
-        ProfileScope ps(d.name, s);
-        kern<<<dim3((unsigned)grid), WAVES_M * WAVES_N * 64, LDS, s>>>(g, head);
-    }
-    const int rc = launch_status();
-    if (rc != SDP_OK || most == 0) return rc;
-    if constexpr (is_tail(OP)) {
-        ProfileScope ps("head_cut", s);
-        const int64_t groups = (int64_t)(g.ntot < kHeadRound ? g.ntot : kHeadRound - 1) * (BM * BN / 4 / 32);
-        head_cut_kernel<BM, BN, WAVES_M, WAVES_N, OP><<<(unsigned)(groups < 2048 ? groups : 2048), 256, 0, s>>>(g, head);
-    }
-    return launch_status();
-}
-template <int EPI, int OP, int KM>
-int launch_head(const GemmDesc& d, const HeadArgs& head, int bm, int bn, int most, hipStream_t s) {
-    // waves high and narrow where the left operand is the one of two LDS reads a fragment: 16 reads a half step instead of 20
-    if (bm == 256 && bn == 256) return launch_head_cfg<256, 256, KM == 1 ? 4 : 2, KM == 1 ? 2 : 4, EPI, OP, KM>(d, head, most, s);
-    if (bm == 128 && bn == 256) return launch_head_cfg<128, 256, 2, 4, EPI, OP, KM>(d, head, most, s);
-    if (bm == 128 && bn == 128) return launch_head_cfg<128, 128, 4, 2, EPI, OP, KM>(d, head, most, s);
-    if (bm == 64 && bn == 64) return launch_head_cfg<64, 64, 2, 2, EPI, OP, KM>(d, head, most, s);
-    if constexpr (EPI != EPI_CODES) {
-        if (bm == 256 && bn == 192) return launch_head_cfg<256, 192, 4, 2, EPI, OP, KM>(d, head, most, s);
-        if (bm == 128 && bn == 192) return launch_head_cfg<128, 192, 4, 2, EPI, OP, KM>(d, head, most, s);
-    }
-    return SDP_ERR_INVALID_ARG; // not reached: the shapes that there are
+template <int BM, int BN, int WAVES_M, int WAVES_N, int OP>
+__global__ __launch_bounds__(256) void head_cut_kernel(Dev g, HeadArgs head) {
+    add_ranges<BM, BN, WAVES_M, WAVES_N, OP>(g, head, blockIdx.x, gridDim.x);
 }
 
 // dW of at most kTwoTermRows tokens, whose depth is held whole: bound by writing dW.  A workgroup takes 64 tokens of the vocabulary x 256 columns, each
@@ -2159,12 +2124,13 @@ struct FewArgs {
     int T;
     float loss_scale;
 };
-__global__ __launch_bounds__(256) void head_dw_few_kernel(FewArgs g) {
+__host__ __device__ inline uint32_t few_groups(const FewArgs& g) { return (uint32_t)((g.V + 63) / 64) * g.groups + 1; }
+__device__ inline void dw_few(const FewArgs& g, uint32_t group) {
     constexpr int kStripRow = 144; // bytes
     __shared__ __attribute__((aligned(16))) unsigned char stage[2 * kTwoTermRows * 128]; // [depth][64] as the depth-major stages above
     __shared__ __attribute__((aligned(16))) unsigned char strips[4 * 16 * kStripRow];
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, lq = lane >> 4, wave = tid >> 6;
-    if (blockIdx.x == gridDim.x - 1) { // at most kTwoTermRows terms: a wave's two each, in fp64 in one order
+    if (group == few_groups(g) - 1) { // at most kTwoTermRows terms: a wave's two each, in fp64 in one order
         if (!g.loss || wave > 0) return;
         static_assert(kTwoTermRows == 128, "two terms a lane");
         double x = (lane < g.T ? (double)g.kl[lane] : 0.0) + (lane + 64 < g.T ? (double)g.kl[lane + 64] : 0.0);
@@ -2173,7 +2139,7 @@ __global__ __launch_bounds__(256) void head_dw_few_kernel(FewArgs g) {
         if (lane == 0) *g.loss = (float)(x * ((double)g.loss_scale * (g.scale_dev ? (double)*g.scale_dev : 1.0)));
         return;
     }
-    const int v0 = (int)(blockIdx.x / g.groups) * 64, n0 = (int)(blockIdx.x % g.groups) * 256 + wave * 64; // a row's parts one after the other
+    const int v0 = (int)(group / g.groups) * 64, n0 = (int)(group % g.groups) * 256 + wave * 64; // a row's parts one after the other
     const int K = g.piece->rows * g.piece->terms, steps = (K + 31) / 32;
     for (int q = tid; q < steps * 32 * 8; q += 256) {
         int row, col;
@@ -2221,6 +2187,55 @@ __global__ __launch_bounds__(256) void head_dw_few_kernel(FewArgs g) {
         }
         __builtin_amdgcn_wave_barrier();
     }
+}
+__global__ __launch_bounds__(256) void head_dw_few_kernel(FewArgs f) { dw_few(f, blockIdx.x); }
+// With dX: the sums of its ranges, by the first `cut` workgroups, come in the same launch.
+template <int BM, int BN, int WAVES_M, int WAVES_N>
+__global__ __launch_bounds__(256) void head_few_kernel(Dev g, HeadArgs head, uint32_t cut, FewArgs f) {
+    if (blockIdx.x < cut) add_ranges<BM, BN, WAVES_M, WAVES_N, OP_HEAD_DX>(g, head, blockIdx.x, cut);
+    else dw_few(f, blockIdx.x - cut);
+}
+
+template <int BM, int BN, int WAVES_M, int WAVES_N, int EPI, int OP, int KM>
+int launch_head_cfg(const GemmDesc& d, const HeadArgs& head, int most, const FewArgs* few, hipStream_t s) {
+    constexpr int LDS = Geometry<BM, BN, WAVES_M, WAVES_N, EPI, KM>::LDS;
+    Dev g;
+    const int drc = describe<BM, BN, EPI, OP>(d, g);
+    if (drc != SDP_OK) return drc;
+    auto kern = sdp_head_gemm_kernel<BM, BN, WAVES_M, WAVES_N, EPI, OP, KM>;
+    static const hipError_t attr = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+    if (attr != hipSuccess) return SDP_ERR_HIP;
+    // as many workgroups as the tiles of any number of tokens, and their cut, may be
+    const int64_t cut = most > 0 ? (int64_t)g.ntot / kHeadRound * kHeadRound + most : 0, grid = cut > g.ntot ? cut : g.ntot;
+    if (grid > 0x7FFFFFFF) return SDP_ERR_SHAPE;
+    {
+        ProfileScope ps(d.name, s);
+        kern<<<dim3((unsigned)grid), WAVES_M * WAVES_N * 64, LDS, s>>>(g, head);
+    }
+    const int rc = launch_status();
+    if (rc != SDP_OK || most == 0) return rc;
+    if constexpr (is_tail(OP)) {
+        ProfileScope ps(few ? "head_dw" : "head_cut", s);
+        const int64_t all = (int64_t)(g.ntot < kHeadRound ? g.ntot : kHeadRound - 1) * (BM * BN / 4 / 32);
+        const uint32_t groups = (uint32_t)(all < 2048 ? all : 2048);
+        if constexpr (OP == OP_HEAD_DX)
+            if (few) head_few_kernel<BM, BN, WAVES_M, WAVES_N><<<groups + few_groups(*few), 256, 0, s>>>(g, head, groups, *few);
+        if (!few) head_cut_kernel<BM, BN, WAVES_M, WAVES_N, OP><<<groups, 256, 0, s>>>(g, head);
+    }
+    return launch_status();
+}
+template <int EPI, int OP, int KM>
+int launch_head(const GemmDesc& d, const HeadArgs& head, int bm, int bn, int most, hipStream_t s, const FewArgs* few = nullptr) {
+    // waves high and narrow where the left operand is the one of two LDS reads a fragment: 16 reads a half step instead of 20
+    if (bm == 256 && bn == 256) return launch_head_cfg<256, 256, KM == 1 ? 4 : 2, KM == 1 ? 2 : 4, EPI, OP, KM>(d, head, most, few, s);
+    if (bm == 128 && bn == 256) return launch_head_cfg<128, 256, 2, 4, EPI, OP, KM>(d, head, most, few, s);
+    if (bm == 128 && bn == 128) return launch_head_cfg<128, 128, 4, 2, EPI, OP, KM>(d, head, most, few, s);
+    if (bm == 64 && bn == 64) return launch_head_cfg<64, 64, 2, 2, EPI, OP, KM>(d, head, most, few, s);
+    if constexpr (EPI != EPI_CODES) {
+        if (bm == 256 && bn == 192) return launch_head_cfg<256, 192, 4, 2, EPI, OP, KM>(d, head, most, few, s);
+        if (bm == 128 && bn == 192) return launch_head_cfg<128, 192, 4, 2, EPI, OP, KM>(d, head, most, few, s);
+    }
+    return SDP_ERR_INVALID_ARG; // not reached: the shapes that there are
 }
 
 GemmDesc extents(int M, int N, int K) {
@@ -2279,13 +2294,18 @@ HeadTiles head_dw_tiles(int rows, int V, int d, int pieces) {
     return cut_tiles(pieces == 1 && head_held(rows) >= 512, rows, [&](const HeadTiles& t, int held) { return cut_us(t, V, d, (held + BK - 1) / BK); });
 }
 
-int gemm_head_dx(const HeadGemm& h, const int32_t* list, void* dX, float* cut_ws, hipStream_t s) {
+static FewArgs few_of(const HeadGemm& h, void* dW) {
+    return {(const uint16_t*)h.P, (const uint16_t*)h.Xt, h.ldp, h.ldt, h.piece, h.V, h.d, (uint32_t)(h.d + 255) / 256, h.scale, h.scale_dev, (uint16_t*)dW, h.loss, h.kl, h.T, h.loss_scale};
+}
+
+int gemm_head_dx(const HeadGemm& h, const int32_t* list, void* dX, float* cut_ws, void* few_dW, hipStream_t s) {
     GemmDesc d = extents(head_held(h.rows), h.d, h.V);
     d.A = h.P, d.lda = h.ldp, d.B = h.W, d.ldb = h.d, d.b_km = 1, d.C = dX, d.ldc = h.d, d.c_scatter = list, d.tail_ws = cut_ws, d.name = "head_dx";
     HeadArgs a{};
     a.piece = h.piece, a.scale = h.scale, a.scale_dev = h.scale_dev;
     const HeadTiles t = head_dx_tiles(h.rows, h.V, h.d);
-    return launch_head<EPI_STORE, OP_HEAD_DX, 2>(d, a, t.bm, t.bn, t.most, s);
+    const FewArgs few = few_of(h, few_dW);
+    return launch_head<EPI_STORE, OP_HEAD_DX, 2>(d, a, t.bm, t.bn, t.most, s, few_dW ? &few : nullptr);
 }
 
 size_t head_sums_bytes(const HeadTiles& t, int V, int d) {
@@ -2294,10 +2314,9 @@ size_t head_sums_bytes(const HeadTiles& t, int V, int d) {
 
 int gemm_head_dw(const HeadGemm& h, void* dW, float* sums, int of, float* cut_ws, hipStream_t s) {
     if (head_dw_sums_loss(h.rows, of ? 2 : 1)) {
-        const uint32_t groups = (uint32_t)(h.d + 255) / 256;
         ProfileScope ps("head_dw", s);
-        const FewArgs f{(const uint16_t*)h.P, (const uint16_t*)h.Xt, h.ldp, h.ldt, h.piece, h.V, h.d, groups, h.scale, h.scale_dev, (uint16_t*)dW, h.loss, h.kl, h.T, h.loss_scale};
-        head_dw_few_kernel<<<(unsigned)((h.V + 63) / 64) * groups + 1, 256, 0, s>>>(f);
+        const FewArgs f = few_of(h, dW);
+        head_dw_few_kernel<<<few_groups(f), 256, 0, s>>>(f);
         return launch_status();
     }
     GemmDesc d = extents((h.V + 7) / 8 * 8, h.d, head_held(h.rows)); // columns of the logits' rows in whole chunks: the last ones are zeros

@@ -530,9 +530,10 @@ int run(const Call& c, unsigned char* ws, hipStream_t s) {
                 else code_rows_kernel<0><<<sdp::grid_of((int64_t)rows * parts), kCodeThreads, lds, s>>>(r);
             }
             rc = sdp::launch_status();
-            if (rc == SDP_OK && c.dX) rc = sdp::gemm_head_dx(h, list + base, c.dX, (float*)(ws + p.cut), s);
             h.loss = p.pieces == 1 ? c.loss : nullptr, h.kl = c.kl, h.T = c.T, h.loss_scale = c.t.scale;
-            if (rc == SDP_OK && c.dW)
+            const bool few = c.dX && c.dW && sdp::head_dw_sums_loss(p.rows, p.pieces);
+            if (rc == SDP_OK && c.dX) rc = sdp::gemm_head_dx(h, list + base, c.dX, (float*)(ws + p.cut), few ? c.dW : nullptr, s);
+            if (rc == SDP_OK && c.dW && !few)
                 rc = sdp::gemm_head_dw(h, c.dW, (float*)(ws + p.sums), p.pieces == 1 ? 0 : i == 0 ? 1 : i == p.pieces - 1 ? 3 : 2, (float*)(ws + p.cut), s);
             continue;
         }

@@ -273,12 +273,12 @@ constexpr float kCodeRange = 96.f;
 // Columns of a block; rate = log2(e) / tau.  (m = rate x largest logit, sum of 2^(rate z - m)) of each go into stats [rows][nblk].
 int head_block(int rows, int V, int d);
 int gemm_head_logits(const HeadGemm& h, float rate, bool codes, float2* stats, int nblk, const int32_t* labels, float* at_label, hipStream_t s);
-// dX[list[row]] = P W, with scratch of head_cut_bytes
-int gemm_head_dx(const HeadGemm& h, const int32_t* list, void* dX, float* cut_ws, hipStream_t s);
+// dX[list[row]] = P W, with scratch of head_cut_bytes; where head_dw_sums_loss says so also dW, few_dW (may be null), in one launch with the sums of dX's ranges
+int gemm_head_dx(const HeadGemm& h, const int32_t* list, void* dX, float* cut_ws, void* few_dW, hipStream_t s);
 // dW = P^T X over pieces of tokens (of: 0 the only one, 1 first, 2 between, 3 last), which share sums of head_sums_bytes; the only one takes
 // scratch of head_cut_bytes instead
 size_t head_sums_bytes(const HeadTiles& dw, int V, int d);
-// whether gemm_head_dw also makes the loss, of the tokens of a call of one piece of `rows`
+// whether a call of one piece of `rows` tokens has its dW by a kernel for few of them, which also makes the loss
 inline bool head_dw_sums_loss(int rows, int pieces) { return pieces == 1 && rows <= kTwoTermRows; }
 int gemm_head_dw(const HeadGemm& h, void* dW, float* sums, int of, float* cut_ws, hipStream_t s);
 // Plain LDS-tiled bf16 contraction, any shape: what the MFMA kernel's address ranges do not take.
