@@ -126,6 +126,7 @@ struct HeadArgs {
     // several, 2: neither first nor last, 3: the last
     float* sums;
     int of;
+    HeadLoss loss;
 };
 
 // q of tail_position(q, ntiles, 0) = position
@@ -2101,9 +2102,29 @@ __device__ inline void add_ranges(Dev g, const HeadArgs& head, uint32_t group, u
         if (range == 0 && m < rows && n < g.N) put(m, n, a);
     }
 }
+// The loss, by a workgroup of 256, in fp64 in one order
+__device__ inline void sum_loss(const HeadLoss& l) {
+    __shared__ double waves[4];
+    if (!l.to) return;
+    const int tid = threadIdx.x;
+    double x = 0.0;
+    for (int t0 = tid; t0 < l.T; t0 += 8 * 256) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = l.kl[min(t0 + i * 256, l.T - 1)];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x += t0 + i * 256 < l.T ? (double)v[i] : 0.0;
+    }
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) x += __shfl_xor(x, d, 64);
+    if ((tid & 63) == 0) waves[tid / 64] = x;
+    __syncthreads();
+    if (tid == 0) *l.to = (float)(((waves[0] + waves[1]) + (waves[2] + waves[3])) * ((double)l.scale * (l.scale_dev ? (double)*l.scale_dev : 1.0)));
+}
 template <int BM, int BN, int WAVES_M, int WAVES_N, int OP>
 __global__ __launch_bounds__(256) void head_cut_kernel(Dev g, HeadArgs head) {
-    add_ranges<BM, BN, WAVES_M, WAVES_N, OP>(g, head, blockIdx.x, gridDim.x);
+    if (blockIdx.x == 0) sum_loss(head.loss);
+    else add_ranges<BM, BN, WAVES_M, WAVES_N, OP>(g, head, blockIdx.x - 1, gridDim.x - 1);
 }
 
 // dW of at most kTwoTermRows tokens, whose depth is held whole: bound by writing dW.  A workgroup takes 64 tokens of the vocabulary x 256 columns, each
@@ -2119,26 +2140,13 @@ struct FewArgs {
     float scale;
     const float* scale_dev;
     uint16_t* dW;
-    float* loss; // may be null: by the last workgroup, which has nothing else to do
-    const float* kl;
-    int T;
-    float loss_scale;
 };
-__host__ __device__ inline uint32_t few_groups(const FewArgs& g) { return (uint32_t)((g.V + 63) / 64) * g.groups + 1; }
+inline uint32_t few_groups(const FewArgs& g) { return (uint32_t)((g.V + 63) / 64) * g.groups; }
 __device__ inline void dw_few(const FewArgs& g, uint32_t group) {
     constexpr int kStripRow = 144; // bytes
     __shared__ __attribute__((aligned(16))) unsigned char stage[2 * kTwoTermRows * 128]; // [depth][64] as the depth-major stages above
     __shared__ __attribute__((aligned(16))) unsigned char strips[4 * 16 * kStripRow];
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, lq = lane >> 4, wave = tid >> 6;
-    if (group == few_groups(g) - 1) { // at most kTwoTermRows terms: a wave's two each, in fp64 in one order
-        if (!g.loss || wave > 0) return;
-        static_assert(kTwoTermRows == 128, "two terms a lane");
-        double x = (lane < g.T ? (double)g.kl[lane] : 0.0) + (lane + 64 < g.T ? (double)g.kl[lane + 64] : 0.0);
-#pragma unroll
-        for (int d = 32; d >= 1; d >>= 1) x += __shfl_xor(x, d, 64);
-        if (lane == 0) *g.loss = (float)(x * ((double)g.loss_scale * (g.scale_dev ? (double)*g.scale_dev : 1.0)));
-        return;
-    }
     const int v0 = (int)(group / g.groups) * 64, n0 = (int)(group % g.groups) * 256 + wave * 64; // a row's parts one after the other
     const int K = g.piece->rows * g.piece->terms, steps = (K + 31) / 32;
     for (int q = tid; q < steps * 32 * 8; q += 256) {
@@ -2188,12 +2196,16 @@ __device__ inline void dw_few(const FewArgs& g, uint32_t group) {
         __builtin_amdgcn_wave_barrier();
     }
 }
-__global__ __launch_bounds__(256) void head_dw_few_kernel(FewArgs f) { dw_few(f, blockIdx.x); }
-// With dX: the sums of its ranges, by the first `cut` workgroups, come in the same launch.
+__global__ __launch_bounds__(256) void head_dw_few_kernel(FewArgs f, HeadLoss loss) {
+    if (blockIdx.x == 0) sum_loss(loss);
+    else dw_few(f, blockIdx.x - 1);
+}
+// With dX: the sums of its ranges, by `cut` workgroups, come in the same launch.
 template <int BM, int BN, int WAVES_M, int WAVES_N>
 __global__ __launch_bounds__(256) void head_few_kernel(Dev g, HeadArgs head, uint32_t cut, FewArgs f) {
-    if (blockIdx.x < cut) add_ranges<BM, BN, WAVES_M, WAVES_N, OP_HEAD_DX>(g, head, blockIdx.x, cut);
-    else dw_few(f, blockIdx.x - cut);
+    if (blockIdx.x == 0) sum_loss(head.loss);
+    else if (blockIdx.x <= cut) add_ranges<BM, BN, WAVES_M, WAVES_N, OP_HEAD_DX>(g, head, blockIdx.x - 1, cut);
+    else dw_few(f, blockIdx.x - 1 - cut);
 }
 
 template <int BM, int BN, int WAVES_M, int WAVES_N, int EPI, int OP, int KM>
@@ -2219,8 +2231,8 @@ int launch_head_cfg(const GemmDesc& d, const HeadArgs& head, int most, const Few
         const int64_t all = (int64_t)(g.ntot < kHeadRound ? g.ntot : kHeadRound - 1) * (BM * BN / 4 / 32);
         const uint32_t groups = (uint32_t)(all < 2048 ? all : 2048);
         if constexpr (OP == OP_HEAD_DX)
-            if (few) head_few_kernel<BM, BN, WAVES_M, WAVES_N><<<groups + few_groups(*few), 256, 0, s>>>(g, head, groups, *few);
-        if (!few) head_cut_kernel<BM, BN, WAVES_M, WAVES_N, OP><<<groups, 256, 0, s>>>(g, head);
+            if (few) head_few_kernel<BM, BN, WAVES_M, WAVES_N><<<1 + groups + few_groups(*few), 256, 0, s>>>(g, head, groups, *few);
+        if (!few) head_cut_kernel<BM, BN, WAVES_M, WAVES_N, OP><<<1 + groups, 256, 0, s>>>(g, head);
     }
     return launch_status();
 }
@@ -2295,14 +2307,14 @@ HeadTiles head_dw_tiles(int rows, int V, int d, int pieces) {
 }
 
 static FewArgs few_of(const HeadGemm& h, void* dW) {
-    return {(const uint16_t*)h.P, (const uint16_t*)h.Xt, h.ldp, h.ldt, h.piece, h.V, h.d, (uint32_t)(h.d + 255) / 256, h.scale, h.scale_dev, (uint16_t*)dW, h.loss, h.kl, h.T, h.loss_scale};
+    return {(const uint16_t*)h.P, (const uint16_t*)h.Xt, h.ldp, h.ldt, h.piece, h.V, h.d, (uint32_t)(h.d + 255) / 256, h.scale, h.scale_dev, (uint16_t*)dW};
 }
 
 int gemm_head_dx(const HeadGemm& h, const int32_t* list, void* dX, float* cut_ws, void* few_dW, hipStream_t s) {
     GemmDesc d = extents(head_held(h.rows), h.d, h.V);
     d.A = h.P, d.lda = h.ldp, d.B = h.W, d.ldb = h.d, d.b_km = 1, d.C = dX, d.ldc = h.d, d.c_scatter = list, d.tail_ws = cut_ws, d.name = "head_dx";
     HeadArgs a{};
-    a.piece = h.piece, a.scale = h.scale, a.scale_dev = h.scale_dev;
+    a.piece = h.piece, a.scale = h.scale, a.scale_dev = h.scale_dev, a.loss = h.loss;
     const HeadTiles t = head_dx_tiles(h.rows, h.V, h.d);
     const FewArgs few = few_of(h, few_dW);
     return launch_head<EPI_STORE, OP_HEAD_DX, 2>(d, a, t.bm, t.bn, t.most, s, few_dW ? &few : nullptr);
@@ -2313,10 +2325,10 @@ size_t head_sums_bytes(const HeadTiles& t, int V, int d) {
 }
 
 int gemm_head_dw(const HeadGemm& h, void* dW, float* sums, int of, float* cut_ws, hipStream_t s) {
-    if (head_dw_sums_loss(h.rows, of ? 2 : 1)) {
+    if (head_dw_few(h.rows, of ? 2 : 1)) {
         ProfileScope ps("head_dw", s);
         const FewArgs f = few_of(h, dW);
-        head_dw_few_kernel<<<few_groups(f), 256, 0, s>>>(f);
+        head_dw_few_kernel<<<1 + few_groups(f), 256, 0, s>>>(f, h.loss);
         return launch_status();
     }
     GemmDesc d = extents((h.V + 7) / 8 * 8, h.d, head_held(h.rows)); // columns of the logits' rows in whole chunks: the last ones are zeros

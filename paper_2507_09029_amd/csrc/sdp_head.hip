@@ -480,6 +480,7 @@ int run(const Call& c, unsigned char* ws, hipStream_t s) {
     sdp::HeadPiece* pieces = bf16 ? (sdp::HeadPiece*)(ws + p.piece) : nullptr;
     const Shapes shapes{p.tx, p.tw, p.rows, p.pieces, c.V, c.d};
     const bool small = p.pieces == 1 && c.T <= (bf16 ? kSmallList : 256); // listed by what gathers
+    const bool with_loss = bf16 && sdp::head_sums_loss(p.rows, p.pieces, c.dX, c.dW);
     uint8_t* has = teacher ? ws + p.has : nullptr;
     if (teacher) {
         sdp::ProfileScope ps("head_entries", s);
@@ -530,8 +531,8 @@ int run(const Call& c, unsigned char* ws, hipStream_t s) {
                 else code_rows_kernel<0><<<sdp::grid_of((int64_t)rows * parts), kCodeThreads, lds, s>>>(r);
             }
             rc = sdp::launch_status();
-            h.loss = p.pieces == 1 ? c.loss : nullptr, h.kl = c.kl, h.T = c.T, h.loss_scale = c.t.scale;
-            const bool few = c.dX && c.dW && sdp::head_dw_sums_loss(p.rows, p.pieces);
+            if (with_loss) h.loss = {c.loss, c.kl, c.T, c.t.scale, c.t.scale_dev};
+            const bool few = c.dX && c.dW && sdp::head_dw_few(p.rows, p.pieces);
             if (rc == SDP_OK && c.dX) rc = sdp::gemm_head_dx(h, list + base, c.dX, (float*)(ws + p.cut), few ? c.dW : nullptr, s);
             if (rc == SDP_OK && c.dW && !few)
                 rc = sdp::gemm_head_dw(h, c.dW, (float*)(ws + p.sums), p.pieces == 1 ? 0 : i == 0 ? 1 : i == p.pieces - 1 ? 3 : 2, (float*)(ws + p.cut), s);
@@ -573,7 +574,7 @@ int run(const Call& c, unsigned char* ws, hipStream_t s) {
             if (rc == SDP_OK && c.dW) rc = sdp::gemm_f32(w, s);
         }
     }
-    if (rc != SDP_OK || !c.loss || (bf16 && c.dW && sdp::head_dw_sums_loss(p.rows, p.pieces))) return rc;
+    if (rc != SDP_OK || !c.loss || with_loss) return rc;
     return sdp::loss_sum(c.kl, c.T, c.t.scale, c.t.scale_dev, c.loss, s);
 }
 

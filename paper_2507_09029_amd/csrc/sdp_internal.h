@@ -248,6 +248,14 @@ __device__ inline HeadCut head_cut(const HeadTiles& t, int tiles, int nk, bool a
     return {head, tail, best, (nk + best - 1) / best};
 }
 #endif
+// *to = scale scale_dev[0] sum kl[0 .. T)
+struct HeadLoss {
+    float* to = nullptr; // may be null
+    const float* kl = nullptr;
+    int T = 0;
+    float scale = 1.f;
+    const float* scale_dev = nullptr;
+};
 struct HeadGemm {
     const void* X = nullptr;  // [rows][d], theirs without gaps
     const void* Xt = nullptr; // [d][ldt]: the same columns by columns, zeros behind the last token to a multiple of 8
@@ -259,11 +267,7 @@ struct HeadGemm {
     const HeadPiece* piece = nullptr;
     float scale = 1.f; // of dX and dW: scale scale_dev[0], in fp32 before they are rounded
     const float* scale_dev = nullptr;
-    // the loss, loss_scale scale_dev[0] sum kl[0 .. T), where head_dw_sums_loss says so
-    float* loss = nullptr;
-    const float* kl = nullptr;
-    int T = 0;
-    float loss_scale = 1.f;
+    HeadLoss loss; // where head_sums_loss says so
 };
 // A logit is kept as its distance from the largest of its block of columns: 16 bits for 0 .. kCodeRange in powers of two, after the division
 // by the temperature.  A step is 0.0015, so that a probability made from it is 5.1e-4 off at most and 2.9e-4 in the mean square: a sixth of what
@@ -273,13 +277,15 @@ constexpr float kCodeRange = 96.f;
 // Columns of a block; rate = log2(e) / tau.  (m = rate x largest logit, sum of 2^(rate z - m)) of each go into stats [rows][nblk].
 int head_block(int rows, int V, int d);
 int gemm_head_logits(const HeadGemm& h, float rate, bool codes, float2* stats, int nblk, const int32_t* labels, float* at_label, hipStream_t s);
-// dX[list[row]] = P W, with scratch of head_cut_bytes; where head_dw_sums_loss says so also dW, few_dW (may be null), in one launch with the sums of dX's ranges
+// Whether a call has its dW by a kernel for few tokens, and whether the loss comes with dX's or dW's second launch: a workgroup's work beside others' up to
+// 8192 tokens, where a launch of its own takes 5 us and a gap.
+inline bool head_dw_few(int rows, int pieces) { return pieces == 1 && rows <= kTwoTermRows; }
+inline bool head_sums_loss(int rows, int pieces, bool dx, bool dw) { return pieces == 1 && ((dx && rows <= 8192) || (dw && head_dw_few(rows, pieces))); }
+// dX[list[row]] = P W, with scratch of head_cut_bytes; where head_dw_few says so also dW, few_dW (may be null), in one launch with the sums of dX's ranges
 int gemm_head_dx(const HeadGemm& h, const int32_t* list, void* dX, float* cut_ws, void* few_dW, hipStream_t s);
 // dW = P^T X over pieces of tokens (of: 0 the only one, 1 first, 2 between, 3 last), which share sums of head_sums_bytes; the only one takes
 // scratch of head_cut_bytes instead
 size_t head_sums_bytes(const HeadTiles& dw, int V, int d);
-// whether a call of one piece of `rows` tokens has its dW by a kernel for few of them, which also makes the loss
-inline bool head_dw_sums_loss(int rows, int pieces) { return pieces == 1 && rows <= kTwoTermRows; }
 int gemm_head_dw(const HeadGemm& h, void* dW, float* sums, int of, float* cut_ws, hipStream_t s);
 // Plain LDS-tiled bf16 contraction, any shape: what the MFMA kernel's address ranges do not take.
 int gemm_simple(const GemmDesc& g, hipStream_t s);
