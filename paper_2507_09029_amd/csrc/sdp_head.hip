@@ -9,7 +9,8 @@
 //   logits   bf16: the contraction's epilogue takes each block's maximum and sum in fp32 and keeps a logit as 16 bits (kCodeRange)
 //   rows     a row's blocks -> its lse and loss; its codes -> its gradient, bf16, in their place.  4 bytes a logit moved beside 6 d operations
 //   dX, dW   contractions on what is stored; dW goes on from piece to piece in fp32 (head.sums), and is rounded once
-// fp32: the same with the logits themselves in fp32 (target_rows) and the fp32 contractions.
+// fp32: the same with the logits themselves in fp32 (target_rows) and the fp32 contractions, over all tokens, of which those without a target are rows of
+// zeros: nothing waits for their number then (a list's launch less: 1023 x 5003 x 511 184 -> 175 us).
 #include <cmath>
 
 #include "sdp_internal.h"
@@ -50,8 +51,8 @@ __device__ inline void plan_piece(const Shapes& g, int rows, sdp::HeadPiece* to)
     if ((threadIdx.x & 63) == 0) *to = {rows, two ? 2 : 1, {}, dx, dw};
 }
 
-// list: the tokens with a target in order, from its front; the others as -1 - token, from its end.  pieces: what each of them has of the former
-// (bf16).  One workgroup: 16384 tokens are one turn.  FROM: 0, 1 labels of 32, 64 bits, 2 what entries_kernel wrote.
+// list: the tokens with a target in order, from its front; the others as -1 - token, from its end.  pieces: what each of them has of the former.
+// One workgroup: 16384 tokens are one turn.  FROM: 0, 1 labels of 32, 64 bits, 2 what entries_kernel wrote.
 template <int FROM>
 __global__ __launch_bounds__(1024) void list_kernel(const void* __restrict__ from, int T, int V, int32_t* __restrict__ list, sdp::HeadPiece* pieces, Shapes g) {
     __shared__ int wave_sums[16];
@@ -92,22 +93,20 @@ __global__ __launch_bounds__(1024) void list_kernel(const void* __restrict__ fro
         before += all;
         __syncthreads();
     }
-    if (!pieces) return;
     for (int p = wave; p < g.pieces; p += 16) {
         const int left = before - p * g.rows;
         plan_piece(g, left < 0 ? 0 : left < g.rows ? left : g.rows, pieces + p);
     }
 }
 
-// The list of at most kSmallList tokens, by every workgroup of TH threads that needs it, in its own LDS; returns how many have a target.  `has`: what
+// The list of at most kSmallList tokens, by every workgroup of 256 threads that needs it, in its own LDS; returns how many have a target.  `has`: what
 // entries_kernel wrote, null with labels.
 constexpr int kSmallList = 1024;
-template <int TH>
 __device__ int small_list(const void* labels, int wide, const uint8_t* has, int T, int V, int32_t* list) {
     __shared__ uint64_t masks[kSmallList / 64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
-    for (int c = 0; c < kSmallList / 64; c += TH / 64) {
+    for (int c = 0; c < kSmallList / 64; c += 4) {
         const int t = (c + wave) * 64 + lane;
         const int at = t < T ? t : T - 1;
         const uint64_t mask = __ballot((has ? has[at] != 0 : sdp::token_id(labels, wide, at, V) >= 0) && t < T);
@@ -117,7 +116,7 @@ __device__ int small_list(const void* labels, int wide, const uint8_t* has, int 
     int before = 0;
     for (int c = 0; c * 64 < T; ++c) {
         const uint64_t mask = masks[c];
-        if (c % (TH / 64) == wave) {
+        if (c % 4 == wave) {
             const int t = c * 64 + lane, mine = before + __popcll(mask & ((1ull << lane) - 1));
             if (t < T) list[mask >> lane & 1 ? mine : T - 1 - (t - mine)] = mask >> lane & 1 ? t : -1 - t;
         }
@@ -153,7 +152,7 @@ __global__ __launch_bounds__(256) void gather_kernel(Gather a) {
     const int32_t* list = a.list;
     int live, terms;
     if constexpr (SMALL) {
-        live = small_list<256>(a.labels_in, a.wide, a.has, a.rows, a.V, small);
+        live = small_list(a.labels_in, a.wide, a.has, a.rows, a.V, small);
         list = small;
         if (r0 == 0 && c0 == 0) {
             for (int i = tid; i < a.rows; i += 256) a.list[i] = small[i];
@@ -193,31 +192,35 @@ __global__ __launch_bounds__(256) void gather_kernel(Gather a) {
     }
 }
 
-// fp32: a wave a row, of any width and alignment
-template <int SMALL>
-__global__ __launch_bounds__(64) void gather_f32_kernel(Gather a) {
+// fp32: rows of X with zeros for tokens without a target, whose products are computed all the same, in their places; list says which have one.  A wave a
+// row, of any width and alignment.
+struct Clean {
+    const float* X;
+    float *Xc, *dX; // dX: zeros for those tokens, may be null
+    int32_t* list;  // of all tokens
+    Targets t;
+    int base, rows, V, d; // the piece's first token
+};
+__global__ __launch_bounds__(64) void clean_f32_kernel(Clean a) {
     typedef Row<0> Rw;
     constexpr int N = Rw::N;
-    __shared__ int32_t small[SMALL ? kSmallList : 1];
     const int64_t row = sdp::group_id();
     if (row >= a.rows) return;
-    if constexpr (SMALL) {
-        small_list<64>(a.labels_in, a.wide, a.has, a.rows, a.V, small);
-        if (row == 0)
-            for (int i = threadIdx.x; i < a.rows; i += 64) a.list[i] = small[i];
-    }
-    const int listed = SMALL ? small[row] : a.list[row], tid = threadIdx.x, d = a.d, whole = Rw::whole(d);
-    const float* x = (const float*)a.X + (int64_t)(listed < 0 ? 0 : listed) * d;
-    float* xc = (float*)a.Xc + row * d;
-    float* dx = (float*)a.dX + (int64_t)(listed < 0 ? -1 - listed : 0) * d;
+    const int tid = threadIdx.x, d = a.d, whole = Rw::whole(d), token = a.base + (int)row;
+    const bool live = sdp::has_entry(a.t, token, a.V);
+    if (tid == 0) a.list[token] = live ? token : -1 - token;
+    const float* x = a.X + (int64_t)token * d;
+    float *xc = a.Xc + row * d, *dx = a.dX + (int64_t)token * d;
     const u32x4 none = {0, 0, 0, 0};
     for (int e = tid * N; e < whole; e += 64 * N) {
-        *(Rw::Piece*)(xc + e) = listed < 0 ? none : Rw::load_some(x, e, whole); // the contractions go over all rows
-        if (listed < 0 && a.dX) *(Rw::Piece*)(dx + e) = none;
+        const u32x4 w = Rw::load_some(x, e, whole);
+        if (!live && a.dX) *(Rw::Piece*)(dx + e) = none;
+        *(Rw::Piece*)(xc + e) = live ? w : none;
     }
     if (whole + tid < d) {
-        xc[whole + tid] = listed < 0 ? 0.f : x[whole + tid];
-        if (listed < 0 && a.dX) dx[whole + tid] = 0.f;
+        const float w = x[whole + tid];
+        if (!live && a.dX) dx[whole + tid] = 0.f;
+        xc[whole + tid] = live ? w : 0.f;
     }
 }
 
@@ -436,7 +439,7 @@ Plan plan(int dtype, int T, int V, int d, int k, bool teacher, bool dx, bool dw)
     };
     const size_t rows = (size_t)p.rows;
     p.list = take((size_t)T * 4);
-    if (teacher) p.has = take((size_t)T);
+    if (bf16 && teacher) p.has = take((size_t)T);
     p.X = take(rows * d * (bf16 ? 2 : 4));
     if (bf16) {
         p.ldz = sdp::line_ld(V, p.rows);
@@ -477,16 +480,16 @@ int run(const Call& c, unsigned char* ws, hipStream_t s) {
     const bool bf16 = c.dtype == SDP_BF16, teacher = c.t.top != nullptr, grads = c.dX || c.dW;
     const Plan p = plan(c.dtype, c.T, c.V, c.d, c.t.k, teacher, c.dX, c.dW);
     int32_t* list = (int32_t*)(ws + p.list);
-    sdp::HeadPiece* pieces = bf16 ? (sdp::HeadPiece*)(ws + p.piece) : nullptr;
+    sdp::HeadPiece* pieces = (sdp::HeadPiece*)(ws + p.piece); // bf16
     const Shapes shapes{p.tx, p.tw, p.rows, p.pieces, c.V, c.d};
-    const bool small = p.pieces == 1 && c.T <= (bf16 ? kSmallList : 256); // listed by what gathers
+    const bool small = p.pieces == 1 && c.T <= kSmallList; // listed by what gathers
     const bool with_loss = bf16 && sdp::head_sums_loss(p.rows, p.pieces, c.dX, c.dW);
-    uint8_t* has = teacher ? ws + p.has : nullptr;
-    if (teacher) {
+    uint8_t* has = bf16 && teacher ? ws + p.has : nullptr;
+    if (has) {
         sdp::ProfileScope ps("head_entries", s);
         entries_kernel<<<sdp::grid_of((c.T + 3) / 4), 256, 0, s>>>(c.t, c.T, c.V, has);
     }
-    if (!small) {
+    if (bf16 && !small) {
         sdp::ProfileScope ps("head_list", s);
         if (teacher) list_kernel<2><<<1, 1024, 0, s>>>(has, c.T, c.V, list, pieces, shapes);
         else if (c.t.wide) list_kernel<1><<<1, 1024, 0, s>>>(c.t.ids, c.T, c.V, list, pieces, shapes);
@@ -500,10 +503,9 @@ int run(const Call& c, unsigned char* ws, hipStream_t s) {
         {
             sdp::ProfileScope ps("head_gather", s);
             const dim3 grid((sdp::head_held(rows) + 63) / 64, (c.d + 63) / 64);
-            if (bf16 && small) gather_kernel<1><<<grid, 256, 0, s>>>(g);
-            else if (bf16) gather_kernel<0><<<grid, 256, 0, s>>>(g);
-            else if (small) gather_f32_kernel<1><<<sdp::grid_of(rows), 64, 0, s>>>(g);
-            else gather_f32_kernel<0><<<sdp::grid_of(rows), 64, 0, s>>>(g);
+            if (!bf16) clean_f32_kernel<<<sdp::grid_of(rows), 64, 0, s>>>({(const float*)c.X, (float*)(ws + p.X), (float*)c.dX, list, c.t, base, rows, c.V, c.d});
+            else if (small) gather_kernel<1><<<grid, 256, 0, s>>>(g);
+            else gather_kernel<0><<<grid, 256, 0, s>>>(g);
         }
         rc = sdp::launch_status();
         if (rc != SDP_OK) return rc;
