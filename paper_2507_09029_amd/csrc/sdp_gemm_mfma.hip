@@ -2102,25 +2102,6 @@ __device__ inline void add_ranges(Dev g, const HeadArgs& head, uint32_t group, u
         if (range == 0 && m < rows && n < g.N) put(m, n, a);
     }
 }
-// The loss, by a workgroup of 256, in fp64 in one order
-__device__ inline void sum_loss(const HeadLoss& l) {
-    __shared__ double waves[4];
-    if (!l.to) return;
-    const int tid = threadIdx.x;
-    double x = 0.0;
-    for (int t0 = tid; t0 < l.T; t0 += 8 * 256) {
-        float v[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = l.kl[min(t0 + i * 256, l.T - 1)];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x += t0 + i * 256 < l.T ? (double)v[i] : 0.0;
-    }
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) x += __shfl_xor(x, d, 64);
-    if ((tid & 63) == 0) waves[tid / 64] = x;
-    __syncthreads();
-    if (tid == 0) *l.to = (float)(((waves[0] + waves[1]) + (waves[2] + waves[3])) * ((double)l.scale * (l.scale_dev ? (double)*l.scale_dev : 1.0)));
-}
 template <int BM, int BN, int WAVES_M, int WAVES_N, int OP>
 __global__ __launch_bounds__(256) void head_cut_kernel(Dev g, HeadArgs head) {
     if (blockIdx.x == 0) sum_loss(head.loss);

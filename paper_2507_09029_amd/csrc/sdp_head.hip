@@ -393,14 +393,21 @@ int f32_dx_ranges(int rows, int V, int d) {
 }
 // their sums, in their order, and the vocabulary's last tokens, which no range has -> the tokens' rows; a workgroup a row
 __global__ __launch_bounds__(256) void f32_dx_sum_kernel(const float* __restrict__ part, int ranges, int rows, int d, const float* __restrict__ Z, int64_t ldz,
-                                                         const float* __restrict__ W, int first, int V, const int32_t* __restrict__ list, float* dX) {
-    const int64_t row = sdp::group_id();
-    if (row >= rows) return;
+                                                         const float* __restrict__ W, int first, int V, const int32_t* __restrict__ list, float* dX,
+                                                         sdp::HeadLoss loss) {
+    const int64_t row = (int64_t)sdp::group_id() - 1;
+    if (row < 0) sdp::sum_loss(loss);
+    if (row < 0 || row >= rows) return;
     const int token = list[row];
     if (token < 0) return; // zeros are there
     for (int c = threadIdx.x; c < d; c += 256) {
-        float x = part[row * d + c];
-        for (int r = 1; r < ranges; ++r) x += part[((int64_t)r * rows + row) * d + c];
+        float of[sdp::kMaxBatch];
+#pragma unroll
+        for (int r = 0; r < sdp::kMaxBatch; ++r) of[r] = part[((int64_t)min(r, ranges - 1) * rows + row) * d + c];
+        float x = of[0];
+#pragma unroll
+        for (int r = 1; r < sdp::kMaxBatch; ++r) x += r < ranges ? of[r] : 0.f;
+#pragma unroll 4
         for (int v = first; v < V; ++v) x = fmaf(Z[row * ldz + v], W[(int64_t)v * d + c], x);
         dX[(int64_t)token * d + c] = x;
     }
@@ -483,7 +490,9 @@ int run(const Call& c, unsigned char* ws, hipStream_t s) {
     sdp::HeadPiece* pieces = (sdp::HeadPiece*)(ws + p.piece); // bf16
     const Shapes shapes{p.tx, p.tw, p.rows, p.pieces, c.V, c.d};
     const bool small = p.pieces == 1 && c.T <= kSmallList; // listed by what gathers
-    const bool with_loss = bf16 && sdp::head_sums_loss(p.rows, p.pieces, c.dX, c.dW);
+    const bool with_loss = sdp::head_sums_loss(p.rows, p.pieces, c.dX, bf16 && c.dW);
+    const sdp::HeadLoss loss{with_loss ? c.loss : nullptr, c.kl, c.T, c.t.scale, c.t.scale_dev};
+    bool summed = bf16 && with_loss;
     uint8_t* has = bf16 && teacher ? ws + p.has : nullptr;
     if (has) {
         sdp::ProfileScope ps("head_entries", s);
@@ -533,7 +542,7 @@ int run(const Call& c, unsigned char* ws, hipStream_t s) {
                 else code_rows_kernel<0><<<sdp::grid_of((int64_t)rows * parts), kCodeThreads, lds, s>>>(r);
             }
             rc = sdp::launch_status();
-            if (with_loss) h.loss = {c.loss, c.kl, c.T, c.t.scale, c.t.scale_dev};
+            h.loss = loss;
             const bool few = c.dX && c.dW && sdp::head_dw_few(p.rows, p.pieces);
             if (rc == SDP_OK && c.dX) rc = sdp::gemm_head_dx(h, list + base, c.dX, (float*)(ws + p.cut), few ? c.dW : nullptr, s);
             if (rc == SDP_OK && c.dW && !few)
@@ -567,16 +576,17 @@ int run(const Call& c, unsigned char* ws, hipStream_t s) {
                 rc = sdp::gemm_f32(x, s);
                 if (rc != SDP_OK) return rc;
                 sdp::ProfileScope ps("head_dx_sum", s);
-                f32_dx_sum_kernel<<<sdp::grid_of(rows), 256, 0, s>>>(part, r, rows, c.d, (const float*)(ws + p.Z), p.ldz, (const float*)c.W, r * depth, c.V,
-                                                                     list + base, (float*)c.dX);
+                f32_dx_sum_kernel<<<sdp::grid_of((int64_t)rows + 1), 256, 0, s>>>(part, r, rows, c.d, (const float*)(ws + p.Z), p.ldz, (const float*)c.W, r * depth, c.V,
+                                                                     list + base, (float*)c.dX, loss);
                 rc = sdp::launch_status();
+                summed = with_loss;
             } else {
                 rc = c.dX ? sdp::gemm_f32(x, s) : SDP_OK;
             }
             if (rc == SDP_OK && c.dW) rc = sdp::gemm_f32(w, s);
         }
     }
-    if (rc != SDP_OK || !c.loss || with_loss) return rc;
+    if (rc != SDP_OK || !c.loss || summed) return rc;
     return sdp::loss_sum(c.kl, c.T, c.t.scale, c.t.scale_dev, c.loss, s);
 }
 

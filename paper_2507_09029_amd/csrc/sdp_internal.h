@@ -248,7 +248,8 @@ __device__ inline HeadCut head_cut(const HeadTiles& t, int tiles, int nk, bool a
     return {head, tail, best, (nk + best - 1) / best};
 }
 #endif
-// *to = scale scale_dev[0] sum kl[0 .. T)
+// *to = scale scale_dev[0] sum kl[0 .. T), beside other workgroups of a launch
+constexpr int kLossTokens = 8192;
 struct HeadLoss {
     float* to = nullptr; // may be null
     const float* kl = nullptr;
@@ -256,6 +257,27 @@ struct HeadLoss {
     float scale = 1.f;
     const float* scale_dev = nullptr;
 };
+#ifdef __HIPCC__
+// by a workgroup of 256, in fp64 in one order
+__device__ inline void sum_loss(const HeadLoss& l) {
+    __shared__ double waves[4];
+    if (!l.to) return;
+    const int tid = threadIdx.x;
+    double x = 0.0;
+    for (int t0 = tid; t0 < l.T; t0 += 8 * 256) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = l.kl[min(t0 + i * 256, l.T - 1)];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x += t0 + i * 256 < l.T ? (double)v[i] : 0.0;
+    }
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) x += __shfl_xor(x, d, 64);
+    if ((tid & 63) == 0) waves[tid / 64] = x;
+    __syncthreads();
+    if (tid == 0) *l.to = (float)(((waves[0] + waves[1]) + (waves[2] + waves[3])) * ((double)l.scale * (l.scale_dev ? (double)*l.scale_dev : 1.0)));
+}
+#endif
 struct HeadGemm {
     const void* X = nullptr;  // [rows][d], theirs without gaps
     const void* Xt = nullptr; // [d][ldt]: the same columns by columns, zeros behind the last token to a multiple of 8
@@ -278,9 +300,9 @@ constexpr float kCodeRange = 96.f;
 int head_block(int rows, int V, int d);
 int gemm_head_logits(const HeadGemm& h, float rate, bool codes, float2* stats, int nblk, const int32_t* labels, float* at_label, hipStream_t s);
 // Whether a call has its dW by a kernel for few tokens, and whether the loss comes with dX's or dW's second launch: a workgroup's work beside others' up to
-// 8192 tokens, where a launch of its own takes 5 us and a gap.
+// kLossTokens, where a launch of its own takes 5 us and a gap.
 inline bool head_dw_few(int rows, int pieces) { return pieces == 1 && rows <= kTwoTermRows; }
-inline bool head_sums_loss(int rows, int pieces, bool dx, bool dw) { return pieces == 1 && ((dx && rows <= 8192) || (dw && head_dw_few(rows, pieces))); }
+inline bool head_sums_loss(int rows, int pieces, bool dx, bool dw) { return pieces == 1 && ((dx && rows <= kLossTokens) || (dw && head_dw_few(rows, pieces))); }
 // dX[list[row]] = P W, with scratch of head_cut_bytes; where head_dw_few says so also dW, few_dW (may be null), in one launch with the sums of dX's ranges
 int gemm_head_dx(const HeadGemm& h, const int32_t* list, void* dX, float* cut_ws, void* few_dW, hipStream_t s);
 // dW = P^T X over pieces of tokens (of: 0 the only one, 1 first, 2 between, 3 last), which share sums of head_sums_bytes; the only one takes
