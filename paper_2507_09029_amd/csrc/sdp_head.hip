@@ -231,16 +231,18 @@ struct EntryLogits {
     float* z; // [row][k]
     int rows, V, d;
 };
-// The entries' logits in fp32: a workgroup a row, a wave four entries at a time.
+// The entries' logits in fp32: a workgroup a row, LANES lanes four entries at a time, as few as hold a row of W: 10000 tokens of 109 entries, d = 80
+// 84.7 us with 64 lanes, 34.6 with 16; 6200 of 104, d = 304 52.5 with 64, 46.4 with 32.
+template <int LANES>
 __global__ __launch_bounds__(256) void entry_logits_kernel(EntryLogits a) {
     typedef Row<1> Rw;
-    constexpr int WAVES = 4, M = 4;
+    constexpr int GROUPS = 256 / LANES, M = 4;
     const int64_t row = sdp::group_id();
     if (row >= a.rows) return;
-    const int listed = a.list[row], lane = threadIdx.x & 63, wave = threadIdx.x >> 6, k = a.t.k;
+    const int listed = a.list[row], lane = threadIdx.x % LANES, group = threadIdx.x / LANES, k = a.t.k;
     if (listed < 0) return;
     const uint16_t* x = a.X + row * a.d;
-    for (int i0 = wave * M; i0 < k; i0 += WAVES * M) {
+    for (int i0 = group * M; i0 - group % (64 / LANES) * M < k; i0 += GROUPS * M) { // (whole waves stay for the sums)
         const uint16_t* w[M];
         float sum[M];
 #pragma unroll
@@ -249,7 +251,7 @@ __global__ __launch_bounds__(256) void entry_logits_kernel(EntryLogits a) {
             w[j] = a.W + (int64_t)(id < 0 ? 0 : id) * a.d;
             sum[j] = 0.f;
         }
-        for (int e = lane * 8; e < a.d; e += 64 * 8) {
+        for (int e = lane * 8; e < a.d; e += LANES * 8) {
             float xv[8];
             Rw::unpack(*(const u32x4*)(x + e), xv);
 #pragma unroll
@@ -262,7 +264,13 @@ __global__ __launch_bounds__(256) void entry_logits_kernel(EntryLogits a) {
         }
 #pragma unroll
         for (int j = 0; j < M; ++j) {
-            const float z = sdp::wave_sum(sum[j]);
+            float z = sum[j];
+            if constexpr (LANES == 64) {
+                z = sdp::wave_sum(z);
+            } else {
+#pragma unroll
+                for (int d = LANES / 2; d >= 1; d >>= 1) z += __shfl_xor(z, d, 64);
+            }
             if (lane == 0 && i0 + j < k) a.z[row * k + i0 + j] = z;
         }
     }
@@ -284,12 +292,11 @@ struct CodeRows {
 
 // A row of codes and its blocks' statistics -> its loss, lse and gradient.  One workgroup a row.  ONCE: around the caches, where the codes are far
 // more than the 256 MB behind the L2s hold: 16384 x 32000 444 -> 396 us, but 3350 x 50001 123 -> 136.
-// Few rows are several workgroups' each, of which all find the row's sum.
-constexpr int kCodeThreads = 256;
-template <int ONCE>
-__global__ __launch_bounds__(kCodeThreads) void code_rows_kernel(CodeRows a) {
+// Few rows are several workgroups' each, of which all find the row's sum.  Short ones are a wave's each (TH = 64): 15397 x 963 38.1 -> 17.6 us, 14187 x 413 33.2 -> 14.3.
+template <int TH, int ONCE>
+__global__ __launch_bounds__(TH) void code_rows_kernel(CodeRows a) {
     typedef Row<1> Rw;
-    constexpr int TH = kCodeThreads, WAVES = TH / 64;
+    constexpr int WAVES = TH / 64;
     __shared__ float lds[3][2][WAVES];
     extern __shared__ unsigned char entry_lds[];
     const uint32_t group = sdp::group_id();
@@ -528,7 +535,10 @@ int run(const Call& c, unsigned char* ws, hipStream_t s) {
             float* z = (float*)(ws + p.z);
             if (teacher) {
                 sdp::ProfileScope ps("head_entry_logits", s);
-                entry_logits_kernel<<<sdp::grid_of(rows), 256, 0, s>>>({(const uint16_t*)h.X, (const uint16_t*)c.W, list + base, c.t, z, rows, c.V, c.d});
+                const EntryLogits e{(const uint16_t*)h.X, (const uint16_t*)c.W, list + base, c.t, z, rows, c.V, c.d};
+                if (c.d <= 128) entry_logits_kernel<16><<<sdp::grid_of(rows), 256, 0, s>>>(e);
+                else if (c.d <= 512) entry_logits_kernel<32><<<sdp::grid_of(rows), 256, 0, s>>>(e);
+                else entry_logits_kernel<64><<<sdp::grid_of(rows), 256, 0, s>>>(e);
             }
             rc = sdp::gemm_head_logits(h, sdp::kLog2e * c.t.inv_tau, grads, stats, p.nblk, g.labels, z, s);
             if (rc != SDP_OK) return rc;
@@ -538,8 +548,10 @@ int run(const Call& c, unsigned char* ws, hipStream_t s) {
             {
                 sdp::ProfileScope ps("head_rows", s);
                 const size_t lds = sdp::Entries::bytes(c.t.k);
-                if (grads && (size_t)rows * p.ldz * 2 >= (size_t)1 << 29) code_rows_kernel<1><<<sdp::grid_of((int64_t)rows * parts), kCodeThreads, lds, s>>>(r);
-                else code_rows_kernel<0><<<sdp::grid_of((int64_t)rows * parts), kCodeThreads, lds, s>>>(r);
+                const dim3 grid = sdp::grid_of((int64_t)rows * parts);
+                if (grads && (size_t)rows * p.ldz * 2 >= (size_t)1 << 29) code_rows_kernel<256, 1><<<grid, 256, lds, s>>>(r);
+                else if (c.V > 2048) code_rows_kernel<256, 0><<<grid, 256, lds, s>>>(r);
+                else code_rows_kernel<64, 0><<<grid, 64, lds, s>>>(r);
             }
             rc = sdp::launch_status();
             h.loss = loss;
@@ -553,9 +565,9 @@ int run(const Call& c, unsigned char* ws, hipStream_t s) {
         d.M = rows, d.N = c.V, d.K = c.d, d.A = ws + p.X, d.lda = c.d, d.B = c.W, d.ldb = c.d, d.C = ws + p.Z, d.ldc = p.ldz, d.name = "head_logits";
         rc = sdp::gemm_f32(d, s);
         if (rc != SDP_OK) return rc;
-        sdp::TargetRows r;
-        r.Z = ws + p.Z, r.dZ = grads ? ws + p.Z : nullptr, r.ldz = p.ldz, r.t = c.t, r.kl = c.kl, r.lse = c.lse, r.rows = rows, r.V = c.V, r.list = list + base;
-        rc = sdp::target_rows(SDP_F32, r, "head_rows", s);
+        sdp::TargetRows of;
+        of.Z = ws + p.Z, of.dZ = grads ? ws + p.Z : nullptr, of.ldz = p.ldz, of.t = c.t, of.kl = c.kl, of.lse = c.lse, of.rows = rows, of.V = c.V, of.list = list + base;
+        rc = sdp::target_rows(SDP_F32, of, "head_rows", s);
         sdp::GemmDesc both[2];
         sdp::GemmDesc &x = both[0], &w = both[1];
         x.M = rows, x.N = c.d, x.K = c.V, x.A = ws + p.Z, x.lda = p.ldz, x.B = c.W, x.ldb = c.d, x.b_km = 1, x.C = c.dX, x.ldc = c.d;
@@ -564,9 +576,11 @@ int run(const Call& c, unsigned char* ws, hipStream_t s) {
         if (i > 0) w.R = c.dW, w.ldr = c.d; // the pieces before
         w.name = "head_dw";
         if (rc != SDP_OK) return rc;
-        rc = c.dX && c.dW ? sdp::gemm_f32_group(both, 2, "head_dx_dw", s) : SDP_ERR_UNSUPPORTED;
+        const int r = f32_dx_ranges(p.rows, c.V, c.d);
+        // in one launch where dX's depth is not what takes longest: 256 x 256, 1024 deep 8.3 us, but 12 x 225, 5083 deep 38.6,
+        // where dX takes 12.4 in ranges and 3.9 for their sums, with the loss, and dW 12.8; 1 x 66, 7746 deep 53.4 and 16.8, 4.0, 8.6
+        rc = c.dX && c.dW && (r == 1 || c.V <= 1536) ? sdp::gemm_f32_group(both, 2, "head_dx_dw", s) : SDP_ERR_UNSUPPORTED;
         if (rc == SDP_ERR_UNSUPPORTED) {
-            const int r = f32_dx_ranges(p.rows, c.V, c.d);
             if (c.dX && r > 1) {
                 const int depth = c.V / r / 4 * 4;
                 float* part = (float*)(ws + p.cut);
