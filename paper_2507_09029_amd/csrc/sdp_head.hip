@@ -292,7 +292,8 @@ struct CodeRows {
 
 // A row of codes and its blocks' statistics -> its loss, lse and gradient.  One workgroup a row.  ONCE: around the caches, where the codes are far
 // more than the 256 MB behind the L2s hold: 16384 x 32000 444 -> 396 us, but 3350 x 50001 123 -> 136.
-// Few rows are several workgroups' each, of which all find the row's sum.  Short ones are a wave's each (TH = 64): 15397 x 963 38.1 -> 17.6 us, 14187 x 413 33.2 -> 14.3.
+// Few rows are several workgroups' each, of which all find the row's sum.  Many short ones are a wave's each (TH = 64): 15397 x 963 38.1 -> 17.6 us,
+// 14187 x 413 33.2 -> 14.3, 6200 x 2442 22.2 -> 14.7, 2000 x 3500 12.5 -> 10.7, but 800 x 3000 7.0 -> 7.6.
 template <int TH, int ONCE>
 __global__ __launch_bounds__(TH) void code_rows_kernel(CodeRows a) {
     typedef Row<1> Rw;
@@ -550,7 +551,7 @@ int run(const Call& c, unsigned char* ws, hipStream_t s) {
                 const size_t lds = sdp::Entries::bytes(c.t.k);
                 const dim3 grid = sdp::grid_of((int64_t)rows * parts);
                 if (grads && (size_t)rows * p.ldz * 2 >= (size_t)1 << 29) code_rows_kernel<256, 1><<<grid, 256, lds, s>>>(r);
-                else if (c.V > 2048) code_rows_kernel<256, 0><<<grid, 256, lds, s>>>(r);
+                else if (rows < 1024 || c.V > 4096) code_rows_kernel<256, 0><<<grid, 256, lds, s>>>(r);
                 else code_rows_kernel<64, 0><<<grid, 64, lds, s>>>(r);
             }
             rc = sdp::launch_status();
