@@ -230,19 +230,21 @@ struct EntryLogits {
     Targets t;
     float* z; // [row][k]
     int rows, V, d;
+    int parts; // workgroups of a row
 };
-// The entries' logits in fp32: a workgroup a row, LANES lanes four entries at a time, as few as hold a row of W: 10000 tokens of 109 entries, d = 80
-// 84.7 us with 64 lanes, 34.6 with 16; 6200 of 104, d = 304 52.5 with 64, 46.4 with 32.
+// The entries' logits in fp32: a workgroup a row, of few rows several, LANES lanes four entries at a time, as few as hold a row of W: 10000 tokens of 109 entries, d = 80
+// 84.7 us with 64 lanes, 34.6 with 16; 6200 of 104, d = 304 52.5 with 64, 46.4 with 32; 76 of 84, d = 832 11.9 with a workgroup a row, 4.5 with six.
 template <int LANES>
 __global__ __launch_bounds__(256) void entry_logits_kernel(EntryLogits a) {
     typedef Row<1> Rw;
     constexpr int GROUPS = 256 / LANES, M = 4;
-    const int64_t row = sdp::group_id();
+    const uint32_t at = sdp::group_id();
+    const int64_t row = at / (uint32_t)a.parts;
     if (row >= a.rows) return;
-    const int listed = a.list[row], lane = threadIdx.x % LANES, group = threadIdx.x / LANES, k = a.t.k;
+    const int listed = a.list[row], lane = threadIdx.x % LANES, group = (int)(at % (uint32_t)a.parts) * GROUPS + threadIdx.x / LANES, k = a.t.k;
     if (listed < 0) return;
     const uint16_t* x = a.X + row * a.d;
-    for (int i0 = group * M; i0 - group % (64 / LANES) * M < k; i0 += GROUPS * M) { // (whole waves stay for the sums)
+    for (int i0 = group * M; i0 - group % (64 / LANES) * M < k; i0 += a.parts * GROUPS * M) { // (whole waves stay for the sums)
         const uint16_t* w[M];
         float sum[M];
 #pragma unroll
@@ -536,10 +538,12 @@ int run(const Call& c, unsigned char* ws, hipStream_t s) {
             float* z = (float*)(ws + p.z);
             if (teacher) {
                 sdp::ProfileScope ps("head_entry_logits", s);
-                const EntryLogits e{(const uint16_t*)h.X, (const uint16_t*)c.W, list + base, c.t, z, rows, c.V, c.d};
-                if (c.d <= 128) entry_logits_kernel<16><<<sdp::grid_of(rows), 256, 0, s>>>(e);
-                else if (c.d <= 512) entry_logits_kernel<32><<<sdp::grid_of(rows), 256, 0, s>>>(e);
-                else entry_logits_kernel<64><<<sdp::grid_of(rows), 256, 0, s>>>(e);
+                const int lanes = c.d <= 128 ? 16 : c.d <= 512 ? 32 : 64, at_once = 256 / lanes * 4;
+                const EntryLogits e{(const uint16_t*)h.X, (const uint16_t*)c.W, list + base, c.t, z, rows, c.V, c.d, rows < 512 ? (c.t.k + at_once - 1) / at_once : 1};
+                const dim3 grid = sdp::grid_of((int64_t)rows * e.parts);
+                if (lanes == 16) entry_logits_kernel<16><<<grid, 256, 0, s>>>(e);
+                else if (lanes == 32) entry_logits_kernel<32><<<grid, 256, 0, s>>>(e);
+                else entry_logits_kernel<64><<<grid, 256, 0, s>>>(e);
             }
             rc = sdp::gemm_head_logits(h, sdp::kLog2e * c.t.inv_tau, grads, stats, p.nblk, g.labels, z, s);
             if (rc != SDP_OK) return rc;
