@@ -10,7 +10,7 @@
 //   rows     a row's blocks -> its lse and loss; its codes -> its gradient, bf16, in their place.  4 bytes a logit moved beside 6 d operations
 //   dX, dW   contractions on what is stored; dW goes on from piece to piece in fp32 (head.sums), and is rounded once
 // fp32: the same with the logits themselves in fp32 (target_rows) and the fp32 contractions, over all tokens, of which those without a target are rows of
-// zeros: nothing waits for their number then (a list's launch less: 1023 x 5003 x 511 184 -> 175 us).
+// zeros: nothing waits for their number then (a list's launch less: 1023 x 5003 x 511 184 -> 180 us).
 #include <cmath>
 
 #include "sdp_internal.h"
@@ -393,7 +393,7 @@ __global__ __launch_bounds__(TH) void code_rows_kernel(CodeRows a) {
 }
 
 // Depth ranges of fp32 dX, whose outputs are few and whose depth is the vocabulary: a launch of few tiles runs as up to four problems.  1023 x 511, 5003
-// deep 97 -> 53 us, and 10 for their sums.
+// deep 97 -> 53 us, and 6 for their sums.
 int f32_dx_ranges(int rows, int V, int d) {
     const int64_t tiles = (int64_t)((rows + 63) / 64) * ((d + 63) / 64);
     int r = tiles > 0 && tiles <= 256 ? (int)(512 / tiles) : 1;
