@@ -354,7 +354,8 @@ __global__ __launch_bounds__(TH) void code_rows_kernel(CodeRows a) {
     uint16_t* second = terms == 2 ? p + piece_rows * a.ldp : nullptr; // the second term's row
     constexpr float kStep = sdp::kCodeRange / 65535.f;
     const int all = (a.V + 7) / 8 * 8, end = min(first + a.columns, all); // codes of columns behind V say 0
-    auto value = [&](uint32_t code, float from) { return code == 65535u ? 0.f : __builtin_amdgcn_exp2f(fmaf((float)code, -kStep, from)) * inv; };
+    // (0 times a sum that is no number is NaN, as every other element of such a row)
+    auto value = [&](uint32_t code, float from) { return (code == 65535u ? 0.f : __builtin_amdgcn_exp2f(fmaf((float)code, -kStep, from))) * inv; };
     auto turn = [&](int e, const u32x4& w, float block) {
         const float from = block - m;
         float v[8];
