@@ -2252,14 +2252,16 @@ double cut_us(const HeadTiles& t, int M, int N, int nk) {
 }
 // The tiles that take least, on the mean of five numbers of tokens, from all that there may be to half of them: those of dX chosen for all
 // tokens took 715 us where a third of 5000 had no label (128 x 256, d = 1600, V = 50001), now 525 and 27 for their ranges' sums.
+// two_terms: rows of outputs whose tiles are all cut ones, n columns wide (HeadPiece); there is room for them at any width.
 template <class F>
-HeadTiles cut_tiles(bool cuts, int rows, F&& us) {
+HeadTiles cut_tiles(bool cuts, int rows, int two_terms, int n, F&& us) {
     HeadTiles best{};
     double least = -1;
     for (int i = 0; i < NUM_SHAPES; ++i) {
         const ShapeInfo& h = kShapes[i];
         const EpilogueCost e = epilogue_cost(EPI_STORE);
-        const HeadTiles t{h.bm, h.bn, (float)h.step1, (float)(e.e0 + e.e1 * h.bm * h.bn / 1024), cuts ? (i == T64x64 ? 1024 : 512) : 0};
+        const int all = (two_terms + h.bm - 1) / h.bm * ((n + h.bn - 1) / h.bn), most = i == T64x64 ? 1024 : 512;
+        const HeadTiles t{h.bm, h.bn, (float)h.step1, (float)(e.e0 + e.e1 * h.bm * h.bn / 1024), !cuts ? 0 : most > all ? most : all};
         double cost = 0;
         for (int eighths = 8; eighths >= 4; --eighths) cost += us(t, head_held((int)(((int64_t)rows * eighths + 7) / 8)));
         if (least < 0 || cost < least) least = cost, best = t;
@@ -2281,10 +2283,10 @@ int gemm_head_logits(const HeadGemm& h, float rate, bool codes, float2* stats, i
 }
 
 HeadTiles head_dx_tiles(int rows, int V, int d) {
-    return cut_tiles(true, rows, [&](const HeadTiles& t, int held) { return cut_us(t, held, d, (V + BK - 1) / BK); });
+    return cut_tiles(true, rows, 2 * (rows < kTwoTermRows ? rows : kTwoTermRows), d, [&](const HeadTiles& t, int held) { return cut_us(t, held, d, (V + BK - 1) / BK); });
 }
 HeadTiles head_dw_tiles(int rows, int V, int d, int pieces) {
-    return cut_tiles(pieces == 1 && head_held(rows) >= 512, rows, [&](const HeadTiles& t, int held) { return cut_us(t, V, d, (held + BK - 1) / BK); });
+    return cut_tiles(pieces == 1 && head_held(rows) >= 512, rows, 0, 0, [&](const HeadTiles& t, int held) { return cut_us(t, V, d, (held + BK - 1) / BK); });
 }
 
 static FewArgs few_of(const HeadGemm& h, void* dW) {

@@ -44,7 +44,7 @@ struct Shapes {
 // by a whole wave
 __device__ inline void plan_piece(const Shapes& g, int rows, sdp::HeadPiece* to) {
     auto tiles = [](const sdp::HeadTiles& t, int m, int n) { return ((m + t.bm - 1) / t.bm) * ((n + t.bn - 1) / t.bn); };
-    const bool two = rows <= sdp::kTwoTermRows && tiles(g.dx, 2 * rows, g.d) <= g.dx.most;
+    const bool two = rows <= sdp::kTwoTermRows; // dX's cut tiles have room for them
     const int held = two ? 2 * rows : rows;
     const sdp::HeadCut dx = sdp::head_cut(g.dx, tiles(g.dx, held, g.d), (g.V + 63) / 64, two);
     const sdp::HeadCut dw = sdp::head_cut(g.dw, tiles(g.dw, g.V, g.d), (held + 63) / 64);
@@ -158,7 +158,7 @@ __global__ __launch_bounds__(256) void gather_kernel(Gather a) {
             for (int i = tid; i < a.rows; i += 256) a.list[i] = small[i];
             if (tid < 64) plan_piece(a.shapes, live, a.piece);
         }
-        terms = live <= sdp::kTwoTermRows ? 2 : 1; // columns of more than the plan has do no harm
+        terms = live <= sdp::kTwoTermRows ? 2 : 1;
     } else {
         live = a.piece->rows, terms = a.piece->terms;
     }
