@@ -468,17 +468,23 @@ int sdp_distill_loss(int dtype, int id_type, int top_dtype, int T, int V, int k,
 
 /* ---------------------------------------------------------------------------------------------
  * The output head and its loss in one: sdp_token_loss on the logits Z = X W^T, with the gradients of the tokens and of the head,
- * without the logits in memory.
+ * without a [T][V] matrix of the caller's: what is held of the logits, for some tokens at a time, lies in the workspace.
  *   nll, lse, loss as there (Z in fp32);   dX = dZ W  [T][d];   dW = dZ^T X  [V][d]
  * It works on as many tokens at a time (64 at least) as keep what it holds of their logits within SDP_HEAD_PIECE_BYTES (2 bytes a logit with
- * SDP_BF16, 4 with SDP_F32), and their X likewise, and on no more than SDP_HEAD_PIECE_TOKENS, so that no sum of dW runs over more before it is
- * added to the others (over 1.2 million tokens at once fp32 sums drifted by 1e-4).  Tokens without a label cost nothing but the zeros of their dX: with SDP_BF16 their products are not computed.  Their X is not
- * looked at.
+ * SDP_BF16, for the loss alone 8 for 32 logits; 4 with SDP_F32), and their X likewise, and on no more than SDP_HEAD_PIECE_TOKENS, so that no sum of
+ * dW runs over more before it is added to the others (over 1.2 million tokens at once fp32 sums drifted by 1e-4).  With SDP_BF16 up to 128 of these
+ * tokens have a second row of 2 bytes a logit (the two terms below): from V = 2 million on, where a piece has fewer than 256 tokens, that takes
+ * more than SDP_HEAD_PIECE_BYTES, up to twice as much.  Tokens without a label cost nothing but the zeros of their dX: with SDP_BF16 their products
+ * are not computed.  Their X is not looked at.
  *   X [T][d], W [V][d] (row-major by token of the vocabulary, like an embedding, which it may be), labels [T] in
  *   nll [T] fp32 out;  lse [T] fp32, may be NULL;  loss [1] fp32, may be NULL
  *   dX [T][d], dW [V][d] out, either may be NULL (not wanted); dX may take the place of X.  dW has every row; sums over tokens are
  *   fp32 and rounded once.
  *   ws: sdp_head_loss_workspace_bytes(dtype, T, V, d, want_dx, want_dw), 256-byte aligned
+ *       Beside the logits it has 4 or 5 bytes a token and a piece's X (SDP_BF16 with dW: twice).  With SDP_BF16 also 8 bytes for 32 or 64 logits, with
+ *       gradients scratch of the products (for dX 16 to 128 MiB by their tiles, however few tokens there are, more from d = 65536 on), and with dW of
+ *       several pieces its sums in fp32; with SDP_F32 and dX of few tiles up to four times X.  While all tokens are one piece it may thus take more
+ *       memory than bf16 logits (16384 x 32000, d = 2048: 1321 MiB, the logits 1000).
  * With SDP_BF16 a probability is held as 16 bits of its logarithm (within 5.2e-4 of it, 0 below 2^-95) while the row's sum is found, but for those of labels and
  * entries; dZ / c is then rounded to bf16 where it enters the two products, as the sum of two bf16 numbers (2^-17) where at most 128 tokens
  * of a piece have a target, and c follows in fp32.  nll, kl, lse and loss come from fp32 logits.

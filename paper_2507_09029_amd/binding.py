@@ -793,7 +793,7 @@ def head_loss_workspace_bytes(dtype, T, V, d, want_dx=True, want_dw=True):
 
 def head_loss(X, W, labels, scale=1.0, scale_dev=None, want_dx=True, want_dw=True, out=None, ws=None):
     """Cross-entropy of the logits X W^T of tokens X [T][d] and head W [V][d] against int32 or int64 labels [T], with the gradients of
-    both, without the logits in memory.
+    both, without a [T][V] tensor of the caller's: the workspace has what is held of the logits, 1 GiB of them at a time.
 
     As token_loss on X W^T: returns (nll [T], lse [T], dX [T][d], dW [V][d], loss [1]); dX and dW are None where they are not wanted.
     `out` = (nll, lse, dX, dW, loss) preallocated: dX may be X, lse and loss may be None."""
@@ -815,7 +815,7 @@ def head_distill_workspace_bytes(dtype, T, V, d, k, want_dx=True, want_dw=True):
 
 
 def head_distill(X, W, ids, top, temperature=1.0, top_lse=None, scale=1.0, scale_dev=None, want_dx=True, want_dw=True, out=None, ws=None):
-    """distill_loss on the logits X W^T of tokens X [T][d] and head W [V][d], with the gradients of both, without the logits in memory.
+    """distill_loss on the logits X W^T of tokens X [T][d] and head W [V][d], with the gradients of both, without a [T][V] tensor of the caller's.
 
     Returns (kl [T], lse [T], dX [T][d], dW [V][d], loss [1]), as head_loss does; the teacher's arguments are distill_loss's."""
     T, d = X.shape
